@@ -373,6 +373,116 @@ fw_status fw_ragged_append(void *K_store, void *V_store, const int64_t *base, co
                            const void *new_K, const void *new_V, int32_t cells, int32_t m, int32_t row_bytes,
                            int32_t *status, void *stream);
 
+/* Attention over whole prompts: causal, grouped heads, sequences of different
+ * lengths packed behind one another (the pass whose keys and window queries
+ * fw_window_score judges).  Sequence s has query rows cu_q[s] .. cu_q[s+1] and
+ * key rows cu_k[s] .. cu_k[s+1]; with lq and lk of them, its query token i sits
+ * at position lk - lq + i and sees the keys j <= lk - lq + i (lk > lq: the new
+ * tokens stand behind lk - lq cached ones).  Query head h reads key head
+ * h / (q_heads / kv_heads):
+ *   x_ij = scale * q_i . k_j,  o_i = sum_j softmax_j(x_i) v_j,
+ *   lse_i = log sum_j exp(x_ij).
+ * A row that sees no key (lk < lq) gets o = 0 and lse = -inf.  Keys a row does
+ * not see have no part in it, whatever they hold (NaN and infinities too). */
+typedef struct {
+    int32_t num_seqs;
+    int32_t q_heads;          /* a multiple of kv_heads, at most 128 x kv_heads  */
+    int32_t kv_heads;
+    int32_t d;                /* 64 or 128                                       */
+    int64_t total_q, total_k; /* rows that q and k, v hold (below 2^31 - 256)    */
+    const void *q, *k, *v;    /* device, bf16, 16-byte aligned: element c of head h
+                                 of row i at i * row stride + h * head stride + c */
+    int64_t q_row, q_head;    /* strides in elements, positive multiples of 8    */
+    int64_t k_row, k_head;
+    int64_t v_row, v_head;
+    const int32_t *cu_q;      /* device [num_seqs + 1], ascending, within [0, total_q] */
+    const int32_t *cu_k;      /* device [num_seqs + 1], ascending, within [0, total_k] */
+    float scale;              /* > 0 (1 / sqrt(d) for attention)                 */
+} fw_prompt;
+/* o: device bf16 [total_q][q_heads][d], 16-byte aligned; lse: device fp32
+ * [total_q][q_heads] (may be NULL); rows of q outside every sequence are not
+ * written.  status [num_seqs] (may be NULL): FW_OK; FW_ERR_INVALID_ARG where
+ * cu_q or cu_k descends or leaves its range (every output is then unspecified);
+ * FW_ERR_TIMEOUT where a bounded wait gave up (the rows concerned are NaN).
+ * The products run on the tensor cores (bf16 inputs, fp32 accumulation; the
+ * weights are rounded to bf16 for the second one), the softmax in fp32. */
+fw_status fw_prompt_attention(const fw_prompt *p, void *o, float *lse, int32_t *status, void *stream);
+
+/* A ragged per-head store held in 8 bits (Sec. 4's ragged storage at half the
+ * bytes).  Cell h (a KV head of one layer of one sequence) owns the rows
+ * [base[h], base[h] + capacity[h]) and fills counts[h] of them.  Each block of
+ * FW_CACHE8_BLOCK rows of a cell has one scale for its keys and one for its
+ * values, 2^e with the least e >= -120 for which the block's largest magnitude
+ * is at most 448 * 2^e (e4m3) or 127 * 2^e (int8); a code is the value times
+ * 2^-e rounded to nearest, ties to even.  (A power of two: the product is exact,
+ * so a code does not depend on how it is computed, e4m3 loses nothing by it, and
+ * every stored value is a bf16 number.)  The bf16 rows of a cell's open block stay
+ * in a ring of FW_CACHE8_TAIL rows (row r in slot r % FW_CACHE8_TAIL), so each
+ * block is quantised from the originals, however its rows came in, and counts[h]
+ * may be set back by up to FW_CACHE8_BLOCK appended rows (a draft that was not
+ * accepted).  Infinities become the largest code of their sign and NaN 0; the
+ * cell's status says so (FW_ERR_NONFINITE).
+ * Per-cell status [cells] of the calls below (may be NULL): FW_OK;
+ * FW_ERR_INVALID_ARG where base is no multiple of FW_CACHE8_BLOCK, the cell's rows
+ * leave the store or its count (its offsets) is out of range, FW_ERR_WORKSPACE
+ * where the rows do not fit the cell's capacity: such a cell is left as it was
+ * (fw_cache8_compact: with a count of 0, fw_cache8_attend: its outputs those of an
+ * empty cell).  A kept position out of range stores a row of zeros, with
+ * FW_ERR_INVALID_ARG. */
+#define FW_CACHE8_BLOCK 32
+#define FW_CACHE8_TAIL 64
+typedef enum { FW_CACHE8_E4M3 = 0, FW_CACHE8_INT8 = 1 } fw_cache8_format;
+typedef struct {
+    int32_t cells;
+    int32_t d;                 /* 64 or 128                                       */
+    int32_t format;            /* fw_cache8_format                                */
+    int64_t rows;              /* rows of the store, a multiple of FW_CACHE8_BLOCK */
+    void *k, *v;               /* device [rows][d] codes, 16-byte aligned         */
+    float *k_scale, *v_scale;  /* device [rows / FW_CACHE8_BLOCK]                 */
+    void *k_tail, *v_tail;     /* device bf16 [cells][FW_CACHE8_TAIL][d], 16-byte aligned */
+    const int64_t *base;       /* device [cells], multiples of FW_CACHE8_BLOCK    */
+    const int32_t *capacity;   /* device [cells]                                  */
+    int32_t *counts;           /* device [cells], in/out                          */
+} fw_cache8;
+/* Fills the store with the kept rows of a bf16 cache: cell h gets the rows
+ * kept_pos[offsets[h] .. offsets[h+1]) of its keys and values, in that order,
+ * and counts[h] = offsets[h+1] - offsets[h] (what fw_contour_alloc gives).
+ * K, V: device bf16, row t of cell h at h * cell_stride + t * row_stride elements
+ * (positive multiples of 8), T rows per cell, 16-byte aligned.  total: the entries
+ * that kept_pos holds (at least offsets[cells]; its size as the host knows it).
+ * Rows of the store past a cell's count keep what they held. */
+fw_status fw_cache8_compact(const fw_cache8 *c, const void *K, const void *V, int32_t T, int64_t cell_stride,
+                            int64_t row_stride, const int64_t *offsets, const int32_t *kept_pos, int64_t total,
+                            int32_t *status, void *stream);
+/* Appends m rows to every cell (new_K, new_V: device bf16 [cells][m][d], 16-byte
+ * aligned) and adds m to counts. */
+fw_status fw_cache8_append(const fw_cache8 *c, const void *new_K, const void *new_V, int32_t m, int32_t *status,
+                           void *stream);
+/* Attention over the store for the m last tokens of every sequence (m = 1: a
+ * decode step; their own rows are in the store).  Cells are (sequence, KV head),
+ * the head fastest; a KV head serves `group` query heads.  With n = counts[h],
+ * token i sees the cell's rows j < n - m + 1 + i.  Output rows as for
+ * fw_prompt_attention: o = 0, lse = -inf where nothing is seen. */
+typedef struct {
+    int32_t kv_heads;        /* cells = sequences x kv_heads                      */
+    int32_t group;           /* query heads per KV head                           */
+    int32_t m;               /* tokens per sequence                               */
+    const void *q;           /* device bf16, 16-byte aligned: element c of query head
+                                h * group + g of token i of sequence b at b * q_seq +
+                                i * q_tok + (h * group + g) * q_head + c           */
+    int64_t q_seq, q_tok, q_head; /* strides in elements, multiples of 8          */
+    float scale;             /* > 0                                               */
+} fw_cache8_query;
+/* o: device bf16 [sequences][m][kv_heads * group][d], 16-byte aligned; lse: device
+ * fp32 of the same rows (may be NULL).  Products in fp16 (codes are exact there;
+ * queries keep their 8 bits within 2^-24 of a row's largest; weights keep 11 bits),
+ * sums and softmax in fp32.  The result does not depend on the order in which
+ * blocks run. */
+fw_status fw_cache8_attend(const fw_cache8 *c, const fw_cache8_query *q, void *o, float *lse, int32_t *status,
+                           void *workspace, size_t workspace_bytes, void *stream);
+/* Workspace bytes (0 for arguments fw_cache8_attend refuses). */
+size_t fw_cache8_attend_workspace(const fw_cache8 *c, const fw_cache8_query *q);
+
 /* Largest cells accepted by fw_contour_alloc_noalloc. */
 #define FW_CONTOUR_NOALLOC_MAX_CELLS 4096
 

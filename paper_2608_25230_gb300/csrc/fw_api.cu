@@ -61,6 +61,51 @@ fw_status device_sms(int *sms)
     return FW_OK;
 }
 
+static bool good_stride(int64_t x) { return x > 0 && x % 8 == 0 && x < ((int64_t)1 << 38); }
+
+static fw_status check_prompt(const fw_prompt *p)
+{
+    if (!p || p->num_seqs < 1 || p->q_heads < 1 || p->kv_heads < 1 || p->q_heads % p->kv_heads != 0)
+        return FW_ERR_INVALID_ARG;
+    if (p->total_q < 0 || p->total_k < 0 || !p->cu_q || !p->cu_k || !(p->scale > 0.f) || !(p->scale < 1e30f))
+        return FW_ERR_INVALID_ARG;
+    if (p->d != 64 && p->d != 128) return FW_ERR_UNSUPPORTED;
+    if (p->q_heads / p->kv_heads > 128) return FW_ERR_UNSUPPORTED;
+    const int64_t lim = ((int64_t)1 << 31) - 256;
+    if (p->total_q >= lim || p->total_k >= lim) return FW_ERR_UNSUPPORTED;
+    if (p->total_q > 0 && (!p->q || !aligned(p->q, 16) || !good_stride(p->q_row) || !good_stride(p->q_head)))
+        return FW_ERR_INVALID_ARG;
+    if (p->total_k > 0 && (!p->k || !p->v || !aligned(p->k, 16) || !aligned(p->v, 16) || !good_stride(p->k_row) ||
+                           !good_stride(p->k_head) || !good_stride(p->v_row) || !good_stride(p->v_head)))
+        return FW_ERR_INVALID_ARG;
+    return FW_OK;
+}
+
+static fw_status check_cache8(const fw_cache8 *c)
+{
+    if (!c || c->cells < 1 || c->rows < 0 || c->rows % FW_CACHE8_BLOCK != 0) return FW_ERR_INVALID_ARG;
+    if (c->format != FW_CACHE8_E4M3 && c->format != FW_CACHE8_INT8) return FW_ERR_INVALID_ARG;
+    if (c->d != 64 && c->d != 128) return FW_ERR_UNSUPPORTED;
+    if (!c->base || !c->capacity || !c->counts || !c->k_tail || !c->v_tail) return FW_ERR_INVALID_ARG;
+    if (c->rows > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return FW_ERR_INVALID_ARG;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_tail, 16) || !aligned(c->v_tail, 16))
+        return FW_ERR_INVALID_ARG;
+    return FW_OK;
+}
+
+static fw_status check_cache8_query(const fw_cache8 *c, const fw_cache8_query *q)
+{
+    const fw_status st = check_cache8(c);
+    if (st != FW_OK) return st;
+    if (!q || q->kv_heads < 1 || q->group < 1 || q->m < 1 || c->cells % q->kv_heads != 0 || !(q->scale > 0.f) ||
+        !(q->scale < 1e30f))
+        return FW_ERR_INVALID_ARG;
+    if ((int64_t)q->group * q->m > 65536) return FW_ERR_UNSUPPORTED;
+    if (!q->q || !aligned(q->q, 16) || q->q_seq % 8 != 0 || q->q_tok % 8 != 0 || q->q_head % 8 != 0)
+        return FW_ERR_INVALID_ARG;
+    return FW_OK;
+}
+
 static fw_status check_rows(const fw_rows *r, RowsDev &R)
 {
     if (!r) return FW_ERR_INVALID_ARG;
@@ -400,6 +445,58 @@ fw_status fw_selector_audit(const fw_rows *rows, const int32_t *s, int32_t nb, c
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < selector_audit_workspace(R, nb))
         return FW_ERR_WORKSPACE;
     return selector_audit(R, s, nb, *topk, es, bits, words, workspace, (cudaStream_t)stream);
+}
+
+fw_status fw_prompt_attention(const fw_prompt *p, void *o, float *lse, int32_t *status, void *stream)
+{
+    const fw_status st = check_prompt(p);
+    if (st != FW_OK) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (p->total_q == 0) {
+        if (status) FW_CUDA_CHECK(cudaMemsetAsync(status, 0, (size_t)p->num_seqs * 4, s));
+        return FW_OK;
+    }
+    if (!o || !aligned(o, 16)) return FW_ERR_INVALID_ARG;
+    return prompt_attention(*p, o, lse, status, s);
+}
+
+fw_status fw_cache8_compact(const fw_cache8 *c, const void *K, const void *V, int32_t T, int64_t cell_stride,
+                            int64_t row_stride, const int64_t *offsets, const int32_t *kept_pos, int64_t total,
+                            int32_t *status, void *stream)
+{
+    const fw_status st = check_cache8(c);
+    if (st != FW_OK) return st;
+    if (T < 1 || total < 0 || !offsets || !K || !V || !aligned(K, 16) || !aligned(V, 16)) return FW_ERR_INVALID_ARG;
+    if (!good_stride(cell_stride) || !good_stride(row_stride)) return FW_ERR_INVALID_ARG;
+    if (total > 0 && !kept_pos) return FW_ERR_INVALID_ARG;
+    if (total >= ((int64_t)1 << 35)) return FW_ERR_UNSUPPORTED;
+    return cache8_compact(*c, K, V, T, cell_stride, row_stride, offsets, kept_pos, total, status, (cudaStream_t)stream);
+}
+
+fw_status fw_cache8_append(const fw_cache8 *c, const void *new_K, const void *new_V, int32_t m, int32_t *status,
+                           void *stream)
+{
+    const fw_status st = check_cache8(c);
+    if (st != FW_OK) return st;
+    if (m < 1 || !new_K || !new_V || !aligned(new_K, 16) || !aligned(new_V, 16)) return FW_ERR_INVALID_ARG;
+    return cache8_append(*c, new_K, new_V, m, status, (cudaStream_t)stream);
+}
+
+size_t fw_cache8_attend_workspace(const fw_cache8 *c, const fw_cache8_query *q)
+{
+    if (check_cache8_query(c, q) != FW_OK) return 0;
+    return cache8_attend_workspace(*c, *q);
+}
+
+fw_status fw_cache8_attend(const fw_cache8 *c, const fw_cache8_query *q, void *o, float *lse, int32_t *status,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    const fw_status st = check_cache8_query(c, q);
+    if (st != FW_OK) return st;
+    if (!o || !aligned(o, 16)) return FW_ERR_INVALID_ARG;
+    const size_t need = cache8_attend_workspace(*c, *q);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return FW_ERR_WORKSPACE;
+    return cache8_attend(*c, *q, o, lse, status, workspace, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -103,6 +103,17 @@ size_t selector_audit_workspace(const RowsDev &R, int nb);
 fw_status selector_audit(const RowsDev &R, const int32_t *s, int nb, const fw_gap_out &topk, float *es,
                          uint32_t *bits, int words, void *ws, cudaStream_t st);
 
+// Attention over packed prompts, and the 8-bit ragged store with its attention.
+fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *status, cudaStream_t s);
+fw_status cache8_compact(const fw_cache8 &c, const void *K, const void *V, int T, int64_t cell_stride,
+                         int64_t row_stride, const int64_t *offsets, const int32_t *kept_pos, int64_t total,
+                         int32_t *status, cudaStream_t s);
+fw_status cache8_append(const fw_cache8 &c, const void *new_K, const void *new_V, int m, int32_t *status,
+                        cudaStream_t s);
+size_t cache8_attend_workspace(const fw_cache8 &c, const fw_cache8_query &q);
+fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, float *lse, int32_t *status, void *ws,
+                        cudaStream_t s);
+
 // A TMA map of a 2-D bf16 tensor [rows][cols] (cols innermost, row stride
 // cols * 2 bytes) read in boxes of box_rows x 64 elements with the 128-byte
 // swizzle.  False if the driver's encoder is unavailable or refuses the map.

@@ -49,6 +49,31 @@ class FwSwapParams(C.Structure):
     _fields_ = [("E", C.c_int32), ("max_swaps", C.c_int32)]
 
 
+class FwPrompt(C.Structure):
+    _fields_ = [("num_seqs", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32),
+                ("total_q", C.c_int64), ("total_k", C.c_int64), ("q", vp), ("k", vp), ("v", vp),
+                ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+                ("v_row", C.c_int64), ("v_head", C.c_int64), ("cu_q", vp), ("cu_k", vp), ("scale", C.c_float)]
+
+
+class FwCache8(C.Structure):
+    _fields_ = [("cells", C.c_int32), ("d", C.c_int32), ("format", C.c_int32), ("rows", C.c_int64), ("k", vp),
+                ("v", vp), ("k_scale", vp), ("v_scale", vp), ("k_tail", vp), ("v_tail", vp), ("base", vp),
+                ("capacity", vp), ("counts", vp)]
+
+
+class FwCache8Query(C.Structure):
+    _fields_ = [("kv_heads", C.c_int32), ("group", C.c_int32), ("m", C.c_int32), ("q", vp), ("q_seq", C.c_int64),
+                ("q_tok", C.c_int64), ("q_head", C.c_int64), ("scale", C.c_float)]
+
+
+_lib.fw_prompt_attention.argtypes = [C.POINTER(FwPrompt), vp, vp, vp, vp]
+_lib.fw_cache8_compact.argtypes = [C.POINTER(FwCache8), vp, vp, C.c_int32, C.c_int64, C.c_int64, vp, vp, C.c_int64, vp,
+                                   vp]
+_lib.fw_cache8_append.argtypes = [C.POINTER(FwCache8), vp, vp, C.c_int32, vp, vp]
+_lib.fw_cache8_attend.argtypes = [C.POINTER(FwCache8), C.POINTER(FwCache8Query), vp, vp, vp, vp, C.c_size_t, vp]
+_lib.fw_cache8_attend_workspace.argtypes = [C.POINTER(FwCache8), C.POINTER(FwCache8Query)]
+_lib.fw_cache8_attend_workspace.restype = C.c_size_t
 _lib.fw_dense_and_topk_gap.argtypes = [C.POINTER(FwRows), vp, C.c_int32, C.POINTER(FwGapOut), vp, C.c_size_t, vp]
 _lib.fw_dense_and_topk_gap_workspace.argtypes = [C.POINTER(FwRows), C.c_int32]
 _lib.fw_dense_and_topk_gap_workspace.restype = C.c_size_t
@@ -100,7 +125,8 @@ _lib.fw_status_string.argtypes = [C.c_int]
 _lib.fw_status_string.restype = C.c_char_p
 _lib.fw_launch_count.restype = C.c_uint64
 for _f in ("fw_dense_and_topk_gap", "fw_swap_refine", "fw_best_subset", "fw_contour_alloc", "fw_ragged_compact",
-           "fw_group_vote", "fw_pool_best_subset", "fw_sync_status"):
+           "fw_group_vote", "fw_pool_best_subset", "fw_sync_status", "fw_prompt_attention", "fw_cache8_compact",
+           "fw_cache8_append", "fw_cache8_attend"):
     getattr(_lib, _f).restype = C.c_int
 
 
@@ -449,6 +475,173 @@ def selector_audit(rows: Rows, s, topk: dict, *, bits=False, stream=None):
                                 words, _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "fw_selector_audit")
     out["_ws"] = ws
+    return out
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _own_buffers(stream, *tensors):
+    # buffers made here on the current stream and used on another: not reused before that stream is done
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor = None, *,
+                     scale: float = None, out=None, stream=None):
+    """fw_prompt_attention.  q: bf16 [rows][q_heads][d], k and v: bf16 [rows][kv_heads][d], any strides that are
+    multiples of 8 with d contiguous; cu_q, cu_k: int32 [sequences + 1] row bounds (cu_k = cu_q if not given).
+    Returns a dict of o (bf16, as q), lse (fp32 [rows][q_heads]) and status [sequences]; such a dict passed as out
+    is written instead."""
+    cu_k = cu_q if cu_k is None else cu_k
+    rows, hq, d = q.shape
+    _need(q.dtype == k.dtype == v.dtype == torch.bfloat16, "q, k and v are bfloat16")
+    _need(k.shape == v.shape and k.shape[2] == d, "k and v are [rows][kv_heads][d], d as in q")
+    _need(d == 1 or (q.stride(2) == k.stride(2) == v.stride(2) == 1), "d is the contiguous axis of q, k and v")
+    _need(cu_q.dtype == cu_k.dtype == torch.int32 and cu_q.is_contiguous() and cu_k.is_contiguous() and
+          cu_q.shape == cu_k.shape and cu_q.dim() == 1, "cu_q and cu_k are contiguous int32 [sequences + 1]")
+    seqs = cu_q.numel() - 1
+    if out is None:
+        out = dict(o=torch.empty(rows, hq, d, dtype=torch.bfloat16, device=q.device),
+                   lse=torch.empty(rows, hq, dtype=torch.float32, device=q.device),
+                   status=torch.empty(max(seqs, 0), dtype=torch.int32, device=q.device))
+        _own_buffers(stream, *out.values())
+    o, lse, status = out["o"], out.get("lse"), out.get("status")
+    _need(o.shape == q.shape and o.dtype == torch.bfloat16 and o.is_contiguous(), "out['o'] is contiguous bfloat16, as q")
+    _need(lse is None or (lse.numel() >= rows * hq and lse.dtype == torch.float32 and lse.is_contiguous()),
+          "out['lse'] is contiguous float32 [rows][q_heads]")
+    _need(status is None or (status.numel() >= seqs and status.dtype == torch.int32 and status.is_contiguous()),
+          "out['status'] is contiguous int32 [sequences]")
+    p = FwPrompt(seqs, hq, k.shape[1], d, rows, k.shape[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), *_rh(q), *_rh(k),
+                 *_rh(v), cu_q.data_ptr(), cu_k.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale)
+    _check(_lib.fw_prompt_attention(C.byref(p), _ptr(o), _ptr(lse), _ptr(status), _stream(stream)),
+           "fw_prompt_attention")
+    return out
+
+
+def _rh(x):
+    """(row, head) strides of a [rows][heads][d] tensor; those of axes of one entry, which torch leaves open, in order."""
+    d = x.shape[2]
+    head = x.stride(1) if x.shape[1] > 1 else d
+    return (x.stride(0) if x.shape[0] > 1 else max(x.shape[1] * head, d)), head
+
+
+CACHE8_BLOCK, CACHE8_TAIL = 32, 64
+_CACHE8_FORMATS = {"e4m3": (0, torch.float8_e4m3fn), "int8": (1, torch.int8)}
+
+
+class Cache8:
+    """A ragged per-head store in 8 bits (fw_cache8) over the caller's tensors: codes k, v [rows][d] (float8_e4m3fn
+    for fmt "e4m3", int8 for "int8"), their scales fp32 [rows / 32], the open blocks' bf16 rows k_tail, v_tail
+    [cells][64][d], and base (int64), capacity and counts (int32), [cells] each."""
+
+    def __init__(self, *, fmt, k, v, k_scale, v_scale, k_tail, v_tail, base, capacity, counts):
+        _need(fmt in _CACHE8_FORMATS, f"fmt is one of {sorted(_CACHE8_FORMATS)}")
+        code, dtype = _CACHE8_FORMATS[fmt]
+        rows, d = k.shape
+        cells = base.numel()
+        _need(k.dtype == v.dtype == dtype and k.shape == v.shape, f"k and v are {dtype} [rows][d]")
+        _need(rows % CACHE8_BLOCK == 0 and k_scale.numel() == v_scale.numel() == rows // CACHE8_BLOCK and
+              k_scale.dtype == v_scale.dtype == torch.float32, "k_scale and v_scale are float32 [rows / 32]")
+        _need(k_tail.dtype == v_tail.dtype == torch.bfloat16 and
+              tuple(k_tail.shape) == tuple(v_tail.shape) == (cells, CACHE8_TAIL, d), "tails are bfloat16 [cells][64][d]")
+        _need(base.dtype == torch.int64 and capacity.dtype == counts.dtype == torch.int32 and
+              capacity.numel() == counts.numel() == cells, "base is int64, capacity and counts are int32, [cells] each")
+        self.tensors = (k, v, k_scale, v_scale, k_tail, v_tail, base, capacity, counts)
+        _need(all(t.is_contiguous() for t in self.tensors), "the store's tensors are contiguous")
+        self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail, self.base, self.capacity, self.counts = \
+            self.tensors
+        self.fmt, self.d, self.cells, self.device = fmt, d, cells, k.device
+        self.c = FwCache8(cells, d, code, rows, *(t.data_ptr() for t in self.tensors))
+        self._ref = C.byref(self.c)
+
+
+def cache8_empty(offsets: torch.Tensor, total: int, d: int, *, fmt: str = "e4m3", room: int = 0) -> Cache8:
+    """A store for cells of offsets[h + 1] - offsets[h] rows (offsets int64 [cells + 1] on the device, at most `total`
+    rows in all) and `room` more each.  Sized on the host from total alone: cell h starts at the multiple of 32 at or
+    behind offsets[h] + h (room + 31), which leaves it its rows without a prefix sum or a synchronisation."""
+    _need(fmt in _CACHE8_FORMATS, f"fmt is one of {sorted(_CACHE8_FORMATS)}")
+    cells, dev = offsets.numel() - 1, offsets.device
+    rows = (int(total) + cells * (room + 31) + 31) // 32 * 32
+    h = torch.arange(cells + 1, device=dev)
+    edge = (offsets + h * (room + 31) + 31) // 32 * 32
+    f = dict(dtype=_CACHE8_FORMATS[fmt][1], device=dev)
+    tail = dict(dtype=torch.bfloat16, device=dev)
+    return Cache8(fmt=fmt, k=torch.empty(rows, d, **f), v=torch.empty(rows, d, **f),
+                  k_scale=torch.empty(rows // 32, dtype=torch.float32, device=dev),
+                  v_scale=torch.empty(rows // 32, dtype=torch.float32, device=dev),
+                  k_tail=torch.empty(cells, CACHE8_TAIL, d, **tail), v_tail=torch.empty(cells, CACHE8_TAIL, d, **tail),
+                  base=edge[:-1].contiguous(), capacity=(edge[1:] - edge[:-1]).to(torch.int32),
+                  counts=torch.zeros(cells, dtype=torch.int32, device=dev))
+
+
+def cache8_compact(cache: Cache8, K: torch.Tensor, V: torch.Tensor, offsets: torch.Tensor, kept_pos: torch.Tensor, *,
+                   status: torch.Tensor = None, stream=None):
+    """fw_cache8_compact: the kept rows of K, V (bf16 [cells][T][d], equal strides that are multiples of 8, d
+    contiguous) quantised into the store, whose counts are set."""
+    cells, T, d = K.shape
+    _need(K.dtype == V.dtype == torch.bfloat16 and K.shape == V.shape and (cells, d) == (cache.cells, cache.d),
+          "K and V are bfloat16 [cells][T][d], as the store's")
+    cs, rs = (K.stride(0) if cells > 1 else T * d), (K.stride(1) if T > 1 else d)
+    _need(K.stride(2) == V.stride(2) == 1 and (cells == 1 or V.stride(0) == cs) and (T == 1 or V.stride(1) == rs),
+          "K and V have equal strides and d contiguous")
+    _need(offsets.dtype == torch.int64 and offsets.numel() == cells + 1 and kept_pos.dtype == torch.int32 and
+          offsets.is_contiguous() and kept_pos.is_contiguous(), "offsets is int64 [cells + 1], kept_pos int32")
+    _check(_lib.fw_cache8_compact(cache._ref, _ptr(K), _ptr(V), T, cs, rs, _ptr(offsets), _ptr(kept_pos),
+                                  kept_pos.numel(), _ptr(status), _stream(stream)), "fw_cache8_compact")
+
+
+def cache8_append(cache: Cache8, new_K: torch.Tensor, new_V: torch.Tensor, *, status: torch.Tensor = None, stream=None):
+    """fw_cache8_append: new_K, new_V (bf16 [cells][m][d], contiguous) behind each cell's rows."""
+    cells, m, d = new_K.shape
+    _need(new_K.dtype == new_V.dtype == torch.bfloat16 and new_K.shape == new_V.shape and new_K.is_contiguous() and
+          new_V.is_contiguous() and (cells, d) == (cache.cells, cache.d),
+          "new_K and new_V are contiguous bfloat16 [cells][m][d], as the store's")
+    _check(_lib.fw_cache8_append(cache._ref, _ptr(new_K), _ptr(new_V), m, _ptr(status), _stream(stream)),
+           "fw_cache8_append")
+
+
+def _cache8_query(cache, q, kv_heads, scale):
+    seqs, m, hq, d = q.shape
+    _need(q.dtype == torch.bfloat16 and q.stride(3) == 1 and d == cache.d, "q is bfloat16 [sequences][m][heads][d]")
+    _need(kv_heads >= 1 and hq % kv_heads == 0 and seqs * kv_heads == cache.cells,
+          "sequences x kv_heads is the store's cells, heads a multiple of kv_heads")
+    st = [q.stride(i) if q.shape[i] > 1 else d for i in range(3)]
+    return FwCache8Query(kv_heads, hq // kv_heads, m, q.data_ptr(), *st, 1.0 / math.sqrt(d) if scale is None else scale)
+
+
+def cache8_attend_workspace(cache: Cache8, q: torch.Tensor, *, kv_heads: int) -> torch.Tensor:
+    """A workspace for cache8_attend calls with queries of q's shape (fw_cache8_attend_workspace)."""
+    c_q = _cache8_query(cache, q, kv_heads, None)
+    return _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
+
+
+def cache8_attend(cache: Cache8, q: torch.Tensor, *, kv_heads: int, scale: float = None, out=None, workspace=None,
+                  stream=None):
+    """fw_cache8_attend.  q: bf16 [sequences][m][q_heads][d] (strides multiples of 8, d contiguous), the queries of
+    each sequence's last m tokens; the store's cells are [sequences][kv_heads].  Returns a dict of o (bf16, as q), lse
+    (fp32 [sequences][m][q_heads]) and status [cells]; such a dict passed as out is written instead."""
+    c_q = _cache8_query(cache, q, kv_heads, scale)
+    if out is None:
+        out = dict(o=torch.empty(q.shape, dtype=torch.bfloat16, device=q.device),
+                   lse=torch.empty(q.shape[:3], dtype=torch.float32, device=q.device),
+                   status=torch.empty(cache.cells, dtype=torch.int32, device=q.device))
+        _own_buffers(stream, *out.values())
+    o, lse, status = out["o"], out.get("lse"), out.get("status")
+    _need(o.shape == q.shape and o.dtype == torch.bfloat16 and o.is_contiguous(), "out['o'] is contiguous bfloat16, as q")
+    _need(lse is None or (lse.shape == q.shape[:3] and lse.dtype == torch.float32 and lse.is_contiguous()),
+          "out['lse'] is contiguous float32 [sequences][m][q_heads]")
+    _need(status is None or (status.numel() >= cache.cells and status.dtype == torch.int32 and status.is_contiguous()),
+          "out['status'] is contiguous int32 [cells]")
+    if workspace is None:
+        workspace = _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
+        _own_buffers(stream, workspace)
+    _check(_lib.fw_cache8_attend(cache._ref, C.byref(c_q), _ptr(o), _ptr(lse), _ptr(status), _ptr(workspace),
+                                 workspace.numel(), _stream(stream)), "fw_cache8_attend")
     return out
 
 

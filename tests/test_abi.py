@@ -112,3 +112,62 @@ def test_window_score_workspace_is_the_votes(lib, cells, T):
     # as the header states it: cells x T fp32 (in whole 256-byte units)
     lib.fw_window_score_workspace.restype = C.c_size_t
     assert lib.fw_window_score_workspace(cells, T) == (cells * T * 4 + 255) // 256 * 256
+
+
+def test_serving_entry_points_are_exported_and_refuse(lib):
+    """fw_prompt_attention and the fw_cache8 calls: bad arguments are answered on the host, nothing is launched."""
+    from paper_2608_25230_gb300 import fw
+
+    P = 256  # never read
+    I, U, W = fw.FW_ERR_INVALID_ARG, fw.FW_ERR_UNSUPPORTED, fw.FW_ERR_WORKSPACE
+    before = fw.launch_count()
+
+    def prompt(o=P, **kw):
+        a = dict(num_seqs=1, q_heads=8, kv_heads=2, d=64, total_q=4, total_k=4, q=P, k=P, v=P, q_row=512, q_head=64,
+                 k_row=128, k_head=64, v_row=128, v_head=64, cu_q=P, cu_k=P, scale=0.125)
+        a.update(kw)
+        return fw._lib.fw_prompt_attention(C.byref(fw.FwPrompt(**a)), o, P, P, None)
+
+    for want, kw in [(I, dict(num_seqs=0)), (I, dict(q_heads=7)), (I, dict(kv_heads=0)), (U, dict(d=96)),
+                     (U, dict(q_heads=258)), (I, dict(total_q=-1)), (U, dict(total_k=1 << 31)), (I, dict(q=264)),
+                     (I, dict(k=None)), (I, dict(k_row=4)), (I, dict(v_head=0)), (I, dict(q_head=-64)),
+                     (I, dict(cu_q=None)), (I, dict(scale=0.0)), (I, dict(scale=float("nan"))), (I, dict(o=None)),
+                     (I, dict(o=P + 8))]:
+        assert prompt(**kw) == want, kw
+    assert fw._lib.fw_prompt_attention(None, P, P, P, None) == I
+
+    def cache(**kw):
+        a = dict(cells=4, d=64, format=0, rows=64, k=P, v=P, k_scale=P, v_scale=P, k_tail=P, v_tail=P, base=P,
+                 capacity=P, counts=P)
+        a.update(kw)
+        return C.byref(fw.FwCache8(**a))
+
+    def query(**kw):
+        a = dict(kv_heads=2, group=4, m=1, q=P, q_seq=512, q_tok=512, q_head=64, scale=0.125)
+        a.update(kw)
+        return C.byref(fw.FwCache8Query(**a))
+
+    for want, kw in [(I, dict(cells=0)), (U, dict(d=32)), (I, dict(format=2)), (I, dict(rows=63)), (I, dict(k=None)),
+                     (I, dict(v=P + 8)), (I, dict(k_scale=None)), (I, dict(v_tail=None)), (I, dict(base=None)),
+                     (I, dict(counts=None))]:
+        c = cache(**kw)
+        assert fw._lib.fw_cache8_compact(c, P, P, 9, 576, 64, P, P, 4, P, None) == want, kw
+        assert fw._lib.fw_cache8_append(c, P, P, 1, P, None) == want, kw
+        assert fw._lib.fw_cache8_attend(c, query(), P, P, P, P, 1 << 40, None) == want, kw
+        assert fw._lib.fw_cache8_attend_workspace(c, query()) == 0
+    c = cache()
+    for args in [(None, P, 9, 576, 64, P, P, 4), (P, P + 2, 9, 576, 64, P, P, 4), (P, P, 0, 576, 64, P, P, 4),
+                 (P, P, 9, 576, 63, P, P, 4), (P, P, 9, -8, 64, P, P, 4), (P, P, 9, 576, 64, None, P, 4),
+                 (P, P, 9, 576, 64, P, None, 4), (P, P, 9, 576, 64, P, P, -1)]:
+        assert fw._lib.fw_cache8_compact(c, *args, P, None) == I, args
+    for args in [(None, P, 1), (P, P + 8, 1), (P, P, 0)]:
+        assert fw._lib.fw_cache8_append(c, *args, P, None) == I, args
+    for want, kw in [(I, dict(kv_heads=3)), (I, dict(kv_heads=0)), (I, dict(group=0)), (I, dict(m=0)), (I, dict(q=None)),
+                     (I, dict(q=P + 8)), (I, dict(q_tok=4)), (I, dict(scale=-1.0)), (U, dict(group=256, m=512))]:
+        assert fw._lib.fw_cache8_attend(c, query(**kw), P, P, P, P, 1 << 40, None) == want, kw
+    assert fw._lib.fw_cache8_attend(c, query(), None, P, P, P, 1 << 40, None) == I
+    need = fw._lib.fw_cache8_attend_workspace(c, query())
+    if need:
+        assert fw._lib.fw_cache8_attend(c, query(), P, P, P, P, need - 1, None) == W
+        assert fw._lib.fw_cache8_attend(c, query(), P, P, P, P + 8, need, None) == W
+    assert fw.launch_count() == before
