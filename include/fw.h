@@ -436,7 +436,8 @@ typedef struct {
     int32_t cells;
     int32_t d;                 /* 64 or 128                                       */
     int32_t format;            /* fw_cache8_format                                */
-    int64_t rows;              /* rows of the store, a multiple of FW_CACHE8_BLOCK */
+    int64_t rows;              /* rows of the store, a multiple of FW_CACHE8_BLOCK
+                                  below 2^31                                      */
     void *k, *v;               /* device [rows][d] codes, 16-byte aligned         */
     float *k_scale, *v_scale;  /* device [rows / FW_CACHE8_BLOCK]                 */
     void *k_tail, *v_tail;     /* device bf16 [cells][FW_CACHE8_TAIL][d], 16-byte aligned */

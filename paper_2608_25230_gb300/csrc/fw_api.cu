@@ -42,6 +42,19 @@ bool make_tma_2d_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tma_2d_bytes(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows)
+{
+    EncodeTiled enc = tma_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {cols};
+    const cuuint32_t box[2] = {(cuuint32_t)cols, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, cols == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 fw_status device_sms(int *sms)
 {
     static std::atomic<int> cache[64];
@@ -88,6 +101,7 @@ static fw_status check_cache8(const fw_cache8 *c)
     if (c->d != 64 && c->d != 128) return FW_ERR_UNSUPPORTED;
     if (!c->base || !c->capacity || !c->counts || !c->k_tail || !c->v_tail) return FW_ERR_INVALID_ARG;
     if (c->rows > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return FW_ERR_INVALID_ARG;
+    if (c->rows >= ((int64_t)1 << 31) || c->cells > (1 << 24)) return FW_ERR_UNSUPPORTED;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_tail, 16) || !aligned(c->v_tail, 16))
         return FW_ERR_INVALID_ARG;
     return FW_OK;
@@ -100,7 +114,7 @@ static fw_status check_cache8_query(const fw_cache8 *c, const fw_cache8_query *q
     if (!q || q->kv_heads < 1 || q->group < 1 || q->m < 1 || c->cells % q->kv_heads != 0 || !(q->scale > 0.f) ||
         !(q->scale < 1e30f))
         return FW_ERR_INVALID_ARG;
-    if ((int64_t)q->group * q->m > 65536) return FW_ERR_UNSUPPORTED;
+    if ((int64_t)q->group * q->m > 65535) return FW_ERR_UNSUPPORTED;
     if (!q->q || !aligned(q->q, 16) || q->q_seq % 8 != 0 || q->q_tok % 8 != 0 || q->q_head % 8 != 0)
         return FW_ERR_INVALID_ARG;
     return FW_OK;

@@ -119,6 +119,9 @@ fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, f
 // swizzle.  False if the driver's encoder is unavailable or refuses the map.
 bool make_tma_2d_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 
+// The same of bytes, [rows][cols] with cols 64 or 128, in boxes of whole rows swizzled over their length.
+bool make_tma_2d_bytes(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+
 // The fp32 FMA throughput probe (a measurement aid).
 fw_status fp32_fma_probe(int blocks, int iters, float *out, cudaStream_t s);
 
