@@ -122,6 +122,11 @@ bool make_tma_2d_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t 
 // The same of bytes, [rows][cols] with cols 64 or 128, in boxes of whole rows swizzled over their length.
 bool make_tma_2d_bytes(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 
+// A 3-D bf16 map [rows][heads][d] with free row and head strides (elements, multiples of 8), read in boxes of
+// box_rows x box_heads x 64 elements with the 128-byte swizzle: row-major, the head faster.
+bool make_tma_heads_bf16(CUtensorMap *m, const void *base, int d, int heads, int64_t rows, int64_t head_stride,
+                         int64_t row_stride, int box_heads, int box_rows);
+
 // The fp32 FMA throughput probe (a measurement aid).
 fw_status fp32_fma_probe(int blocks, int iters, float *out, cudaStream_t s);
 

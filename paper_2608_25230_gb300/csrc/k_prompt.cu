@@ -3,78 +3,466 @@
 // j <= lk - lq + i:
 //   x_j = scale q_i . k_j,  o_i = sum_j softmax_j(x) v_j,  lse_i = log sum_j e^x_j.
 //
-// A warp per (query row, head) goes over the keys with a running maximum and sum.
+// Bound: the tensor cores (two products of 128 x 128 x d per block of 128 keys).
+// The query heads of a KV head are rows of the same product, so a tile of 128 rows
+// is floor(128 / group) tokens with all their heads, and a CTA holds two tiles of
+// consecutive tokens against one stream of keys and values (TMA, 128-byte swizzle,
+// a ring of tiles).  On tcgen05, S = Q K^T goes to TMEM; the tile's four softmax
+// warps, a thread per row, read it, write the weights over it in bf16, and O += P V
+// takes them from there: while one tile's rows are in the softmax the other tile's
+// products run.  A weight is 2^(x - ref): ref is the row's maximum as of the last
+// time that it had grown by more than 2^8, so the rescaling of O in TMEM, which the
+// softmax threads do themselves, is rare; sum and output are of the same ref, so the
+// quotient is exact.  Warp 8 issues the copies, warp 9 the products (and owns the
+// TMEM).  Warp 10 looks over the values of blocks that some row does not see in full:
+// a weight of 0 does not make 0 of a NaN or an infinity, so it puts 0 in their place,
+// and the rows that do see them add them when they are written.
+//
+// Slots of 2 x floor(128 / group) tokens: sequence i's are numbered from
+// floor(cu_q[i] / slot) + i on, which leaves room for all of them without a prefix
+// sum; a CTA finds its sequence by a search over cu_q.  The last slots, whose rows
+// see the most keys, come first.
 #include <cuda_bf16.h>
 
 #include "fw_internal.h"
+#include "tc_sm100.cuh"
 
 namespace fw {
 namespace {
 
+constexpr int PK = 128;                  // keys of a block
+// blocks that some row of a slot does not see in full: the first and the last row's ends are
+// at most 255 keys apart
+constexpr int PG = 3;
+constexpr int PT = 32 * 11;              // 8 softmax warps, copies, products, guard
+constexpr uint32_t P_WAIT = 1u << 22;    // polls before a wait gives up
+constexpr float GROW = 8.f;              // octaves a row's maximum may be above its reference
+
 struct PromptArgs {
-    fw_prompt p;
+    const int32_t *cu_q, *cu_k;
+    int64_t total_q, total_k;
+    int num_seqs, q_heads, kv_heads, group, slots;
+    const uint16_t *v;
+    int64_t v_row, v_head;
     float scale2;  // scale * log2(e)
     uint16_t *o;
     float *lse;
     int32_t *status;
 };
 
-// sequence bounds within their ranges
-__device__ __forceinline__ bool seq_ok(const fw_prompt &p, int s)
+template <int D> struct PCfg {
+    static constexpr int NB = D / 64;              // 128-byte boxes across d
+    static constexpr int QT = 128 * D * 2;         // bytes of a tile of queries
+    static constexpr int KT = PK * D * 2;          // bytes of a tile of keys or values
+    static constexpr int STAGES = D == 128 ? 5 : 8;
+    static constexpr size_t SMEM = 1024 + 2 * QT + (size_t)STAGES * KT;
+    static constexpr uint32_t O_COL = 256;         // TMEM: S of the tiles at 0 and 128, O behind them
+};
+
+__device__ __forceinline__ float ex2(float x)
 {
-    const int q0 = p.cu_q[s], q1 = p.cu_q[s + 1], k0 = p.cu_k[s], k1 = p.cu_k[s + 1];
-    return q0 >= 0 && q1 >= q0 && q1 <= p.total_q && k0 >= 0 && k1 >= k0 && k1 <= p.total_k;
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void tma_load_3d(void *dst, const void *tmap, int x, int y, int z, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+        "[%5];" ::"r"(tc::smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(tc::smem_u32(bar))
+        : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, bool acc)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+                 "r"(a), "l"(bdesc), "r"(idesc), "r"((uint32_t)acc)
+                 : "memory");
+}
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// sequence bounds within their ranges
+__device__ __forceinline__ bool seq_ok(const PromptArgs &a, int s)
+{
+    const int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
+    return q0 >= 0 && q1 >= q0 && q1 <= a.total_q && k0 >= 0 && k1 >= k0 && k1 <= a.total_k;
 }
 
-template <int D> __global__ void __launch_bounds__(128) k_prompt(const PromptArgs a)
+template <int D>
+__global__ void __launch_bounds__(PT, 1)
+    k_prompt(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+             const __grid_constant__ CUtensorMap tmV, const PromptArgs a)
 {
-    constexpr int N = D / 32;
-    const fw_prompt &p = a.p;
-    const int lane = threadIdx.x & 31, head = blockIdx.y, hk = head / (p.q_heads / p.kv_heads);
-    if (blockIdx.x == 0 && blockIdx.y == 0 && a.status)
-        for (int s = threadIdx.x; s < p.num_seqs; s += 128) a.status[s] = seq_ok(p, s) ? FW_OK : FW_ERR_INVALID_ARG;
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (row >= p.total_q) return;
-    int lo = 0, hi = p.num_seqs;  // the last sequence that starts at or before the row
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (p.cu_q[mid] <= row) lo = mid; else hi = mid;
+    using C = PCfg<D>;
+    extern __shared__ uint8_t smraw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *sQ = sm, *sKV = sm + 2 * C::QT;
+    __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2], p_full[2], o_done[2], v_in[PG], v_ok[PG];
+    __shared__ uint32_t s_taddr;
+    __shared__ int s_seq, s_err, s_odd;
+
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const int slot = a.slots - 1 - (int)(blockIdx.x / a.kv_heads), hk = blockIdx.x % a.kv_heads;
+    const int TT = 128 / a.group, ST = 2 * TT;  // tokens of a tile and of a slot
+
+    if (blockIdx.x == 0 && a.status)  // (before any wait can have given up)
+        for (int s = tid; s < a.num_seqs; s += PT) a.status[s] = seq_ok(a, s) ? FW_OK : FW_ERR_INVALID_ARG;
+    if (wid == 0) {
+        // the last sequence whose slots start at or before this one: 32 probes at a time
+        int lo = 0, hi = a.num_seqs;
+        bool any = true;
+        do {
+            const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+            const unsigned hit = __ballot_sync(FW_FULL, i < hi && a.cu_q[min(i, hi - 1)] / ST + i <= slot);
+            if (hit == 0) {
+                any = false;
+                break;
+            }
+            lo += (__popc(hit) - 1) * step;
+            hi = min(lo + step, hi);
+        } while (hi - lo > 1);
+        if (lane == 0) s_seq = any ? lo : -1;
+    } else if (tid == 32) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            tc::mbar_init(&full[s], 1);
+            tc::mbar_init(&empty[s], 1);
+        }
+        tc::mbar_init(&q_full, 1);
+        for (int t = 0; t < 2; ++t) {
+            tc::mbar_init(&s_full[t], 1);
+            tc::mbar_init(&p_full[t], 4);
+            tc::mbar_init(&o_done[t], 1);
+        }
+        for (int g = 0; g < PG; ++g) {
+            tc::mbar_init(&v_in[g], 1);
+            tc::mbar_init(&v_ok[g], 1);
+        }
+        tc::mbar_init_fence();
+        s_err = 0;
+        s_odd = 0;
     }
-    if (!seq_ok(p, lo) || row < p.cu_q[lo] || row >= p.cu_q[lo + 1]) return;
-    const int k0 = p.cu_k[lo], lk = p.cu_k[lo + 1] - k0;
-    const int seen = lk - (p.cu_q[lo + 1] - p.cu_q[lo]) + (row - p.cu_q[lo]) + 1;
-    const uint16_t *q = (const uint16_t *)p.q + row * p.q_row + head * p.q_head;
-    float qv[N], acc[N], mx = -INFINITY;
-    double l = 0.0;  // (thousands of terms one after another)
-    for (int u = 0; u < N; ++u) qv[u] = bf16_to_f32(q[lane + 32 * u]), acc[u] = 0.f;
-    for (int j = 0; j < seen; ++j) {
-        const uint16_t *k = (const uint16_t *)p.k + (int64_t)(k0 + j) * p.k_row + hk * p.k_head;
-        const uint16_t *v = (const uint16_t *)p.v + (int64_t)(k0 + j) * p.v_row + hk * p.v_head;
-        float x = 0.f;
-        for (int u = 0; u < N; ++u) x = fmaf(qv[u], bf16_to_f32(k[lane + 32 * u]), x);
-        x = warp_sum(x) * a.scale2;
-        const float mn = fmaxf(mx, x), f = exp2f(mx - mn), e = exp2f(x - mn);
-        mx = mn;
-        l = l * f + e;
-        for (int u = 0; u < N; ++u) acc[u] = acc[u] * f + e * bf16_to_f32(v[lane + 32 * u]);
+    __syncthreads();
+    const int seq = s_seq;
+    if (seq < 0 || !seq_ok(a, seq)) return;
+    const int q0 = a.cu_q[seq], lq = a.cu_q[seq + 1] - q0, k0 = a.cu_k[seq], lk = a.cu_k[seq + 1] - k0;
+    const int t0 = (slot - (q0 / ST + seq)) * ST;  // the slot's first token in the sequence
+    if (t0 < 0 || t0 >= lq) return;
+    const int tiles = t0 + TT < lq ? 2 : 1;
+    // keys that the first token sees, and blocks of keys that each tile's last one does
+    const int seen0 = max(0, lk - lq + t0 + 1);
+    int nb[2];
+    nb[0] = (max(0, lk - lq + min(t0 + TT, lq)) + PK - 1) / PK;
+    nb[1] = tiles == 2 ? (max(0, lk - lq + min(t0 + ST, lq)) + PK - 1) / PK : 0;
+    const int J = max(nb[0], nb[1]), jm = seen0 / PK;  // blocks from jm on are not seen in full by every row
+
+    if (wid == 9) tc::tmem_alloc(&s_taddr, 512);
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t taddr = s_taddr;
+
+    // Copy i of the ring (K of block 0, V of block 0, K of block 1, ...) arrives on its stage's barrier;
+    // the values that the guard looks over on one of their own, which the guard can wait for without
+    // following the stage's phases (no stage of theirs is used again: at most five copies come behind the first).
+    static_assert(C::STAGES >= 2 * PG - 1, "stages of guarded values");
+    auto arrival = [&](int i) { return (i & 1) && (i >> 1) >= jm ? &v_in[min((i >> 1) - jm, PG - 1)] : &full[i % C::STAGES]; };
+    auto arrival_phase = [&](int i) { return (i & 1) && (i >> 1) >= jm ? 0u : (uint32_t)(i / C::STAGES) & 1u; };
+
+    if (wid == 8) {
+        // ------------------------------------------------------------ copies
+        if (lane == 0 && J > 0) {
+            tc::tma_prefetch_desc(&tmQ);
+            tc::tma_prefetch_desc(&tmK);
+            tc::tma_prefetch_desc(&tmV);
+            const uint32_t qbytes = (uint32_t)(128 * a.group * TT);  // (one box: 64 columns of a tile's rows)
+            tc::mbar_arrive_expect_tx(&q_full, qbytes * C::NB * tiles);
+            for (int t = 0; t < tiles; ++t)
+                for (int h = 0; h < C::NB; ++h)
+                    tma_load_3d(sQ + t * C::QT + h * (128 * 128), &tmQ, 64 * h, hk * a.group, q0 + t0 + t * TT, &q_full);
+            int issued = 0;
+            bool ok = true;
+            for (int i = 0; i < 2 * J; ++i) {
+                const int s = i % C::STAGES;
+                if (i >= C::STAGES && !tc::mbar_wait(&empty[s], (uint32_t)(i / C::STAGES - 1) & 1u, P_WAIT)) {
+                    ok = false;
+                    break;
+                }
+                uint64_t *bar = arrival(i);
+                tc::mbar_arrive_expect_tx(bar, C::KT);
+                for (int h = 0; h < C::NB; ++h)
+                    tma_load_3d(sKV + s * C::KT + h * (PK * 128), (i & 1) ? &tmV : &tmK, 64 * h, hk, k0 + (i >> 1) * PK, bar);
+                ++issued;
+            }
+            if (!ok) atomicOr(&s_err, 1);
+            // every copy has landed before the CTA's memory goes
+            for (int i = max(0, issued - C::STAGES); i < issued; ++i)
+                if (!tc::mbar_wait(arrival(i), arrival_phase(i), P_WAIT)) atomicOr(&s_err, 1);
+            if (!tc::mbar_wait(&q_full, 0, P_WAIT)) atomicOr(&s_err, 1);
+        }
+        __syncwarp();
+    } else if (wid == 9) {
+        // ---------------------------------------------------------- products
+        if (lane == 0 && J > 0) {
+            constexpr uint32_t id_s = tc::idesc_bf16_f32(128, PK, false, false);
+            constexpr uint32_t id_o = tc::idesc_bf16_f32(128, D, false, true);
+            const uint64_t qd = tc::sdesc_sw128(tc::smem_u32(sQ), 16, 1024);
+            const uint64_t kd = tc::sdesc_sw128(tc::smem_u32(sKV), 16, 1024);
+            const uint64_t vd = tc::sdesc_sw128(tc::smem_u32(sKV), PK * 128, 1024);
+            bool ok = tc::mbar_wait(&q_full, 0, P_WAIT);
+            auto wait_full = [&](int i) {
+                if (ok) ok = tc::mbar_wait(arrival(i), arrival_phase(i), P_WAIT);
+            };
+            auto qk = [&](int t, int j) {
+                const int s = (2 * j) % C::STAGES;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    const uint32_t off = (ks >> 2) * (128 * 128) + (ks & 3) * 32;
+                    tc::mma_bf16(taddr + t * PK, qd + ((t * C::QT + off) >> 4), kd + ((s * C::KT + off) >> 4), id_s, ks > 0);
+                }
+                tc::commit(&s_full[t]);
+            };
+            wait_full(0);
+            if (ok) {
+                tc::fence_after_sync();
+                for (int t = 0; t < tiles; ++t)
+                    if (nb[t] > 0) qk(t, 0);
+                tc::commit(&empty[0]);
+            }
+            int done[2] = {0, 0};
+            for (int j = 0; ok && j < J; ++j) {
+                if (j >= jm) ok = tc::mbar_wait(&v_ok[min(j - jm, PG - 1)], 0, P_WAIT);
+                wait_full(2 * j + 1);
+                if (j + 1 < J) wait_full(2 * j + 2);
+                const int s = (2 * j + 1) % C::STAGES;
+                for (int t = 0; t < tiles && ok; ++t) {
+                    if (j < nb[t]) {
+                        ok = tc::mbar_wait(&p_full[t], (uint32_t)j & 1u, P_WAIT);
+                        if (!ok) break;
+                        tc::fence_after_sync();
+#pragma unroll
+                        for (int ks = 0; ks < PK / 16; ++ks)
+                            mma_bf16_ts(taddr + C::O_COL + t * D, taddr + t * PK + ks * 8, vd + ((s * C::KT + ks * 2048) >> 4),
+                                        id_o, j > 0 || ks > 0);
+                        tc::commit(&o_done[t]);
+                        done[t] = j + 1;
+                    }
+                    if (t == tiles - 1) tc::commit(&empty[s]);
+                    if (j + 1 < nb[t]) qk(t, j + 1);
+                    if (t == tiles - 1 && j + 1 < J) tc::commit(&empty[(2 * j + 2) % C::STAGES]);
+                }
+            }
+            if (!ok) atomicOr(&s_err, 1);
+            // the products have completed before the TMEM can be freed
+            for (int t = 0; t < tiles; ++t)
+                if (done[t] > 0 && !tc::mbar_wait(&o_done[t], (uint32_t)(done[t] - 1) & 1u, P_WAIT)) atomicOr(&s_err, 1);
+        }
+        __syncwarp();
+    } else if (wid == 10) {
+        // ------------------------------------------------------------- guard
+        bool ok = true;
+        for (int j = jm; ok && j < J; ++j) {
+            const int s = (2 * j + 1) % C::STAGES;
+            ok = tc::mbar_wait(&v_in[min(j - jm, PG - 1)], 0, P_WAIT);
+            if (!ok) break;
+            uint4 *v = reinterpret_cast<uint4 *>(sKV + s * C::KT);
+            bool odd = false;
+#pragma unroll 8
+            for (int p = lane; p < C::KT / 16; p += 32) {
+                const uint4 x = v[p];
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                bool bad = false;
+#pragma unroll
+                for (int z = 0; z < 4; ++z) bad |= (w[z] & 0x7f80u) == 0x7f80u || (w[z] & 0x7f800000u) == 0x7f800000u;
+                if (bad) {
+                    uint32_t y[4];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        y[z] = ((w[z] & 0x7f80u) == 0x7f80u ? 0u : w[z] & 0xffffu) |
+                               ((w[z] & 0x7f800000u) == 0x7f800000u ? 0u : w[z] & 0xffff0000u);
+                    v[p] = make_uint4(y[0], y[1], y[2], y[3]);
+                    odd = true;
+                }
+            }
+            if (__any_sync(FW_FULL, odd)) {
+                tc::fence_async_smem();
+                s_odd = 1;
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&v_ok[min(j - jm, PG - 1)]);
+        }
+        if (!ok && lane == 0) atomicOr(&s_err, 1);
+    } else {
+        // ----------------------------------------------------------- softmax
+        const int t = wid >> 2, r = tid & 127;
+        if (t < tiles) {
+            const int tok = min(t0 + t * TT + r / a.group, lq - 1);
+            const bool live = r < TT * a.group && t0 + t * TT + r / a.group < lq;
+            const int seen = max(0, lk - lq + tok + 1), n = nb[t];
+            const uint32_t lanes = (uint32_t)((wid & 3) * 32) << 16;
+            const uint32_t sS = taddr + lanes + t * PK, sO = taddr + lanes + C::O_COL + t * D;
+            const float c2 = a.scale2;
+            float ref = -INFINITY, l = 0.f;
+            bool ok = true;
+            for (int j = 0; j < n; ++j) {
+                if (ok) ok = tc::mbar_wait(&s_full[t], (uint32_t)j & 1u, P_WAIT);
+                if (!__all_sync(FW_FULL, ok)) {
+                    ok = false;
+                    break;
+                }
+                tc::fence_after_sync();
+                float x[PK];
+#pragma unroll
+                for (int i = 0; i < PK; i += 32) tc::ld32(sS + i, *reinterpret_cast<float(*)[32]>(x + i));
+                if (__any_sync(FW_FULL, (j + 1) * PK > seen)) {
+                    const int lim = seen - j * PK;
+#pragma unroll
+                    for (int i = 0; i < PK; ++i) x[i] = i < lim ? x[i] : -INFINITY;
+                }
+                float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                for (int i = 4; i < PK; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
+                const float xm = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c2;
+                const bool need = xm > ref + GROW;
+                if (__any_sync(FW_FULL, need)) {
+                    const float now = need ? xm : ref;  // (a row's result does not depend on its neighbours)
+                    const float f = now == ref ? 1.f : ex2(ref - now);
+                    l *= f;
+                    ref = now;
+                    if (j > 0) {
+                        ok = tc::mbar_wait(&o_done[t], (uint32_t)(j - 1) & 1u, P_WAIT);
+                        if (!__all_sync(FW_FULL, ok)) {
+                            ok = false;
+                            break;
+                        }
+                        tc::fence_after_sync();
+#pragma unroll 1
+                        for (int i = 0; i < D; i += 32) {
+                            float y[32];
+                            tc::ld32(sO + i, y);
+                            uint32_t z[32];
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) z[e] = __float_as_uint(y[e] * f);
+                            st32(sO + i, z);
+                        }
+                        wait_st();
+                    }
+                }
+                const float off = ref == -INFINITY ? 0.f : ref;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int i = 0; i < 64; i += 2) {
+                        const float u = ex2(fmaf(x[64 * h + i], c2, -off)), w = ex2(fmaf(x[64 * h + i + 1], c2, -off));
+                        sum[(i >> 1) & 3] += u + w;
+                        p[i >> 1] = pack_bf16(u, w);
+                    }
+                    st32(sS + 32 * h, p);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                wait_st();
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&p_full[t]);
+            }
+            // ------------------------------------------------------ epilogue
+            if (ok && n > 0) ok = tc::mbar_wait(&o_done[t], (uint32_t)(n - 1) & 1u, P_WAIT);
+            if (ok && J > jm) ok = tc::mbar_wait(&v_ok[min(J - 1 - jm, PG - 1)], 0, P_WAIT);  // (the guard is done)
+            ok = __all_sync(FW_FULL, ok);
+            if (!ok && lane == 0) atomicOr(&s_err, 1);
+            tc::fence_after_sync();
+            const bool odd = *(volatile int *)&s_odd != 0;
+            const int64_t row = (int64_t)(q0 + tok) * a.q_heads + hk * a.group + r % a.group;
+            const float inv = !ok ? NAN : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+            for (int i = 0; i < D; i += 32) {
+                float y[32];
+                if (ok && n > 0) {
+                    tc::ld32(sO + i, y);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) y[e] = l == 0.f && ok ? 0.f : y[e] * inv;
+                if (odd && live) {  // the values the guard took out, for the rows that see them
+                    for (int j = jm * PK; j < seen; ++j) {
+                        const uint16_t *src = a.v + (int64_t)(k0 + j) * a.v_row + hk * a.v_head + i;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const uint16_t b = src[e];
+                            if ((b & 0x7f80u) == 0x7f80u) y[e] += bf16_to_f32(b);
+                        }
+                    }
+                }
+                if (live) {
+                    uint4 *dst = reinterpret_cast<uint4 *>(a.o + row * D + i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        dst[e] = make_uint4(pack_bf16(y[8 * e], y[8 * e + 1]), pack_bf16(y[8 * e + 2], y[8 * e + 3]),
+                                            pack_bf16(y[8 * e + 4], y[8 * e + 5]), pack_bf16(y[8 * e + 6], y[8 * e + 7]));
+                }
+            }
+            if (live && a.lse)
+                a.lse[row] = !ok ? NAN : l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+        }
     }
-    const int64_t out = (int64_t)row * p.q_heads + head;
-    for (int u = 0; u < N; ++u)
-        a.o[out * D + lane + 32 * u] = __bfloat16_as_ushort(__float2bfloat16_rn(seen > 0 ? acc[u] / (float)l : 0.f));
-    if (a.lse && lane == 0) a.lse[out] = seen > 0 ? (mx + log2f((float)l)) * 0.6931471805599453f : -INFINITY;
+    tc::fence_before_sync();
+    __syncthreads();
+    if (tid == 0 && s_err && a.status) a.status[seq] = FW_ERR_TIMEOUT;
+    if (wid == 9) {
+        tc::fence_after_sync();
+        tc::tmem_dealloc(taddr, 512);
+    }
 }
 
 }  // namespace
 
 fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *status, cudaStream_t s)
 {
-    const PromptArgs a{p, p.scale * 1.4426950408889634f, (uint16_t *)o, lse, status};
-    if (p.q_heads > 65535) return FW_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((p.total_q + 3) / 4), (unsigned)p.q_heads);
-    if (p.d == 128)
-        FW_LAUNCH(k_prompt<128>, grid, 128, 0, s, a);
-    else
-        FW_LAUNCH(k_prompt<64>, grid, 128, 0, s, a);
+    const int group = p.q_heads / p.kv_heads, TT = 128 / group, ST = 2 * TT;
+    const int64_t slots = p.total_q / ST + p.num_seqs;
+    if (slots * p.kv_heads >= ((int64_t)1 << 31)) return FW_ERR_UNSUPPORTED;
+    CUtensorMap mq, mk, mv;
+    // (without keys no copy is issued: any valid map does)
+    const bool keys = p.total_k > 0;
+    if (!make_tma_heads_bf16(&mq, p.q, p.d, p.q_heads, p.total_q, p.q_head, p.q_row, group, TT) ||
+        !make_tma_heads_bf16(&mk, keys ? p.k : p.q, p.d, p.kv_heads, keys ? p.total_k : 1, keys ? p.k_head : p.d,
+                             keys ? p.k_row : (int64_t)p.d * p.kv_heads, 1, PK) ||
+        !make_tma_heads_bf16(&mv, keys ? p.v : p.q, p.d, p.kv_heads, keys ? p.total_k : 1, keys ? p.v_head : p.d,
+                             keys ? p.v_row : (int64_t)p.d * p.kv_heads, 1, PK))
+        return FW_ERR_CUDA;
+    const PromptArgs a{p.cu_q,  p.cu_k,     p.total_q, p.total_k, p.num_seqs, p.q_heads, p.kv_heads,
+                       group,   (int)slots, (const uint16_t *)p.v, p.v_row,   p.v_head,  p.scale * 1.4426950408889634f,
+                       (uint16_t *)o, lse,  status};
+    const unsigned grid = (unsigned)(slots * p.kv_heads);
+    if (p.d == 128) {
+        FW_CUDA_CHECK(cudaFuncSetAttribute(k_prompt<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PCfg<128>::SMEM));
+        FW_LAUNCH(k_prompt<128>, grid, PT, PCfg<128>::SMEM, s, mq, mk, mv, a);
+    } else {
+        FW_CUDA_CHECK(cudaFuncSetAttribute(k_prompt<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PCfg<64>::SMEM));
+        FW_LAUNCH(k_prompt<64>, grid, PT, PCfg<64>::SMEM, s, mq, mk, mv, a);
+    }
     return FW_OK;
 }
 
