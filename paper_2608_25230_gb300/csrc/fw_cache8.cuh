@@ -53,42 +53,54 @@ template <int FMT> __device__ __forceinline__ int scale_exponent(uint32_t a)
     return max(-120, (int)(a >> 7) - 127 - up + ((a & 0x7f) > mant ? 1 : 0));
 }
 
-// Largest finite magnitude (bf16 bits) of 8 values into top; true where one is not finite.
-__device__ __forceinline__ bool piece_top(const uint4 &x, uint32_t &top)
+// bf16 bits of the largest code times 2^e, M 2^e (-120 <= e <= 119)
+template <int FMT> __device__ __forceinline__ uint32_t top_code_bits(int e)
 {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = w[i] & 0x7fff, hi = (w[i] >> 16) & 0x7fff;
-        odd |= lo >= 0x7f80 || hi >= 0x7f80;
-        top = max(top, max(lo >= 0x7f80 ? 0u : lo, hi >= 0x7f80 ? 0u : hi));
-    }
-    return odd;
+    return FMT == FW_CACHE8_E4M3 ? (uint32_t)(e + 8 + 127) << 7 | 0x60u : (uint32_t)(e + 6 + 127) << 7 | 0x7eu;
 }
 
-// Codes of two values already divided by the scale; infinities saturate, NaN is 0.
-template <int FMT> __device__ __forceinline__ uint32_t encode2(float a, float b)
+// Largest magnitudes (bf16 bits) of the even and the odd ones of 8 values into the halves of top;
+// infinities and NaN are the largest (0x7f80 and above).
+__device__ __forceinline__ uint32_t piece_top(const uint4 &x, uint32_t top)
 {
-    a = a != a ? 0.f : a;
-    b = b != b ? 0.f : b;
-    if constexpr (FMT == FW_CACHE8_E4M3) {
-        uint16_t r;  // (the second operand is the low byte)
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-        return r;
-    } else {
-        const int i = __float2int_rn(fminf(fmaxf(a, -127.f), 127.f)), j = __float2int_rn(fminf(fmaxf(b, -127.f), 127.f));
-        return (uint32_t)(i & 0xff) | (uint32_t)(j & 0xff) << 8;
-    }
+    const uint32_t m = 0x7fff7fffu;
+    return __vmaxu2(__vmaxu2(__vmaxu2(top, x.x & m), __vmaxu2(x.y & m, x.z & m)), x.w & m);
 }
+__device__ __forceinline__ uint32_t top_of(uint32_t pair) { return max(pair & 0xffffu, pair >> 16); }
+
+// 8 values with their NaN put to 0 and their infinities to the largest magnitude `lim` (bf16 bits).
+__device__ __forceinline__ uint4 finite_piece(const uint4 &x, uint32_t lim)
+{
+    uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int sh = 16 * (i & 1);
+        const uint32_t b = (w[i >> 1] >> sh) & 0xffffu, mag = b & 0x7fffu;
+        const uint32_t y = mag > 0x7f80u ? 0u : mag == 0x7f80u ? (b & 0x8000u) | lim : b;
+        w[i >> 1] = (w[i >> 1] & ~(0xffffu << sh)) | y << sh;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Codes of 8 values times inv, whose magnitudes are at most the largest code.
 template <int FMT> __device__ __forceinline__ uint2 encode8(const uint4 &x, float inv)
 {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     uint32_t r[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        r[i] = encode2<FMT>(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
-    return make_uint2(r[0] | r[1] << 16, r[2] | r[3] << 16);
+    for (int i = 0; i < 4; ++i) {
+        const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xffff0000u);
+        if constexpr (FMT == FW_CACHE8_E4M3) {
+            uint16_t c;  // (the second operand is the low byte)
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(b * inv), "f"(a * inv));
+            r[i] = c;
+        } else {
+            // the sum's one rounding is to the integer, whose low byte is the sum's
+            const float up = 12582912.f;  // 1.5 * 2^23
+            r[i] = __byte_perm(__float_as_uint(fmaf(a, inv, up)), __float_as_uint(fmaf(b, inv, up)), 0x0040);
+        }
+    }
+    return make_uint2(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410));
 }
 
 }  // namespace cache8

@@ -270,8 +270,9 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
 #pragma unroll
                 for (int f = 0; f < 2; ++f) {
                     x[e][f] = r < rows ? *reinterpret_cast<const uint4 *>(src + 64 * e + 16 * c + 8 * f) : make_uint4(0, 0, 0, 0);
-                    piece_top(x[e][f], top);
+                    top = piece_top(x[e][f], top);
                 }
+            top = top_of(top);
             top = max(top, __shfl_xor_sync(FW_FULL, top, 1));
             top = max(top, __shfl_xor_sync(FW_FULL, top, 2));
             // the largest magnitude's exponent to 14 (2^14 .. 2^15)

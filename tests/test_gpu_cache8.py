@@ -378,3 +378,46 @@ def test_attend_offsets_past_32_bits(fw):
     check_cell(cache, 1, 0, torch.cat([K[1], new[1]]))
     check_cell(cache, 0, 1, torch.cat([V[0, :40], new[0]]))
     check_attend(cache, q, out, 2, float(torch.tensor(1 / math.sqrt(d), dtype=torch.float32)))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_compact_many_cells_of_unlike_counts(fw, fmt):
+    """Thousands of cells, most with fewer rows than a block, some empty; without a status too."""
+    cells, T, d = 3001, 70, 64
+    gen = torch.Generator("cuda").manual_seed(21)
+    counts = torch.randint(0, 71, (cells,), generator=torch.Generator().manual_seed(21)) * (torch.arange(cells) % 3 != 1)
+    counts[1500:1700] = 0
+    counts = counts.tolist()
+    K, V = rand(gen, cells, T, d), rand(gen, cells, T, d)
+    pos, o = picks(gen, counts, T), off(counts)
+    caches = [fw.cache8_empty(o, pos.numel(), d, fmt=fmt) for _ in range(2)]
+    st = torch.empty(cells, dtype=torch.int32, device="cuda")
+    fw.cache8_compact(caches[0], K, V, o, pos, status=st)
+    fw.cache8_compact(caches[1], K, V, o, pos)
+    torch.cuda.synchronize()
+    assert not bool(st.any()) and caches[1].counts.tolist() == counts
+    for h in list(range(0, cells, 97)) + [1499, 1500, 1699, 1700, cells - 1]:
+        for c in caches:
+            p = pos[int(o[h]):int(o[h + 1])].long()
+            check_cell(c, h, 0, K[h, p])
+            check_cell(c, h, 1, V[h, p])
+
+
+def test_long_appends_report_and_refuse(fw):
+    """Appends of several blocks: non-finite rows and full cells, cell by cell."""
+    gen = torch.Generator("cuda").manual_seed(22)
+    d, start, m = 128, [5, 40, 32], 150
+    K = rand(gen, 3, 64, d)
+    o, pos = off(start), torch.cat([torch.arange(c, device="cuda") for c in start]).to(torch.int32)
+    cache = fw.cache8_empty(o, pos.numel(), d, room=m)
+    fw.cache8_compact(cache, K, K, o, pos)
+    cache.capacity[1] = 40 + m - 1
+    new = rand(gen, 3, m, d)
+    new[2, 77, 5] = float("inf")
+    st = torch.empty(3, dtype=torch.int32, device="cuda")
+    fw.cache8_append(cache, new, new, status=st)
+    torch.cuda.synchronize()
+    assert st.tolist() == [0, fw.FW_ERR_WORKSPACE, fw.FW_ERR_NONFINITE]
+    for h in (0, 2):
+        check_cell(cache, h, 1, torch.cat([K[h, :start[h]], new[h]]))
+    check_cell(cache, 1, 0, K[1, :40])
