@@ -13,8 +13,8 @@
 // products run.  A weight is 2^(x - ref): ref is the row's maximum as of the last
 // time that it had grown by more than 2^8, so the rescaling of O in TMEM, which the
 // softmax threads do themselves, is rare; sum and output are of the same ref, so the
-// quotient is exact.  Warp 8 issues the copies, warp 9 the products (and owns the
-// TMEM).  Warp 10 looks over the values of blocks that some row does not see in full:
+// quotient is exact.  Warp 8 issues the copies, warps 9 and 11 the products of a
+// tile each (9 owns the TMEM).  Warp 10 looks over the values of blocks that some row does not see in full:
 // a weight of 0 does not make 0 of a NaN or an infinity, so it puts 0 in their place,
 // and the rows that do see them add them when they are written.
 //
@@ -31,10 +31,11 @@ namespace fw {
 namespace {
 
 constexpr int PK = 128;                  // keys of a block
+constexpr int PC = 1;                    // parts of a block's weights, handed over one by one
 // blocks that some row of a slot does not see in full: the first and the last row's ends are
 // at most 255 keys apart
 constexpr int PG = 3;
-constexpr int PT = 32 * 11;              // 8 softmax warps, copies, products, guard
+constexpr int PT = 32 * 12;              // 8 softmax warps, copies, products of a tile, guard, of the other
 constexpr uint32_t P_WAIT = 1u << 22;    // polls before a wait gives up
 constexpr float GROW = 8.f;              // octaves a row's maximum may be above its reference
 
@@ -87,6 +88,69 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t bde
                  "r"(a), "l"(bdesc), "r"(idesc), "r"((uint32_t)acc)
                  : "memory");
 }
+// 128 consecutive fp32 columns of this warp's 32 TMEM lanes, waited on in the same statement
+__device__ __forceinline__ void ld128(uint32_t taddr, float (&v)[128])
+{
+    uint32_t r[128];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x128.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, "
+        "%35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, "
+        "%56, %57, %58, %59, %60, %61, %62, %63, %64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, "
+        "%77, %78, %79, %80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, %96, %97, "
+        "%98, %99, %100, %101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, %112, %113, %114, "
+        "%115, %116, %117, %118, %119, %120, %121, %122, %123, %124, %125, %126, %127}, [%128];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]),
+          "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
+          "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
+          "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
+          "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]),
+          "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]),
+          "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]),
+          "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]),
+          "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]),
+          "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]),
+          "=r"(r[104]), "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]),
+          "=r"(r[111]), "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]),
+          "=r"(r[118]), "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]),
+          "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 128; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\t"
+        "mov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
 __device__ __forceinline__ void st32(uint32_t taddr, const uint32_t *r)
 {
     asm volatile(
@@ -99,6 +163,23 @@ __device__ __forceinline__ void st32(uint32_t taddr, const uint32_t *r)
         : "memory");
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// true for one lane of a warp that is there as a whole
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
+// a warp's stores to TMEM are complete and known to the products' warp
+__device__ __forceinline__ void hand_over(uint64_t *bar, int lane)
+{
+    wait_st();
+    tc::fence_before_sync();
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(bar);
+}
 
 // sequence bounds within their ranges
 __device__ __forceinline__ bool seq_ok(const PromptArgs &a, int s)
@@ -116,7 +197,7 @@ __global__ void __launch_bounds__(PT, 1)
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
     uint8_t *sQ = sm, *sKV = sm + 2 * C::QT;
-    __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2], p_full[2], o_done[2], v_in[PG], v_ok[PG];
+    __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2], p_full[2][PC], o_done[2], drained[2], v_in[PG], v_ok[PG];
     __shared__ uint32_t s_taddr;
     __shared__ int s_seq, s_err, s_odd;
 
@@ -141,24 +222,6 @@ __global__ void __launch_bounds__(PT, 1)
             hi = min(lo + step, hi);
         } while (hi - lo > 1);
         if (lane == 0) s_seq = any ? lo : -1;
-    } else if (tid == 32) {
-        for (int s = 0; s < C::STAGES; ++s) {
-            tc::mbar_init(&full[s], 1);
-            tc::mbar_init(&empty[s], 1);
-        }
-        tc::mbar_init(&q_full, 1);
-        for (int t = 0; t < 2; ++t) {
-            tc::mbar_init(&s_full[t], 1);
-            tc::mbar_init(&p_full[t], 4);
-            tc::mbar_init(&o_done[t], 1);
-        }
-        for (int g = 0; g < PG; ++g) {
-            tc::mbar_init(&v_in[g], 1);
-            tc::mbar_init(&v_ok[g], 1);
-        }
-        tc::mbar_init_fence();
-        s_err = 0;
-        s_odd = 0;
     }
     __syncthreads();
     const int seq = s_seq;
@@ -174,6 +237,26 @@ __global__ void __launch_bounds__(PT, 1)
     nb[1] = tiles == 2 ? (max(0, lk - lq + min(t0 + ST, lq)) + PK - 1) / PK : 0;
     const int J = max(nb[0], nb[1]), jm = seen0 / PK;  // blocks from jm on are not seen in full by every row
 
+    if (tid == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            tc::mbar_init(&full[s], 1);
+            tc::mbar_init(&empty[s], tiles);
+        }
+        tc::mbar_init(&q_full, 1);
+        for (int t = 0; t < 2; ++t) {
+            tc::mbar_init(&s_full[t], 1);
+            for (int c = 0; c < PC; ++c) tc::mbar_init(&p_full[t][c], 4);
+            tc::mbar_init(&o_done[t], 1);
+            tc::mbar_init(&drained[t], 1);
+        }
+        for (int g = 0; g < PG; ++g) {
+            tc::mbar_init(&v_in[g], 1);
+            tc::mbar_init(&v_ok[g], 1);
+        }
+        tc::mbar_init_fence();
+        s_err = 0;
+        s_odd = 0;
+    }
     if (wid == 9) tc::tmem_alloc(&s_taddr, 512);
     tc::fence_before_sync();
     __syncthreads();
@@ -219,61 +302,83 @@ __global__ void __launch_bounds__(PT, 1)
             if (!tc::mbar_wait(&q_full, 0, P_WAIT)) atomicOr(&s_err, 1);
         }
         __syncwarp();
-    } else if (wid == 9) {
+    } else if (wid == 9 || wid == 11) {
         // ---------------------------------------------------------- products
-        if (lane == 0 && J > 0) {
+        // A warp per tile: what issuing costs (waits, commits) hides behind the other tile's products.  The
+        // whole warp waits and an elected lane issues: with the waits inside the one lane's branch the
+        // operands are not kept in uniform registers, and an instruction took 100 clocks to issue.
+        const int t = wid == 11;
+        if (t < tiles && J > 0) {
             constexpr uint32_t id_s = tc::idesc_bf16_f32(128, PK, false, false);
             constexpr uint32_t id_o = tc::idesc_bf16_f32(128, D, false, true);
-            const uint64_t qd = tc::sdesc_sw128(tc::smem_u32(sQ), 16, 1024);
+            const uint64_t qd = tc::sdesc_sw128(tc::smem_u32(sQ) + t * C::QT, 16, 1024);
             const uint64_t kd = tc::sdesc_sw128(tc::smem_u32(sKV), 16, 1024);
             const uint64_t vd = tc::sdesc_sw128(tc::smem_u32(sKV), PK * 128, 1024);
+            const uint32_t tS = taddr + t * PK, tO = taddr + C::O_COL + t * D;
+            const int n = nb[t];
             bool ok = tc::mbar_wait(&q_full, 0, P_WAIT);
-            auto wait_full = [&](int i) {
-                if (ok) ok = tc::mbar_wait(arrival(i), arrival_phase(i), P_WAIT);
+            int st = 0;         // stage of the next copy of the ring
+            uint32_t ph = 0;    // and its phase
+            auto wait_copy = [&](bool guarded, int j) {
+                if (ok) ok = guarded ? tc::mbar_wait(&v_ok[min(j - jm, PG - 1)], 0, P_WAIT) &&
+                                           tc::mbar_wait(&v_in[min(j - jm, PG - 1)], 0, P_WAIT)
+                                     : tc::mbar_wait(&full[st], ph, P_WAIT);
+                const int s = st;
+                if (++st == C::STAGES) st = 0, ph ^= 1u;
+                return s;
             };
-            auto qk = [&](int t, int j) {
-                const int s = (2 * j) % C::STAGES;
+            auto qk = [&](int s) {  // S = Q K^T
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
                     const uint32_t off = (ks >> 2) * (128 * 128) + (ks & 3) * 32;
-                    tc::mma_bf16(taddr + t * PK, qd + ((t * C::QT + off) >> 4), kd + ((s * C::KT + off) >> 4), id_s, ks > 0);
+                    tc::mma_bf16(tS, qd + (off >> 4), kd + ((s * C::KT + off) >> 4), id_s, ks > 0);
                 }
                 tc::commit(&s_full[t]);
+                tc::commit(&empty[s]);
             };
-            wait_full(0);
-            if (ok) {
+            const int s0 = wait_copy(false, 0);
+            ok = __all_sync(FW_FULL, ok);
+            if (ok && n > 0) {
                 tc::fence_after_sync();
-                for (int t = 0; t < tiles; ++t)
-                    if (nb[t] > 0) qk(t, 0);
-                tc::commit(&empty[0]);
+                if (elect_one()) qk(s0);
+                __syncwarp();
             }
-            int done[2] = {0, 0};
-            for (int j = 0; ok && j < J; ++j) {
-                if (j >= jm) ok = tc::mbar_wait(&v_ok[min(j - jm, PG - 1)], 0, P_WAIT);
-                wait_full(2 * j + 1);
-                if (j + 1 < J) wait_full(2 * j + 2);
-                const int s = (2 * j + 1) % C::STAGES;
-                for (int t = 0; t < tiles && ok; ++t) {
-                    if (j < nb[t]) {
-                        ok = tc::mbar_wait(&p_full[t], (uint32_t)j & 1u, P_WAIT);
-                        if (!ok) break;
-                        tc::fence_after_sync();
+            int done = 0;
+            for (int j = 0; ok && j < n; ++j) {
+                const int sv = wait_copy(j >= jm, j), sk = j + 1 < n ? wait_copy(false, 0) : 0;
 #pragma unroll
-                        for (int ks = 0; ks < PK / 16; ++ks)
-                            mma_bf16_ts(taddr + C::O_COL + t * D, taddr + t * PK + ks * 8, vd + ((s * C::KT + ks * 2048) >> 4),
-                                        id_o, j > 0 || ks > 0);
-                        tc::commit(&o_done[t]);
-                        done[t] = j + 1;
+                for (int c = 0; c < PC; ++c) {
+                    ok = __all_sync(FW_FULL, ok && tc::mbar_wait(&p_full[t][c], (uint32_t)j & 1u, P_WAIT));
+                    if (!ok) break;
+                    tc::fence_after_sync();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = c * (PK / 16 / PC); ks < (c + 1) * (PK / 16 / PC); ++ks)  // O += P V
+                            mma_bf16_ts(tO, tS + ks * 8, vd + ((sv * C::KT + ks * 2048) >> 4), id_o, j > 0 || ks > 0);
+                        if (c == PC - 1) {
+                            tc::commit(&o_done[t]);
+                            tc::commit(&empty[sv]);
+                            if (j + 1 < n) qk(sk);
+                        }
                     }
-                    if (t == tiles - 1) tc::commit(&empty[s]);
-                    if (j + 1 < nb[t]) qk(t, j + 1);
-                    if (t == tiles - 1 && j + 1 < J) tc::commit(&empty[(2 * j + 2) % C::STAGES]);
+                    __syncwarp();
+                    if (c == PC - 1) done = j + 1;
                 }
             }
-            if (!ok) atomicOr(&s_err, 1);
+            // blocks that only the other tile's rows see: their stages are free as far as this tile goes
+            if (n == 0 && ok && lane == 0) tc::mbar_arrive(&empty[s0]);
+            for (int i = max(2 * n, 1); ok && i < 2 * J; ++i) {
+                const int s = wait_copy((i & 1) && (i >> 1) >= jm, i >> 1);
+                if (ok && lane == 0) tc::mbar_arrive(&empty[s]);
+            }
+            if (!__all_sync(FW_FULL, ok)) atomicOr(&s_err, 1);
             // the products have completed before the TMEM can be freed
-            for (int t = 0; t < tiles; ++t)
-                if (done[t] > 0 && !tc::mbar_wait(&o_done[t], (uint32_t)(done[t] - 1) & 1u, P_WAIT)) atomicOr(&s_err, 1);
+            if (done > 0 && !tc::mbar_wait(&o_done[t], (uint32_t)(done - 1) & 1u, P_WAIT)) atomicOr(&s_err, 1);
+            if (!ok) {  // (and those issued before a wait gave up)
+                if (elect_one()) tc::commit(&drained[t]);
+                __syncwarp();
+                tc::mbar_wait(&drained[t], 0, P_WAIT);
+            }
         }
         __syncwarp();
     } else if (wid == 10) {
@@ -330,17 +435,24 @@ __global__ void __launch_bounds__(PT, 1)
                 }
                 tc::fence_after_sync();
                 float x[PK];
-#pragma unroll
-                for (int i = 0; i < PK; i += 32) tc::ld32(sS + i, *reinterpret_cast<float(*)[32]>(x + i));
+                ld128(sS, x);
                 if (__any_sync(FW_FULL, (j + 1) * PK > seen)) {
                     const int lim = seen - j * PK;
 #pragma unroll
                     for (int i = 0; i < PK; ++i) x[i] = i < lim ? x[i] : -INFINITY;
                 }
-                float top[4] = {x[0], x[1], x[2], x[3]};
+                float top[8];
 #pragma unroll
-                for (int i = 4; i < PK; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
-                const float xm = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c2;
+                for (int i = 0; i < 8; ++i) top[i] = x[i];
+#pragma unroll
+                for (int i = 8; i < PK; i += 16)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top[e] = i + e + 8 < PK ? fmaxf(fmaxf(top[e], x[i + e]), x[i + e + 8]) : fmaxf(top[e], x[i + e]);
+#pragma unroll
+                for (int e = 4; e > 0; e >>= 1)
+#pragma unroll
+                    for (int i = 0; i < e; ++i) top[i] = fmaxf(top[i], top[i + e]);
+                const float xm = top[0] * c2;
                 const bool need = xm > ref + GROW;
                 if (__any_sync(FW_FULL, need)) {
                     const float now = need ? xm : ref;  // (a row's result does not depend on its neighbours)
@@ -366,24 +478,29 @@ __global__ void __launch_bounds__(PT, 1)
                         wait_st();
                     }
                 }
-                const float off = ref == -INFINITY ? 0.f : ref;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                const float off = ref == -INFINITY ? 0.f : -ref;
+                const float2 cc = make_float2(c2, c2), oo = make_float2(off, off);
+                float2 sum[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t p[32];
+                for (int i = 0; i < 4; ++i) sum[i] = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) {
-                        const float u = ex2(fmaf(x[64 * h + i], c2, -off)), w = ex2(fmaf(x[64 * h + i + 1], c2, -off));
-                        sum[(i >> 1) & 3] += u + w;
-                        p[i >> 1] = pack_bf16(u, w);
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float2 u = fma2(make_float2(x[32 * c + i], x[32 * c + i + 1]), cc, oo);
+                        u.x = ex2(u.x);
+                        u.y = ex2(u.y);
+                        sum[(i >> 1) & 3] = add2(sum[(i >> 1) & 3], u);
+                        p[i >> 1] = pack_bf16(u.x, u.y);
                     }
-                    st32(sS + 32 * h, p);
+                    // (the part before this one has arrived by now)
+                    if (c > 0 && c % (4 / PC) == 0) hand_over(&p_full[t][c / (4 / PC) - 1], lane);
+                    st16(sS + 16 * c, p);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                wait_st();
-                tc::fence_before_sync();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&p_full[t]);
+                hand_over(&p_full[t][PC - 1], lane);
+                sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+                l += sum[0].x + sum[0].y;
             }
             // ------------------------------------------------------ epilogue
             if (ok && n > 0) ok = tc::mbar_wait(&o_done[t], (uint32_t)(n - 1) & 1u, P_WAIT);
