@@ -31,12 +31,11 @@ namespace fw {
 namespace {
 
 constexpr int PK = 128;                  // keys of a block
-constexpr int PC = 1;                    // parts of a block's weights, handed over one by one
 // blocks that some row of a slot does not see in full: the first and the last row's ends are
 // at most 255 keys apart
 constexpr int PG = 3;
 constexpr int PT = 32 * 12;              // 8 softmax warps, copies, products of a tile, guard, of the other
-constexpr uint32_t P_WAIT = 1u << 22;    // polls before a wait gives up
+constexpr uint32_t P_WAIT = 1u << 20;    // polls before a wait gives up (seconds)
 constexpr float GROW = 8.f;              // octaves a row's maximum may be above its reference
 
 struct PromptArgs {
@@ -57,6 +56,8 @@ template <int D> struct PCfg {
     static constexpr int KT = PK * D * 2;          // bytes of a tile of keys or values
     static constexpr int STAGES = D == 128 ? 5 : 8;
     static constexpr size_t SMEM = 1024 + 2 * QT + (size_t)STAGES * KT;
+    static constexpr int NS = D == 128 ? 1 : 2;    // parts of a block of scores
+    static constexpr int SK = PK / NS;             // keys of a part
     static constexpr uint32_t O_COL = 256;         // TMEM: S of the tiles at 0 and 128, O behind them
 };
 
@@ -89,7 +90,7 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t bde
                  : "memory");
 }
 // 128 consecutive fp32 columns of this warp's 32 TMEM lanes, waited on in the same statement
-__device__ __forceinline__ void ld128(uint32_t taddr, float (&v)[128])
+__device__ __forceinline__ void ld_scores(uint32_t taddr, float (&v)[128])
 {
     uint32_t r[128];
     asm volatile(
@@ -123,6 +124,35 @@ __device__ __forceinline__ void ld128(uint32_t taddr, float (&v)[128])
 #pragma unroll
     for (int i = 0; i < 128; ++i) v[i] = __uint_as_float(r[i]);
 }
+// 64 consecutive fp32 columns of this warp's 32 TMEM lanes, waited on in the same statement
+__device__ __forceinline__ void ld_scores(uint32_t taddr, float (&v)[64])
+{
+    uint32_t r[64];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, "
+        "%34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, "
+        "%54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile(
@@ -150,17 +180,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "=f"(r.x), "=f"(r.y)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
-}
-__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t *r)
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -197,7 +216,7 @@ __global__ void __launch_bounds__(PT, 1)
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
     uint8_t *sQ = sm, *sKV = sm + 2 * C::QT;
-    __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2], p_full[2][PC], o_done[2], drained[2], v_in[PG], v_ok[PG];
+    __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2][C::NS], p_full[2][C::NS], o_done[2], drained[2], v_in[PG], v_ok[PG];
     __shared__ uint32_t s_taddr;
     __shared__ int s_seq, s_err, s_odd;
 
@@ -244,8 +263,10 @@ __global__ void __launch_bounds__(PT, 1)
         }
         tc::mbar_init(&q_full, 1);
         for (int t = 0; t < 2; ++t) {
-            tc::mbar_init(&s_full[t], 1);
-            for (int c = 0; c < PC; ++c) tc::mbar_init(&p_full[t][c], 4);
+            for (int u = 0; u < C::NS; ++u) {
+                tc::mbar_init(&s_full[t][u], 1);
+                tc::mbar_init(&p_full[t][u], 4);
+            }
             tc::mbar_init(&o_done[t], 1);
             tc::mbar_init(&drained[t], 1);
         }
@@ -309,7 +330,7 @@ __global__ void __launch_bounds__(PT, 1)
         // operands are not kept in uniform registers, and an instruction took 100 clocks to issue.
         const int t = wid == 11;
         if (t < tiles && J > 0) {
-            constexpr uint32_t id_s = tc::idesc_bf16_f32(128, PK, false, false);
+            constexpr uint32_t id_s = tc::idesc_bf16_f32(128, C::SK, false, false);
             constexpr uint32_t id_o = tc::idesc_bf16_f32(128, D, false, true);
             const uint64_t qd = tc::sdesc_sw128(tc::smem_u32(sQ) + t * C::QT, 16, 1024);
             const uint64_t kd = tc::sdesc_sw128(tc::smem_u32(sKV), 16, 1024);
@@ -327,44 +348,47 @@ __global__ void __launch_bounds__(PT, 1)
                 if (++st == C::STAGES) st = 0, ph ^= 1u;
                 return s;
             };
-            auto qk = [&](int s) {  // S = Q K^T
+            auto qk = [&](int s, int u) {  // a part of S = Q K^T
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
                     const uint32_t off = (ks >> 2) * (128 * 128) + (ks & 3) * 32;
-                    tc::mma_bf16(tS, qd + (off >> 4), kd + ((s * C::KT + off) >> 4), id_s, ks > 0);
+                    tc::mma_bf16(tS + u * C::SK, qd + (off >> 4), kd + ((s * C::KT + u * (C::SK * 128) + off) >> 4), id_s,
+                                 ks > 0);
                 }
-                tc::commit(&s_full[t]);
-                tc::commit(&empty[s]);
+                tc::commit(&s_full[t][u]);
+                if (u == C::NS - 1) tc::commit(&empty[s]);
             };
             const int s0 = wait_copy(false, 0);
             ok = __all_sync(FW_FULL, ok);
             if (ok && n > 0) {
                 tc::fence_after_sync();
-                if (elect_one()) qk(s0);
+                if (elect_one())
+                    for (int u = 0; u < C::NS; ++u) qk(s0, u);
                 __syncwarp();
             }
-            int done = 0;
             for (int j = 0; ok && j < n; ++j) {
                 const int sv = wait_copy(j >= jm, j), sk = j + 1 < n ? wait_copy(false, 0) : 0;
 #pragma unroll
-                for (int c = 0; c < PC; ++c) {
-                    ok = __all_sync(FW_FULL, ok && tc::mbar_wait(&p_full[t][c], (uint32_t)j & 1u, P_WAIT));
+                for (int u = 0; u < C::NS; ++u) {
+                    ok = __all_sync(FW_FULL, ok && tc::mbar_wait(&p_full[t][u], (uint32_t)j & 1u, P_WAIT));
                     if (!ok) break;
                     tc::fence_after_sync();
                     if (elect_one()) {
 #pragma unroll
-                        for (int ks = c * (PK / 16 / PC); ks < (c + 1) * (PK / 16 / PC); ++ks)  // O += P V
-                            mma_bf16_ts(tO, tS + ks * 8, vd + ((sv * C::KT + ks * 2048) >> 4), id_o, j > 0 || ks > 0);
-                        if (c == PC - 1) {
-                            tc::commit(&o_done[t]);
-                            tc::commit(&empty[sv]);
-                            if (j + 1 < n) qk(sk);
-                        }
+                        for (int ks = 0; ks < C::SK / 16; ++ks)  // O += P V
+                            mma_bf16_ts(tO, tS + u * C::SK + ks * 8,
+                                        vd + ((sv * C::KT + (u * (C::SK / 16) + ks) * 2048) >> 4), id_o, j > 0 || u > 0 || ks > 0);
+                        tc::commit(&o_done[t]);
+                        if (u == C::NS - 1) tc::commit(&empty[sv]);
+                        if (j + 1 < n) qk(sk, u);
                     }
                     __syncwarp();
-                    if (c == PC - 1) done = j + 1;
                 }
             }
+            // The products have completed before O is read and the TMEM freed.  (A barrier of its own: o_done
+            // may be one or two phases behind here, and its parity does not tell which.)
+            if (elect_one()) tc::commit(&drained[t]);
+            __syncwarp();
             // blocks that only the other tile's rows see: their stages are free as far as this tile goes
             if (n == 0 && ok && lane == 0) tc::mbar_arrive(&empty[s0]);
             for (int i = max(2 * n, 1); ok && i < 2 * J; ++i) {
@@ -372,13 +396,7 @@ __global__ void __launch_bounds__(PT, 1)
                 if (ok && lane == 0) tc::mbar_arrive(&empty[s]);
             }
             if (!__all_sync(FW_FULL, ok)) atomicOr(&s_err, 1);
-            // the products have completed before the TMEM can be freed
-            if (done > 0 && !tc::mbar_wait(&o_done[t], (uint32_t)(done - 1) & 1u, P_WAIT)) atomicOr(&s_err, 1);
-            if (!ok) {  // (and those issued before a wait gave up)
-                if (elect_one()) tc::commit(&drained[t]);
-                __syncwarp();
-                tc::mbar_wait(&drained[t], 0, P_WAIT);
-            }
+            if (!tc::mbar_wait(&drained[t], 0, P_WAIT)) atomicOr(&s_err, 1);
         }
         __syncwarp();
     } else if (wid == 10) {
@@ -427,83 +445,76 @@ __global__ void __launch_bounds__(PT, 1)
             const float c2 = a.scale2;
             float ref = -INFINITY, l = 0.f;
             bool ok = true;
-            for (int j = 0; j < n; ++j) {
-                if (ok) ok = tc::mbar_wait(&s_full[t], (uint32_t)j & 1u, P_WAIT);
+            for (int i = 0; i < n * C::NS; ++i) {  // part i: keys i SK ..
+                const int u = i % C::NS;
+                const uint32_t sP = sS + u * C::SK;
+                if (ok) ok = tc::mbar_wait(&s_full[t][u], (uint32_t)(i / C::NS) & 1u, P_WAIT);
                 if (!__all_sync(FW_FULL, ok)) {
                     ok = false;
                     break;
                 }
                 tc::fence_after_sync();
-                float x[PK];
-                ld128(sS, x);
-                if (__any_sync(FW_FULL, (j + 1) * PK > seen)) {
-                    const int lim = seen - j * PK;
+                float x[C::SK];
+                ld_scores(sP, x);
+                if (__any_sync(FW_FULL, (i + 1) * C::SK > seen)) {
+                    const int lim = seen - i * C::SK;
 #pragma unroll
-                    for (int i = 0; i < PK; ++i) x[i] = i < lim ? x[i] : -INFINITY;
+                    for (int e = 0; e < C::SK; ++e) x[e] = e < lim ? x[e] : -INFINITY;
                 }
-                float top[8];
+                float top[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top[i] = x[i];
+                for (int e = 0; e < 4; ++e) top[e] = max3(x[3 * e], x[3 * e + 1], x[3 * e + 2]);
 #pragma unroll
-                for (int i = 8; i < PK; i += 16)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) top[e] = i + e + 8 < PK ? fmaxf(fmaxf(top[e], x[i + e]), x[i + e + 8]) : fmaxf(top[e], x[i + e]);
-#pragma unroll
-                for (int e = 4; e > 0; e >>= 1)
-#pragma unroll
-                    for (int i = 0; i < e; ++i) top[i] = fmaxf(top[i], top[i + e]);
-                const float xm = top[0] * c2;
+                for (int e = 12; e + 1 < C::SK; e += 2) top[(e >> 1) & 3] = max3(top[(e >> 1) & 3], x[e], x[e + 1]);
+                const float xm = fmaxf(max3(top[0], top[1], top[2]), top[3]) * c2;
                 const bool need = xm > ref + GROW;
                 if (__any_sync(FW_FULL, need)) {
                     const float now = need ? xm : ref;  // (a row's result does not depend on its neighbours)
                     const float f = now == ref ? 1.f : ex2(ref - now);
                     l *= f;
                     ref = now;
-                    if (j > 0) {
-                        ok = tc::mbar_wait(&o_done[t], (uint32_t)(j - 1) & 1u, P_WAIT);
+                    if (i > 0) {
+                        ok = tc::mbar_wait(&o_done[t], (uint32_t)(i - 1) & 1u, P_WAIT);
                         if (!__all_sync(FW_FULL, ok)) {
                             ok = false;
                             break;
                         }
                         tc::fence_after_sync();
 #pragma unroll 1
-                        for (int i = 0; i < D; i += 32) {
-                            float y[32];
-                            tc::ld32(sO + i, y);
-                            uint32_t z[32];
+                        for (int h = 0; h < D; h += 16) {
+                            float y[16];
+                            tc::ld16(sO + h, y);
+                            uint32_t z[16];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) z[e] = __float_as_uint(y[e] * f);
-                            st32(sO + i, z);
+                            for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(y[e] * f);
+                            st16(sO + h, z);
                         }
-                        wait_st();
                     }
                 }
                 const float off = ref == -INFINITY ? 0.f : -ref;
                 const float2 cc = make_float2(c2, c2), oo = make_float2(off, off);
                 float2 sum[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] = make_float2(0.f, 0.f);
+                for (int e = 0; e < 4; ++e) sum[e] = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < C::SK / 32; ++c) {
                     uint32_t p[16];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float2 u = fma2(make_float2(x[32 * c + i], x[32 * c + i + 1]), cc, oo);
-                        u.x = ex2(u.x);
-                        u.y = ex2(u.y);
-                        sum[(i >> 1) & 3] = add2(sum[(i >> 1) & 3], u);
-                        p[i >> 1] = pack_bf16(u.x, u.y);
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 w = fma2(make_float2(x[32 * c + e], x[32 * c + e + 1]), cc, oo);
+                        w.x = ex2(w.x);
+                        w.y = ex2(w.y);
+                        sum[(e >> 1) & 3] = add2(sum[(e >> 1) & 3], w);
+                        p[e >> 1] = pack_bf16(w.x, w.y);
                     }
-                    // (the part before this one has arrived by now)
-                    if (c > 0 && c % (4 / PC) == 0) hand_over(&p_full[t][c / (4 / PC) - 1], lane);
-                    st16(sS + 16 * c, p);
+                    st16(sP + 16 * c, p);
                 }
-                hand_over(&p_full[t][PC - 1], lane);
+                hand_over(&p_full[t][u], lane);
                 sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
                 l += sum[0].x + sum[0].y;
             }
             // ------------------------------------------------------ epilogue
-            if (ok && n > 0) ok = tc::mbar_wait(&o_done[t], (uint32_t)(n - 1) & 1u, P_WAIT);
+            if (ok && n > 0) ok = tc::mbar_wait(&drained[t], 0, P_WAIT);
             if (ok && J > jm) ok = tc::mbar_wait(&v_ok[min(J - 1 - jm, PG - 1)], 0, P_WAIT);  // (the guard is done)
             ok = __all_sync(FW_FULL, ok);
             if (!ok && lane == 0) atomicOr(&s_err, 1);
