@@ -56,7 +56,9 @@ template <int D> struct PCfg {
     static constexpr int KT = PK * D * 2;          // bytes of a tile of keys or values
     static constexpr int STAGES = D == 128 ? 5 : 8;
     static constexpr size_t SMEM = 1024 + 2 * QT + (size_t)STAGES * KT;
-    static constexpr int NS = D == 128 ? 1 : 2;    // parts of a block of scores
+    // Parts of a block of scores: with two, the next part's product runs under the softmax of this one (d = 128,
+    // 16,384 tokens x 32 heads: 1.46 ms in one part, 1.37 in two).
+    static constexpr int NS = 2;
     static constexpr int SK = PK / NS;             // keys of a part
     static constexpr uint32_t O_COL = 256;         // TMEM: S of the tiles at 0 and 128, O behind them
 };
@@ -191,6 +193,17 @@ __device__ __forceinline__ bool elect_one()
     return p != 0;
 }
 
+// each lane waits for a phase of a barrier of its own, the warp for all of them
+__device__ __forceinline__ bool wait_lanes(uint64_t *bar, uint32_t parity, uint32_t limit)
+{
+    bool done = false;
+    for (uint32_t it = 0; it < limit; ++it) {
+        done = done || tc::mbar_wait(bar, parity, 1);
+        if (__all_sync(FW_FULL, done)) return true;
+    }
+    return false;
+}
+
 // a warp's stores to TMEM are complete and known to the products' warp
 __device__ __forceinline__ void hand_over(uint64_t *bar, int lane)
 {
@@ -220,7 +233,8 @@ __global__ void __launch_bounds__(PT, 1)
     __shared__ uint32_t s_taddr;
     __shared__ int s_seq, s_err, s_odd;
 
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    // (by a shuffle, so that the compiler knows the warp's role for the same in all lanes)
+    const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(FW_FULL, tid >> 5, 0);
     const int slot = a.slots - 1 - (int)(blockIdx.x / a.kv_heads), hk = blockIdx.x % a.kv_heads;
     const int TT = 128 / a.group, ST = 2 * TT;  // tokens of a tile and of a slot
 
@@ -282,7 +296,7 @@ __global__ void __launch_bounds__(PT, 1)
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    const uint32_t taddr = s_taddr;
+    const uint32_t taddr = __shfl_sync(FW_FULL, s_taddr, 0);
 
     // Copy i of the ring (K of block 0, V of block 0, K of block 1, ...) arrives on its stage's barrier;
     // the values that the guard looks over on one of their own, which the guard can wait for without
@@ -340,14 +354,16 @@ __global__ void __launch_bounds__(PT, 1)
             bool ok = tc::mbar_wait(&q_full, 0, P_WAIT);
             int st = 0;         // stage of the next copy of the ring
             uint32_t ph = 0;    // and its phase
-            auto wait_copy = [&](bool guarded, int j) {
-                if (ok) ok = guarded ? tc::mbar_wait(&v_ok[min(j - jm, PG - 1)], 0, P_WAIT) &&
-                                           tc::mbar_wait(&v_in[min(j - jm, PG - 1)], 0, P_WAIT)
-                                     : tc::mbar_wait(&full[st], ph, P_WAIT);
+            // the barrier and parity that the next copy arrives with, and its stage
+            auto next_copy = [&](bool guarded, int j, uint64_t *&bar, uint32_t &parity) {
+                bar = guarded ? &v_ok[min(j - jm, PG - 1)] : &full[st];
+                parity = guarded ? 0u : ph;
                 const int s = st;
                 if (++st == C::STAGES) st = 0, ph ^= 1u;
                 return s;
             };
+            uint64_t *bar;
+            uint32_t parity;
             auto qk = [&](int s, int u) {  // a part of S = Q K^T
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
@@ -358,8 +374,8 @@ __global__ void __launch_bounds__(PT, 1)
                 tc::commit(&s_full[t][u]);
                 if (u == C::NS - 1) tc::commit(&empty[s]);
             };
-            const int s0 = wait_copy(false, 0);
-            ok = __all_sync(FW_FULL, ok);
+            const int s0 = next_copy(false, 0, bar, parity);
+            ok = __all_sync(FW_FULL, ok && tc::mbar_wait(bar, parity, P_WAIT));
             if (ok && n > 0) {
                 tc::fence_after_sync();
                 if (elect_one())
@@ -367,10 +383,21 @@ __global__ void __launch_bounds__(PT, 1)
                 __syncwarp();
             }
             for (int j = 0; ok && j < n; ++j) {
-                const int sv = wait_copy(j >= jm, j), sk = j + 1 < n ? wait_copy(false, 0) : 0;
+                // The weights, V of this block and K of the next are waited for together, a lane each: a wait takes
+                // 200 clocks even where nothing is left to wait for (it queues behind the softmax's exponentials).
+                uint64_t *pb = &p_full[t][0];
+                uint32_t pp = (uint32_t)j & 1u;
+                const int sv = next_copy(j >= jm, j, bar, parity);
+                if (lane == 1) pb = bar, pp = parity;
+                if (lane == 2 && j >= jm) pb = &v_in[min(j - jm, PG - 1)], pp = 0u;
+                int sk = 0;
+                if (j + 1 < n) {
+                    sk = next_copy(false, 0, bar, parity);
+                    if (lane == 3) pb = bar, pp = parity;
+                }
 #pragma unroll
                 for (int u = 0; u < C::NS; ++u) {
-                    ok = __all_sync(FW_FULL, ok && tc::mbar_wait(&p_full[t][u], (uint32_t)j & 1u, P_WAIT));
+                    ok = wait_lanes(u == 0 ? pb : &p_full[t][u], u == 0 ? pp : (uint32_t)j & 1u, P_WAIT);
                     if (!ok) break;
                     tc::fence_after_sync();
                     if (elect_one()) {
@@ -392,7 +419,8 @@ __global__ void __launch_bounds__(PT, 1)
             // blocks that only the other tile's rows see: their stages are free as far as this tile goes
             if (n == 0 && ok && lane == 0) tc::mbar_arrive(&empty[s0]);
             for (int i = max(2 * n, 1); ok && i < 2 * J; ++i) {
-                const int s = wait_copy((i & 1) && (i >> 1) >= jm, i >> 1);
+                const int s = next_copy((i & 1) && (i >> 1) >= jm, i >> 1, bar, parity);
+                ok = tc::mbar_wait(bar, parity, P_WAIT);
                 if (ok && lane == 0) tc::mbar_arrive(&empty[s]);
             }
             if (!__all_sync(FW_FULL, ok)) atomicOr(&s_err, 1);
