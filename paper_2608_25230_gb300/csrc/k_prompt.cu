@@ -91,41 +91,6 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d, uint32_t a, uint64_t bde
                  "r"(a), "l"(bdesc), "r"(idesc), "r"((uint32_t)acc)
                  : "memory");
 }
-// 128 consecutive fp32 columns of this warp's 32 TMEM lanes, waited on in the same statement
-__device__ __forceinline__ void ld_scores(uint32_t taddr, float (&v)[128])
-{
-    uint32_t r[128];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x128.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
-        "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, "
-        "%35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, "
-        "%56, %57, %58, %59, %60, %61, %62, %63, %64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, "
-        "%77, %78, %79, %80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, %96, %97, "
-        "%98, %99, %100, %101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, %112, %113, %114, "
-        "%115, %116, %117, %118, %119, %120, %121, %122, %123, %124, %125, %126, %127}, [%128];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]),
-          "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]),
-          "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
-          "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]),
-          "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]),
-          "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]),
-          "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]),
-          "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]),
-          "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]),
-          "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]),
-          "=r"(r[104]), "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]),
-          "=r"(r[111]), "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]),
-          "=r"(r[118]), "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]),
-          "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
-        : "r"(taddr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 128; ++i) v[i] = __uint_as_float(r[i]);
-}
 // 64 consecutive fp32 columns of this warp's 32 TMEM lanes, waited on in the same statement
 __device__ __forceinline__ void ld_scores(uint32_t taddr, float (&v)[64])
 {
@@ -231,7 +196,7 @@ __global__ void __launch_bounds__(PT, 1)
     uint8_t *sQ = sm, *sKV = sm + 2 * C::QT;
     __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2][C::NS], p_full[2][C::NS], o_done[2], drained[2], v_in[PG], v_ok[PG];
     __shared__ uint32_t s_taddr;
-    __shared__ int s_seq, s_err, s_odd;
+    __shared__ int s_seq[5], s_err, s_odd;  // (s_seq: the sequence, its query and key rows)
 
     // (by a shuffle, so that the compiler knows the warp's role for the same in all lanes)
     const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(FW_FULL, tid >> 5, 0);
@@ -254,14 +219,48 @@ __global__ void __launch_bounds__(PT, 1)
             lo += (__popc(hit) - 1) * step;
             hi = min(lo + step, hi);
         } while (hi - lo > 1);
-        if (lane == 0) s_seq = any ? lo : -1;
+        if (lane < 4) s_seq[1 + lane] = (lane < 2 ? a.cu_q : a.cu_k)[lo + (lane & 1)];
+        if (lane == 0) s_seq[0] = any ? lo : -1;
+    } else if (wid == 8) {
+        if (lane < C::STAGES) {
+            tc::mbar_init(&full[lane], 1);
+            tc::mbar_init(&empty[lane], 2);
+        } else if (lane < C::STAGES + PG) {
+            tc::mbar_init(&v_in[lane - C::STAGES], 1);
+            tc::mbar_init(&v_ok[lane - C::STAGES], 1);
+        } else if (lane < C::STAGES + PG + 2) {
+            const int t = lane - C::STAGES - PG;
+            for (int u = 0; u < C::NS; ++u) {
+                tc::mbar_init(&s_full[t][u], 1);
+                tc::mbar_init(&p_full[t][u], 4);
+            }
+            tc::mbar_init(&o_done[t], 1);
+            tc::mbar_init(&drained[t], 1);
+        } else if (lane == 31) {
+            tc::mbar_init(&q_full, 1);
+            s_err = 0;
+            s_odd = 0;
+        }
+        tc::mbar_init_fence();
+    } else if (wid == 9) {
+        tc::tmem_alloc(&s_taddr, 512);
+    } else if (wid == 10 && lane == 0) {
+        tc::tma_prefetch_desc(&tmQ);
+        tc::tma_prefetch_desc(&tmK);
+        tc::tma_prefetch_desc(&tmV);
     }
+    tc::fence_before_sync();
     __syncthreads();
-    const int seq = s_seq;
-    if (seq < 0 || !seq_ok(a, seq)) return;
-    const int q0 = a.cu_q[seq], lq = a.cu_q[seq + 1] - q0, k0 = a.cu_k[seq], lk = a.cu_k[seq + 1] - k0;
+    tc::fence_after_sync();
+    const uint32_t taddr = __shfl_sync(FW_FULL, s_taddr, 0);
+    const int seq = s_seq[0], q0 = s_seq[1], q1 = s_seq[2], k0 = s_seq[3], k1 = s_seq[4];
+    const bool valid = seq >= 0 && q0 >= 0 && q1 >= q0 && q1 <= a.total_q && k0 >= 0 && k1 >= k0 && k1 <= a.total_k;
+    const int lq = valid ? q1 - q0 : 0, lk = valid ? k1 - k0 : 0;
     const int t0 = (slot - (q0 / ST + seq)) * ST;  // the slot's first token in the sequence
-    if (t0 < 0 || t0 >= lq) return;
+    if (!valid || t0 < 0 || t0 >= lq) {  // (a sequence out of range, or a slot behind its last token)
+        if (wid == 9) tc::tmem_dealloc(taddr, 512);
+        return;
+    }
     const int tiles = t0 + TT < lq ? 2 : 1;
     // keys that the first token sees, and blocks of keys that each tile's last one does
     const int seen0 = max(0, lk - lq + t0 + 1);
@@ -269,34 +268,6 @@ __global__ void __launch_bounds__(PT, 1)
     nb[0] = (max(0, lk - lq + min(t0 + TT, lq)) + PK - 1) / PK;
     nb[1] = tiles == 2 ? (max(0, lk - lq + min(t0 + ST, lq)) + PK - 1) / PK : 0;
     const int J = max(nb[0], nb[1]), jm = seen0 / PK;  // blocks from jm on are not seen in full by every row
-
-    if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) {
-            tc::mbar_init(&full[s], 1);
-            tc::mbar_init(&empty[s], tiles);
-        }
-        tc::mbar_init(&q_full, 1);
-        for (int t = 0; t < 2; ++t) {
-            for (int u = 0; u < C::NS; ++u) {
-                tc::mbar_init(&s_full[t][u], 1);
-                tc::mbar_init(&p_full[t][u], 4);
-            }
-            tc::mbar_init(&o_done[t], 1);
-            tc::mbar_init(&drained[t], 1);
-        }
-        for (int g = 0; g < PG; ++g) {
-            tc::mbar_init(&v_in[g], 1);
-            tc::mbar_init(&v_ok[g], 1);
-        }
-        tc::mbar_init_fence();
-        s_err = 0;
-        s_odd = 0;
-    }
-    if (wid == 9) tc::tmem_alloc(&s_taddr, 512);
-    tc::fence_before_sync();
-    __syncthreads();
-    tc::fence_after_sync();
-    const uint32_t taddr = __shfl_sync(FW_FULL, s_taddr, 0);
 
     // Copy i of the ring (K of block 0, V of block 0, K of block 1, ...) arrives on its stage's barrier;
     // the values that the guard looks over on one of their own, which the guard can wait for without
@@ -308,9 +279,6 @@ __global__ void __launch_bounds__(PT, 1)
     if (wid == 8) {
         // ------------------------------------------------------------ copies
         if (lane == 0 && J > 0) {
-            tc::tma_prefetch_desc(&tmQ);
-            tc::tma_prefetch_desc(&tmK);
-            tc::tma_prefetch_desc(&tmV);
             const uint32_t qbytes = (uint32_t)(128 * a.group * TT);  // (one box: 64 columns of a tile's rows)
             tc::mbar_arrive_expect_tx(&q_full, qbytes * C::NB * tiles);
             for (int t = 0; t < tiles; ++t)
@@ -364,6 +332,10 @@ __global__ void __launch_bounds__(PT, 1)
             };
             uint64_t *bar;
             uint32_t parity;
+            auto free_stage = [&](int s) {  // once the products so far have read it; a tile alone arrives for both
+                tc::commit(&empty[s]);
+                if (tiles == 1) tc::commit(&empty[s]);
+            };
             auto qk = [&](int s, int u) {  // a part of S = Q K^T
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
@@ -372,7 +344,7 @@ __global__ void __launch_bounds__(PT, 1)
                                  ks > 0);
                 }
                 tc::commit(&s_full[t][u]);
-                if (u == C::NS - 1) tc::commit(&empty[s]);
+                if (u == C::NS - 1) free_stage(s);
             };
             const int s0 = next_copy(false, 0, bar, parity);
             ok = __all_sync(FW_FULL, ok && tc::mbar_wait(bar, parity, P_WAIT));
@@ -406,7 +378,7 @@ __global__ void __launch_bounds__(PT, 1)
                             mma_bf16_ts(tO, tS + u * C::SK + ks * 8,
                                         vd + ((sv * C::KT + (u * (C::SK / 16) + ks) * 2048) >> 4), id_o, j > 0 || u > 0 || ks > 0);
                         tc::commit(&o_done[t]);
-                        if (u == C::NS - 1) tc::commit(&empty[sv]);
+                        if (u == C::NS - 1) free_stage(sv);
                         if (j + 1 < n) qk(sk, u);
                     }
                     __syncwarp();
@@ -434,23 +406,26 @@ __global__ void __launch_bounds__(PT, 1)
             const int s = (2 * j + 1) % C::STAGES;
             ok = tc::mbar_wait(&v_in[min(j - jm, PG - 1)], 0, P_WAIT);
             if (!ok) break;
-            uint4 *v = reinterpret_cast<uint4 *>(sKV + s * C::KT);
+            uint4 *v = reinterpret_cast<uint4 *>(sKV + s * C::KT) + lane;
             bool odd = false;
-#pragma unroll 8
-            for (int p = lane; p < C::KT / 16; p += 32) {
-                const uint4 x = v[p];
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                bool bad = false;
+#pragma unroll 1
+            for (int p = 0; p < C::KT / 512; p += 8) {
+                uint4 x[8];
+                uint32_t top = 0;  // the largest magnitudes of the even and the odd columns
 #pragma unroll
-                for (int z = 0; z < 4; ++z) bad |= (w[z] & 0x7f80u) == 0x7f80u || (w[z] & 0x7f800000u) == 0x7f800000u;
-                if (bad) {
-                    uint32_t y[4];
+                for (int z = 0; z < 8; ++z) x[z] = v[32 * (p + z)];
 #pragma unroll
-                    for (int z = 0; z < 4; ++z)
-                        y[z] = ((w[z] & 0x7f80u) == 0x7f80u ? 0u : w[z] & 0xffffu) |
-                               ((w[z] & 0x7f800000u) == 0x7f800000u ? 0u : w[z] & 0xffff0000u);
-                    v[p] = make_uint4(y[0], y[1], y[2], y[3]);
+                for (int z = 0; z < 8; ++z)
+                    top = __vmaxu2(__vmaxu2(__vmaxu2(top, x[z].x & 0x7fff7fffu), __vmaxu2(x[z].y & 0x7fff7fffu, x[z].z & 0x7fff7fffu)),
+                                   x[z].w & 0x7fff7fffu);
+                if (max(top & 0xffffu, top >> 16) >= 0x7f80u) {
                     odd = true;
+                    for (int z = 0; z < 8; ++z) {
+                        uint32_t *w = reinterpret_cast<uint32_t *>(v + 32 * (p + z));
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = ((w[e] & 0x7f80u) == 0x7f80u ? 0u : w[e] & 0xffffu) |
+                                   ((w[e] & 0x7f800000u) == 0x7f800000u ? 0u : w[e] & 0xffff0000u);
+                    }
                 }
             }
             if (__any_sync(FW_FULL, odd)) {
@@ -542,7 +517,8 @@ __global__ void __launch_bounds__(PT, 1)
                 l += sum[0].x + sum[0].y;
             }
             // ------------------------------------------------------ epilogue
-            if (ok && n > 0) ok = tc::mbar_wait(&drained[t], 0, P_WAIT);
+            // (its queries' memory is written below: without products, the copy has to have landed)
+            if (ok && J > 0) ok = n > 0 ? tc::mbar_wait(&drained[t], 0, P_WAIT) : tc::mbar_wait(&q_full, 0, P_WAIT);
             if (ok && J > jm) ok = tc::mbar_wait(&v_ok[min(J - 1 - jm, PG - 1)], 0, P_WAIT);  // (the guard is done)
             ok = __all_sync(FW_FULL, ok);
             if (!ok && lane == 0) atomicOr(&s_err, 1);
@@ -550,6 +526,10 @@ __global__ void __launch_bounds__(PT, 1)
             const bool odd = *(volatile int *)&s_odd != 0;
             const int64_t row = (int64_t)(q0 + tok) * a.q_heads + hk * a.group + r % a.group;
             const float inv = !ok ? NAN : l == 0.f ? 0.f : 1.f / l;
+            // The rows go out by way of the tile's queries' memory (the products have read them), a warp's 32 rows its
+            // own: whole rows a store.  (A row a lane: 32 lines an instruction, 6,200 clocks for a CTA's rows.)
+            constexpr int PCS = D / 8;  // 16-byte pieces of a row
+            uint4 *stage = reinterpret_cast<uint4 *>(sQ + t * C::QT) + (r & ~31) * PCS;
 #pragma unroll 1
             for (int i = 0; i < D; i += 32) {
                 float y[32];
@@ -571,13 +551,18 @@ __global__ void __launch_bounds__(PT, 1)
                         }
                     }
                 }
-                if (live) {
-                    uint4 *dst = reinterpret_cast<uint4 *>(a.o + row * D + i);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        dst[e] = make_uint4(pack_bf16(y[8 * e], y[8 * e + 1]), pack_bf16(y[8 * e + 2], y[8 * e + 3]),
-                                            pack_bf16(y[8 * e + 4], y[8 * e + 5]), pack_bf16(y[8 * e + 6], y[8 * e + 7]));
-                }
+                for (int e = 0; e < 4; ++e)
+                    stage[lane * PCS + ((i / 8 + e) ^ (lane & 7))] =
+                        make_uint4(pack_bf16(y[8 * e], y[8 * e + 1]), pack_bf16(y[8 * e + 2], y[8 * e + 3]),
+                                   pack_bf16(y[8 * e + 4], y[8 * e + 5]), pack_bf16(y[8 * e + 6], y[8 * e + 7]));
+            }
+            __syncwarp();
+#pragma unroll 4
+            for (int p = 0; p < 32; p += 32 / PCS) {
+                const int k = p + lane / PCS, c = lane % PCS;
+                const int64_t to = __shfl_sync(FW_FULL, live ? row : -1, k);
+                if (to >= 0) reinterpret_cast<uint4 *>(a.o + to * D)[c] = stage[k * PCS + (c ^ (k & 7))];
             }
             if (live && a.lse)
                 a.lse[row] = !ok ? NAN : l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
