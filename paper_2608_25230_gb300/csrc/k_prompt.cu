@@ -41,7 +41,7 @@ constexpr float GROW = 8.f;              // octaves a row's maximum may be above
 struct PromptArgs {
     const int32_t *cu_q, *cu_k;
     int64_t total_q, total_k;
-    int num_seqs, q_heads, kv_heads, group, slots;
+    int num_seqs, q_heads, kv_heads, group, slots, TT;  // TT: tokens of a tile
     const uint16_t *v;
     int64_t v_row, v_head;
     float scale2;  // scale * log2(e)
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(PT, 1)
     // (by a shuffle, so that the compiler knows the warp's role for the same in all lanes)
     const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(FW_FULL, tid >> 5, 0);
     const int slot = a.slots - 1 - (int)(blockIdx.x / a.kv_heads), hk = blockIdx.x % a.kv_heads;
-    const int TT = 128 / a.group, ST = 2 * TT;  // tokens of a tile and of a slot
+    const int TT = a.TT, ST = 2 * TT;  // tokens of a tile and of a slot
 
     if (blockIdx.x == 0 && a.status)  // (before any wait can have given up)
         for (int s = tid; s < a.num_seqs; s += PT) a.status[s] = seq_ok(a, s) ? FW_OK : FW_ERR_INVALID_ARG;
@@ -531,34 +531,36 @@ __global__ void __launch_bounds__(PT, 1)
             constexpr int PCS = D / 8;  // 16-byte pieces of a row
             uint4 *stage = reinterpret_cast<uint4 *>(sQ + t * C::QT) + (r & ~31) * PCS;
 #pragma unroll 1
-            for (int i = 0; i < D; i += 32) {
-                float y[32];
+            for (int i = 0; i < D; i += 64) {
+                float y[64];
                 if (ok && n > 0) {
-                    tc::ld32(sO + i, y);
+                    ld_scores(sO + i, y);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) y[e] = 0.f;
+                    for (int e = 0; e < 64; ++e) y[e] = 0.f;
                 }
+                // (a row that sees nothing has no O where its tile saw nothing: its sum is 0 and so is it)
 #pragma unroll
-                for (int e = 0; e < 32; ++e) y[e] = l == 0.f && ok ? 0.f : y[e] * inv;
+                for (int e = 0; e < 64; ++e) y[e] = l == 0.f && ok ? 0.f : y[e] * inv;
                 if (odd && live) {  // the values the guard took out, for the rows that see them
+#pragma unroll 1
                     for (int j = jm * PK; j < seen; ++j) {
                         const uint16_t *src = a.v + (int64_t)(k0 + j) * a.v_row + hk * a.v_head + i;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
+                        for (int e = 0; e < 64; ++e) {
                             const uint16_t b = src[e];
                             if ((b & 0x7f80u) == 0x7f80u) y[e] += bf16_to_f32(b);
                         }
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 8; ++e)
                     stage[lane * PCS + ((i / 8 + e) ^ (lane & 7))] =
                         make_uint4(pack_bf16(y[8 * e], y[8 * e + 1]), pack_bf16(y[8 * e + 2], y[8 * e + 3]),
                                    pack_bf16(y[8 * e + 4], y[8 * e + 5]), pack_bf16(y[8 * e + 6], y[8 * e + 7]));
             }
             __syncwarp();
-#pragma unroll 4
+#pragma unroll 8
             for (int p = 0; p < 32; p += 32 / PCS) {
                 const int k = p + lane / PCS, c = lane % PCS;
                 const int64_t to = __shfl_sync(FW_FULL, live ? row : -1, k);
@@ -594,7 +596,7 @@ fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *sta
                              keys ? p.v_row : (int64_t)p.d * p.kv_heads, 1, PK))
         return FW_ERR_CUDA;
     const PromptArgs a{p.cu_q,  p.cu_k,     p.total_q, p.total_k, p.num_seqs, p.q_heads, p.kv_heads,
-                       group,   (int)slots, (const uint16_t *)p.v, p.v_row,   p.v_head,  p.scale * 1.4426950408889634f,
+                       group,   (int)slots, TT, (const uint16_t *)p.v, p.v_row,   p.v_head,  p.scale * 1.4426950408889634f,
                        (uint16_t *)o, lse,  status};
     const unsigned grid = (unsigned)(slots * p.kv_heads);
     if (p.d == 128) {
