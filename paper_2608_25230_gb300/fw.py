@@ -483,12 +483,38 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+# the raw handle of a device's current stream, without the Stream object that torch.cuda.current_stream makes (2 us)
+_current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _raw_stream(stream, tensor):
+    return stream.cuda_stream if stream is not None else _current_raw(tensor.get_device())
+
+
 def _own_buffers(stream, *tensors):
     # buffers made here on the current stream and used on another: not reused before that stream is done
     if stream is not None:
         for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+            t.record_stream(stream)
+
+
+def _attention_out(out, q, items, stream):
+    """(o, lse, status, the dict) of a call's outputs: those of `out`, checked, or new ones."""
+    if out is None:
+        out = dict(o=torch.empty(q.shape, dtype=torch.bfloat16, device=q.device),
+                   lse=torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device),
+                   status=torch.empty(items, dtype=torch.int32, device=q.device))
+        _own_buffers(stream, *out.values())
+        return out["o"].data_ptr(), out["lse"].data_ptr(), out["status"].data_ptr(), out
+    o, lse, status = out["o"], out.get("lse"), out.get("status")
+    if o.shape != q.shape or o.dtype is not torch.bfloat16 or not o.is_contiguous():
+        raise ValueError("out['o'] is contiguous bfloat16 of q's shape")
+    if lse is not None and (lse.shape != q.shape[:-1] or lse.dtype is not torch.float32 or not lse.is_contiguous()):
+        raise ValueError("out['lse'] is contiguous float32 of q's shape without its last axis")
+    if status is not None and (status.numel() < items or status.dtype is not torch.int32 or not status.is_contiguous()):
+        raise ValueError(f"out['status'] is contiguous int32, {items} entries")
+    return o.data_ptr(), lse.data_ptr() if lse is not None else None, status.data_ptr() if status is not None else None, out
 
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor = None, *,
@@ -497,37 +523,38 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     multiples of 8 with d contiguous; cu_q, cu_k: int32 [sequences + 1] row bounds (cu_k = cu_q if not given).
     Returns a dict of o (bf16, as q), lse (fp32 [rows][q_heads]) and status [sequences]; such a dict passed as out
     is written instead."""
-    cu_k = cu_q if cu_k is None else cu_k
+    if cu_k is None:
+        cu_k = cu_q
     rows, hq, d = q.shape
-    _need(q.dtype == k.dtype == v.dtype == torch.bfloat16, "q, k and v are bfloat16")
-    _need(k.shape == v.shape and k.shape[2] == d, "k and v are [rows][kv_heads][d], d as in q")
-    _need(d == 1 or (q.stride(2) == k.stride(2) == v.stride(2) == 1), "d is the contiguous axis of q, k and v")
-    _need(cu_q.dtype == cu_k.dtype == torch.int32 and cu_q.is_contiguous() and cu_k.is_contiguous() and
-          cu_q.shape == cu_k.shape and cu_q.dim() == 1, "cu_q and cu_k are contiguous int32 [sequences + 1]")
-    seqs = cu_q.numel() - 1
-    if out is None:
-        out = dict(o=torch.empty(rows, hq, d, dtype=torch.bfloat16, device=q.device),
-                   lse=torch.empty(rows, hq, dtype=torch.float32, device=q.device),
-                   status=torch.empty(max(seqs, 0), dtype=torch.int32, device=q.device))
-        _own_buffers(stream, *out.values())
-    o, lse, status = out["o"], out.get("lse"), out.get("status")
-    _need(o.shape == q.shape and o.dtype == torch.bfloat16 and o.is_contiguous(), "out['o'] is contiguous bfloat16, as q")
-    _need(lse is None or (lse.numel() >= rows * hq and lse.dtype == torch.float32 and lse.is_contiguous()),
-          "out['lse'] is contiguous float32 [rows][q_heads]")
-    _need(status is None or (status.numel() >= seqs and status.dtype == torch.int32 and status.is_contiguous()),
-          "out['status'] is contiguous int32 [sequences]")
-    p = FwPrompt(seqs, hq, k.shape[1], d, rows, k.shape[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), *_rh(q), *_rh(k),
-                 *_rh(v), cu_q.data_ptr(), cu_k.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale)
-    _check(_lib.fw_prompt_attention(C.byref(p), _ptr(o), _ptr(lse), _ptr(status), _stream(stream)),
-           "fw_prompt_attention")
+    keys, hk, dk = k.shape
+    bf16, i32 = torch.bfloat16, torch.int32
+    if q.dtype is not bf16 or k.dtype is not bf16 or v.dtype is not bf16:
+        raise ValueError("q, k and v are bfloat16")
+    if v.shape != k.shape or dk != d:
+        raise ValueError("k and v are [rows][kv_heads][d], d as in q")
+    (qr, qh, q1), (kr, kh, k1), (vr, vh, v1) = q.stride(), k.stride(), v.stride()
+    if not q1 == k1 == v1 == 1:
+        raise ValueError("d is the contiguous axis of q, k and v")
+    if cu_q.dtype is not i32 or cu_k.dtype is not i32 or cu_q.dim() != 1 or cu_q.shape != cu_k.shape or not (
+            cu_q.is_contiguous() and cu_k.is_contiguous()):
+        raise ValueError("cu_q and cu_k are contiguous int32 [sequences + 1]")
+    # (strides of axes of one entry, which torch leaves open)
+    if hq == 1:
+        qh = d
+    if hk == 1:
+        kh = vh = d
+    if rows <= 1:
+        qr = hq * qh
+    if keys <= 1:
+        kr, vr = hk * kh, hk * vh
+    seqs = cu_q.shape[0] - 1
+    o, lse, status, out = _attention_out(out, q, seqs, stream)
+    p = FwPrompt(seqs, hq, hk, d, rows, keys, q.data_ptr(), k.data_ptr(), v.data_ptr(), qr, qh, kr, kh, vr, vh,
+                 cu_q.data_ptr(), cu_k.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale)
+    st = _lib.fw_prompt_attention(C.byref(p), o, lse, status, _raw_stream(stream, q))
+    if st != FW_OK:
+        raise FwError(st, "fw_prompt_attention")
     return out
-
-
-def _rh(x):
-    """(row, head) strides of a [rows][heads][d] tensor; those of axes of one entry, which torch leaves open, in order."""
-    d = x.shape[2]
-    head = x.stride(1) if x.shape[1] > 1 else d
-    return (x.stride(0) if x.shape[0] > 1 else max(x.shape[1] * head, d)), head
 
 
 CACHE8_BLOCK, CACHE8_TAIL = 32, 64
@@ -579,39 +606,60 @@ def cache8_empty(offsets: torch.Tensor, total: int, d: int, *, fmt: str = "e4m3"
                   counts=torch.zeros(cells, dtype=torch.int32, device=dev))
 
 
+def _status_ptr(status, cells):
+    if status is None:
+        return None
+    if status.dtype is not torch.int32 or status.numel() < cells or not status.is_contiguous():
+        raise ValueError("status is contiguous int32 [cells]")
+    return status.data_ptr()
+
+
 def cache8_compact(cache: Cache8, K: torch.Tensor, V: torch.Tensor, offsets: torch.Tensor, kept_pos: torch.Tensor, *,
                    status: torch.Tensor = None, stream=None):
     """fw_cache8_compact: the kept rows of K, V (bf16 [cells][T][d], equal strides that are multiples of 8, d
     contiguous) quantised into the store, whose counts are set."""
     cells, T, d = K.shape
-    _need(K.dtype == V.dtype == torch.bfloat16 and K.shape == V.shape and (cells, d) == (cache.cells, cache.d),
-          "K and V are bfloat16 [cells][T][d], as the store's")
-    cs, rs = (K.stride(0) if cells > 1 else T * d), (K.stride(1) if T > 1 else d)
-    _need(K.stride(2) == V.stride(2) == 1 and (cells == 1 or V.stride(0) == cs) and (T == 1 or V.stride(1) == rs),
-          "K and V have equal strides and d contiguous")
-    _need(offsets.dtype == torch.int64 and offsets.numel() == cells + 1 and kept_pos.dtype == torch.int32 and
-          offsets.is_contiguous() and kept_pos.is_contiguous(), "offsets is int64 [cells + 1], kept_pos int32")
-    _check(_lib.fw_cache8_compact(cache._ref, _ptr(K), _ptr(V), T, cs, rs, _ptr(offsets), _ptr(kept_pos),
-                                  kept_pos.numel(), _ptr(status), _stream(stream)), "fw_cache8_compact")
+    if K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16 or V.shape != K.shape or cells != cache.cells or \
+            d != cache.d:
+        raise ValueError("K and V are bfloat16 [cells][T][d], as the store's")
+    (cs, rs, one), (vcs, vrs, vone) = K.stride(), V.stride()
+    if cells == 1:
+        cs = vcs = T * d
+    if T == 1:
+        rs = vrs = d
+    if one != 1 or vone != 1 or cs != vcs or rs != vrs:
+        raise ValueError("K and V have equal strides and d contiguous")
+    if offsets.dtype is not torch.int64 or offsets.numel() != cells + 1 or kept_pos.dtype is not torch.int32 or not (
+            offsets.is_contiguous() and kept_pos.is_contiguous()):
+        raise ValueError("offsets is contiguous int64 [cells + 1], kept_pos contiguous int32")
+    st = _lib.fw_cache8_compact(cache._ref, K.data_ptr(), V.data_ptr(), T, cs, rs, offsets.data_ptr(),
+                                kept_pos.data_ptr(), kept_pos.numel(), _status_ptr(status, cells), _raw_stream(stream, K))
+    if st != FW_OK:
+        raise FwError(st, "fw_cache8_compact")
 
 
 def cache8_append(cache: Cache8, new_K: torch.Tensor, new_V: torch.Tensor, *, status: torch.Tensor = None, stream=None):
     """fw_cache8_append: new_K, new_V (bf16 [cells][m][d], contiguous) behind each cell's rows."""
     cells, m, d = new_K.shape
-    _need(new_K.dtype == new_V.dtype == torch.bfloat16 and new_K.shape == new_V.shape and new_K.is_contiguous() and
-          new_V.is_contiguous() and (cells, d) == (cache.cells, cache.d),
-          "new_K and new_V are contiguous bfloat16 [cells][m][d], as the store's")
-    _check(_lib.fw_cache8_append(cache._ref, _ptr(new_K), _ptr(new_V), m, _ptr(status), _stream(stream)),
-           "fw_cache8_append")
+    if new_K.dtype is not torch.bfloat16 or new_V.dtype is not torch.bfloat16 or new_V.shape != new_K.shape or not (
+            new_K.is_contiguous() and new_V.is_contiguous()) or cells != cache.cells or d != cache.d:
+        raise ValueError("new_K and new_V are contiguous bfloat16 [cells][m][d], as the store's")
+    st = _lib.fw_cache8_append(cache._ref, new_K.data_ptr(), new_V.data_ptr(), m, _status_ptr(status, cells),
+                               _raw_stream(stream, new_K))
+    if st != FW_OK:
+        raise FwError(st, "fw_cache8_append")
 
 
 def _cache8_query(cache, q, kv_heads, scale):
     seqs, m, hq, d = q.shape
-    _need(q.dtype == torch.bfloat16 and q.stride(3) == 1 and d == cache.d, "q is bfloat16 [sequences][m][heads][d]")
-    _need(kv_heads >= 1 and hq % kv_heads == 0 and seqs * kv_heads == cache.cells,
-          "sequences x kv_heads is the store's cells, heads a multiple of kv_heads")
-    st = [q.stride(i) if q.shape[i] > 1 else d for i in range(3)]
-    return FwCache8Query(kv_heads, hq // kv_heads, m, q.data_ptr(), *st, 1.0 / math.sqrt(d) if scale is None else scale)
+    s0, s1, s2, one = q.stride()
+    if q.dtype is not torch.bfloat16 or one != 1 or d != cache.d:
+        raise ValueError("q is bfloat16 [sequences][m][heads][d], d contiguous and the store's")
+    if kv_heads < 1 or hq % kv_heads or seqs * kv_heads != cache.cells:
+        raise ValueError("sequences x kv_heads is the store's cells, heads a multiple of kv_heads")
+    # (strides of axes of one entry, which torch leaves open)
+    return FwCache8Query(kv_heads, hq // kv_heads, m, q.data_ptr(), s0 if seqs > 1 else d, s1 if m > 1 else d,
+                         s2 if hq > 1 else d, 1.0 / math.sqrt(d) if scale is None else scale)
 
 
 def cache8_attend_workspace(cache: Cache8, q: torch.Tensor, *, kv_heads: int) -> torch.Tensor:
@@ -624,24 +672,17 @@ def cache8_attend(cache: Cache8, q: torch.Tensor, *, kv_heads: int, scale: float
                   stream=None):
     """fw_cache8_attend.  q: bf16 [sequences][m][q_heads][d] (strides multiples of 8, d contiguous), the queries of
     each sequence's last m tokens; the store's cells are [sequences][kv_heads].  Returns a dict of o (bf16, as q), lse
-    (fp32 [sequences][m][q_heads]) and status [cells]; such a dict passed as out is written instead."""
+    (fp32 [sequences][m][q_heads]) and status [cells]; such a dict passed as out is written instead.  A workspace
+    (cache8_attend_workspace) serves one call at a time."""
     c_q = _cache8_query(cache, q, kv_heads, scale)
-    if out is None:
-        out = dict(o=torch.empty(q.shape, dtype=torch.bfloat16, device=q.device),
-                   lse=torch.empty(q.shape[:3], dtype=torch.float32, device=q.device),
-                   status=torch.empty(cache.cells, dtype=torch.int32, device=q.device))
-        _own_buffers(stream, *out.values())
-    o, lse, status = out["o"], out.get("lse"), out.get("status")
-    _need(o.shape == q.shape and o.dtype == torch.bfloat16 and o.is_contiguous(), "out['o'] is contiguous bfloat16, as q")
-    _need(lse is None or (lse.shape == q.shape[:3] and lse.dtype == torch.float32 and lse.is_contiguous()),
-          "out['lse'] is contiguous float32 [sequences][m][q_heads]")
-    _need(status is None or (status.numel() >= cache.cells and status.dtype == torch.int32 and status.is_contiguous()),
-          "out['status'] is contiguous int32 [cells]")
+    o, lse, status, out = _attention_out(out, q, cache.cells, stream)
     if workspace is None:
         workspace = _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
         _own_buffers(stream, workspace)
-    _check(_lib.fw_cache8_attend(cache._ref, C.byref(c_q), _ptr(o), _ptr(lse), _ptr(status), _ptr(workspace),
-                                 workspace.numel(), _stream(stream)), "fw_cache8_attend")
+    st = _lib.fw_cache8_attend(cache._ref, C.byref(c_q), o, lse, status, workspace.data_ptr(), workspace.numel(),
+                               _raw_stream(stream, q))
+    if st != FW_OK:
+        raise FwError(st, "fw_cache8_attend")
     return out
 
 
