@@ -3,14 +3,15 @@
 // j < n - m + 1 + i:
 //   x_j = scale (q . kc_j) sk,  o = sum_j softmax_j(x) vc_j sv,  lse = log sum_j e^x_j.
 //
-// Bound: the codes' bytes, each read once from memory.  The blocks of all cells
-// in a row are divided evenly over one CTA per SM, whatever the cells' lengths, so
-// a CTA takes the end of one cell, whole cells and the start of another; its eight
-// warps take every eighth block each and fetch them by TMA into a ring of their
-// own, so no warp waits for another before a cell's end.  There the warps' states
-// (running maximum, sum, output) are joined through shared memory; a cell within
-// one CTA is done with that, the parts of the others go to the workspace and a
-// second kernel, launched behind the first one's tail, joins them in their order.
+// Bound: the codes' bytes, each read once from memory.  Two ways over the cells:
+//   few cells (k_cache8_attend_few): a cluster of CTAs per cell, its blocks dealt out
+//   to all their warps, whose states are joined through (distributed) shared memory;
+//   many (k_cache8_attend): the blocks of all cells in a row are divided evenly over the
+//   warps of the GPU, whatever the cells' lengths, so a warp takes the end of one cell,
+//   whole cells and the start of another, and waits for no other warp; the parts of
+//   cells that several warps share go to the workspace, and a second kernel, launched
+//   behind the first one's tail, joins them in their order.
+// Every warp fetches its blocks by TMA into a ring of its own.
 //
 // A block of 32 rows against 8 query rows, transposed on the warp-wide fp16 tensor
 // instructions (a few rows of queries cannot fill a tcgen05 tile, and the stream of
@@ -49,8 +50,8 @@ struct AttendArgs {
     int32_t *status;
     int G;               // CTAs along the blocks
     int32_t *start;      // workspace: [cells] first unit of each cell
-    int32_t *plan;       // workspace: units per CTA
-    float2 *part_ml;     // workspace: [tiles of rows][G][2][rows of a tile] (max, sum)
+    int32_t *plan;       // workspace: units per warp
+    float2 *part_ml;     // workspace: [tiles of rows][warps][2][rows of a tile] (max, sum)
     float *part_o;       // workspace: the same with D columns
 };
 
@@ -76,6 +77,27 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a float at this CTA's shared address p, as CTA `rank` of the cluster has it
+__device__ __forceinline__ float remote(const float *p, int rank)
+{
+    float v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}"
+                 : "=f"(v)
+                 : "r"(tc::smem_u32(p)), "r"(rank)
+                 : "memory");
+    return v;
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
 {
@@ -116,7 +138,8 @@ template <int D> struct Cfg {
     static constexpr int RING = AW * STAGES * 2 * BLK;       // 192 KB
     static constexpr int LDO = D + 4;                        // floats of a row in the joining buffer
     static constexpr int JOIN = AW * 8 * LDO * 4;
-    static constexpr size_t SMEM = 1024 + RING + JOIN;
+    static constexpr size_t SMEM = 1024 + RING;
+    static constexpr size_t SMEM_FEW = 1024 + RING + JOIN;
 };
 
 // Position of a cell's row among the MMA's: row g of each 8 is key kappa(g).  It keeps
@@ -130,141 +153,59 @@ template <int D> __device__ __forceinline__ int piece(int r, int x)
     return D == 128 ? r * 128 + ((x ^ (r & 7)) << 4) : r * 64 + ((x ^ ((r >> 1) & 3)) << 4);
 }
 
-template <int D, int FMT, int NT>
-__global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__ CUtensorMap tmK,
-                                                         const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
-{
-    using C = Cfg<D>;
-    constexpr int MT = D / 16;        // 16-column tiles of the output
-    constexpr int RT = 8 * NT;        // query rows of a CTA
-    constexpr int H = D / 64;         // 64-byte halves of a row
-    extern __shared__ uint8_t smraw[];
-    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
-    float *s_o = reinterpret_cast<float *>(sm + C::RING);
-    __shared__ __align__(8) uint64_t full[AW][C::STAGES];
-    __shared__ float2 s_ml[AW][8];
-    __shared__ int s_scan[AW], s_h0, s_b0, s_err;
-
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT, rows = a.group * a.m;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (lane == 0)
-        for (int s = 0; s < C::STAGES; ++s) tc::mbar_init(&full[wid][s], 1);
-    tc::mbar_init_fence();
-    if (tid == 0) s_err = 0;
-
-    // ---- the units (blocks) of all cells, divided evenly over the CTAs
-    const int per = (a.s.cells + AT - 1) / AT;
-    const int h_lo = min(tid * per, a.s.cells), h_hi = min(h_lo + per, a.s.cells);
-    int mine = 0;
-    for (int h = h_lo; h < h_hi; ++h) {
-        int64_t base;
-        int n;
-        fw_status st;
-        mine += cell_blocks(a.s, h, base, n, st);
-        if (cta == 0 && tile == 0 && a.status) a.status[h] = st;
-    }
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(FW_FULL, incl, o);
-        if (lane >= o) incl += y;
-    }
-    if (lane == 31) s_scan[wid] = incl;
-    __syncthreads();
-    int total = 0, before = incl - mine;
-#pragma unroll
-    for (int w = 0; w < AW; ++w) {
-        if (w < wid) before += s_scan[w];
-        total += s_scan[w];
-    }
-    // at least a block for every warp of a CTA: fewer parts to join
-    const int quota = max((total + a.G - 1) / a.G, AW);
-    const int u0 = min(cta * quota, total), u1 = min(u0 + quota, total);
-    if (u0 >= before && u0 < before + mine) {  // the cell of the CTA's first unit
-        int at = before;
-        for (int h = h_lo; h < h_hi; ++h) {
-            int64_t base;
-            int n;
-            fw_status st;
-            const int nb = cell_blocks(a.s, h, base, n, st);
-            if (u0 < at + nb) {
-                s_h0 = h;
-                s_b0 = u0 - at;
-                break;
-            }
-            at += nb;
-        }
-    }
-    if (cta == 0 && tile == 0) {
-        int at = before;
-        for (int h = h_lo; h < h_hi; ++h) {
-            int64_t base;
-            int n;
-            fw_status st;
-            a.start[h] = at;
-            at += cell_blocks(a.s, h, base, n, st);
-        }
-        if (tid == 0) *a.plan = quota;
-    }
-    __syncthreads();
-    if (u0 >= u1) return;
-
-    // ---- queries: rows of 8, permuted like the codes, below 2^15
-    uint8_t *ring = sm + wid * C::STAGES * 2 * C::BLK;
-    // the warp's producer: its next unit to fetch, by cell
-    int pu = u0 + wid, ph = s_h0, pb = s_b0 + wid, pn, pnb;
-    int64_t pbase;
-    fw_status pst;
-    uint32_t pphase = 0;  // fetches so far
-    pnb = cell_blocks(a.s, ph, pbase, pn, pst);
-    auto fetch = [&]() {
-        if (pu >= u1) return;
-        while (pb >= pnb && ph + 1 < a.s.cells) {  // (a unit is left, so a cell holds it)
-            pb -= pnb;
-            pnb = cell_blocks(a.s, ++ph, pbase, pn, pst);
-        }
-        const int s = pphase % C::STAGES;
-        if (lane == 0) {
-            tc::mbar_arrive_expect_tx(&full[wid][s], 2 * C::BLK);
-            const int32_t r = (int32_t)(pbase / BR) + pb;
-            tc::tma_load_2d(ring + s * 2 * C::BLK, &tmK, 0, r * BR, &full[wid][s]);
-            tc::tma_load_2d(ring + s * 2 * C::BLK + C::BLK, &tmV, 0, r * BR, &full[wid][s]);
-        }
-        ++pphase;
-        pu += AW;
-        pb += AW;
-    };
-#pragma unroll 1
-    for (int s = 0; s < C::STAGES; ++s) fetch();
-
-    int h = s_h0, b = s_b0, u = u0;  // the segment: blocks of one cell
-    uint32_t cphase = 0;             // blocks consumed by this warp
+// A warp's ring of blocks.
+template <int D> struct Ring {
+    uint8_t *mem;
+    uint64_t *full;
+    uint32_t issued = 0, used = 0;
     bool ok = true;
-    while (u < u1) {
-        int64_t base;
-        int n;
-        fw_status st;
-        int nb = cell_blocks(a.s, h, base, n, st);
-        while (b >= nb && h + 1 < a.s.cells) {  // cells without rows, and the next cell
-            b -= nb;
-            nb = cell_blocks(a.s, ++h, base, n, st);
-        }
-        if (b >= nb) break;  // (never, unless the counts change under the call)
-        const int bend = min(nb, b + (u1 - u));
-        const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
 
-        // this thread's part of the queries: row g of each 8, 16 consecutive columns of each half
-        uint32_t qf[NT][H][8];
-        float rf[NT][2];     // logits' factor of rows 2c, 2c + 1
-        int seen[NT][2];     // rows of the cell they see
+    __device__ void fetch(const CUtensorMap *tmK, const CUtensorMap *tmV, int64_t row, int lane)
+    {
+        using C = Cfg<D>;
+        const int s = issued % C::STAGES;
+        if (lane == 0) {
+            tc::mbar_arrive_expect_tx(&full[s], 2 * C::BLK);
+            tc::tma_load_2d(mem + s * 2 * C::BLK, tmK, 0, (int32_t)row, &full[s]);
+            tc::tma_load_2d(mem + s * 2 * C::BLK + C::BLK, tmV, 0, (int32_t)row, &full[s]);
+        }
+        ++issued;
+    }
+    // the next block, or null where the wait gave up
+    __device__ const uint8_t *next()
+    {
+        using C = Cfg<D>;
+        const int s = used % C::STAGES;
+        if (ok) ok = tc::mbar_wait(&full[s], (used / C::STAGES) & 1u, A_WAIT);
+        if (!ok) return nullptr;
+        ++used;
+        return mem + s * 2 * C::BLK;
+    }
+    // copies still under way land before the CTA's memory goes
+    __device__ void drain()
+    {
+        using C = Cfg<D>;
+        for (; used < issued; ++used) tc::mbar_wait(&full[used % C::STAGES], (used / C::STAGES) & 1u, A_WAIT);
+    }
+};
+
+// A warp's queries and running softmax over blocks of one cell, NT tiles of 8 query rows.
+template <int D, int FMT, int NT> struct Rows {
+    static constexpr int MT = D / 16;  // 16-column tiles of the output
+    static constexpr int H = D / 64;   // 64-byte halves of a row
+    uint32_t qf[NT][H][8];             // row g of each 8, 16 consecutive columns of each half
+    float rf[NT][2];                   // logits' factor of rows 2c, 2c + 1
+    float O[NT][MT][4], mx[NT][2], l[NT][2];
+
+    __device__ __forceinline__ void start(const AttendArgs &a, int seq, int hk, int row0, int lane)
+    {
+        const int g = lane >> 2, c = lane & 3, rows = a.group * a.m;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int r = row0 + 8 * t + g;
+            const int r = row0 + 8 * t + g, i = r / a.group;
+            const uint16_t *src = a.q + seq * a.q_seq + i * a.q_tok + (int64_t)(hk * a.group + r - i * a.group) * a.q_head;
             uint4 x[H][2];
             uint32_t top = 0;
-            const int i = r / a.group;
-            const uint16_t *src = a.q + seq * a.q_seq + i * a.q_tok + (int64_t)(hk * a.group + r - i * a.group) * a.q_head;
 #pragma unroll
             for (int e = 0; e < H; ++e)
 #pragma unroll
@@ -291,151 +232,143 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 rf[t][e] = __shfl_sync(FW_FULL, fac, (2 * c + e) * 4);
-                seen[t][e] = n - a.m + 1 + (row0 + 8 * t + 2 * c + e) / a.group;
+                mx[t][e] = -INFINITY;
+                l[t][e] = 0.f;
             }
+#pragma unroll
+            for (int i2 = 0; i2 < MT; ++i2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[t][i2][e] = 0.f;
         }
-        const int all = n - a.m + 1;  // rows that every query sees
+    }
 
-        float O[NT][MT][4], mx[NT][2], l[NT][2];
+    // One block, rows 32 blk .. of a cell of n; `read` is called once the tile has been read.
+    template <typename F>
+    __device__ __forceinline__ void block(const AttendArgs &a, const uint8_t *tk, float sk, float sv, int blk, int n, int row0,
+                                          int lane, F read)
+    {
+        const int g = lane >> 2, c = lane & 3;
+        const uint8_t *tv = tk + Cfg<D>::BLK;
+        // S^T: two tiles of 16 keys
+        float S[NT][2][4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            mx[t][0] = mx[t][1] = -INFINITY;
-            l[t][0] = l[t][1] = 0.f;
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int z = 0; z < 8; ++z) S[t][z >> 2][z & 3] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) O[t][i][e] = 0.f;
-        }
-        // the warp's first block at or behind b: units u0 + wid + 8 i
-        const int first = b + ((wid - (u - u0)) & (AW - 1));
-#pragma unroll 1
-        for (int blk = first; blk < bend; blk += AW) {
-            const int s = cphase % C::STAGES;
-            const float sk = a.s.ks[base / BR + blk], sv = a.s.vs[base / BR + blk];
-            if (ok) ok = tc::mbar_wait(&full[wid][s], (cphase / C::STAGES) & 1u, A_WAIT);
-            if (!ok) break;
-            ++cphase;
-            const uint8_t *tk = ring + s * 2 * C::BLK, *tv = tk + C::BLK;
-            // S^T: two tiles of 16 keys
-            float S[NT][2][4];
+        for (int z = 0; z < 2; ++z)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int e = 0; e < H; ++e) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(tk + piece<D>(16 * z + kappa(g), 4 * e + c));
+                const uint4 y = *reinterpret_cast<const uint4 *>(tk + piece<D>(16 * z + 8 + kappa(g), 4 * e + c));
+                const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                for (int z = 0; z < 8; ++z) S[t][z >> 2][z & 3] = 0.f;
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t a0, a1, a2, a3;
+                    decode4<FMT>(xw[k], a0, a2);
+                    decode4<FMT>(yw[k], a1, a3);
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
-#pragma unroll
-                for (int e = 0; e < H; ++e) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(tk + piece<D>(16 * z + kappa(g), 4 * e + c));
-                    const uint4 y = *reinterpret_cast<const uint4 *>(tk + piece<D>(16 * z + 8 + kappa(g), 4 * e + c));
-                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint32_t a0, a1, a2, a3;
-                        decode4<FMT>(xw[k], a0, a2);
-                        decode4<FMT>(yw[k], a1, a3);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) mma(S[t][z], a0, a1, a2, a3, qf[t][e][2 * k], qf[t][e][2 * k + 1]);
-                    }
-                }
-            // weights: keys kappa(g) + 8 i of rows 2c, 2c + 1
-            const int j0 = blk * BR + kappa(g);
-            const bool masked = blk * BR + BR > all;
-            uint32_t pb4[NT][4];
-            bool grew = false;
-            float al[NT][2];
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float f = rf[t][e] * sk;
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float &x = S[t][i >> 1][2 * (i & 1) + e];
-                        x *= f;
-                        if (masked && j0 + 8 * i >= seen[t][e]) x = -INFINITY;
-                        top = fmaxf(top, x);
-                    }
-                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 4));
-                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 8));
-                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 16));
-                    const float old = mx[t][e], now = fmaxf(old, top);
-                    grew |= now > old;
-                    al[t][e] = now > old ? ex2(old - now) : 1.f;  // (0 where nothing was seen before)
-                    mx[t][e] = now;
-                    const float ref = now == -INFINITY ? 0.f : now - P_UP;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float &x = S[t][i >> 1][2 * (i & 1) + e];
-                        x = ex2(x - ref);
-                        sum += x;
-                    }
-                    l[t][e] = fmaf(l[t][e], al[t][e], sum);
-                }
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    pb4[t][i] = transpose8x8(pack_f16(S[t][i >> 1][2 * (i & 1)], S[t][i >> 1][2 * (i & 1) + 1]));
-            if (__any_sync(FW_FULL, grew)) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) O[t][i][e] *= al[t][e & 1];
-            }
-            // O^T += sv V^T P^T: keys kappa(2c), kappa(2c + 1), 8 behind them, then 16
-            const bool stale = blk * BR + BR > n;
-            constexpr int VW = D / 32;  // words of a row's D / 8 columns
-            uint32_t v[8][VW];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int key = 8 * (i >> 1) + kappa(2 * c + (i & 1));
-                if constexpr (D == 128) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(tv + piece<D>(key, g));
-                    v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2 *>(tv + piece<D>(key, g >> 1) + 8 * (g & 1));
-                    v[i][0] = x.x, v[i][1] = x.y;
-                }
-                if (stale && blk * BR + key >= n) {  // rows behind the count hold anything
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) v[i][w] = 0;
+                    for (int t = 0; t < NT; ++t) mma(S[t][z], a0, a1, a2, a3, qf[t][e][2 * k], qf[t][e][2 * k + 1]);
                 }
             }
-            __syncwarp();
-            fetch();  // every lane has read the stage
+        // weights: keys kappa(g) + 8 i of rows 2c, 2c + 1
+        const int j0 = blk * BR + kappa(g), all = n - a.m + 1;  // rows that every query sees
+        const bool masked = blk * BR + BR > all;
+        uint32_t p4[NT][4];
+        bool grew = false;
+        float al[NT][2];
 #pragma unroll
-            for (int w = 0; w < VW; ++w) {
-                // columns 4w .. 4w + 3 of the thread's: pairs of keys side by side
-                uint32_t p[4][4];  // [pair of keys][column]
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float f = rf[t][e] * sk;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) S[t][i >> 1][2 * (i & 1) + e] *= f;
+                if (masked) {
+                    const int seen = all + (row0 + 8 * t + 2 * c + e) / a.group;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (j0 + 8 * i >= seen) S[t][i >> 1][2 * (i & 1) + e] = -INFINITY;
+                }
+                float top = fmaxf(fmaxf(S[t][0][e], S[t][0][2 + e]), fmaxf(S[t][1][e], S[t][1][2 + e]));
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 16));
+                const float old = mx[t][e], now = fmaxf(old, top);
+                grew |= now > old;
+                al[t][e] = now > old ? ex2(old - now) : 1.f;  // (0 where nothing was seen before)
+                mx[t][e] = now;
+                const float ref = now == -INFINITY ? 0.f : now - P_UP;
+                float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    decode4<FMT>(__byte_perm(v[2 * i][w], v[2 * i + 1][w], 0x5140), p[i][0], p[i][1]);
-                    decode4<FMT>(__byte_perm(v[2 * i][w], v[2 * i + 1][w], 0x7362), p[i][2], p[i][3]);
+                    float &x = S[t][i >> 1][2 * (i & 1) + e];
+                    x = ex2(x - ref);
+                    sum += x;
                 }
+                l[t][e] = fmaf(l[t][e], al[t][e], sum);
+            }
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        float x[4] = {0.f, 0.f, 0.f, 0.f};
-                        mma(x, p[0][2 * f], p[0][2 * f + 1], p[1][2 * f], p[1][2 * f + 1], pb4[t][0], pb4[t][1]);
-                        mma(x, p[2][2 * f], p[2][2 * f + 1], p[3][2 * f], p[3][2 * f + 1], pb4[t][2], pb4[t][3]);
+            for (int i = 0; i < 4; ++i)
+                p4[t][i] = transpose8x8(pack_f16(S[t][i >> 1][2 * (i & 1)], S[t][i >> 1][2 * (i & 1) + 1]));
+        if (__any_sync(FW_FULL, grew)) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) O[t][2 * w + f][e] = fmaf(sv, x[e], O[t][2 * w + f][e]);
-                    }
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) O[t][i][e] *= al[t][e & 1];
+        }
+        // O^T += sv V^T P^T: keys kappa(2c), kappa(2c + 1), 8 behind them, then 16
+        const bool stale = blk * BR + BR > n;
+        constexpr int VW = D / 32;  // words of a row's D / 8 columns
+        uint32_t v[8][VW];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int key = 8 * (i >> 1) + kappa(2 * c + (i & 1));
+            if constexpr (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(tv + piece<D>(key, g));
+                v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(tv + piece<D>(key, g >> 1) + 8 * (g & 1));
+                v[i][0] = x.x, v[i][1] = x.y;
+            }
+            if (stale && blk * BR + key >= n) {  // rows behind the count hold anything
+#pragma unroll
+                for (int w = 0; w < VW; ++w) v[i][w] = 0;
             }
         }
-        if (!ok) s_err = 1;
-        // ---- the warps' states joined, 8 rows at a time
-        const bool whole = b == 0 && bend == nb;
-        const int part = cta * 2 + (u == u0 ? 0 : 1);
+        __syncwarp();
+        read();  // every lane has read the tile
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (row0 + 8 * t >= rows) break;
+        for (int w = 0; w < VW; ++w) {
+            // columns 4w .. 4w + 3 of the thread's: pairs of keys side by side
+            uint32_t p[4][4];  // [pair of keys][column]
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                decode4<FMT>(__byte_perm(v[2 * i][w], v[2 * i + 1][w], 0x5140), p[i][0], p[i][1]);
+                decode4<FMT>(__byte_perm(v[2 * i][w], v[2 * i + 1][w], 0x7362), p[i][2], p[i][3]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma(x, p[0][2 * f], p[0][2 * f + 1], p[1][2 * f], p[1][2 * f + 1], p4[t][0], p4[t][1]);
+                    mma(x, p[2][2 * f], p[2][2 * f + 1], p[3][2 * f], p[3][2 * f + 1], p4[t][2], p4[t][3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) O[t][2 * w + f][e] = fmaf(sv, x[e], O[t][2 * w + f][e]);
+                }
+        }
+    }
+
+    // The sums over all lanes of a row.
+    __device__ __forceinline__ void close()
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float sum = l[t][e];
@@ -444,59 +377,175 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
                 sum += __shfl_xor_sync(FW_FULL, sum, 16);
                 l[t][e] = sum;
             }
-            __syncthreads();
-            if (g == 0) {
-                s_ml[wid][2 * c] = make_float2(mx[t][0], l[t][0]);
-                s_ml[wid][2 * c + 1] = make_float2(mx[t][1], l[t][1]);
-            }
+    }
+};
+
+// Index of query row r of cell (seq, hk) in the outputs.
+__device__ __forceinline__ int64_t out_row(const AttendArgs &a, int seq, int hk, int r)
+{
+    const int i = r / a.group;
+    return ((int64_t)seq * a.m + i) * a.kv_heads * a.group + hk * a.group + (r - i * a.group);
+}
+// lse of a row with running maximum mx and sum l of 2^(x - mx + P_UP)
+__device__ __forceinline__ float lse_of(float mx, float l)
+{
+    return l == 0.f ? -INFINITY : (mx - P_UP + log2f(l)) * 0.6931471805599453f;
+}
+
+template <int D, int FMT, int NT>
+__global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__ CUtensorMap tmK,
+                                                         const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
+{
+    using C = Cfg<D>;
+    constexpr int MT = D / 16, RT = 8 * NT;  // RT: query rows of a CTA
+    extern __shared__ uint8_t smraw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
+    __shared__ __align__(8) uint64_t full[AW][C::STAGES];
+    __shared__ int s_scan[AW], s_h0[AW], s_b0[AW];
+
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT, rows = a.group * a.m;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (lane < C::STAGES) tc::mbar_init(&full[wid][lane], 1);
+    tc::mbar_init_fence();
+
+    // ---- the units (blocks) of all cells, divided evenly over the warps of all CTAs
+    const int per = (a.s.cells + AT - 1) / AT;
+    const int h_lo = min(tid * per, a.s.cells), h_hi = min(h_lo + per, a.s.cells);
+    int mine = 0;
+    for (int h = h_lo; h < h_hi; ++h) {
+        int64_t base;
+        int n;
+        fw_status st;
+        mine += cell_blocks(a.s, h, base, n, st);
+        if (cta == 0 && tile == 0 && a.status) a.status[h] = st;
+    }
+    int incl = mine;
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(FW_FULL, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) s_scan[wid] = incl;
+    __syncthreads();
+    int total = 0, before = incl - mine;
 #pragma unroll
-                for (int i = 0; i < MT; i += 2)
-                    *reinterpret_cast<float4 *>(s_o + (wid * 8 + 2 * c + e) * C::LDO + g * (D / 8) + 2 * i) =
-                        make_float4(O[t][i][e], O[t][i][2 + e], O[t][i + 1][e], O[t][i + 1][2 + e]);
-            __syncthreads();
-            const int r = row0 + 8 * t + wid;  // a warp per row
-            if (r < rows) {
-                float M = -INFINITY, L = 0.f, acc[D / 32];
-#pragma unroll
-                for (int w = 0; w < AW; ++w) M = fmaxf(M, s_ml[w][wid].x);
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
-#pragma unroll
-                for (int w = 0; w < AW; ++w) {
-                    const float2 ml = s_ml[w][wid];
-                    const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2(ml.x - M);
-                    L = fmaf(f, ml.y, L);
-#pragma unroll
-                    for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(f, s_o[(w * 8 + wid) * C::LDO + lane + 32 * i], acc[i]);
+    for (int w = 0; w < AW; ++w) {
+        if (w < wid) before += s_scan[w];
+        total += s_scan[w];
+    }
+    // consecutive ranges go to different CTAs; at least two blocks each, so that there is less to join
+    const int quota = max((total + a.G * AW - 1) / (a.G * AW), 2);
+    {
+        int at = before;
+        for (int h = h_lo; h < h_hi; ++h) {
+            int64_t base;
+            int n;
+            fw_status st;
+            const int nb = cell_blocks(a.s, h, base, n, st);
+            // the warps of this CTA whose ranges begin in the cell
+            for (int w = 0; w < AW; ++w) {
+                const int64_t u = (int64_t)(w * a.G + cta) * quota;
+                if (u >= at && u < at + nb) {
+                    s_h0[w] = h;
+                    s_b0[w] = (int)(u - at);
                 }
-                if (s_err) L = NAN;
-                if (whole) {
-                    const int i = r / a.group;
-                    const int64_t out = ((int64_t)seq * a.m + i) * a.kv_heads * a.group + hk * a.group + (r - i * a.group);
-                    const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-                    for (int e = 0; e < D / 32; ++e)
-                        a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
-                    if (a.lse && lane == 0) a.lse[out] = L == 0.f ? -INFINITY : (M - P_UP + log2f(L)) * 0.6931471805599453f;
-                } else {
-                    const int64_t at = ((int64_t)tile * a.G * 2 + part) * RT + 8 * t + wid;
-                    if (lane == 0) a.part_ml[at] = make_float2(M, L);
-#pragma unroll
-                    for (int e = 0; e < D / 32; ++e) a.part_o[at * D + lane + 32 * e] = acc[e];
-                }
             }
+            if (cta == 0 && tile == 0) a.start[h] = at;
+            at += nb;
         }
-        if (s_err && tid == 0 && a.status) a.status[h] = FW_ERR_TIMEOUT;
+        if (cta == 0 && tile == 0 && tid == 0) *a.plan = quota;
+    }
+    __syncthreads();
+    const int gw = wid * a.G + cta;
+    const int64_t first = (int64_t)gw * quota;
+    if (first >= total) return;
+    int u = (int)first;
+    const int u1 = min(u + quota, total);
+
+    Ring<D> ring;
+    ring.mem = sm + wid * C::STAGES * 2 * C::BLK;
+    ring.full = full[wid];
+    // the warp's producer: its next unit to fetch, by cell
+    int pu = u, ph = s_h0[wid], pb = s_b0[wid], pn, pnb;
+    int64_t pbase;
+    fw_status pst;
+    pnb = cell_blocks(a.s, ph, pbase, pn, pst);
+    auto fetch = [&]() {
+        if (pu >= u1) return;
+        while (pb >= pnb && ph + 1 < a.s.cells) {  // (a unit is left, so a cell holds it)
+            pb -= pnb;
+            pnb = cell_blocks(a.s, ++ph, pbase, pn, pst);
+        }
+        ring.fetch(&tmK, &tmV, pbase + (int64_t)pb * BR, lane);
+        ++pu;
+        ++pb;
+    };
+#pragma unroll 1
+    for (int s = 0; s < C::STAGES; ++s) fetch();
+
+    int h = s_h0[wid], b = s_b0[wid];  // the segment: blocks of one cell
+    Rows<D, FMT, NT> R;
+    while (u < u1) {
+        int64_t base;
+        int n;
+        fw_status st;
+        int nb = cell_blocks(a.s, h, base, n, st);
+        while (b >= nb && h + 1 < a.s.cells) {  // cells without rows, and the next cell
+            b -= nb;
+            nb = cell_blocks(a.s, ++h, base, n, st);
+        }
+        if (b >= nb) break;  // (never, unless the counts change under the call)
+        const int bend = min(nb, b + (u1 - u));
+        const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
+        R.start(a, seq, hk, row0, lane);
+        const float *ks = a.s.ks + base / BR, *vs = a.s.vs + base / BR;
+        float sk = ks[b], sv = vs[b];
+#pragma unroll 1
+        for (int blk = b; blk < bend; ++blk) {
+            const float k = sk, v = sv;
+            if (blk + 1 < bend) sk = ks[blk + 1], sv = vs[blk + 1];
+            const uint8_t *tk = ring.next();
+            if (!tk) break;
+            R.block(a, tk, k, v, blk, n, row0, lane, fetch);
+        }
+        R.close();
+        const bool whole = b == 0 && bend == nb;
+        const int seg = u == (int)first ? 0 : 1;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = row0 + 8 * t + 2 * c + e;
+                if (r >= rows) continue;
+                const float sum = ring.ok ? R.l[t][e] : NAN;
+                if (whole) {
+                    const int64_t out = out_row(a, seq, hk, r);
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    uint32_t w[MT];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) w[i] = pack_bf16(R.O[t][i][e] * inv, R.O[t][i][2 + e] * inv);
+                    uint4 *dst = reinterpret_cast<uint4 *>(a.o + out * D + g * (D / 8));
+#pragma unroll
+                    for (int i = 0; i < MT; i += 4) dst[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                    if (a.lse && g == 0) a.lse[out] = lse_of(R.mx[t][e], sum);
+                } else {
+                    const int64_t at = (((int64_t)tile * a.G * AW + gw) * 2 + seg) * RT + 8 * t + 2 * c + e;
+                    if (g == 0) a.part_ml[at] = make_float2(R.mx[t][e], sum);
+                    float4 *dst = reinterpret_cast<float4 *>(a.part_o + at * D + g * (D / 8));
+#pragma unroll
+                    for (int i = 0; i < MT; i += 2)
+                        dst[i / 2] = make_float4(R.O[t][i][e], R.O[t][i][2 + e], R.O[t][i + 1][e], R.O[t][i + 1][2 + e]);
+                }
+            }
+        if (!ring.ok && lane == 0 && a.status) a.status[h] = FW_ERR_TIMEOUT;
         u += bend - b;
         b = bend;
     }
-    // copies of this warp that are still under way land before the CTA's memory goes
-    for (; cphase < pphase; ++cphase) tc::mbar_wait(&full[wid][cphase % C::STAGES], (cphase / C::STAGES) & 1u, A_WAIT);
+    ring.drain();
 }
 
-// The parts of a cell that spans several CTAs, joined in their order; empty cells' outputs.
+// The parts of a cell that several warps share, joined in their order; empty cells' outputs.
 // A CTA per (cell, query row): four warps take every fourth part each.
 template <int D> __global__ void __launch_bounds__(128) k_cache8_join(const AttendArgs a, int RT)
 {
@@ -509,15 +558,17 @@ template <int D> __global__ void __launch_bounds__(128) k_cache8_join(const Atte
     int n;
     fw_status st;
     const int nb = cell_blocks(a.s, h, base, n, st), quota = *a.plan, s = a.start[h];
-    const int c0 = s / quota, c1 = nb > 0 ? (s + nb - 1) / quota : c0;
-    if (nb > 0 && c0 == c1) return;
+    const int w0 = s / quota, w1 = nb > 0 ? (s + nb - 1) / quota : w0;
+    if (nb > 0 && w0 == w1) return;
     float M = -INFINITY, L = 0.f, acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    if (nb > 0)
-        for (int p = c0 + wid; p <= c1; p += 4) {
-            const int seg = p == c0 && s > p * quota ? 1 : 0;
-            const int64_t at = ((int64_t)(r / RT) * a.G * 2 + 2 * p + seg) * RT + r % RT;
+    if (nb > 0) {
+        const int64_t tile0 = (int64_t)(r / RT) * a.G * AW;
+#pragma unroll 4
+        for (int p = w0 + wid; p <= w1; p += 4) {
+            const int seg = p == w0 && s > p * quota ? 1 : 0;
+            const int64_t at = ((tile0 + p) * 2 + seg) * RT + r % RT;
             const float2 ml = a.part_ml[at];
             const float now = fmaxf(M, ml.x);
             const float f = M == now ? 1.f : ex2(M - now), y = ml.x == now ? 1.f : ex2(ml.x - now);
@@ -526,6 +577,7 @@ template <int D> __global__ void __launch_bounds__(128) k_cache8_join(const Atte
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], f, a.part_o[at * D + lane + 32 * e] * y);
         }
+    }
     if (lane == 0) s_ml[wid] = make_float2(M, L);
 #pragma unroll
     for (int e = 0; e < E; ++e) s_o[wid][lane + 32 * e] = acc[e];
@@ -542,35 +594,182 @@ template <int D> __global__ void __launch_bounds__(128) k_cache8_join(const Atte
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = fmaf(f, s_o[w][lane + 32 * e], acc[e]);
     }
-    const int seq = h / a.kv_heads, i = r / a.group;
-    const int64_t out = ((int64_t)seq * a.m + i) * a.kv_heads * a.group + (h - seq * a.kv_heads) * a.group + (r - i * a.group);
+    const int seq = h / a.kv_heads;
+    const int64_t out = out_row(a, seq, h - seq * a.kv_heads, r);
     const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
-    if (a.lse && lane == 0) a.lse[out] = L == 0.f ? -INFINITY : (M - P_UP + log2f(L)) * 0.6931471805599453f;
+    if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
 }
 
-// Query rows of a CTA: 8 where they suffice (a row more costs the second product's and
-// the statistics' work again), else 16 and as many rounds over the store as that takes.
-int row_tile(const fw_cache8_query &q) { return q.group * q.m <= 8 ? 8 : 16; }
+// Eight states of a row joined: their (maximum, sum) and E of a lane's columns.
+template <int E, typename FM, typename FO>
+__device__ __forceinline__ void join8(FM ml_of, FO o_of, float &M, float &L, float (&acc)[E])
+{
+    float2 ml[8];
+    M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) ml[w] = ml_of(w), M = fmaxf(M, ml[w].x);
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        const float f = ml[w].x == M ? 1.f : ex2(ml[w].x - M);
+        L = fmaf(f, ml[w].y, L);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(f, o_of(w, e), acc[e]);
+    }
+}
+
+// A cluster of FEW CTAs per cell and tile of rows, its blocks dealt out to their warps one by one.
+constexpr int FEW = 8;
+template <int D, int FMT, int NT>
+__global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
+    k_cache8_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
+{
+    using C = Cfg<D>;
+    constexpr int MT = D / 16, RT = 8 * NT, E = D / 32;
+    extern __shared__ uint8_t smraw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
+    float *s_o = reinterpret_cast<float *>(sm + C::RING);  // [AW][8][LDO]
+    __shared__ __align__(8) uint64_t full[AW][C::STAGES];
+    __shared__ float2 s_ml[AW][8];
+    __shared__ float2 s_pml[8];
+
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int h = blockIdx.x / FEW, rank = blockIdx.x % FEW, row0 = blockIdx.y * RT, rows = a.group * a.m;
+    if (lane < C::STAGES) tc::mbar_init(&full[wid][lane], 1);
+    tc::mbar_init_fence();
+    __syncwarp();
+    int64_t base;
+    int n;
+    fw_status st;
+    const int nb = cell_blocks(a.s, h, base, n, st);
+    if (rank == 0 && blockIdx.y == 0 && tid == 0 && a.status) a.status[h] = st;
+    Ring<D> ring;
+    ring.mem = sm + wid * C::STAGES * 2 * C::BLK;
+    ring.full = full[wid];
+    int pb = rank + FEW * wid;  // (the first blocks go to different CTAs)
+    auto fetch = [&]() {
+        if (pb >= nb) return;
+        ring.fetch(&tmK, &tmV, base + (int64_t)pb * BR, lane);
+        pb += FEW * AW;
+    };
+#pragma unroll 1
+    for (int s = 0; s < C::STAGES; ++s) fetch();
+    const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
+    Rows<D, FMT, NT> R;
+    R.start(a, seq, hk, row0, lane);
+    const float *ks = a.s.ks + base / BR, *vs = a.s.vs + base / BR;
+#pragma unroll 1
+    for (int blk = rank + FEW * wid; blk < nb; blk += FEW * AW) {
+        const float sk = ks[blk], sv = vs[blk];
+        const uint8_t *tk = ring.next();
+        if (!tk) break;
+        R.block(a, tk, sk, sv, blk, n, row0, lane, fetch);
+    }
+    R.close();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (row0 + 8 * t >= rows) break;
+        // ---- the warps' rows joined in the CTA, a warp per row
+        if (t > 0) cluster_sync();  // (the rows before have been read)
+        if (g == 0) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s_ml[wid][2 * c + e] = make_float2(R.mx[t][e], ring.ok ? R.l[t][e] : NAN);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < MT; i += 2)
+                *reinterpret_cast<float4 *>(s_o + (wid * 8 + 2 * c + e) * C::LDO + g * (D / 8) + 2 * i) =
+                    make_float4(R.O[t][i][e], R.O[t][i][2 + e], R.O[t][i + 1][e], R.O[t][i + 1][2 + e]);
+        __syncthreads();
+        float M, L, acc[E];
+        join8<E>([&](int w) { return s_ml[w][wid]; }, [&](int w, int e) { return s_o[(w * 8 + wid) * C::LDO + lane + 32 * e]; },
+                 M, L, acc);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_o[wid * C::LDO + lane + 32 * e] = acc[e];  // (its row in the first warp's place)
+        if (lane == 0) s_pml[wid] = make_float2(M, L);
+        cluster_sync();
+        // ---- and over the cluster's CTAs, a CTA per row
+        const int r = row0 + 8 * t + rank;
+        if (wid == 0 && r < rows) {
+            join8<E>([&](int w) { return make_float2(remote(&s_pml[rank].x, w), remote(&s_pml[rank].y, w)); },
+                     [&](int w, int e) { return remote(&s_o[rank * C::LDO + lane + 32 * e], w); }, M, L, acc);
+            const int64_t out = out_row(a, seq, hk, r);
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
+            if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
+        }
+    }
+    ring.drain();
+    if (!ring.ok && lane == 0 && a.status) a.status[h] = FW_ERR_TIMEOUT;
+    cluster_sync();  // no CTA leaves while another reads its rows
+}
+static_assert(FEW == 8 && AW == 8, "a CTA and a warp per row of 8");
+
+// Query rows of a CTA: as few tiles of 8 as hold them, as far as registers go (a second round over
+// the store costs its fetches and products again).
+int row_tile(const fw_cache8 &c, const fw_cache8_query &q)
+{
+    const int rows = q.group * q.m;
+    return rows <= 8 ? 8 : rows <= 16 || c.d == 128 ? 16 : 32;
+}
+
+// Whether the cells are so few, and hold so little at most, that a cluster each is faster.
+bool few_cells(const fw_cache8 &c, int tiles, int sms)
+{
+    return (int64_t)c.cells * tiles * FEW <= sms && c.rows <= (int64_t)c.cells * 16384;
+}
 
 struct Plan {
+    bool few;
     int G, RT, tiles;
     size_t start, plan, ml, o, bytes;
 };
-fw_status plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
+void plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
 {
-    if (device_sms(&p.G) != FW_OK) p.G = 152;  // no device: the size query still answers
-    p.RT = row_tile(q);
+    int sms = 0;
+    if (device_sms(&sms) != FW_OK) sms = 152;  // no device: the size query still answers
+    p.RT = row_tile(c, q);
     p.tiles = (q.group * q.m + p.RT - 1) / p.RT;
-    p.start = 0;
+    p.few = few_cells(c, p.tiles, sms);
+    p.G = std::max(1, sms / p.tiles);  // one wave
+    p.start = p.plan = p.ml = p.o = p.bytes = 0;
+    if (p.few) return;
     p.plan = align256((size_t)c.cells * 4);
     p.ml = p.plan + 256;
-    const size_t parts = (size_t)p.tiles * p.G * 2 * p.RT;
+    const size_t parts = (size_t)p.tiles * p.G * AW * 2 * p.RT;
     p.o = p.ml + align256(parts * 8);
     p.bytes = p.o + align256(parts * c.d * 4);
+}
+
+template <typename K>
+fw_status launch(K kernel, int grid, int tiles, size_t smem, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a,
+                 cudaStream_t s)
+{
+    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    FW_LAUNCH(kernel, dim3((unsigned)grid, (unsigned)tiles), AT, smem, s, mk, mv, a);
     return FW_OK;
+}
+template <int D, int FMT>
+fw_status attend(const Plan &p, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
+{
+    constexpr int NTL = D == 128 ? 2 : 4;  // tiles of 8 rows at most
+    using C = Cfg<D>;
+    if (p.few) {
+        const int grid = cells * FEW;
+        if (p.RT == 8) return launch(k_cache8_attend_few<D, FMT, 1>, grid, p.tiles, C::SMEM_FEW, mk, mv, a, s);
+        if (p.RT == 16) return launch(k_cache8_attend_few<D, FMT, 2>, grid, p.tiles, C::SMEM_FEW, mk, mv, a, s);
+        return launch(k_cache8_attend_few<D, FMT, NTL>, grid, p.tiles, C::SMEM_FEW, mk, mv, a, s);
+    }
+    if (p.RT == 8) return launch(k_cache8_attend<D, FMT, 1>, p.G, p.tiles, C::SMEM, mk, mv, a, s);
+    if (p.RT == 16) return launch(k_cache8_attend<D, FMT, 2>, p.G, p.tiles, C::SMEM, mk, mv, a, s);
+    return launch(k_cache8_attend<D, FMT, NTL>, p.G, p.tiles, C::SMEM, mk, mv, a, s);
 }
 
 }  // namespace
@@ -578,7 +777,8 @@ fw_status plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
 size_t cache8_attend_workspace(const fw_cache8 &c, const fw_cache8_query &q)
 {
     Plan p;
-    return plan_of(c, q, p) == FW_OK ? p.bytes : 0;
+    plan_of(c, q, p);
+    return p.bytes;
 }
 
 fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, float *lse, int32_t *status, void *ws,
@@ -589,22 +789,16 @@ fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, f
     CUtensorMap mk, mv;
     // (a store without rows has no blocks to fetch: any valid map does)
     const uint64_t rows = std::max<int64_t>(c.rows, BR);
-    if (!make_tma_2d_bytes(&mk, c.rows ? c.k : ws, rows, (uint64_t)c.d, BR) ||
-        !make_tma_2d_bytes(&mv, c.rows ? c.v : ws, rows, (uint64_t)c.d, BR))
+    if (!make_tma_2d_bytes(&mk, c.rows ? c.k : o, rows, (uint64_t)c.d, BR) ||
+        !make_tma_2d_bytes(&mv, c.rows ? c.v : o, rows, (uint64_t)c.d, BR))
         return FW_ERR_CUDA;
     uint8_t *w = (uint8_t *)ws;
-    const AttendArgs a{store(c),  q.kv_heads, q.group, q.m, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
+    const AttendArgs a{store(c), q.kv_heads, q.group, q.m, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
                        q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, p.G, (int32_t *)(w + p.start),
                        (int32_t *)(w + p.plan), (float2 *)(w + p.ml), (float *)(w + p.o)};
-    auto attend = [&](auto kernel, size_t smem) -> fw_status {
-        FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        FW_LAUNCH(kernel, dim3((unsigned)p.G, (unsigned)p.tiles), AT, smem, s, mk, mv, a);
-        return FW_OK;
-    };
     fw_status st = FW_OK;
-    FW_CACHE8_DISPATCH(c, st = p.RT == 8 ? attend(k_cache8_attend<D, FMT, 1>, Cfg<D>::SMEM)
-                                         : attend(k_cache8_attend<D, FMT, 2>, Cfg<D>::SMEM));
-    if (st != FW_OK) return st;
+    FW_CACHE8_DISPATCH(c, st = attend<D, FMT>(p, c.cells, mk, mv, a, s));
+    if (st != FW_OK || p.few) return st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
