@@ -20,7 +20,8 @@
 //
 // Slots of 2 x floor(128 / group) tokens: sequence i's are numbered from
 // floor(cu_q[i] / slot) + i on, which leaves room for all of them without a prefix
-// sum; a CTA finds its sequence by a search over cu_q.  The last slots, whose rows
+// sum; a CTA finds its sequence by a search over cu_q.  Where there are few slots, a cluster of CTAs takes the
+// blocks of one, and its rows' parts are joined through distributed shared memory.  The last slots, whose rows
 // see the most keys, come first.
 #include <cuda_bf16.h>
 
@@ -34,6 +35,8 @@ constexpr int PK = 128;                  // keys of a block
 // blocks that some row of a slot does not see in full: the first and the last row's ends are
 // at most 255 keys apart
 constexpr int PG = 3;
+constexpr int MAX_PARTS = 8;             // CTAs of a cluster
+constexpr int SPLIT = 12, MIN_PART = 4;  // blocks of keys a slot is split from, and of a part at least
 constexpr int PT = 32 * 12;              // 8 softmax warps, copies, products of a tile, guard, of the other
 constexpr uint32_t P_WAIT = 1u << 20;    // polls before a wait gives up (seconds)
 constexpr float GROW = 8.f;              // octaves a row's maximum may be above its reference
@@ -41,7 +44,8 @@ constexpr float GROW = 8.f;              // octaves a row's maximum may be above
 struct PromptArgs {
     const int32_t *cu_q, *cu_k;
     int64_t total_q, total_k;
-    int num_seqs, q_heads, kv_heads, group, slots, TT;  // TT: tokens of a tile
+    int num_seqs, q_heads, kv_heads, group, slots;
+    int TT, parts;  // tokens of a tile; CTAs (of a cluster) that a slot's keys are split over
     const uint16_t *v;
     int64_t v_row, v_head;
     float scale2;  // scale * log2(e)
@@ -150,6 +154,26 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ void cluster_sync()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the floats at this CTA's shared address p (aligned to their size), as CTA `rank` of the cluster has them
+__device__ __forceinline__ void remote(const float *p, int rank, float (&v)[2])
+{
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %2, %3;\n\tld.shared::cluster.v2.f32 {%0, %1}, [a];\n\t}"
+                 : "=f"(v[0]), "=f"(v[1])
+                 : "r"(tc::smem_u32(p)), "r"(rank)
+                 : "memory");
+}
+__device__ __forceinline__ void remote(const float *p, int rank, float (&v)[4])
+{
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                 : "r"(tc::smem_u32(p)), "r"(rank)
+                 : "memory");
+}
 // true for one lane of a warp that is there as a whole
 __device__ __forceinline__ bool elect_one()
 {
@@ -200,7 +224,8 @@ __global__ void __launch_bounds__(PT, 1)
 
     // (by a shuffle, so that the compiler knows the warp's role for the same in all lanes)
     const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(FW_FULL, tid >> 5, 0);
-    const int slot = a.slots - 1 - (int)(blockIdx.x / a.kv_heads), hk = blockIdx.x % a.kv_heads;
+    const int part = blockIdx.x % a.parts, item = blockIdx.x / a.parts;
+    const int slot = a.slots - 1 - item / a.kv_heads, hk = item % a.kv_heads;
     const int TT = a.TT, ST = 2 * TT;  // tokens of a tile and of a slot
 
     if (blockIdx.x == 0 && a.status)  // (before any wait can have given up)
@@ -267,7 +292,16 @@ __global__ void __launch_bounds__(PT, 1)
     int nb[2];
     nb[0] = (max(0, lk - lq + min(t0 + TT, lq)) + PK - 1) / PK;
     nb[1] = tiles == 2 ? (max(0, lk - lq + min(t0 + ST, lq)) + PK - 1) / PK : 0;
-    const int J = max(nb[0], nb[1]), jm = seen0 / PK;  // blocks from jm on are not seen in full by every row
+    int J = max(nb[0], nb[1]), jm = seen0 / PK;  // blocks from jm on are not seen in full by every row
+    int j0 = 0;                                  // this CTA's part: blocks j0 .. j0 + J, counted from j0 below
+    if (a.parts > 1) {
+        j0 = J * part / a.parts;
+        const int j1 = J * (part + 1) / a.parts;
+        for (int t = 0; t < 2; ++t) nb[t] = max(0, min(nb[t], j1) - j0);
+        J = j1 - j0;
+        jm = min(max(jm - j0, 0), J);
+    }
+    const int kb = k0 + j0 * PK;  // the part's first key row
 
     // Copy i of the ring (K of block 0, V of block 0, K of block 1, ...) arrives on its stage's barrier;
     // the values that the guard looks over on one of their own, which the guard can wait for without
@@ -295,7 +329,7 @@ __global__ void __launch_bounds__(PT, 1)
                 uint64_t *bar = arrival(i);
                 tc::mbar_arrive_expect_tx(bar, C::KT);
                 for (int h = 0; h < C::NB; ++h)
-                    tma_load_3d(sKV + s * C::KT + h * (PK * 128), (i & 1) ? &tmV : &tmK, 64 * h, hk, k0 + (i >> 1) * PK, bar);
+                    tma_load_3d(sKV + s * C::KT + h * (PK * 128), (i & 1) ? &tmV : &tmK, 64 * h, hk, kb + (i >> 1) * PK, bar);
                 ++issued;
             }
             if (!ok) atomicOr(&s_err, 1);
@@ -442,7 +476,7 @@ __global__ void __launch_bounds__(PT, 1)
         if (t < tiles) {
             const int tok = min(t0 + t * TT + r / a.group, lq - 1);
             const bool live = r < TT * a.group && t0 + t * TT + r / a.group < lq;
-            const int seen = max(0, lk - lq + tok + 1), n = nb[t];
+            const int seen = min(max(0, lk - lq + tok + 1 - j0 * PK), J * PK), n = nb[t];
             const uint32_t lanes = (uint32_t)((wid & 3) * 32) << 16;
             const uint32_t sS = taddr + lanes + t * PK, sO = taddr + lanes + C::O_COL + t * D;
             const float c2 = a.scale2;
@@ -525,7 +559,12 @@ __global__ void __launch_bounds__(PT, 1)
             tc::fence_after_sync();
             const bool odd = *(volatile int *)&s_odd != 0;
             const int64_t row = (int64_t)(q0 + tok) * a.q_heads + hk * a.group + r % a.group;
-            const float inv = !ok ? NAN : l == 0.f ? 0.f : 1.f / l;
+            // (of a part: as it is, the parts' sums come later)
+            const float inv = !ok ? NAN : a.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+            if (a.parts > 1 && ok && J > 0) {  // both tiles' products are done with the memory the parts are left in
+                ok = tc::mbar_wait(&drained[t], 0, P_WAIT) && (tiles == 1 || tc::mbar_wait(&drained[t ^ 1], 0, P_WAIT));
+                if (!__all_sync(FW_FULL, ok)) ok = false;
+            }
             // The rows go out by way of the tile's queries' memory (the products have read them), a warp's 32 rows its
             // own: whole rows a store.  (A row a lane: 32 lines an instruction, 6,200 clocks for a CTA's rows.)
             constexpr int PCS = D / 8;  // 16-byte pieces of a row
@@ -545,13 +584,20 @@ __global__ void __launch_bounds__(PT, 1)
                 if (odd && live) {  // the values the guard took out, for the rows that see them
 #pragma unroll 1
                     for (int j = jm * PK; j < seen; ++j) {
-                        const uint16_t *src = a.v + (int64_t)(k0 + j) * a.v_row + hk * a.v_head + i;
+                        const uint16_t *src = a.v + (int64_t)(kb + j) * a.v_row + hk * a.v_head + i;
 #pragma unroll
                         for (int e = 0; e < 64; ++e) {
                             const uint16_t b = src[e];
                             if ((b & 0x7f80u) == 0x7f80u) y[e] += bf16_to_f32(b);
                         }
                     }
+                }
+                if (a.parts > 1) {
+                    float4 *dst = reinterpret_cast<float4 *>(sKV) + (t * 128 + r) * (D / 4);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        dst[(i / 4 + e) ^ (r & 7)] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+                    continue;
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -560,23 +606,87 @@ __global__ void __launch_bounds__(PT, 1)
                                    pack_bf16(y[8 * e + 4], y[8 * e + 5]), pack_bf16(y[8 * e + 6], y[8 * e + 7]));
             }
             __syncwarp();
+            if (a.parts > 1) reinterpret_cast<float2 *>(sQ)[t * 128 + r] = make_float2(ref, ok ? l : NAN);
 #pragma unroll 8
-            for (int p = 0; p < 32; p += 32 / PCS) {
+            for (int p = 0; a.parts == 1 && p < 32; p += 32 / PCS) {
                 const int k = p + lane / PCS, c = lane % PCS;
                 const int64_t to = __shfl_sync(FW_FULL, live ? row : -1, k);
                 if (to >= 0) reinterpret_cast<uint4 *>(a.o + to * D)[c] = stage[k * PCS + (c ^ (k & 7))];
             }
-            if (live && a.lse)
+            if (live && a.lse && a.parts == 1)
                 a.lse[row] = !ok ? NAN : l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
         }
     }
     tc::fence_before_sync();
     __syncthreads();
+    if (a.parts > 1) {
+        // The parts of every row joined over the cluster: a CTA takes every parts-th row, a warp a row at a time.
+        cluster_sync();
+        for (int r = part + a.parts * wid; r < tiles * 128; r += a.parts * (PT / 32)) {
+            const int i = r & 127, tok = t0 + (r >> 7) * TT + i / a.group;
+            if (i >= TT * a.group || tok >= lq) continue;
+            // (columns 4 lane .. of 32 lanes, or 2 lane ..: one piece of 16 bytes, or half of one)
+            const float *src = reinterpret_cast<float *>(sKV) + r * D +
+                               (D == 128 ? 4 * (lane ^ (r & 7)) : 4 * ((lane >> 1) ^ (r & 7)) + 2 * (lane & 1));
+            float m[MAX_PARTS], l[MAX_PARTS], x[MAX_PARTS][D / 32];
+#pragma unroll
+            for (int p = 0; p < MAX_PARTS; ++p) {  // (all reads under way at once)
+                const bool in = p < a.parts;
+                float ml[2] = {-INFINITY, 0.f};
+                if (in) remote(reinterpret_cast<float *>(sQ) + 2 * r, p, ml);
+                m[p] = ml[0];
+                l[p] = ml[1];
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) x[p][e] = 0.f;
+                if (in) remote(src, p, x[p]);
+            }
+            float M = -INFINITY, L = 0.f, y[D / 32];
+#pragma unroll
+            for (int p = 0; p < MAX_PARTS; ++p) M = fmaxf(M, m[p]);
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) y[e] = 0.f;
+#pragma unroll
+            for (int p = 0; p < MAX_PARTS; ++p) {
+                const float f = m[p] == M ? 1.f : ex2(m[p] - M);
+                L = fmaf(f, l[p], L);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) y[e] = fmaf(f, x[p][e], y[e]);
+            }
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+            const int64_t row = (int64_t)(q0 + tok) * a.q_heads + hk * a.group + i % a.group;
+            uint32_t *dst = reinterpret_cast<uint32_t *>(a.o + row * D + lane * (D / 32));
+#pragma unroll
+            for (int e = 0; e < D / 32; e += 2) dst[e / 2] = pack_bf16(L == 0.f ? 0.f : y[e] * inv, L == 0.f ? 0.f : y[e + 1] * inv);
+            if (a.lse && lane == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        }
+        cluster_sync();  // no CTA leaves while another reads its rows
+    }
     if (tid == 0 && s_err && a.status) a.status[seq] = FW_ERR_TIMEOUT;
     if (wid == 9) {
         tc::fence_after_sync();
         tc::tmem_dealloc(taddr, 512);
     }
+}
+
+template <typename K>
+fw_status launch(K kernel, size_t smem, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv,
+                 const PromptArgs &a, cudaStream_t s)
+{
+    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)a.parts;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.slots * a.kv_heads * a.parts));
+    cfg.blockDim = dim3(PT);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = a.parts > 1 ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mq, mk, mv, a);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }
 
 }  // namespace
@@ -585,7 +695,18 @@ fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *sta
 {
     const int group = p.q_heads / p.kv_heads, TT = 128 / group, ST = 2 * TT;
     const int64_t slots = p.total_q / ST + p.num_seqs;
-    if (slots * p.kv_heads >= ((int64_t)1 << 31)) return FW_ERR_UNSUPPORTED;
+    if (slots * p.kv_heads >= ((int64_t)1 << 31)) return FW_ERR_UNSUPPORTED;  // (parts only where this is small)
+    // Few rows against long keys: the keys of a slot split over a cluster, as long as the CTAs fit the SMs once.  The
+    // joining costs several blocks' time, so only from SPLIT blocks on average on, and MIN_PART or more to a part
+    // (one sequence, 8 x 4 heads, d = 128: 17 rows against 16,384 keys 130 us whole, 24 in 8 parts; 256 against 2,048
+    // 28.4 whole, 26.3 in 2; d = 64, 128 against 1,024 16.2 whole, 19.1 in 2).
+    int sms = 0;
+    const fw_status st = device_sms(&sms);
+    if (st != FW_OK) return st;
+    const int64_t blocks = p.total_k / ((int64_t)p.num_seqs * PK);
+    int parts = 1;
+    while (blocks >= SPLIT && parts < MAX_PARTS && slots * p.kv_heads * parts * 2 <= sms && blocks >= MIN_PART * parts * 2)
+        parts *= 2;
     CUtensorMap mq, mk, mv;
     // (without keys no copy is issued: any valid map does)
     const bool keys = p.total_k > 0;
@@ -596,17 +717,10 @@ fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *sta
                              keys ? p.v_row : (int64_t)p.d * p.kv_heads, 1, PK))
         return FW_ERR_CUDA;
     const PromptArgs a{p.cu_q,  p.cu_k,     p.total_q, p.total_k, p.num_seqs, p.q_heads, p.kv_heads,
-                       group,   (int)slots, TT, (const uint16_t *)p.v, p.v_row,   p.v_head,  p.scale * 1.4426950408889634f,
+                       group,   (int)slots, TT, parts, (const uint16_t *)p.v, p.v_row,   p.v_head,  p.scale * 1.4426950408889634f,
                        (uint16_t *)o, lse,  status};
-    const unsigned grid = (unsigned)(slots * p.kv_heads);
-    if (p.d == 128) {
-        FW_CUDA_CHECK(cudaFuncSetAttribute(k_prompt<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PCfg<128>::SMEM));
-        FW_LAUNCH(k_prompt<128>, grid, PT, PCfg<128>::SMEM, s, mq, mk, mv, a);
-    } else {
-        FW_CUDA_CHECK(cudaFuncSetAttribute(k_prompt<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PCfg<64>::SMEM));
-        FW_LAUNCH(k_prompt<64>, grid, PT, PCfg<64>::SMEM, s, mq, mk, mv, a);
-    }
-    return FW_OK;
+    return p.d == 128 ? launch(k_prompt<128>, PCfg<128>::SMEM, mq, mk, mv, a, s)
+                      : launch(k_prompt<64>, PCfg<64>::SMEM, mq, mk, mv, a, s);
 }
 
 }  // namespace fw

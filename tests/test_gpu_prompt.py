@@ -194,3 +194,39 @@ def test_prompt_bad_bounds_are_reported(fw):
         bad = [b < a or a < 0 or b > 40 for a, b in zip(bounds, bounds[1:])]
         got = out["status"].tolist()
         assert [s == fw.FW_ERR_INVALID_ARG for s in got] == bad
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[(1, 20000)], [(17, 4097)], [(3, 9000), (130, 7000)], [(300, 2100), (1, 4000), (0, 9000)],
+                                  [(64, 1024)], [(40, 20), (5, 9000)]])
+@pytest.mark.parametrize("hk,g", [(1, 1), (2, 4), (1, 12)])
+def test_prompt_few_rows_against_long_keys(fw, hk, g, d, lens):
+    """Slots so few that their keys are split over several CTAs and joined."""
+    gen = torch.Generator("cuda").manual_seed(hk + g + d)
+    lq, lk = [a for a, _ in lens], [b for _, b in lens]
+    q, k, v = rand(gen, sum(lq), hk * g, d, amp=1.5), rand(gen, sum(lk), hk, d), rand(gen, sum(lk), hk, d)
+    out = fw.prompt_attention(q, k, v, cu(lq), cu(lk))
+    torch.cuda.synchronize()
+    check(out, q, k, v, lens, 1 / math.sqrt(d))
+    again = fw.prompt_attention(q, k, v, cu(lq), cu(lk))
+    torch.cuda.synchronize()
+    assert torch.equal(out["o"], again["o"]) and torch.equal(out["lse"], again["lse"])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_unseen_values_with_keys_split(fw, d):
+    gen = torch.Generator("cuda").manual_seed(31)
+    T, lq = 6000, 90
+    q, k, v = rand(gen, lq, 4, d), rand(gen, T, 2, d), rand(gen, T, 2, d)
+    clean = fw.prompt_attention(q, k, v, cu([lq]), cu([T]))
+    for at, bad in ((T - 50, float("nan")), (T - lq, float("inf")), (T - 1, float("-inf")), (700, float("inf"))):
+        y = v.clone()
+        y[at, 0, 5] = bad
+        out = fw.prompt_attention(q, k, y, cu([lq]), cu([T]))
+        torch.cuda.synchronize()
+        first = max(0, at - (T - lq))
+        o, co = out["o"], clean["o"]
+        assert torch.equal(o[:first], co[:first]) and torch.equal(o[:, 2:], co[:, 2:])
+        assert not bool(torch.isfinite(o[first:, :2, 5]).any())
+        rest = [c for c in range(d) if c != 5]
+        assert torch.equal(o[first:, :2][..., rest], co[first:, :2][..., rest])
