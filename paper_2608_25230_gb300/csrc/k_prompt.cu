@@ -37,7 +37,6 @@ constexpr int PK = 128;                  // keys of a block
 constexpr int PG = 3;
 constexpr int MAX_PARTS = 8;             // CTAs of a cluster
 constexpr int SPLIT = 12, MIN_PART = 4;  // blocks of keys a slot is split from, and of a part at least
-constexpr int PT = 32 * 12;              // 8 softmax warps, copies, products of a tile, guard, of the other
 constexpr uint32_t P_WAIT = 1u << 20;    // polls before a wait gives up (seconds)
 constexpr float GROW = 8.f;              // octaves a row's maximum may be above its reference
 
@@ -54,17 +53,22 @@ struct PromptArgs {
     int32_t *status;
 };
 
-template <int D> struct PCfg {
+template <int D, int TILES> struct PCfg {
     static constexpr int NB = D / 64;              // 128-byte boxes across d
     static constexpr int QT = 128 * D * 2;         // bytes of a tile of queries
     static constexpr int KT = PK * D * 2;          // bytes of a tile of keys or values
-    static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr size_t SMEM = 1024 + 2 * QT + (size_t)STAGES * KT;
+    static constexpr int STAGES = D == 64 && TILES == 2 ? 8 : 5;
+    static constexpr size_t SMEM = 1024 + TILES * QT + (size_t)STAGES * KT;
     // Parts of a block of scores: with two, the next part's product runs under the softmax of this one (d = 128,
     // 16,384 tokens x 32 heads: 1.46 ms in one part, 1.37 in two).
     static constexpr int NS = 2;
     static constexpr int SK = PK / NS;             // keys of a part
-    static constexpr uint32_t O_COL = 256;         // TMEM: S of the tiles at 0 and 128, O behind them
+    static constexpr uint32_t COLS = 256 * TILES;  // TMEM columns
+    static constexpr uint32_t O_COL = PK * TILES;  // S of the tiles first, O behind them
+    // the softmax's warps, then those of the copies, the products, the guard, and of the other tile's products
+    static constexpr int W_COPY = 4 * TILES, W_MMA = W_COPY + 1, W_GUARD = W_COPY + 2, W_MMA1 = W_COPY + 3;
+    static constexpr int THREADS = 32 * (W_COPY + 4);
+    static constexpr int CTAS = D == 64 && TILES == 1 ? 2 : 1;  // per SM
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -209,15 +213,16 @@ __device__ __forceinline__ bool seq_ok(const PromptArgs &a, int s)
     return q0 >= 0 && q1 >= q0 && q1 <= a.total_q && k0 >= 0 && k1 >= k0 && k1 <= a.total_k;
 }
 
-template <int D>
-__global__ void __launch_bounds__(PT, 1)
+template <int D, int TILES>
+__global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
     k_prompt(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
              const __grid_constant__ CUtensorMap tmV, const PromptArgs a)
 {
-    using C = PCfg<D>;
+    using C = PCfg<D, TILES>;
+    constexpr int PT = C::THREADS;
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
-    uint8_t *sQ = sm, *sKV = sm + 2 * C::QT;
+    uint8_t *sQ = sm, *sKV = sm + TILES * C::QT;
     __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2][C::NS], p_full[2][C::NS], o_done[2], drained[2], v_in[PG], v_ok[PG];
     __shared__ uint32_t s_taddr;
     __shared__ int s_seq[5], s_err, s_odd;  // (s_seq: the sequence, its query and key rows)
@@ -226,7 +231,7 @@ __global__ void __launch_bounds__(PT, 1)
     const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(FW_FULL, tid >> 5, 0);
     const int part = blockIdx.x % a.parts, item = blockIdx.x / a.parts;
     const int slot = a.slots - 1 - item / a.kv_heads, hk = item % a.kv_heads;
-    const int TT = a.TT, ST = 2 * TT;  // tokens of a tile and of a slot
+    const int TT = a.TT, ST = TILES * TT;  // tokens of a tile and of a slot
 
     if (blockIdx.x == 0 && a.status)  // (before any wait can have given up)
         for (int s = tid; s < a.num_seqs; s += PT) a.status[s] = seq_ok(a, s) ? FW_OK : FW_ERR_INVALID_ARG;
@@ -246,7 +251,7 @@ __global__ void __launch_bounds__(PT, 1)
         } while (hi - lo > 1);
         if (lane < 4) s_seq[1 + lane] = (lane < 2 ? a.cu_q : a.cu_k)[lo + (lane & 1)];
         if (lane == 0) s_seq[0] = any ? lo : -1;
-    } else if (wid == 8) {
+    } else if (wid == C::W_COPY) {
         if (lane < C::STAGES) {
             tc::mbar_init(&full[lane], 1);
             tc::mbar_init(&empty[lane], 2);
@@ -267,9 +272,9 @@ __global__ void __launch_bounds__(PT, 1)
             s_odd = 0;
         }
         tc::mbar_init_fence();
-    } else if (wid == 9) {
-        tc::tmem_alloc(&s_taddr, 512);
-    } else if (wid == 10 && lane == 0) {
+    } else if (wid == C::W_MMA) {
+        tc::tmem_alloc(&s_taddr, C::COLS);
+    } else if (wid == C::W_GUARD && lane == 0) {
         tc::tma_prefetch_desc(&tmQ);
         tc::tma_prefetch_desc(&tmK);
         tc::tma_prefetch_desc(&tmV);
@@ -283,15 +288,15 @@ __global__ void __launch_bounds__(PT, 1)
     const int lq = valid ? q1 - q0 : 0, lk = valid ? k1 - k0 : 0;
     const int t0 = (slot - (q0 / ST + seq)) * ST;  // the slot's first token in the sequence
     if (!valid || t0 < 0 || t0 >= lq) {  // (a sequence out of range, or a slot behind its last token)
-        if (wid == 9) tc::tmem_dealloc(taddr, 512);
+        if (wid == C::W_MMA) tc::tmem_dealloc(taddr, C::COLS);
         return;
     }
-    const int tiles = t0 + TT < lq ? 2 : 1;
+    const int tiles = TILES == 2 && t0 + TT < lq ? 2 : 1;
     // keys that the first token sees, and blocks of keys that each tile's last one does
     const int seen0 = max(0, lk - lq + t0 + 1);
     int nb[2];
     nb[0] = (max(0, lk - lq + min(t0 + TT, lq)) + PK - 1) / PK;
-    nb[1] = tiles == 2 ? (max(0, lk - lq + min(t0 + ST, lq)) + PK - 1) / PK : 0;
+    nb[1] = TILES == 2 && tiles == 2 ? (max(0, lk - lq + min(t0 + ST, lq)) + PK - 1) / PK : 0;
     int J = max(nb[0], nb[1]), jm = seen0 / PK;  // blocks from jm on are not seen in full by every row
     int j0 = 0;                                  // this CTA's part: blocks j0 .. j0 + J, counted from j0 below
     if (a.parts > 1) {
@@ -310,7 +315,7 @@ __global__ void __launch_bounds__(PT, 1)
     auto arrival = [&](int i) { return (i & 1) && (i >> 1) >= jm ? &v_in[min((i >> 1) - jm, PG - 1)] : &full[i % C::STAGES]; };
     auto arrival_phase = [&](int i) { return (i & 1) && (i >> 1) >= jm ? 0u : (uint32_t)(i / C::STAGES) & 1u; };
 
-    if (wid == 8) {
+    if (wid == C::W_COPY) {
         // ------------------------------------------------------------ copies
         if (lane == 0 && J > 0) {
             const uint32_t qbytes = (uint32_t)(128 * a.group * TT);  // (one box: 64 columns of a tile's rows)
@@ -339,12 +344,12 @@ __global__ void __launch_bounds__(PT, 1)
             if (!tc::mbar_wait(&q_full, 0, P_WAIT)) atomicOr(&s_err, 1);
         }
         __syncwarp();
-    } else if (wid == 9 || wid == 11) {
+    } else if (wid == C::W_MMA || (TILES == 2 && wid == C::W_MMA1)) {
         // ---------------------------------------------------------- products
         // A warp per tile: what issuing costs (waits, commits) hides behind the other tile's products.  The
         // whole warp waits and an elected lane issues: with the waits inside the one lane's branch the
         // operands are not kept in uniform registers, and an instruction took 100 clocks to issue.
-        const int t = wid == 11;
+        const int t = wid == C::W_MMA1;
         if (t < tiles && J > 0) {
             constexpr uint32_t id_s = tc::idesc_bf16_f32(128, C::SK, false, false);
             constexpr uint32_t id_o = tc::idesc_bf16_f32(128, D, false, true);
@@ -433,7 +438,7 @@ __global__ void __launch_bounds__(PT, 1)
             if (!tc::mbar_wait(&drained[t], 0, P_WAIT)) atomicOr(&s_err, 1);
         }
         __syncwarp();
-    } else if (wid == 10) {
+    } else if (wid == C::W_GUARD) {
         // ------------------------------------------------------------- guard
         bool ok = true;
         for (int j = jm; ok && j < J; ++j) {
@@ -470,7 +475,7 @@ __global__ void __launch_bounds__(PT, 1)
             if (lane == 0) tc::mbar_arrive(&v_ok[min(j - jm, PG - 1)]);
         }
         if (!ok && lane == 0) atomicOr(&s_err, 1);
-    } else {
+    } else if (wid < 4 * TILES) {
         // ----------------------------------------------------------- softmax
         const int t = wid >> 2, r = tid & 127;
         if (t < tiles) {
@@ -662,25 +667,34 @@ __global__ void __launch_bounds__(PT, 1)
         cluster_sync();  // no CTA leaves while another reads its rows
     }
     if (tid == 0 && s_err && a.status) a.status[seq] = FW_ERR_TIMEOUT;
-    if (wid == 9) {
+    if (wid == C::W_MMA) {
         tc::fence_after_sync();
-        tc::tmem_dealloc(taddr, 512);
+        tc::tmem_dealloc(taddr, C::COLS);
     }
 }
 
-template <typename K>
-fw_status launch(K kernel, size_t smem, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv,
-                 const PromptArgs &a, cudaStream_t s)
+// Whether a CTA takes one tile instead of two: where the CTAs of two would not fill half of the SMs (512 tokens, 8 x 4
+// heads, d = 128: 10.9 us against 13.6), and for d = 64, where two such CTAs fit an SM and one starts and ends while the
+// other computes (16 prompts of 300 tokens 32.3 us against 35.1, 8,192 tokens 291 against 302).
+bool one_tile(int d, int64_t ctas_of_two, int sms)
 {
-    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    return d == 64 || ctas_of_two * 2 <= sms;
+}
+
+template <int D, int TILES>
+fw_status launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const PromptArgs &a, cudaStream_t s)
+{
+    using C = PCfg<D, TILES>;
+    const auto kernel = k_prompt<D, TILES>;
+    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)a.parts;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.slots * a.kv_heads * a.parts));
-    cfg.blockDim = dim3(PT);
-    cfg.dynamicSmemBytes = smem;
+    cfg.blockDim = dim3(C::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = a.parts > 1 ? 1 : 0;
@@ -693,16 +707,18 @@ fw_status launch(K kernel, size_t smem, const CUtensorMap &mq, const CUtensorMap
 
 fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *status, cudaStream_t s)
 {
-    const int group = p.q_heads / p.kv_heads, TT = 128 / group, ST = 2 * TT;
-    const int64_t slots = p.total_q / ST + p.num_seqs;
+    const int group = p.q_heads / p.kv_heads, TT = 128 / group;
+    int sms = 0;
+    const fw_status st = device_sms(&sms);
+    if (st != FW_OK) return st;
+    auto slots_of = [&](int tiles) { return p.total_q / (tiles * TT) + p.num_seqs; };
+    const int tiles = one_tile(p.d, slots_of(2) * p.kv_heads, sms) ? 1 : 2;
+    const int64_t slots = slots_of(tiles);
     if (slots * p.kv_heads >= ((int64_t)1 << 31)) return FW_ERR_UNSUPPORTED;  // (parts only where this is small)
     // Few rows against long keys: the keys of a slot split over a cluster, as long as the CTAs fit the SMs once.  The
     // joining costs several blocks' time, so only from SPLIT blocks on average on, and MIN_PART or more to a part
     // (one sequence, 8 x 4 heads, d = 128: 17 rows against 16,384 keys 130 us whole, 24 in 8 parts; 256 against 2,048
     // 28.4 whole, 26.3 in 2; d = 64, 128 against 1,024 16.2 whole, 19.1 in 2).
-    int sms = 0;
-    const fw_status st = device_sms(&sms);
-    if (st != FW_OK) return st;
     const int64_t blocks = p.total_k / ((int64_t)p.num_seqs * PK);
     int parts = 1;
     while (blocks >= SPLIT && parts < MAX_PARTS && slots * p.kv_heads * parts * 2 <= sms && blocks >= MIN_PART * parts * 2)
@@ -717,10 +733,10 @@ fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *sta
                              keys ? p.v_row : (int64_t)p.d * p.kv_heads, 1, PK))
         return FW_ERR_CUDA;
     const PromptArgs a{p.cu_q,  p.cu_k,     p.total_q, p.total_k, p.num_seqs, p.q_heads, p.kv_heads,
-                       group,   (int)slots, TT, parts, (const uint16_t *)p.v, p.v_row,   p.v_head,  p.scale * 1.4426950408889634f,
-                       (uint16_t *)o, lse,  status};
-    return p.d == 128 ? launch(k_prompt<128>, PCfg<128>::SMEM, mq, mk, mv, a, s)
-                      : launch(k_prompt<64>, PCfg<64>::SMEM, mq, mk, mv, a, s);
+                       group,   (int)slots, TT, parts, (const uint16_t *)p.v, p.v_row,   p.v_head,
+                       p.scale * 1.4426950408889634f, (uint16_t *)o, lse,  status};
+    if (p.d == 128) return tiles == 1 ? launch<128, 1>(mq, mk, mv, a, s) : launch<128, 2>(mq, mk, mv, a, s);
+    return tiles == 1 ? launch<64, 1>(mq, mk, mv, a, s) : launch<64, 2>(mq, mk, mv, a, s);
 }
 
 }  // namespace fw
