@@ -24,6 +24,7 @@
 // instruction's layout asks for scattered ones, and the operand on the other side
 // follows.
 #include <algorithm>
+#include <type_traits>
 
 #include "fw_cache8.cuh"
 #include "tc_sm100.cuh"
@@ -562,61 +563,91 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
     ring.drain();
 }
 
-// The parts of a cell that several warps share, joined in their order; empty cells' outputs.
-// A CTA per (cell, query row): four warps take every fourth part each.
-template <int D> __global__ void __launch_bounds__(128) k_cache8_join(const AttendArgs a, int RT)
+// The parts of a cell that several warps share, joined in their order; empty cells' outputs.  Each of a CTA's W warps
+// takes a row, or (SPREAD) all of them one row's parts, where there are few rows and so the parts may be many:
+// a CTA per row of 64 cells x 20 rows came in 8 waves of small CTAs behind the first kernel, 7 us.
+template <int D, int W, bool SPREAD> __global__ void __launch_bounds__(32 * W) k_cache8_join(const AttendArgs a, int RT)
 {
     constexpr int E = D / 32;
-    __shared__ float s_o[4][D];
-    __shared__ float2 s_ml[4];
+    using Vec = typename std::conditional<D == 128, float4, float2>::type;
+    __shared__ float s_o[SPREAD ? W : 1][D];
+    __shared__ float2 s_ml[W];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int h = blockIdx.x, r = blockIdx.y, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int h = blockIdx.x, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int r = SPREAD ? blockIdx.y : blockIdx.y * W + wid;
     int64_t base;
     int n;
     fw_status st;
     const int nb = cell_blocks(a.s, h, base, n, st), quota = *a.plan, s = a.start[h];
-    const int w0 = s / quota, w1 = nb > 0 ? (s + nb - 1) / quota : w0;
-    if (nb > 0 && w0 == w1) return;
+    const int w0 = s / quota, w1 = nb > 0 ? (s + nb - 1) / quota + 1 : w0;  // the cell's warps
+    if (w1 == w0 + 1) return;
+    if (r >= a.group * a.m) return;  // (SPREAD: no row of the grid is)
+    const int64_t tile0 = (int64_t)(r / RT) * a.G * AW;
+    auto part_at = [&](int p) {
+        const int seg = p == w0 && s > p * quota ? 1 : 0;
+        return ((tile0 + p) * 2 + seg) * RT + r % RT;
+    };
+    // this warp's parts: 32 maxima and sums at a time, then their columns
+    const int all = w1 - w0, each = SPREAD ? (all + W - 1) / W : all;
+    const int p0 = SPREAD ? w0 + min(wid * each, all) : w0, p1 = min(p0 + each, w1);
     float M = -INFINITY, L = 0.f, acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    if (nb > 0) {
-        const int64_t tile0 = (int64_t)(r / RT) * a.G * AW;
-#pragma unroll 4
-        for (int p = w0 + wid; p <= w1; p += 4) {
-            const int seg = p == w0 && s > p * quota ? 1 : 0;
-            const int64_t at = ((tile0 + p) * 2 + seg) * RT + r % RT;
-            const float2 ml = a.part_ml[at];
-            const float now = fmaxf(M, ml.x);
-            const float f = M == now ? 1.f : ex2(M - now), y = ml.x == now ? 1.f : ex2(ml.x - now);
-            M = now;
-            L = fmaf(L, f, ml.y * y);
+    for (int q = p0; q < p1; q += 32) {
+        // (the columns of B parts are asked for before the maxima are looked at, and B at a time after that)
+        constexpr int B = 64 / E;
+        const int cnt = min(32, p1 - q);
+        const float2 ml = lane < cnt ? a.part_ml[part_at(q + lane)] : make_float2(-INFINITY, 0.f);
+        float f = 0.f;
+        for (int i = 0; i < cnt; i += B) {
+            Vec x[B];
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(acc[e], f, a.part_o[at * D + lane + 32 * e] * y);
+            for (int u = 0; u < B; ++u) {
+                x[u] = Vec{};
+                if (i + u < cnt) x[u] = *reinterpret_cast<const Vec *>(a.part_o + part_at(q + i + u) * D + lane * E);
+            }
+            if (i == 0) {
+                const float now = fmaxf(M, warp_max(ml.x)), old = M == now ? 1.f : ex2(M - now);
+                f = ml.x == now ? 1.f : ex2(ml.x - now);
+                M = now;
+                L = fmaf(L, old, warp_sum(f * ml.y));
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] *= old;
+            }
+#pragma unroll
+            for (int u = 0; u < B; ++u) {
+                const float g = __shfl_sync(FW_FULL, f, i + u);
+#pragma unroll
+                for (int e = 0; e < E; ++e)  // (a part that is not there is 0, its factor 0 or 1)
+                    acc[e] = fmaf(g, reinterpret_cast<const float *>(&x[u])[e], acc[e]);
+            }
         }
     }
-    if (lane == 0) s_ml[wid] = make_float2(M, L);
+    if constexpr (SPREAD) {
+        if (lane == 0) s_ml[wid] = make_float2(M, L);
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_o[wid][lane + 32 * e] = acc[e];
-    __syncthreads();
-    if (wid != 0) return;
-    M = fmaxf(fmaxf(s_ml[0].x, s_ml[1].x), fmaxf(s_ml[2].x, s_ml[3].x));
-    L = 0.f;
+        for (int e = 0; e < E; ++e) s_o[wid][lane * E + e] = acc[e];
+        __syncthreads();
+        if (wid != 0) return;
+        const float2 ml = lane < W ? s_ml[lane] : make_float2(-INFINITY, 0.f);
+        M = warp_max(ml.x);
+        const float f = ml.x == M ? 1.f : ex2(ml.x - M);
+        L = warp_sum(f * ml.y);
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float f = s_ml[w].x == M ? 1.f : ex2(s_ml[w].x - M);
-        L = fmaf(f, s_ml[w].y, L);
+        for (int w = 0; w < W; ++w) {
+            const float g = __shfl_sync(FW_FULL, f, w);
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(f, s_o[w][lane + 32 * e], acc[e]);
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(g, s_o[w][lane * E + e], acc[e]);
+        }
     }
     const int seq = h / a.kv_heads;
     const int64_t out = out_row(a, seq, h - seq * a.kv_heads, r);
     const float inv = L == 0.f ? 0.f : 1.f / L;
+    uint32_t *dst = reinterpret_cast<uint32_t *>(a.o + out * D + lane * E);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
+    for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
     if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
 }
 
@@ -820,17 +851,21 @@ fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, f
     fw_status st = FW_OK;
     FW_CACHE8_DISPATCH(c, st = attend<D, FMT>(p, c.cells, mk, mv, a, s));
     if (st != FW_OK || p.few) return st;
+    const int qrows = q.group * q.m;
+    // rows so few that they would not keep the GPU's warps busy: every row's parts over a CTA
+    const bool spread = (int64_t)c.cells * qrows <= 4 * p.G * p.tiles;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)c.cells, (unsigned)(q.group * q.m));
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3((unsigned)c.cells, (unsigned)(spread ? qrows : (qrows + 7) / 8));
+    cfg.blockDim = dim3(spread ? 512 : 256);
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const cudaError_t e = c.d == 128 ? cudaLaunchKernelEx(&cfg, k_cache8_join<128>, a, p.RT)
-                                     : cudaLaunchKernelEx(&cfg, k_cache8_join<64>, a, p.RT);
+    const auto join = c.d == 128 ? (spread ? k_cache8_join<128, 16, true> : k_cache8_join<128, 8, false>)
+                                 : (spread ? k_cache8_join<64, 16, true> : k_cache8_join<64, 8, false>);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, join, a, p.RT);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }

@@ -421,3 +421,17 @@ def test_long_appends_report_and_refuse(fw):
     for h in (0, 2):
         check_cell(cache, h, 1, torch.cat([K[h, :start[h]], new[h]]))
     check_cell(cache, 1, 0, K[1, :40])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv_heads,g,m,counts", [(1, 4, 1, [40000]), (2, 8, 3, [70000, 20]), (8, 4, 5, [1] * 40 + [30000] + [3] * 39)])
+def test_attend_one_long_cell(fw, d, kv_heads, g, m, counts):
+    """One cell with nearly all rows, shared by most of the GPU's warps."""
+    gen = torch.Generator("cuda").manual_seed(d + g)
+    cache = filled(fw, gen, counts, d, "int8")
+    q = (1.5 * torch.randn(len(counts) // kv_heads, m, kv_heads * g, d, generator=gen, device="cuda")).to(torch.bfloat16)
+    out = fw.cache8_attend(cache, q, kv_heads=kv_heads)
+    again = fw.cache8_attend(cache, q, kv_heads=kv_heads)
+    torch.cuda.synchronize()
+    check_attend(cache, q, out, kv_heads, float(torch.tensor(1 / math.sqrt(d), dtype=torch.float32)))
+    assert torch.equal(out["o"], again["o"]) and torch.equal(out["lse"], again["lse"])
