@@ -35,7 +35,7 @@ namespace {
 using namespace cache8;
 
 constexpr int BR = FW_CACHE8_BLOCK;
-constexpr int AW = 8;                   // warps of a CTA
+constexpr int AW = 8;                   // warps of a CTA of the few-cells kernel
 constexpr int AT = 32 * AW;
 constexpr uint32_t A_WAIT = 1u << 22;   // polls before a wait gives up
 constexpr float P_UP = 14.f;            // weights are 2^(x - max + P_UP)
@@ -49,7 +49,7 @@ struct AttendArgs {
     uint16_t *o;
     float *lse;
     int32_t *status;
-    int G;               // CTAs along the blocks
+    int G, warps;        // CTAs along the blocks, and their warps
     int32_t *start;      // workspace: [cells] first unit of each cell
     int32_t *plan;       // workspace: units per warp
     float2 *part_ml;     // workspace: [tiles of rows][warps][2][rows of a tile] (max, sum)
@@ -133,12 +133,15 @@ template <int FMT> __device__ __forceinline__ void decode4(uint32_t w, uint32_t 
     }
 }
 
-template <int D> struct Cfg {
-    static constexpr int STAGES = D == 128 ? 3 : 6;
+// W warps of a CTA with rings of STAGES blocks.  Two blocks a warp keep the memory busy (128 KB an SM); with three, each
+// waits longer in the queue and the GPU's warps finish further apart (64 x 8 cells of 16,384 rows, d = 128: 309 us, 329
+// with three).
+template <int D, int W> struct Cfg {
+    static constexpr int STAGES = D == 128 ? 2 : 3;
     static constexpr int BLK = BR * D;                       // bytes of a block's codes
-    static constexpr int RING = AW * STAGES * 2 * BLK;       // 192 KB
+    static constexpr int RING = W * STAGES * 2 * BLK;
     static constexpr int LDO = D + 4;                        // floats of a row in the joining buffer
-    static constexpr int JOIN = AW * 8 * LDO * 4;
+    static constexpr int JOIN = W * 8 * LDO * 4;
     static constexpr size_t SMEM = 1024 + RING;
     static constexpr size_t SMEM_FEW = 1024 + RING + JOIN;
 };
@@ -155,7 +158,8 @@ template <int D> __device__ __forceinline__ int piece(int r, int x)
 }
 
 // A warp's ring of blocks.
-template <int D> struct Ring {
+template <int D, int STAGES> struct Ring {
+    static constexpr int BLK = BR * D;
     uint8_t *mem;
     uint64_t *full;
     uint32_t issued = 0, used = 0;
@@ -163,30 +167,27 @@ template <int D> struct Ring {
 
     __device__ void fetch(const CUtensorMap *tmK, const CUtensorMap *tmV, int64_t row, int lane)
     {
-        using C = Cfg<D>;
-        const int s = issued % C::STAGES;
+        const int s = issued % STAGES;
         if (lane == 0) {
-            tc::mbar_arrive_expect_tx(&full[s], 2 * C::BLK);
-            tc::tma_load_2d(mem + s * 2 * C::BLK, tmK, 0, (int32_t)row, &full[s]);
-            tc::tma_load_2d(mem + s * 2 * C::BLK + C::BLK, tmV, 0, (int32_t)row, &full[s]);
+            tc::mbar_arrive_expect_tx(&full[s], 2 * BLK);
+            tc::tma_load_2d(mem + s * 2 * BLK, tmK, 0, (int32_t)row, &full[s]);
+            tc::tma_load_2d(mem + s * 2 * BLK + BLK, tmV, 0, (int32_t)row, &full[s]);
         }
         ++issued;
     }
     // the next block, or null where the wait gave up
     __device__ const uint8_t *next()
     {
-        using C = Cfg<D>;
-        const int s = used % C::STAGES;
-        if (ok) ok = tc::mbar_wait(&full[s], (used / C::STAGES) & 1u, A_WAIT);
+        const int s = used % STAGES;
+        if (ok) ok = tc::mbar_wait(&full[s], (used / STAGES) & 1u, A_WAIT);
         if (!ok) return nullptr;
         ++used;
-        return mem + s * 2 * C::BLK;
+        return mem + s * 2 * BLK;
     }
     // copies still under way land before the CTA's memory goes
     __device__ void drain()
     {
-        using C = Cfg<D>;
-        for (; used < issued; ++used) tc::mbar_wait(&full[used % C::STAGES], (used / C::STAGES) & 1u, A_WAIT);
+        for (; used < issued; ++used) tc::mbar_wait(&full[used % STAGES], (used / STAGES) & 1u, A_WAIT);
     }
 };
 
@@ -261,7 +262,7 @@ template <int D, int FMT, int NT> struct Rows {
                                           int lane, F read)
     {
         const int g = lane >> 2, c = lane & 3;
-        const uint8_t *tv = tk + Cfg<D>::BLK;
+        const uint8_t *tv = tk + BR * D;
         // S^T: two tiles of 16 keys
         float S[NT][2][4];
 #pragma unroll
@@ -405,16 +406,17 @@ __device__ __forceinline__ float lse_of(float mx, float l)
     return l == 0.f ? -INFINITY : (mx - P_UP + log2f(l)) * 0.6931471805599453f;
 }
 
-template <int D, int FMT, int NT>
-__global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__ CUtensorMap tmK,
+template <int D, int FMT, int NT, int W>
+__global__ void __launch_bounds__(32 * W, 1) k_cache8_attend(const __grid_constant__ CUtensorMap tmK,
                                                          const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
 {
-    using C = Cfg<D>;
+    using C = Cfg<D, W>;
+    constexpr int AT = 32 * W;
     constexpr int MT = D / 16, RT = 8 * NT;  // RT: query rows of a CTA
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
-    __shared__ __align__(8) uint64_t full[AW][C::STAGES];
-    __shared__ int s_scan[AW], s_h0[AW], s_b0[AW];
+    __shared__ __align__(8) uint64_t full[W][C::STAGES];
+    __shared__ int s_scan[W], s_h0[W], s_b0[W];
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
     const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT, rows = a.group * a.m;
@@ -445,12 +447,12 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
     __syncthreads();
     int total = 0, before = incl - mine;
 #pragma unroll
-    for (int w = 0; w < AW; ++w) {
+    for (int w = 0; w < W; ++w) {
         if (w < wid) before += s_scan[w];
         total += s_scan[w];
     }
     // consecutive ranges go to different CTAs; at least two blocks each, so that there is less to join
-    const int quota = max((total + a.G * AW - 1) / (a.G * AW), 2);
+    const int quota = max((total + a.G * W - 1) / (a.G * W), 2);
     {
         int at = before;
         for (int h = h_lo; h < h_hi; ++h) {
@@ -459,7 +461,7 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
             fw_status st;
             const int nb = h == h_lo ? nb_lo : cell_blocks(a.s, h, base, n, st);
             // the warps of this CTA whose ranges begin in the cell
-            for (int w = 0; w < AW; ++w) {
+            for (int w = 0; w < W; ++w) {
                 const int64_t u = (int64_t)(w * a.G + cta) * quota;
                 if (u >= at && u < at + nb) {
                     s_h0[w] = h;
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
     int u = (int)first;
     const int u1 = min(u + quota, total);
 
-    Ring<D> ring;
+    Ring<D, C::STAGES> ring;
     ring.mem = sm + wid * C::STAGES * 2 * C::BLK;
     ring.full = full[wid];
     // the warp's producer: its next unit to fetch, by cell
@@ -548,7 +550,7 @@ __global__ void __launch_bounds__(AT, 1) k_cache8_attend(const __grid_constant__
                     for (int i = 0; i < MT; i += 4) dst[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
                     if (a.lse && g == 0) a.lse[out] = lse_of(R.mx[t][e], sum);
                 } else {
-                    const int64_t at = (((int64_t)tile * a.G * AW + gw) * 2 + seg) * RT + 8 * t + 2 * c + e;
+                    const int64_t at = (((int64_t)tile * a.warps + gw) * 2 + seg) * RT + 8 * t + 2 * c + e;
                     if (g == 0) a.part_ml[at] = make_float2(R.mx[t][e], sum);
                     float4 *dst = reinterpret_cast<float4 *>(a.part_o + at * D + g * (D / 8));
 #pragma unroll
@@ -582,7 +584,7 @@ template <int D, int W, bool SPREAD> __global__ void __launch_bounds__(32 * W) k
     const int w0 = s / quota, w1 = nb > 0 ? (s + nb - 1) / quota + 1 : w0;  // the cell's warps
     if (w1 == w0 + 1) return;
     if (r >= a.group * a.m) return;  // (SPREAD: no row of the grid is)
-    const int64_t tile0 = (int64_t)(r / RT) * a.G * AW;
+    const int64_t tile0 = (int64_t)(r / RT) * a.warps;
     auto part_at = [&](int p) {
         const int seg = p == w0 && s > p * quota ? 1 : 0;
         return ((tile0 + p) * 2 + seg) * RT + r % RT;
@@ -676,7 +678,7 @@ template <int D, int FMT, int NT>
 __global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
     k_cache8_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
 {
-    using C = Cfg<D>;
+    using C = Cfg<D, AW>;
     constexpr int MT = D / 16, RT = 8 * NT, E = D / 32;
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
@@ -695,7 +697,7 @@ __global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
     fw_status st;
     const int nb = cell_blocks(a.s, h, base, n, st);
     if (rank == 0 && blockIdx.y == 0 && tid == 0 && a.status) a.status[h] = st;
-    Ring<D> ring;
+    Ring<D, C::STAGES> ring;
     ring.mem = sm + wid * C::STAGES * 2 * C::BLK;
     ring.full = full[wid];
     int pb = rank + FEW * wid;  // (the first blocks go to different CTAs)
@@ -770,15 +772,21 @@ int row_tile(const fw_cache8 &c, const fw_cache8_query &q)
     return rows <= 8 ? 8 : rows <= 16 || c.d == 128 ? 16 : rows <= 24 ? 24 : 32;
 }
 
-// Whether the cells are so few, and hold so little at most, that a cluster each is faster.
-bool few_cells(const fw_cache8 &c, int tiles, int sms)
+// Warps of a CTA of the many-cells kernel: as many as its registers allow (d = 64, 8 rows: 64 x 8 cells of 16,384 rows
+// 189 us with 8 warps).
+constexpr int warps_of(int d, int RT) { return d == 64 && RT == 8 ? 16 : 8; }
+
+// Whether the cells are so few, and hold so little at most, that a cluster each is faster: up to 14 of them (clusters of
+// 8 whole SMs; cells of about 4,096 rows, d = 128: 8 cells 6.8 us against 10.7, 14 cells 8.6 against 11.7, but 16 cells,
+// which do not all find their SMs at once, 12.9 against 11.9).
+bool few_cells(const fw_cache8 &c, int tiles)
 {
-    return (int64_t)c.cells * tiles * FEW <= sms && c.rows <= (int64_t)c.cells * 16384;
+    return (int64_t)c.cells * tiles <= 14 && c.rows <= (int64_t)c.cells * 16384;
 }
 
 struct Plan {
     bool few;
-    int G, RT, tiles;
+    int G, W, RT, tiles;
     size_t start, plan, ml, o, bytes;
 };
 void plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
@@ -787,41 +795,43 @@ void plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
     if (device_sms(&sms) != FW_OK) sms = 152;  // no device: the size query still answers
     p.RT = row_tile(c, q);
     p.tiles = (q.group * q.m + p.RT - 1) / p.RT;
-    p.few = few_cells(c, p.tiles, sms);
+    p.few = few_cells(c, p.tiles);
     p.G = std::max(1, sms / p.tiles);  // one wave
+    p.W = warps_of(c.d, p.RT);
     p.start = p.plan = p.ml = p.o = p.bytes = 0;
     if (p.few) return;
     p.plan = align256((size_t)c.cells * 4);
     p.ml = p.plan + 256;
-    const size_t parts = (size_t)p.tiles * p.G * AW * 2 * p.RT;
+    const size_t parts = (size_t)p.tiles * p.G * p.W * 2 * p.RT;
     p.o = p.ml + align256(parts * 8);
     p.bytes = p.o + align256(parts * c.d * 4);
 }
 
 template <typename K>
-fw_status launch(K kernel, int grid, int tiles, size_t smem, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a,
-                 cudaStream_t s)
+fw_status launch(K kernel, int grid, int tiles, int threads, size_t smem, const CUtensorMap &mk, const CUtensorMap &mv,
+                 const AttendArgs &a, cudaStream_t s)
 {
     FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    FW_LAUNCH(kernel, dim3((unsigned)grid, (unsigned)tiles), AT, smem, s, mk, mv, a);
+    FW_LAUNCH(kernel, dim3((unsigned)grid, (unsigned)tiles), threads, smem, s, mk, mv, a);
     return FW_OK;
+}
+template <int D, int FMT, int NT>
+fw_status launch_tiles(const Plan &p, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
+{
+    constexpr int W = warps_of(D, 8 * NT);
+    return p.few ? launch(k_cache8_attend_few<D, FMT, NT>, cells * FEW, p.tiles, AT, Cfg<D, AW>::SMEM_FEW, mk, mv, a, s)
+                 : launch(k_cache8_attend<D, FMT, NT, W>, p.G, p.tiles, 32 * W, Cfg<D, W>::SMEM, mk, mv, a, s);
 }
 template <int D, int FMT>
 fw_status attend(const Plan &p, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
 {
-    constexpr int N3 = D == 128 ? 2 : 3, N4 = D == 128 ? 2 : 4;  // (with d = 128 two tiles of 8 rows at most)
-    using C = Cfg<D>;
-    if (p.few) {
-        const int grid = cells * FEW;
-        if (p.RT == 8) return launch(k_cache8_attend_few<D, FMT, 1>, grid, p.tiles, C::SMEM_FEW, mk, mv, a, s);
-        if (p.RT == 16) return launch(k_cache8_attend_few<D, FMT, 2>, grid, p.tiles, C::SMEM_FEW, mk, mv, a, s);
-        if (p.RT == 24) return launch(k_cache8_attend_few<D, FMT, N3>, grid, p.tiles, C::SMEM_FEW, mk, mv, a, s);
-        return launch(k_cache8_attend_few<D, FMT, N4>, grid, p.tiles, C::SMEM_FEW, mk, mv, a, s);
+    if (p.RT == 8) return launch_tiles<D, FMT, 1>(p, cells, mk, mv, a, s);
+    if (p.RT == 16) return launch_tiles<D, FMT, 2>(p, cells, mk, mv, a, s);
+    if constexpr (D == 64) {  // (with d = 128 two tiles of 8 rows at most)
+        if (p.RT == 24) return launch_tiles<D, FMT, 3>(p, cells, mk, mv, a, s);
+        return launch_tiles<D, FMT, 4>(p, cells, mk, mv, a, s);
     }
-    if (p.RT == 8) return launch(k_cache8_attend<D, FMT, 1>, p.G, p.tiles, C::SMEM, mk, mv, a, s);
-    if (p.RT == 16) return launch(k_cache8_attend<D, FMT, 2>, p.G, p.tiles, C::SMEM, mk, mv, a, s);
-    if (p.RT == 24) return launch(k_cache8_attend<D, FMT, N3>, p.G, p.tiles, C::SMEM, mk, mv, a, s);
-    return launch(k_cache8_attend<D, FMT, N4>, p.G, p.tiles, C::SMEM, mk, mv, a, s);
+    return FW_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -846,7 +856,7 @@ fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, f
         return FW_ERR_CUDA;
     uint8_t *w = (uint8_t *)ws;
     const AttendArgs a{store(c), q.kv_heads, q.group, q.m, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
-                       q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, p.G, (int32_t *)(w + p.start),
+                       q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, p.G, p.G * p.W, (int32_t *)(w + p.start),
                        (int32_t *)(w + p.plan), (float2 *)(w + p.ml), (float *)(w + p.o)};
     fw_status st = FW_OK;
     FW_CACHE8_DISPATCH(c, st = attend<D, FMT>(p, c.cells, mk, mv, a, s));
