@@ -492,6 +492,13 @@ def _raw_stream(stream, tensor):
     return stream.cuda_stream if stream is not None else _current_raw(tensor.get_device())
 
 
+def _one_device(*tensors):
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != dev or dev < 0:
+            raise ValueError("the tensors of a call are on one GPU")
+
+
 def _own_buffers(stream, *tensors):
     # buffers made here on the current stream and used on another: not reused before that stream is done
     if stream is not None:
@@ -514,6 +521,10 @@ def _attention_out(out, q, items, stream):
         raise ValueError("out['lse'] is contiguous float32 of q's shape without its last axis")
     if status is not None and (status.numel() < items or status.dtype is not torch.int32 or not status.is_contiguous()):
         raise ValueError(f"out['status'] is contiguous int32, {items} entries")
+    dev = q.get_device()
+    if o.get_device() != dev or (lse is not None and lse.get_device() != dev) or (
+            status is not None and status.get_device() != dev):
+        raise ValueError("out's tensors are on q's GPU")
     return o.data_ptr(), lse.data_ptr() if lse is not None else None, status.data_ptr() if status is not None else None, out
 
 
@@ -538,6 +549,9 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     if cu_q.dtype is not i32 or cu_k.dtype is not i32 or cu_q.dim() != 1 or cu_q.shape != cu_k.shape or not (
             cu_q.is_contiguous() and cu_k.is_contiguous()):
         raise ValueError("cu_q and cu_k are contiguous int32 [sequences + 1]")
+    dev = q.get_device()
+    if dev < 0 or k.get_device() != dev or v.get_device() != dev or cu_q.get_device() != dev or cu_k.get_device() != dev:
+        raise ValueError("the tensors of a call are on one GPU")
     # (strides of axes of one entry, which torch leaves open)
     if hq == 1:
         qh = d
@@ -578,13 +592,23 @@ class Cache8:
               tuple(k_tail.shape) == tuple(v_tail.shape) == (cells, CACHE8_TAIL, d), "tails are bfloat16 [cells][64][d]")
         _need(base.dtype == torch.int64 and capacity.dtype == counts.dtype == torch.int32 and
               capacity.numel() == counts.numel() == cells, "base is int64, capacity and counts are int32, [cells] each")
+        _need(d in (64, 128) and cells >= 1, "d is 64 or 128, and there is a cell")
         self.tensors = (k, v, k_scale, v_scale, k_tail, v_tail, base, capacity, counts)
         _need(all(t.is_contiguous() for t in self.tensors), "the store's tensors are contiguous")
+        _one_device(*self.tensors)
         self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail, self.base, self.capacity, self.counts = \
             self.tensors
-        self.fmt, self.d, self.cells, self.device = fmt, d, cells, k.device
+        self.fmt, self.d, self.cells, self.device, self.index = fmt, d, cells, k.device, k.get_device()
         self.c = FwCache8(cells, d, code, rows, *(t.data_ptr() for t in self.tensors))
         self._ref = C.byref(self.c)
+
+    def part(self, first: int, cells: int) -> "Cache8":
+        """The cells first .. first + cells (a layer's, say) as a store of their own over the same memory."""
+        _need(0 <= first and cells >= 1 and first + cells <= self.cells, "cells within the store's")
+        cut = slice(first, first + cells)
+        return Cache8(fmt=self.fmt, k=self.k, v=self.v, k_scale=self.k_scale, v_scale=self.v_scale,
+                      k_tail=self.k_tail[cut], v_tail=self.v_tail[cut], base=self.base[cut],
+                      capacity=self.capacity[cut], counts=self.counts[cut])
 
 
 def cache8_empty(offsets: torch.Tensor, total: int, d: int, *, fmt: str = "e4m3", room: int = 0) -> Cache8:
@@ -609,8 +633,8 @@ def cache8_empty(offsets: torch.Tensor, total: int, d: int, *, fmt: str = "e4m3"
 def _status_ptr(status, cells):
     if status is None:
         return None
-    if status.dtype is not torch.int32 or status.numel() < cells or not status.is_contiguous():
-        raise ValueError("status is contiguous int32 [cells]")
+    if status.dtype is not torch.int32 or status.numel() < cells or not status.is_contiguous() or not status.is_cuda:
+        raise ValueError("status is contiguous int32 [cells] on the GPU")
     return status.data_ptr()
 
 
@@ -632,6 +656,8 @@ def cache8_compact(cache: Cache8, K: torch.Tensor, V: torch.Tensor, offsets: tor
     if offsets.dtype is not torch.int64 or offsets.numel() != cells + 1 or kept_pos.dtype is not torch.int32 or not (
             offsets.is_contiguous() and kept_pos.is_contiguous()):
         raise ValueError("offsets is contiguous int64 [cells + 1], kept_pos contiguous int32")
+    if not K.get_device() == V.get_device() == offsets.get_device() == kept_pos.get_device() == cache.index:
+        raise ValueError("the tensors of a call are on the store's GPU")
     st = _lib.fw_cache8_compact(cache._ref, K.data_ptr(), V.data_ptr(), T, cs, rs, offsets.data_ptr(),
                                 kept_pos.data_ptr(), kept_pos.numel(), _status_ptr(status, cells), _raw_stream(stream, K))
     if st != FW_OK:
@@ -644,6 +670,8 @@ def cache8_append(cache: Cache8, new_K: torch.Tensor, new_V: torch.Tensor, *, st
     if new_K.dtype is not torch.bfloat16 or new_V.dtype is not torch.bfloat16 or new_V.shape != new_K.shape or not (
             new_K.is_contiguous() and new_V.is_contiguous()) or cells != cache.cells or d != cache.d:
         raise ValueError("new_K and new_V are contiguous bfloat16 [cells][m][d], as the store's")
+    if not new_K.get_device() == new_V.get_device() == cache.index:
+        raise ValueError("the tensors of a call are on the store's GPU")
     st = _lib.fw_cache8_append(cache._ref, new_K.data_ptr(), new_V.data_ptr(), m, _status_ptr(status, cells),
                                _raw_stream(stream, new_K))
     if st != FW_OK:
@@ -675,6 +703,8 @@ def cache8_attend(cache: Cache8, q: torch.Tensor, *, kv_heads: int, scale: float
     (fp32 [sequences][m][q_heads]) and status [cells]; such a dict passed as out is written instead.  A workspace
     (cache8_attend_workspace) serves one call at a time."""
     c_q = _cache8_query(cache, q, kv_heads, scale)
+    if q.get_device() != cache.index:
+        raise ValueError("q is on the store's GPU")
     o, lse, status, out = _attention_out(out, q, cache.cells, stream)
     if workspace is None:
         workspace = _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
