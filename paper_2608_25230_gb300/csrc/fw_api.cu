@@ -88,6 +88,17 @@ fw_status device_sms(int *sms)
     return FW_OK;
 }
 
+fw_status big_smem(const void *kernel, size_t bytes, std::atomic<uint64_t> &done)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return FW_ERR_CUDA;
+    const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return FW_OK;
+    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return FW_OK;
+}
+
 static bool good_stride(int64_t x) { return x > 0 && x % 8 == 0 && x < ((int64_t)1 << 38); }
 
 static fw_status check_prompt(const fw_prompt *p)

@@ -133,6 +133,10 @@ fw_status fp32_fma_probe(int blocks, int iters, float *out, cudaStream_t s);
 // Number of SMs of the current device (queried once per device).
 fw_status device_sms(int *sms);
 
+// Lets a kernel have `bytes` of dynamic shared memory on the current device; `done` (a bit per device) remembers
+// for which it has been said, half a microsecond of host time a call.
+fw_status big_smem(const void *kernel, size_t bytes, std::atomic<uint64_t> &done);
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace fw

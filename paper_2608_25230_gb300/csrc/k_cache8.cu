@@ -19,7 +19,7 @@ using namespace cache8;
 constexpr int BR = FW_CACHE8_BLOCK, TL = FW_CACHE8_TAIL;
 
 constexpr int QT = 128;        // threads of a CTA
-constexpr int compact_ctas(int d) { return d == 128 ? 6 : 10; }  // CTAs of the compaction per SM
+constexpr int compact_ctas(int d) { return d == 128 ? 8 : 12; }  // CTAs of the compaction per SM
 
 // A block's rows as a CTA holds them: thread t has the 16-byte pieces of column 8 * (t % LPR) of
 // rows t / LPR + RS * i.

@@ -43,6 +43,7 @@ constexpr float P_UP = 14.f;            // weights are 2^(x - max + P_UP)
 struct AttendArgs {
     Store s;
     int kv_heads, group, m;
+    uint32_t group_inv;  // 2^32 / group + 1 (0 for a group of 1)
     const uint16_t *q;
     int64_t q_seq, q_tok, q_head;
     float scale2;  // scale * log2(e)
@@ -55,6 +56,9 @@ struct AttendArgs {
     float2 *part_ml;     // workspace: [tiles of rows][warps][2][rows of a tile] (max, sum)
     float *part_o;       // workspace: the same with D columns
 };
+
+// r / group for a query row r: both are below 2^16, so the product's upper half is exact
+__device__ __forceinline__ int token_of(const AttendArgs &a, int r) { return a.group_inv ? __umulhi(r, a.group_inv) : r; }
 
 // Blocks of a cell (0 where the cell is not valid), and its status.
 __device__ __forceinline__ int cell_blocks(const Store &s, int h, int64_t &base, int &n, fw_status &st)
@@ -209,7 +213,7 @@ template <int D, int FMT, int NT> struct Rows {
         const int g = lane >> 2, c = lane & 3, rows = a.group * a.m;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int r = row0 + 8 * t + g, i = r / a.group;
+            const int r = row0 + 8 * t + g, i = token_of(a, r);
             const uint16_t *src = a.q + seq * a.q_seq + i * a.q_tok + (int64_t)(hk * a.group + r - i * a.group) * a.q_head;
 #pragma unroll
             for (int e = 0; e < H; ++e)
@@ -299,7 +303,7 @@ template <int D, int FMT, int NT> struct Rows {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) S[t][i >> 1][2 * (i & 1) + e] *= f;
                 if (masked) {
-                    const int seen = all + (row0 + 8 * t + 2 * c + e) / a.group;
+                    const int seen = all + token_of(a, row0 + 8 * t + 2 * c + e);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (j0 + 8 * i >= seen) S[t][i >> 1][2 * (i & 1) + e] = -INFINITY;
@@ -397,7 +401,7 @@ template <int D, int FMT, int NT> struct Rows {
 // Index of query row r of cell (seq, hk) in the outputs.
 __device__ __forceinline__ int64_t out_row(const AttendArgs &a, int seq, int hk, int r)
 {
-    const int i = r / a.group;
+    const int i = token_of(a, r);
     return ((int64_t)seq * a.m + i) * a.kv_heads * a.group + hk * a.group + (r - i * a.group);
 }
 // lse of a row with running maximum mx and sum l of 2^(x - mx + P_UP)
@@ -809,9 +813,10 @@ void plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
 
 template <typename K>
 fw_status launch(K kernel, int grid, int tiles, int threads, size_t smem, const CUtensorMap &mk, const CUtensorMap &mv,
-                 const AttendArgs &a, cudaStream_t s)
+                 const AttendArgs &a, std::atomic<uint64_t> &done, cudaStream_t s)
 {
-    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const fw_status st = big_smem((const void *)kernel, smem, done);
+    if (st != FW_OK) return st;
     FW_LAUNCH(kernel, dim3((unsigned)grid, (unsigned)tiles), threads, smem, s, mk, mv, a);
     return FW_OK;
 }
@@ -819,8 +824,9 @@ template <int D, int FMT, int NT>
 fw_status launch_tiles(const Plan &p, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
 {
     constexpr int W = warps_of(D, 8 * NT);
-    return p.few ? launch(k_cache8_attend_few<D, FMT, NT>, cells * FEW, p.tiles, AT, Cfg<D, AW>::SMEM_FEW, mk, mv, a, s)
-                 : launch(k_cache8_attend<D, FMT, NT, W>, p.G, p.tiles, 32 * W, Cfg<D, W>::SMEM, mk, mv, a, s);
+    static std::atomic<uint64_t> few{0}, many{0};
+    return p.few ? launch(k_cache8_attend_few<D, FMT, NT>, cells * FEW, p.tiles, AT, Cfg<D, AW>::SMEM_FEW, mk, mv, a, few, s)
+                 : launch(k_cache8_attend<D, FMT, NT, W>, p.G, p.tiles, 32 * W, Cfg<D, W>::SMEM, mk, mv, a, many, s);
 }
 template <int D, int FMT>
 fw_status attend(const Plan &p, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
@@ -855,7 +861,8 @@ fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, f
         !make_tma_2d_bytes(&mv, c.rows ? c.v : o, rows, (uint64_t)c.d, BR))
         return FW_ERR_CUDA;
     uint8_t *w = (uint8_t *)ws;
-    const AttendArgs a{store(c), q.kv_heads, q.group, q.m, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
+    const uint32_t inv = q.group > 1 ? (uint32_t)(((uint64_t)1 << 32) / q.group + 1) : 0;
+    const AttendArgs a{store(c), q.kv_heads, q.group, q.m, inv, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
                        q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, p.G, p.G * p.W, (int32_t *)(w + p.start),
                        (int32_t *)(w + p.plan), (float2 *)(w + p.ml), (float *)(w + p.o)};
     fw_status st = FW_OK;

@@ -686,7 +686,9 @@ fw_status launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap
 {
     using C = PCfg<D, TILES>;
     const auto kernel = k_prompt<D, TILES>;
-    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+    static std::atomic<uint64_t> done{0};
+    const fw_status st = big_smem((const void *)kernel, C::SMEM, done);
+    if (st != FW_OK) return st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)a.parts;
