@@ -18,24 +18,29 @@ using namespace cache8;
 
 constexpr int BR = FW_CACHE8_BLOCK, TL = FW_CACHE8_TAIL;
 
-constexpr int QT = 128;        // threads of a CTA
-constexpr int compact_ctas(int d) { return d == 128 ? 8 : 12; }  // CTAs of the compaction per SM
+// Threads of a CTA: the compaction's hold four pieces of the keys and four of the values each (d = 64, 108 cells x 22,554
+// rows to an eighth: 19.5 us, 28.6 with 128 threads of two); the appends, of one block, are faster with more (512 cells x 7
+// rows: 4.7 us, 5.6 with 64).
+__host__ __device__ constexpr int compact_threads(int d) { return d; }
+constexpr int AT = 128;
+constexpr int compact_ctas(int d) { return d == 128 ? 8 : 16; }  // CTAs of the compaction per SM
 
 // A block's rows as a CTA holds them: thread t has the 16-byte pieces of column 8 * (t % LPR) of
 // rows t / LPR + RS * i.
-template <int D> struct Lay {
-    static constexpr int LPR = D / 8, RS = QT / LPR, N = BR / RS;
+template <int D, int T> struct Lay {
+    static constexpr int THREADS = T;
+    static constexpr int LPR = D / 8, RS = THREADS / LPR, N = BR / RS, WARPS = THREADS / 32;
 };
 
 // Quantises the keys x[0] and the values x[1] of one block: the scales from the CTA's largest
 // magnitudes, then the codes.  Rows at or past nrow are not filled (and hold zeros).  Every thread of the
 // CTA calls it; s_max is free again two barriers later, so calls alternate between two.  Returns whether
 // the block holds values that are not finite (the same for every thread).
-template <int D, int FMT>
-__device__ __forceinline__ bool quantise_block(const Store &s, int64_t row, int nrow, uint4 (&x)[2][Lay<D>::N],
-                                               uint32_t (&s_max)[2][QT / 32])
+template <int D, int FMT, int T>
+__device__ __forceinline__ bool quantise_block(const Store &s, int64_t row, int nrow, uint4 (&x)[2][Lay<D, T>::N],
+                                               uint32_t (&s_max)[2][Lay<D, T>::WARPS])
 {
-    using L = Lay<D>;
+    using L = Lay<D, T>;
     const int tid = threadIdx.x, col = tid % L::LPR, r0 = tid / L::LPR;
     uint32_t top[2];
 #pragma unroll
@@ -51,7 +56,7 @@ __device__ __forceinline__ bool quantise_block(const Store &s, int64_t row, int 
     for (int kv = 0; kv < 2; ++kv) {
         top[kv] = 0;
 #pragma unroll
-        for (int w = 0; w < QT / 32; ++w) top[kv] = max(top[kv], s_max[kv][w]);
+        for (int w = 0; w < L::WARPS; ++w) top[kv] = max(top[kv], s_max[kv][w]);
     }
     const bool odd = max(top[0], top[1]) >= 0x7f80u;
     if (odd) {  // (rare, and uniform: the scale is that of the finite values)
@@ -66,7 +71,7 @@ __device__ __forceinline__ bool quantise_block(const Store &s, int64_t row, int 
             __syncthreads();
             top[kv] = 0;
 #pragma unroll
-            for (int w = 0; w < QT / 32; ++w) top[kv] = max(top[kv], s_max[kv][w]);
+            for (int w = 0; w < L::WARPS; ++w) top[kv] = max(top[kv], s_max[kv][w]);
 #pragma unroll
             for (int i = 0; i < L::N; ++i) x[kv][i] = finite_piece(x[kv][i], top_code_bits<FMT>(scale_exponent<FMT>(top[kv])));
         }
@@ -127,10 +132,10 @@ __global__ void __launch_bounds__(256) k_cache8_status(const CompactArgs a)
 // written, 90 % of the measured copy rate (3.4 ms a CTA per cell, 180 us with an unpacked search for the largest magnitude,
 // which left the integer pipe at 65 %).
 template <int D, int FMT>
-__global__ void __launch_bounds__(QT, compact_ctas(D)) k_cache8_compact(const CompactArgs a)
+__global__ void __launch_bounds__(Lay<D, compact_threads(D)>::THREADS, compact_ctas(D)) k_cache8_compact(const CompactArgs a)
 {
-    using L = Lay<D>;
-    __shared__ uint32_t s_max[2][2][QT / 32];
+    using L = Lay<D, compact_threads(D)>;
+    __shared__ uint32_t s_max[2][2][Lay<D, compact_threads(D)>::WARPS];
     __shared__ int s_cell;
     const int tid = threadIdx.x, lane = tid & 31, col = tid % L::LPR, r0 = tid / L::LPR;
     const int64_t run = (a.slots + gridDim.x - 1) / gridDim.x;
@@ -189,7 +194,7 @@ __global__ void __launch_bounds__(QT, compact_ctas(D)) k_cache8_compact(const Co
                         *reinterpret_cast<uint4 *>(a.s.tail(kv) + ((int64_t)h * TL + (b + r) % TL) * D + 8 * col) = x[kv][i];
             }
         }
-        const bool odd = quantise_block<D, FMT>(a.s, base + b, nrow, x, s_max[flip]);
+        const bool odd = quantise_block<D, FMT, L::THREADS>(a.s, base + b, nrow, x, s_max[flip]);
         flip ^= 1;
         if (a.status) {
             if (off) atomicMax(a.status + h, FW_ERR_INVALID_ARG);
@@ -219,9 +224,9 @@ __device__ __forceinline__ fw_status append_cell(const AppendArgs &a, int h, int
 // others from the new ones.
 template <int D, int FMT, bool RING>
 __device__ __forceinline__ bool append_block(const AppendArgs &a, int h, int64_t base, int n, int b,
-                                             uint32_t (&s_max)[2][QT / 32])
+                                             uint32_t (&s_max)[2][Lay<D, AT>::WARPS])
 {
-    using L = Lay<D>;
+    using L = Lay<D, AT>;
     const int tid = threadIdx.x, col = tid % L::LPR, r0 = tid / L::LPR, end = n + a.m;
     uint4 x[2][L::N];
 #pragma unroll
@@ -236,7 +241,7 @@ __device__ __forceinline__ bool append_block(const AppendArgs &a, int h, int64_t
             if (RING && r >= n && r < end) *reinterpret_cast<uint4 *>(a.s.tail(kv) + slot) = x[kv][i];
         }
     }
-    return quantise_block<D, FMT>(a.s, base + b, min(BR, end - b), x, s_max);
+    return quantise_block<D, FMT, AT>(a.s, base + b, min(BR, end - b), x, s_max);
 }
 
 // Bound: latency, one read of the rows, a barrier and the write (256 cells x 1 row and 512 x 7: about 3 us).
@@ -244,9 +249,9 @@ __device__ __forceinline__ bool append_block(const AppendArgs &a, int h, int64_t
 // the count.  (The rows of the ring that it reads are fewer than 32 before the new ones: no slot of
 // theirs is written.)
 constexpr int ONE_CTA = BR;
-template <int D, int FMT> __global__ void __launch_bounds__(QT) k_cache8_append(const AppendArgs a)
+template <int D, int FMT> __global__ void __launch_bounds__(Lay<D, AT>::THREADS) k_cache8_append(const AppendArgs a)
 {
-    __shared__ uint32_t s_max[2][2][QT / 32];
+    __shared__ uint32_t s_max[2][2][Lay<D, AT>::WARPS];
     const int h = blockIdx.x, tid = threadIdx.x;
     int64_t base;
     int n;
@@ -272,9 +277,9 @@ __global__ void __launch_bounds__(256) k_cache8_append_status(const AppendArgs a
     int n;
     if (h < a.s.cells) a.status[h] = append_cell(a, h, base, n);
 }
-template <int D, int FMT> __global__ void __launch_bounds__(QT) k_cache8_append_blocks(const AppendArgs a, int blocks)
+template <int D, int FMT> __global__ void __launch_bounds__(Lay<D, AT>::THREADS) k_cache8_append_blocks(const AppendArgs a, int blocks)
 {
-    __shared__ uint32_t s_max[2][QT / 32];
+    __shared__ uint32_t s_max[2][Lay<D, AT>::WARPS];
     const int h = blockIdx.x / blocks, i = blockIdx.x - h * blocks;
     int64_t base;
     int n;
@@ -314,7 +319,7 @@ fw_status cache8_compact(const fw_cache8 &c, const void *K, const void *V, int T
     const fw_status st = device_sms(&sms);
     if (st != FW_OK) return st;
     const unsigned grid = (unsigned)std::min<int64_t>(a.slots, (int64_t)sms * compact_ctas(c.d));
-    FW_CACHE8_DISPATCH(c, FW_LAUNCH((k_cache8_compact<D, FMT>), grid, QT, 0, s, a));
+    FW_CACHE8_DISPATCH(c, FW_LAUNCH((k_cache8_compact<D, FMT>), grid, compact_threads(D), 0, s, a));
     return FW_OK;
 }
 
@@ -323,14 +328,14 @@ fw_status cache8_append(const fw_cache8 &c, const void *new_K, const void *new_V
 {
     const AppendArgs a{store(c), (const uint16_t *)new_K, (const uint16_t *)new_V, m, status};
     if (m <= ONE_CTA) {
-        FW_CACHE8_DISPATCH(c, FW_LAUNCH((k_cache8_append<D, FMT>), (unsigned)c.cells, QT, 0, s, a));
+        FW_CACHE8_DISPATCH(c, FW_LAUNCH((k_cache8_append<D, FMT>), (unsigned)c.cells, AT, 0, s, a));
         return FW_OK;
     }
     const int64_t blocks = ((int64_t)m + 2 * BR - 2) / BR;  // that m rows can touch
     if (blocks * c.cells >= ((int64_t)1 << 31)) return FW_ERR_UNSUPPORTED;
     if (status) FW_LAUNCH(k_cache8_append_status, (unsigned)((c.cells + 255) / 256), 256, 0, s, a);
     FW_CACHE8_DISPATCH(c, {
-        FW_LAUNCH((k_cache8_append_blocks<D, FMT>), (unsigned)(blocks * c.cells), QT, 0, s, a, (int)blocks);
+        FW_LAUNCH((k_cache8_append_blocks<D, FMT>), (unsigned)(blocks * c.cells), AT, 0, s, a, (int)blocks);
         FW_LAUNCH(k_cache8_append_end<D>, (unsigned)c.cells, 256, 0, s, a);
     });
     return FW_OK;
