@@ -27,6 +27,7 @@
 // follows.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "fw_cache8.cuh"
 #include "tc_sm100.cuh"
@@ -53,6 +54,7 @@ struct AttendArgs {
     float *lse;
     int32_t *status;
     int G, warps;        // CTAs along the blocks, and their warps
+    int cluster;         // CTAs of a cell (few cells)
     int32_t *start;      // workspace: [cells] first unit of each cell
     int32_t *plan;       // workspace: units per warp
     float2 *part_ml;     // workspace: [tiles of rows][warps][2][rows of a tile] (max, sum)
@@ -678,10 +680,10 @@ __device__ __forceinline__ void join8(FM ml_of, FO o_of, float &M, float &L, flo
     }
 }
 
-// A cluster of FEW CTAs per cell and tile of rows, its blocks dealt out to their warps one by one.
+// A cluster of up to FEW CTAs per cell and tile of rows, its blocks dealt out to their warps one by one.
 constexpr int FEW = 8;
 template <int D, int FMT, int NT>
-__global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
+__global__ void __launch_bounds__(AT, 1)
     k_cache8_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
 {
     using C = Cfg<D, AW>;
@@ -694,7 +696,7 @@ __global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
     __shared__ float2 s_pml[8];
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int h = blockIdx.x / FEW, rank = blockIdx.x % FEW, row0 = blockIdx.y * RT, rows = a.group * a.m;
+    const int h = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, row0 = blockIdx.y * RT, rows = a.group * a.m;
     if (lane < C::STAGES) tc::mbar_init(&full[wid][lane], 1);
     tc::mbar_init_fence();
     __syncwarp();
@@ -706,11 +708,11 @@ __global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
     Ring<D, C::STAGES> ring;
     ring.mem = sm + wid * C::STAGES * 2 * C::BLK;
     ring.full = full[wid];
-    int pb = rank + FEW * wid;  // (the first blocks go to different CTAs)
+    int pb = rank + a.cluster * wid;  // (the first blocks go to different CTAs)
     auto fetch = [&]() {
         if (pb >= nb) return;
         ring.fetch(&tmK, &tmV, base + (int64_t)pb * BR, lane);
-        pb += FEW * AW;
+        pb += a.cluster * AW;
     };
     const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
     Rows<D, FMT, NT> R;
@@ -721,7 +723,7 @@ __global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
     R.start(raw, a, lane);
     const float *ks = a.s.ks + base / BR, *vs = a.s.vs + base / BR;
 #pragma unroll 1
-    for (int blk = rank + FEW * wid; blk < nb; blk += FEW * AW) {
+    for (int blk = rank + a.cluster * wid; blk < nb; blk += a.cluster * AW) {
         const float sk = ks[blk], sv = vs[blk];
         const uint8_t *tk = ring.next();
         if (!tk) break;
@@ -751,11 +753,12 @@ __global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
         for (int e = 0; e < E; ++e) s_o[wid * C::LDO + lane + 32 * e] = acc[e];  // (its row in the first warp's place)
         if (lane == 0) s_pml[wid] = make_float2(M, L);
         cluster_sync();
-        // ---- and over the cluster's CTAs, a CTA per row
-        const int r = row0 + 8 * t + rank;
-        if (wid == 0 && r < rows) {
-            join8<E>([&](int w) { return make_float2(remote(&s_pml[rank].x, w), remote(&s_pml[rank].y, w)); },
-                     [&](int w, int e) { return remote(&s_o[rank * C::LDO + lane + 32 * e], w); }, M, L, acc);
+        // ---- and over the cluster's CTAs: rows dealt out to them and their warps
+        const int r8 = rank + a.cluster * wid, r = row0 + 8 * t + r8;
+        if (r8 < 8 && r < rows) {
+            join8<E>([&](int w) { return w < a.cluster ? make_float2(remote(&s_pml[r8].x, w), remote(&s_pml[r8].y, w))
+                                                      : make_float2(-INFINITY, 0.f); },
+                     [&](int w, int e) { return w < a.cluster ? remote(&s_o[r8 * C::LDO + lane + 32 * e], w) : 0.f; }, M, L, acc);
             const int64_t out = out_row(a, seq, hk, r);
             const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
@@ -768,7 +771,7 @@ __global__ void __launch_bounds__(AT, 1) __cluster_dims__(FEW, 1, 1)
     if (!ring.ok && lane == 0 && a.status) a.status[h] = FW_ERR_TIMEOUT;
     cluster_sync();  // no CTA leaves while another reads its rows
 }
-static_assert(FEW == 8 && AW == 8, "a CTA and a warp per row of 8");
+static_assert(FEW == 8 && AW == 8, "a warp per row of 8, eight states to join");
 
 // Query rows of a CTA: as few tiles of 8 as hold them, as far as registers go (a second round over
 // the store costs its fetches and products again).
@@ -782,16 +785,23 @@ int row_tile(const fw_cache8 &c, const fw_cache8_query &q)
 // 189 us with 8 warps).
 constexpr int warps_of(int d, int RT) { return d == 64 && RT == 8 ? 16 : 8; }
 
-// Whether the cells are so few, and hold so little at most, that a cluster each is faster: up to 14 of them (clusters of
-// 8 whole SMs; cells of about 4,096 rows, d = 128: 8 cells 6.8 us against 10.7, 14 cells 8.6 against 11.7, but 16 cells,
-// which do not all find their SMs at once, 12.9 against 11.9).
-bool few_cells(const fw_cache8 &c, int tiles)
+// CTAs of a cell where the cells are few and hold little at most, so that a cluster each is faster, else 0.  (Per-layer
+// calls, d = 128, clusters against ranges: 8 cells of 4,096 rows 7.2 us against 10.7; 16 cells in 8 each, whose clusters of
+// whole SMs do not all find them at once, 12.9 against 11.9, of 1,000 rows in 4 each 7.1 against 10.3, of 3,300 13.6 against
+// 11.6; 48 cells of 500 in 2 each 7.4 against 13.2, of 2,000 16.8 against 15.4: the longest cell decides.)
+int cluster_of(const fw_cache8 &c, int tiles)
 {
-    return (int64_t)c.cells * tiles <= 14 && c.rows <= (int64_t)c.cells * 16384;
+    struct Rule {
+        int ctas;
+        int64_t cells, rows;
+    };
+    for (const Rule &r : {Rule{8, 14, 8192}, Rule{4, 36, 2560}, Rule{2, 72, 1280}})
+        if ((int64_t)c.cells * tiles <= r.cells && c.rows <= r.rows * c.cells) return r.ctas;
+    return 0;
 }
 
 struct Plan {
-    bool few;
+    int few;  // CTAs of a cell's cluster, or 0
     int G, W, RT, tiles;
     size_t start, plan, ml, o, bytes;
 };
@@ -801,7 +811,7 @@ void plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
     if (device_sms(&sms) != FW_OK) sms = 152;  // no device: the size query still answers
     p.RT = row_tile(c, q);
     p.tiles = (q.group * q.m + p.RT - 1) / p.RT;
-    p.few = few_cells(c, p.tiles);
+    p.few = cluster_of(c, p.tiles);
     p.G = std::max(1, sms / p.tiles);  // one wave
     p.W = warps_of(c.d, p.RT);
     p.start = p.plan = p.ml = p.o = p.bytes = 0;
@@ -814,21 +824,33 @@ void plan_of(const fw_cache8 &c, const fw_cache8_query &q, Plan &p)
 }
 
 template <typename K>
-fw_status launch(K kernel, int grid, int tiles, int threads, size_t smem, const CUtensorMap &mk, const CUtensorMap &mv,
-                 const AttendArgs &a, std::atomic<uint64_t> &done, cudaStream_t s)
+fw_status launch(K kernel, int grid, int tiles, int cluster, int threads, size_t smem, const CUtensorMap &mk,
+                 const CUtensorMap &mv, const AttendArgs &a, std::atomic<uint64_t> &done, cudaStream_t s)
 {
     const fw_status st = big_smem((const void *)kernel, smem, done);
     if (st != FW_OK) return st;
-    FW_LAUNCH(kernel, dim3((unsigned)grid, (unsigned)tiles), threads, smem, s, mk, mv, a);
-    return FW_OK;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)tiles);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mk, mv, a);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }
 template <int D, int FMT, int NT>
 fw_status launch_tiles(const Plan &p, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
 {
     constexpr int W = warps_of(D, 8 * NT);
     static std::atomic<uint64_t> few{0}, many{0};
-    return p.few ? launch(k_cache8_attend_few<D, FMT, NT>, cells * FEW, p.tiles, AT, Cfg<D, AW>::SMEM_FEW, mk, mv, a, few, s)
-                 : launch(k_cache8_attend<D, FMT, NT, W>, p.G, p.tiles, 32 * W, Cfg<D, W>::SMEM, mk, mv, a, many, s);
+    return p.few ? launch(k_cache8_attend_few<D, FMT, NT>, cells * p.few, p.tiles, p.few, AT, Cfg<D, AW>::SMEM_FEW, mk, mv, a, few, s)
+                 : launch(k_cache8_attend<D, FMT, NT, W>, p.G, p.tiles, 0, 32 * W, Cfg<D, W>::SMEM, mk, mv, a, many, s);
 }
 template <int D, int FMT>
 fw_status attend(const Plan &p, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
@@ -865,7 +887,7 @@ fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, f
     uint8_t *w = (uint8_t *)ws;
     const uint32_t inv = q.group > 1 ? (uint32_t)(((uint64_t)1 << 32) / q.group + 1) : 0;
     const AttendArgs a{store(c), q.kv_heads, q.group, q.m, inv, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
-                       q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, p.G, p.G * p.W, (int32_t *)(w + p.start),
+                       q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, p.G, p.G * p.W, p.few, (int32_t *)(w + p.start),
                        (int32_t *)(w + p.plan), (float2 *)(w + p.ml), (float *)(w + p.o)};
     fw_status st = FW_OK;
     FW_CACHE8_DISPATCH(c, st = attend<D, FMT>(p, c.cells, mk, mv, a, s));

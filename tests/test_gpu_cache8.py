@@ -435,3 +435,20 @@ def test_attend_one_long_cell(fw, d, kv_heads, g, m, counts):
     torch.cuda.synchronize()
     check_attend(cache, q, out, kv_heads, float(torch.tensor(1 / math.sqrt(d), dtype=torch.float32)))
     assert torch.equal(out["o"], again["o"]) and torch.equal(out["lse"], again["lse"])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("seqs,kv_heads,g,m", [(3, 8, 4, 1), (7, 4, 8, 2), (20, 3, 7, 1), (9, 8, 16, 1), (1, 14, 4, 9)])
+def test_attend_cells_between_few_and_many(fw, fmt, d, seqs, kv_heads, g, m):
+    """Short cells in clusters of every size, among them empty ones, and the calls around where the rule changes."""
+    gen = torch.Generator("cuda").manual_seed(seqs)
+    cells = seqs * kv_heads
+    for top in (40, 1500, 6000):
+        counts = [int(x) for x in torch.randint(0, top, (cells,), generator=torch.Generator().manual_seed(cells + top))]
+        counts[1] = 0
+        cache = filled(fw, gen, counts, d, fmt)
+        q = (1.5 * torch.randn(seqs, m, kv_heads * g, d, generator=gen, device="cuda")).to(torch.bfloat16)
+        out = fw.cache8_attend(cache, q, kv_heads=kv_heads)
+        torch.cuda.synchronize()
+        check_attend(cache, q, out, kv_heads, float(torch.tensor(1 / math.sqrt(d), dtype=torch.float32)))
