@@ -4,7 +4,7 @@
 //   x_j = scale (q . kc_j) sk,  o = sum_j softmax_j(x) vc_j sv,  lse = log sum_j e^x_j.
 //
 // Bound: the codes' bytes, each read once from memory.  Two ways over the cells:
-//   few cells (k_cache8_attend_few): a cluster of CTAs per cell, its blocks dealt out
+//   few short cells (k_cache8_attend_few): a cluster of 2 to 8 CTAs per cell, its blocks dealt out
 //   to all their warps, whose states are joined through (distributed) shared memory;
 //   many (k_cache8_attend): the blocks of all cells in a row are divided evenly over the
 //   warps of the GPU, whatever the cells' lengths, so a warp takes the end of one cell,
@@ -13,7 +13,7 @@
 //   behind the first one's tail, joins them in their order.
 // Every warp fetches its blocks by TMA into a ring of its own.  64 x 8 cells of about 16,384 rows, d = 128:
 // 306 us, 6.9 TB/s, the measured copy rate; 32 x 8 cells of 4,096 48 us (5.3 TB/s: the warps finish
-// 14 us apart, and the joining follows them); 8 cells of 4,096 6.8 us (latency).
+// 14 us apart, and the joining follows them); 8 cells of 4,096 7.2 us (latency).
 //
 // A block of 32 rows against 8 query rows, transposed on the warp-wide fp16 tensor
 // instructions (a few rows of queries cannot fill a tcgen05 tile, and the stream of
@@ -424,7 +424,8 @@ __global__ void __launch_bounds__(32 * W, 1) k_cache8_attend(const __grid_consta
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
     __shared__ __align__(8) uint64_t full[W][C::STAGES];
-    __shared__ int s_scan[W], s_h0[W], s_b0[W];
+    __shared__ int s_scan[W], s_h0[W], s_b0[W], s_n0[W];  // (s_*0: where each warp's range begins)
+    __shared__ int64_t s_base0[W];
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
     const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT, rows = a.group * a.m;
@@ -435,13 +436,14 @@ __global__ void __launch_bounds__(32 * W, 1) k_cache8_attend(const __grid_consta
     // ---- the units (blocks) of all cells, divided evenly over the warps of all CTAs
     const int per = (a.s.cells + AT - 1) / AT;
     const int h_lo = min(tid * per, a.s.cells), h_hi = min(h_lo + per, a.s.cells);
-    int mine = 0, nb_lo = 0;
+    int mine = 0, nb_lo = 0, n_lo = 0;
+    int64_t base_lo = 0;
     for (int h = h_lo; h < h_hi; ++h) {
         int64_t base;
         int n;
         fw_status st;
         const int nb = cell_blocks(a.s, h, base, n, st);
-        if (h == h_lo) nb_lo = nb;
+        if (h == h_lo) nb_lo = nb, n_lo = n, base_lo = base;
         mine += nb;
         if (cta == 0 && tile == 0 && a.status) a.status[h] = st;
     }
@@ -464,8 +466,8 @@ __global__ void __launch_bounds__(32 * W, 1) k_cache8_attend(const __grid_consta
     {
         int at = before;
         for (int h = h_lo; h < h_hi; ++h) {
-            int64_t base;
-            int n;
+            int64_t base = base_lo;
+            int n = n_lo;
             fw_status st;
             const int nb = h == h_lo ? nb_lo : cell_blocks(a.s, h, base, n, st);
             // the warps of this CTA whose ranges begin in the cell
@@ -474,6 +476,8 @@ __global__ void __launch_bounds__(32 * W, 1) k_cache8_attend(const __grid_consta
                 if (u >= at && u < at + nb) {
                     s_h0[w] = h;
                     s_b0[w] = (int)(u - at);
+                    s_n0[w] = n;
+                    s_base0[w] = base;
                 }
             }
             if (cta == 0 && tile == 0) a.start[h] = at;
@@ -492,10 +496,9 @@ __global__ void __launch_bounds__(32 * W, 1) k_cache8_attend(const __grid_consta
     ring.mem = sm + wid * C::STAGES * 2 * C::BLK;
     ring.full = full[wid];
     // the warp's producer: its next unit to fetch, by cell
-    int pu = u, ph = s_h0[wid], pb = s_b0[wid], pn, pnb;
-    int64_t pbase;
+    int pu = u, ph = s_h0[wid], pb = s_b0[wid], pn = s_n0[wid], pnb = (pn + BR - 1) / BR;
+    int64_t pbase = s_base0[wid];
     fw_status pst;
-    pnb = cell_blocks(a.s, ph, pbase, pn, pst);
     auto fetch = [&]() {
         if (pu >= u1) return;
         while (pb >= pnb && ph + 1 < a.s.cells) {  // (a unit is left, so a cell holds it)
@@ -514,10 +517,10 @@ __global__ void __launch_bounds__(32 * W, 1) k_cache8_attend(const __grid_consta
 
     int h = s_h0[wid], b = s_b0[wid];  // the segment: blocks of one cell
     while (u < u1) {
-        int64_t base;
-        int n;
+        int64_t base = s_base0[wid];
+        int n = s_n0[wid];
         fw_status st;
-        int nb = cell_blocks(a.s, h, base, n, st);
+        int nb = u == (int)first ? (n + BR - 1) / BR : cell_blocks(a.s, h, base, n, st);
         while (b >= nb && h + 1 < a.s.cells) {  // cells without rows, and the next cell
             b -= nb;
             nb = cell_blocks(a.s, ++h, base, n, st);
@@ -781,8 +784,8 @@ int row_tile(const fw_cache8 &c, const fw_cache8_query &q)
     return rows <= 8 ? 8 : rows <= 16 || c.d == 128 ? 16 : rows <= 24 ? 24 : 32;
 }
 
-// Warps of a CTA of the many-cells kernel: as many as its registers allow (d = 64, 8 rows: 64 x 8 cells of 16,384 rows
-// 189 us with 8 warps).
+// Warps of a CTA of the many-cells kernel: 16 where a warp's registers allow it (d = 64, 8 rows: 32 x 8 cells of 4,096 rows
+// 31 us, 36 with 8), else 8 (d = 64, 24 rows: 64 cells of 1,537 18.4 us, 19.7 with 12, which spill).
 constexpr int warps_of(int d, int RT) { return d == 64 && RT == 8 ? 16 : 8; }
 
 // CTAs of a cell where the cells are few and hold little at most, so that a cluster each is faster, else 0.  (Per-layer
