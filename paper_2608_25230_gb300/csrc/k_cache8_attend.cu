@@ -148,10 +148,12 @@ template <int D, int W> struct Cfg {
     static constexpr int STAGES = D == 128 ? 2 : 3;
     static constexpr int BLK = BR * D;                       // bytes of a block's codes
     static constexpr int RING = W * STAGES * 2 * BLK;
-    static constexpr int LDO = D + 4;                        // floats of a row in the joining buffer
-    static constexpr int JOIN = W * 8 * LDO * 4;
     static constexpr size_t SMEM = 1024 + RING;
-    static constexpr size_t SMEM_FEW = 1024 + RING + JOIN;
+};
+// The few-cells kernel's: the warps' rows of 8 behind the rings.
+template <int D> struct CfgFew : Cfg<D, AW> {
+    static constexpr int LDO = D + 4;  // floats of a row
+    static constexpr size_t SMEM = Cfg<D, AW>::SMEM + AW * 8 * LDO * 4;
 };
 
 // Position of a cell's row among the MMA's: row g of each 8 is key kappa(g).  It keeps
@@ -689,7 +691,7 @@ template <int D, int FMT, int NT>
 __global__ void __launch_bounds__(AT, 1)
     k_cache8_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
 {
-    using C = Cfg<D, AW>;
+    using C = CfgFew<D>;
     constexpr int MT = D / 16, RT = 8 * NT, E = D / 32;
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
@@ -852,7 +854,7 @@ fw_status launch_tiles(const Plan &p, int cells, const CUtensorMap &mk, const CU
 {
     constexpr int W = warps_of(D, 8 * NT);
     static std::atomic<uint64_t> few{0}, many{0};
-    return p.few ? launch(k_cache8_attend_few<D, FMT, NT>, cells * p.few, p.tiles, p.few, AT, Cfg<D, AW>::SMEM_FEW, mk, mv, a, few, s)
+    return p.few ? launch(k_cache8_attend_few<D, FMT, NT>, cells * p.few, p.tiles, p.few, AT, CfgFew<D>::SMEM, mk, mv, a, few, s)
                  : launch(k_cache8_attend<D, FMT, NT, W>, p.G, p.tiles, 0, 32 * W, Cfg<D, W>::SMEM, mk, mv, a, many, s);
 }
 template <int D, int FMT>

@@ -9,20 +9,20 @@
 // 291 us, 0.94 PFLOP/s.  The weights are rounded to bf16 for the second product, which wants both its operands of one
 // type; sums and statistics are of the unrounded ones.
 // The query heads of a KV head are rows of the same product, so a tile of 128 rows
-// is floor(128 / group) tokens with all their heads, and a CTA holds two tiles of
+// is floor(128 / group) tokens with all their heads, and a CTA holds one tile or two of
 // consecutive tokens against one stream of keys and values (TMA, 128-byte swizzle,
 // a ring of tiles).  On tcgen05, S = Q K^T goes to TMEM; the tile's four softmax
 // warps, a thread per row, read it, write the weights over it in bf16, and O += P V
 // takes them from there: while one tile's rows are in the softmax the other tile's
-// products run.  A weight is 2^(x - ref): ref is the row's maximum as of the last
+// products (another CTA's, where a CTA holds one) run.  A weight is 2^(x - ref): ref is the row's maximum as of the last
 // time that it had grown by more than 2^8, so the rescaling of O in TMEM, which the
 // softmax threads do themselves, is rare; sum and output are of the same ref, so the
-// quotient is exact.  Warp 8 issues the copies, warps 9 and 11 the products of a
-// tile each (9 owns the TMEM).  Warp 10 looks over the values of blocks that some row does not see in full:
+// quotient is exact.  Behind the softmax's warps one issues the copies, one per tile its
+// products (the first owns the TMEM), and one looks over the values of blocks that some row does not see in full:
 // a weight of 0 does not make 0 of a NaN or an infinity, so it puts 0 in their place,
 // and the rows that do see them add them when they are written.
 //
-// Slots of 2 x floor(128 / group) tokens: sequence i's are numbered from
+// Slots are the tokens of a CTA's tiles: sequence i's are numbered from
 // floor(cu_q[i] / slot) + i on, which leaves room for all of them without a prefix
 // sum; a CTA finds its sequence by a search over cu_q.  Where there are few slots, a cluster of CTAs takes the
 // blocks of one, and its rows' parts are joined through distributed shared memory.  The last slots, whose rows
@@ -227,7 +227,8 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
     uint8_t *sQ = sm, *sKV = sm + TILES * C::QT;
-    __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full, s_full[2][C::NS], p_full[2][C::NS], o_done[2], drained[2], v_in[PG], v_ok[PG];
+    __shared__ __align__(8) uint64_t full[C::STAGES], empty[C::STAGES], q_full;
+    __shared__ __align__(8) uint64_t s_full[2][C::NS], p_full[2][C::NS], o_done[2], drained[2], v_in[PG], v_ok[PG];
     __shared__ uint32_t s_taddr;
     __shared__ int s_seq[5], s_err, s_odd;  // (s_seq: the sequence, its query and key rows)
 
