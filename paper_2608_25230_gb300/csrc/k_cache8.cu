@@ -24,6 +24,7 @@ constexpr int BR = FW_CACHE8_BLOCK, TL = FW_CACHE8_TAIL;
 __host__ __device__ constexpr int compact_threads(int d) { return d; }
 constexpr int AT = 128;
 constexpr int compact_ctas(int d) { return d == 128 ? 8 : 16; }  // CTAs of the compaction per SM
+constexpr int CHECK = 512;                                       // cells that one of its CTAs looks over
 
 // A block's rows as a CTA holds them: thread t has the 16-byte pieces of column 8 * (t % LPR) of
 // rows t / LPR + RS * i.
@@ -98,8 +99,15 @@ struct CompactArgs {
     const int64_t *offsets;
     const int32_t *kept_pos;
     int64_t total, slots;
+    int checks, walks;  // CTAs that look over the cells, and behind them those that walk the slots
     int32_t *status;
 };
+
+// Whether a cell's offsets are in order; if all cells' are, they ascend within [0, total].
+__device__ __forceinline__ bool offsets_ok(const CompactArgs &a, int h)
+{
+    return a.offsets[h] >= 0 && a.offsets[h + 1] >= a.offsets[h] && a.offsets[h + 1] <= a.total;
+}
 
 // A cell's rows in the compaction: its count, or 0 and why.
 __device__ __forceinline__ fw_status compact_cell(const CompactArgs &a, int h, int64_t &o0, int64_t &base, int &n)
@@ -108,7 +116,7 @@ __device__ __forceinline__ fw_status compact_cell(const CompactArgs &a, int h, i
     o0 = a.offsets[h];
     const int64_t o1 = a.offsets[h + 1];
     fw_status st = cell_rows(a.s, h, base, cap);
-    if (st == FW_OK && (o0 < 0 || o1 < o0 || o1 > a.total)) st = FW_ERR_INVALID_ARG;
+    if (st == FW_OK && !offsets_ok(a, h)) st = FW_ERR_INVALID_ARG;
     if (st == FW_OK && o1 - o0 > cap) st = FW_ERR_WORKSPACE;
     n = st == FW_OK ? (int)(o1 - o0) : 0;
     return st;
@@ -128,7 +136,10 @@ __global__ void __launch_bounds__(256) k_cache8_status(const CompactArgs a)
 // room for all of them (and one at least) without a prefix sum; a CTA takes a run of consecutive
 // slots, finds its first one's cell by a search over the offsets and goes on from there.  All of a
 // block's reads, keys and values, are under way at once (16 KB at d = 128), and the next block's
-// positions with them.  256 cells x 32,768 rows to an eighth, d = 128: 133 us, 6.1 TB/s of rows read and codes
+// positions with them.  The first CTAs write the cells' counts and look at their offsets: the slots hold every cell's
+// blocks only if all offsets ascend within [0, total].  Where they do not, the first of these CTAs that sees it takes every
+// block of every cell that is in order itself, one after another (about a microsecond a block; what the walk writes of
+// them is the same), so that a cell's offsets concern no other cell.  256 cells x 32,768 rows to an eighth, d = 128: 133 us, 6.1 TB/s of rows read and codes
 // written, 90 % of the measured copy rate (3.4 ms a CTA per cell, 180 us with an unpacked search for the largest magnitude,
 // which left the integer pipe at 65 %).
 template <int D, int FMT>
@@ -138,10 +149,25 @@ __global__ void __launch_bounds__(Lay<D, compact_threads(D)>::THREADS, compact_c
     __shared__ uint32_t s_max[2][2][Lay<D, compact_threads(D)>::WARPS];
     __shared__ int s_cell;
     const int tid = threadIdx.x, lane = tid & 31, col = tid % L::LPR, r0 = tid / L::LPR;
-    const int64_t run = (a.slots + gridDim.x - 1) / gridDim.x;
-    const int64_t s0 = run * blockIdx.x, s1 = min(s0 + run, a.slots);
+    const bool all = (int)blockIdx.x < a.checks;  // cell after cell instead of a run of the slots
+    if (all) {
+        const int lo = blockIdx.x * CHECK, hi = min(lo + CHECK, a.s.cells);
+        bool bad = false;
+        for (int c = lo + tid; c < hi; c += L::THREADS) {
+            int64_t o0, base;
+            int n;
+            compact_cell(a, c, o0, base, n);
+            a.s.counts[c] = n;
+            bad |= !offsets_ok(a, c);
+        }
+        if (!__syncthreads_or(bad)) return;
+        for (int c = 0; c < lo; c += L::THREADS)  // (lo is a multiple of THREADS)
+            if (__syncthreads_or(!offsets_ok(a, c + tid))) return;
+    }
+    const int64_t run = (a.slots + a.walks - 1) / a.walks;
+    const int64_t s0 = all ? 0 : run * (blockIdx.x - a.checks), s1 = all ? INT64_MAX : min(s0 + run, a.slots);
     auto first_slot = [&](int h) { return a.offsets[h] / BR + h; };  // (h <= cells)
-    if (tid < 32) {
+    if (tid < 32 && !all) {
         int lo = 0, hi = a.s.cells;  // the last cell whose slots start at or before s0: 32 probes at a time
         do {
             const int step = (hi - lo + 31) / 32, i = lo + lane * step;
@@ -152,7 +178,7 @@ __global__ void __launch_bounds__(Lay<D, compact_threads(D)>::THREADS, compact_c
         if (lane == 0) s_cell = lo;
     }
     __syncthreads();
-    int h = s_cell - 1, n = 0, flip = 0;
+    int h = all ? -1 : s_cell - 1, n = 0, flip = 0;
     int64_t o0 = 0, base = 0, f0 = 0, f1 = s0;  // the cell's first kept position, first row, slots
     int pos[L::N];
     int64_t ahead = -1;  // the index of the positions that pos holds
@@ -165,9 +191,8 @@ __global__ void __launch_bounds__(Lay<D, compact_threads(D)>::THREADS, compact_c
         if (slot >= f1) {
             if (++h >= a.s.cells) break;
             compact_cell(a, h, o0, base, n);
-            f0 = first_slot(h);
-            f1 = first_slot(h + 1);
-            if (slot == f0 && tid == 0) a.s.counts[h] = n;
+            f0 = all ? slot : first_slot(h);
+            f1 = all ? slot + max(1, (n + BR - 1) / BR) : first_slot(h + 1);
         }
         const int64_t b = (slot - f0) * BR;
         if (b < 0 || b >= n) continue;  // (uniform)
@@ -312,14 +337,16 @@ fw_status cache8_compact(const fw_cache8 &c, const void *K, const void *V, int T
                          int64_t row_stride, const int64_t *offsets, const int32_t *kept_pos, int64_t total,
                          int32_t *status, cudaStream_t s)
 {
-    const CompactArgs a{store(c), (const uint16_t *)K, (const uint16_t *)V, T,     cell_stride, row_stride,
-                        offsets,  kept_pos,            total,               total / BR + c.cells, status};
-    if (status) FW_LAUNCH(k_cache8_status, (unsigned)((c.cells + 255) / 256), 256, 0, s, a);
     int sms = 0;
     const fw_status st = device_sms(&sms);
     if (st != FW_OK) return st;
-    const unsigned grid = (unsigned)std::min<int64_t>(a.slots, (int64_t)sms * compact_ctas(c.d));
-    FW_CACHE8_DISPATCH(c, FW_LAUNCH((k_cache8_compact<D, FMT>), grid, compact_threads(D), 0, s, a));
+    const int64_t slots = total / BR + c.cells, wave = (int64_t)sms * compact_ctas(c.d);
+    const int checks = (c.cells + CHECK - 1) / CHECK;
+    const int walks = (int)std::min(slots, std::max(wave - checks, wave / 2));  // (one wave, the checks with it)
+    const CompactArgs a{store(c), (const uint16_t *)K, (const uint16_t *)V, T, cell_stride, row_stride, offsets,
+                        kept_pos, total, slots, checks, walks, status};
+    if (status) FW_LAUNCH(k_cache8_status, (unsigned)((c.cells + 255) / 256), 256, 0, s, a);
+    FW_CACHE8_DISPATCH(c, FW_LAUNCH((k_cache8_compact<D, FMT>), (unsigned)(checks + walks), compact_threads(D), 0, s, a));
     return FW_OK;
 }
 

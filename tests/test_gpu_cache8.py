@@ -452,3 +452,57 @@ def test_attend_cells_between_few_and_many(fw, fmt, d, seqs, kv_heads, g, m):
         out = fw.cache8_attend(cache, q, kv_heads=kv_heads)
         torch.cuda.synchronize()
         check_attend(cache, q, out, kv_heads, float(torch.tensor(1 / math.sqrt(d), dtype=torch.float32)))
+
+
+@pytest.mark.parametrize("d,fmt", [(64, "int8"), (128, "e4m3")])
+@pytest.mark.parametrize("offsets,total", [
+    ([0, 100, 50, 150], 150), ([0, 500, 100, 600], 600), ([0, 40, 400, 80, 120], 400), ([0, 150, 0, 150, 0, 150], 150),
+    ([0, 40, 80, 120, 160], 60), ([-5, 40, 80], 80), ([0, 40, -2 ** 62, 80, 2 ** 62, 80], 80), ([70, 33, 33, 0], 70)])
+def test_compact_offsets_out_of_order_concern_their_cells_only(fw, offsets, total, d, fmt):
+    """Cells whose offsets descend or leave the positions are refused, with a count of 0; all others get their rows, in a
+    store that held others before."""
+    gen = torch.Generator("cuda").manual_seed(total)
+    cells, T = len(offsets) - 1, 600
+    K, V = rand(gen, cells, T, d), rand(gen, cells, T, d)
+    pos = torch.randint(0, T, (total,), generator=gen, device="cuda", dtype=torch.int32)
+    o = torch.tensor(offsets, dtype=torch.int64, device="cuda")
+    ok = [0 <= a <= b <= total for a, b in zip(offsets, offsets[1:])]
+    for status in (torch.full((cells,), -1, dtype=torch.int32, device="cuda"), None):
+        cache = fw.cache8_empty(off([600] * cells), 600 * cells, d, fmt=fmt)
+        cache.counts.fill_(77)
+        cache.k.view(torch.int8).fill_(17)
+        fw.cache8_compact(cache, K, V, o, pos, status=status)
+        torch.cuda.synchronize()
+        if status is not None:
+            assert status.tolist() == [0 if x else fw.FW_ERR_INVALID_ARG for x in ok]
+        for h in range(cells):
+            if ok[h]:
+                p = pos[offsets[h]:offsets[h + 1]].long()
+                check_cell(cache, h, 0, K[h, p])
+                check_cell(cache, h, 1, V[h, p])
+            else:
+                assert int(cache.counts[h]) == 0
+            b, n = int(cache.base[h]), int(cache.counts[h])
+            assert bool((cache.k.view(torch.int8)[b + n:b + 600] == 17).all())
+
+
+@pytest.mark.parametrize("bad", [[3], [1400], [5, 700, 1999], [511, 512, 1024]])
+def test_compact_offsets_out_of_order_among_many_cells(fw, bad):
+    cells, T, d = 2000, 70, 64
+    gen = torch.Generator("cuda").manual_seed(bad[0])
+    counts = torch.randint(0, 71, (cells,), generator=torch.Generator().manual_seed(bad[0])).tolist()
+    K = rand(gen, cells, T, d)
+    pos, o = picks(gen, counts, T), off(counts)
+    cache = fw.cache8_empty(off([T] * cells), T * cells, d)
+    cache.counts.fill_(9)
+    for b in bad:  # (an offset that both of its cells cannot take)
+        o[b] = pos.numel() + 1 + b
+    st = torch.empty(cells, dtype=torch.int32, device="cuda")
+    fw.cache8_compact(cache, K, K, o, pos, status=st)
+    torch.cuda.synchronize()
+    refused = sorted({c for b in bad for c in (b - 1, b)})
+    assert torch.nonzero(st).flatten().tolist() == refused
+    want = [0 if h in refused else c for h, c in enumerate(counts)]
+    assert cache.counts.tolist() == want
+    for h in [h for h in range(0, cells, 61) if want[h]] + [h for b in bad for h in (b - 3, b - 2, b + 1, b + 2) if h < cells and want[h]]:
+        check_cell(cache, h, 0, K[h, pos[int(o[h]):int(o[h + 1])].long()])
