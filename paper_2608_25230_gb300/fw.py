@@ -486,10 +486,23 @@ def _need(ok, what):
 # the raw handle of a device's current stream, without the Stream object that torch.cuda.current_stream makes (2 us)
 _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _raw_stream(stream, tensor):
-    return stream.cuda_stream if stream is not None else _current_raw(tensor.get_device())
+def _on_current(dev):
+    # the library launches on the current GPU, and a default stream's handle is 0 on every GPU
+    if dev != _current_device():
+        raise ValueError(f"the tensors are on GPU {dev}, which is not the current one")
+
+
+def _raw_stream(stream, dev):
+    """The handle of the stream that a call on GPU `dev` runs on."""
+    if stream is None and dev == _current_device():
+        return _current_raw(dev)
+    _on_current(dev)
+    if stream.device.index != dev:
+        raise ValueError("the stream is one of the tensors' GPU")
+    return stream.cuda_stream
 
 
 def _one_device(*tensors):
@@ -552,6 +565,7 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     dev = q.get_device()
     if dev < 0 or k.get_device() != dev or v.get_device() != dev or cu_q.get_device() != dev or cu_k.get_device() != dev:
         raise ValueError("the tensors of a call are on one GPU")
+    handle = _raw_stream(stream, dev)
     # (strides of axes of one entry, which torch leaves open)
     if hq == 1:
         qh = d
@@ -565,7 +579,7 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     o, lse, status, out = _attention_out(out, q, seqs, stream)
     p = FwPrompt(seqs, hq, hk, d, rows, keys, q.data_ptr(), k.data_ptr(), v.data_ptr(), qr, qh, kr, kh, vr, vh,
                  cu_q.data_ptr(), cu_k.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale)
-    st = _lib.fw_prompt_attention(C.byref(p), o, lse, status, _raw_stream(stream, q))
+    st = _lib.fw_prompt_attention(C.byref(p), o, lse, status, handle)
     if st != FW_OK:
         raise FwError(st, "fw_prompt_attention")
     return out
@@ -659,7 +673,8 @@ def cache8_compact(cache: Cache8, K: torch.Tensor, V: torch.Tensor, offsets: tor
     if not K.get_device() == V.get_device() == offsets.get_device() == kept_pos.get_device() == cache.index:
         raise ValueError("the tensors of a call are on the store's GPU")
     st = _lib.fw_cache8_compact(cache._ref, K.data_ptr(), V.data_ptr(), T, cs, rs, offsets.data_ptr(),
-                                kept_pos.data_ptr(), kept_pos.numel(), _status_ptr(status, cells), _raw_stream(stream, K))
+                                kept_pos.data_ptr(), kept_pos.numel(), _status_ptr(status, cells),
+                                _raw_stream(stream, cache.index))
     if st != FW_OK:
         raise FwError(st, "fw_cache8_compact")
 
@@ -673,7 +688,7 @@ def cache8_append(cache: Cache8, new_K: torch.Tensor, new_V: torch.Tensor, *, st
     if not new_K.get_device() == new_V.get_device() == cache.index:
         raise ValueError("the tensors of a call are on the store's GPU")
     st = _lib.fw_cache8_append(cache._ref, new_K.data_ptr(), new_V.data_ptr(), m, _status_ptr(status, cells),
-                               _raw_stream(stream, new_K))
+                               _raw_stream(stream, cache.index))
     if st != FW_OK:
         raise FwError(st, "fw_cache8_append")
 
@@ -693,6 +708,7 @@ def _cache8_query(cache, q, kv_heads, scale):
 def cache8_attend_workspace(cache: Cache8, q: torch.Tensor, *, kv_heads: int) -> torch.Tensor:
     """A workspace for cache8_attend calls with queries of q's shape (fw_cache8_attend_workspace)."""
     c_q = _cache8_query(cache, q, kv_heads, None)
+    _on_current(cache.index)
     return _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
 
 
@@ -705,12 +721,12 @@ def cache8_attend(cache: Cache8, q: torch.Tensor, *, kv_heads: int, scale: float
     c_q = _cache8_query(cache, q, kv_heads, scale)
     if q.get_device() != cache.index:
         raise ValueError("q is on the store's GPU")
+    handle = _raw_stream(stream, cache.index)
     o, lse, status, out = _attention_out(out, q, cache.cells, stream)
     if workspace is None:
         workspace = _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
         _own_buffers(stream, workspace)
-    st = _lib.fw_cache8_attend(cache._ref, C.byref(c_q), o, lse, status, workspace.data_ptr(), workspace.numel(),
-                               _raw_stream(stream, q))
+    st = _lib.fw_cache8_attend(cache._ref, C.byref(c_q), o, lse, status, workspace.data_ptr(), workspace.numel(), handle)
     if st != FW_OK:
         raise FwError(st, "fw_cache8_attend")
     return out

@@ -68,3 +68,79 @@ def test_calls_on_a_store_refuse(fw):
                  (bf(1, 1, 4, 64), 0), (bf(1, 1, 64, 4).transpose(2, 3), 2), (bf(1, 1, 4, 64), 2)]:
         with pytest.raises(ValueError):
             fw.cache8_attend(c, q, kv_heads=h)
+
+
+class On(torch.Tensor):
+    """A tensor that says it is on the GPU of its `index`."""
+    index = 0
+
+    def get_device(self):
+        return type(self).index
+
+
+class OnSecond(On):
+    index = 1
+
+
+class StandInLibrary:
+    """Takes the calls that the binding lets through."""
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+class StandInStream:
+    def __init__(self, index, handle):
+        self.device, self.cuda_stream = torch.device("cuda", index), handle
+
+
+def serving_calls(fw, kind, stream=None):
+    """The four calls and the workspace's on tensors of `kind`, ready to be made."""
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(kind)
+
+    class Stand:
+        cells, d, device, index, _ref = 2, 64, torch.device("cpu"), kind.index, None
+
+    i32, K, q = torch.int32, t(2, 9, 64), t(1, 1, 4, 64)
+    outs = dict(o=t(1, 1, 4, 64), lse=t(1, 1, 4, dtype=torch.float32), status=t(2, dtype=i32))
+    return {
+        "fw_prompt_attention": lambda: fw.prompt_attention(t(5, 8, 64), t(5, 2, 64), t(5, 2, 64), t(2, dtype=i32), stream=stream,
+                                                           out=dict(o=t(5, 8, 64))),
+        "fw_cache8_compact": lambda: fw.cache8_compact(Stand(), K, K, t(3, dtype=torch.int64), t(2, dtype=i32), stream=stream),
+        "fw_cache8_append": lambda: fw.cache8_append(Stand(), K, K, stream=stream),
+        "fw_cache8_attend": lambda: fw.cache8_attend(Stand(), q, kv_heads=2, out=outs, workspace=t(256, dtype=torch.uint8),
+                                                     stream=stream),
+        "fw_cache8_attend_workspace": lambda: fw.cache8_attend_workspace(Stand(), q, kv_heads=2),
+    }
+
+
+def test_calls_off_the_current_gpu_are_refused(fw, monkeypatch):
+    """The library launches on the current GPU: tensors or a stream of another one do not get that far."""
+    lib = StandInLibrary()
+    monkeypatch.setattr(fw, "_lib", lib)
+    monkeypatch.setattr(fw, "_current_raw", lambda index: 70 + index)
+    monkeypatch.setattr(fw, "_current_device", lambda: 0, raising=False)
+    for name, call in serving_calls(fw, OnSecond).items():
+        with pytest.raises(ValueError, match="current"):
+            call()
+    for name, call in serving_calls(fw, On, StandInStream(1, 5)).items():
+        if name != "fw_cache8_attend_workspace":
+            with pytest.raises(ValueError, match="stream"):
+                call()
+    assert not lib.calls
+    # on the current GPU, with its current stream or one that is given
+    for kind, index in ((On, 0), (OnSecond, 1)):
+        monkeypatch.setattr(fw, "_current_device", lambda: index)
+        for stream, handle in ((None, 70 + index), (StandInStream(index, 5), 5)):
+            for name, call in serving_calls(fw, kind, stream).items():
+                lib.calls.clear()
+                call()
+                assert [c[0] for c in lib.calls] == [name]
+                if name != "fw_cache8_attend_workspace":
+                    assert lib.calls[0][1][-1] == handle
