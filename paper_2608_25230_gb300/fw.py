@@ -644,11 +644,12 @@ def cache8_empty(offsets: torch.Tensor, total: int, d: int, *, fmt: str = "e4m3"
                   counts=torch.zeros(cells, dtype=torch.int32, device=dev))
 
 
-def _status_ptr(status, cells):
+def _status_ptr(status, cache):
     if status is None:
         return None
-    if status.dtype is not torch.int32 or status.numel() < cells or not status.is_contiguous() or not status.is_cuda:
-        raise ValueError("status is contiguous int32 [cells] on the GPU")
+    if status.dtype is not torch.int32 or status.numel() < cache.cells or not status.is_contiguous() or (
+            status.get_device() != cache.index):
+        raise ValueError("status is contiguous int32 [cells] on the store's GPU")
     return status.data_ptr()
 
 
@@ -673,7 +674,7 @@ def cache8_compact(cache: Cache8, K: torch.Tensor, V: torch.Tensor, offsets: tor
     if not K.get_device() == V.get_device() == offsets.get_device() == kept_pos.get_device() == cache.index:
         raise ValueError("the tensors of a call are on the store's GPU")
     st = _lib.fw_cache8_compact(cache._ref, K.data_ptr(), V.data_ptr(), T, cs, rs, offsets.data_ptr(),
-                                kept_pos.data_ptr(), kept_pos.numel(), _status_ptr(status, cells),
+                                kept_pos.data_ptr(), kept_pos.numel(), _status_ptr(status, cache),
                                 _raw_stream(stream, cache.index))
     if st != FW_OK:
         raise FwError(st, "fw_cache8_compact")
@@ -687,7 +688,7 @@ def cache8_append(cache: Cache8, new_K: torch.Tensor, new_V: torch.Tensor, *, st
         raise ValueError("new_K and new_V are contiguous bfloat16 [cells][m][d], as the store's")
     if not new_K.get_device() == new_V.get_device() == cache.index:
         raise ValueError("the tensors of a call are on the store's GPU")
-    st = _lib.fw_cache8_append(cache._ref, new_K.data_ptr(), new_V.data_ptr(), m, _status_ptr(status, cells),
+    st = _lib.fw_cache8_append(cache._ref, new_K.data_ptr(), new_V.data_ptr(), m, _status_ptr(status, cache),
                                _raw_stream(stream, cache.index))
     if st != FW_OK:
         raise FwError(st, "fw_cache8_append")
@@ -726,6 +727,8 @@ def cache8_attend(cache: Cache8, q: torch.Tensor, *, kv_heads: int, scale: float
     if workspace is None:
         workspace = _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
         _own_buffers(stream, workspace)
+    elif workspace.get_device() != cache.index or not workspace.is_contiguous():
+        raise ValueError("workspace is contiguous on the store's GPU")
     st = _lib.fw_cache8_attend(cache._ref, C.byref(c_q), o, lse, status, workspace.data_ptr(), workspace.numel(), handle)
     if st != FW_OK:
         raise FwError(st, "fw_cache8_attend")

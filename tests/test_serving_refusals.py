@@ -144,3 +144,35 @@ def test_calls_off_the_current_gpu_are_refused(fw, monkeypatch):
                 assert [c[0] for c in lib.calls] == [name]
                 if name != "fw_cache8_attend_workspace":
                     assert lib.calls[0][1][-1] == handle
+
+
+def test_status_and_workspace_elsewhere_are_refused(fw, monkeypatch):
+    """A status or a workspace that the GPU of the store does not hold, or not in one piece, does not reach the library."""
+    lib = StandInLibrary()
+    monkeypatch.setattr(fw, "_lib", lib)
+    monkeypatch.setattr(fw, "_current_raw", lambda index: 0)
+    monkeypatch.setattr(fw, "_current_device", lambda: 0)
+
+    class Stand:
+        cells, d, device, index, _ref = 2, 64, torch.device("cpu"), 0, None
+
+    def t(*shape, dtype=torch.bfloat16, kind=On):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(kind)
+
+    i32, u8, K, q = torch.int32, torch.uint8, t(2, 9, 64), t(1, 1, 4, 64)
+    off, pos = t(3, dtype=torch.int64), t(2, dtype=i32)
+    outs = dict(o=t(1, 1, 4, 64))
+    for kind in (OnSecond, torch.Tensor):
+        st, ws = t(2, dtype=i32, kind=kind), t(256, dtype=u8, kind=kind)
+        with pytest.raises(ValueError):
+            fw.cache8_compact(Stand(), K, K, off, pos, status=st)
+        with pytest.raises(ValueError):
+            fw.cache8_append(Stand(), K, K, status=st)
+        with pytest.raises(ValueError):
+            fw.cache8_attend(Stand(), q, kv_heads=2, out=outs, workspace=ws)
+    with pytest.raises(ValueError):
+        fw.cache8_attend(Stand(), q, kv_heads=2, out=outs, workspace=t(1, dtype=u8).expand(256))
+    assert not lib.calls
+    fw.cache8_append(Stand(), K, K, status=t(2, dtype=i32))
+    fw.cache8_attend(Stand(), q, kv_heads=2, out=outs, workspace=t(256, dtype=u8))
+    assert [c[0] for c in lib.calls] == ["fw_cache8_append", "fw_cache8_attend"]
