@@ -7,6 +7,7 @@ is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import math
 import os
@@ -512,20 +513,22 @@ def _one_device(*tensors):
             raise ValueError("the tensors of a call are on one GPU")
 
 
-def _own_buffers(stream, *tensors):
-    # buffers made here on the current stream and used on another: not reused before that stream is done
-    if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+def _made_on(stream):
+    # buffers for a call on another stream come from that stream's memory: what the current stream has
+    # freed, work still under way there may be using
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
 def _attention_out(out, q, items, stream):
     """(o, lse, status, the dict) of a call's outputs: those of `out`, checked, or new ones."""
     if out is None:
-        out = dict(o=torch.empty(q.shape, dtype=torch.bfloat16, device=q.device),
-                   lse=torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device),
-                   status=torch.empty(items, dtype=torch.int32, device=q.device))
-        _own_buffers(stream, *out.values())
+        with _made_on(stream):
+            out = dict(o=torch.empty(q.shape, dtype=torch.bfloat16, device=q.device),
+                       lse=torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device),
+                       status=torch.empty(items, dtype=torch.int32, device=q.device))
+        if stream is not None:  # the caller reads them on the current one
+            for t in out.values():
+                t.record_stream(torch.cuda.current_stream(q.device))
         return out["o"].data_ptr(), out["lse"].data_ptr(), out["status"].data_ptr(), out
     o, lse, status = out["o"], out.get("lse"), out.get("status")
     if o.shape != q.shape or o.dtype is not torch.bfloat16 or not o.is_contiguous():
@@ -725,8 +728,8 @@ def cache8_attend(cache: Cache8, q: torch.Tensor, *, kv_heads: int, scale: float
     handle = _raw_stream(stream, cache.index)
     o, lse, status, out = _attention_out(out, q, cache.cells, stream)
     if workspace is None:
-        workspace = _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
-        _own_buffers(stream, workspace)
+        with _made_on(stream):
+            workspace = _ws(_lib.fw_cache8_attend_workspace(cache._ref, C.byref(c_q)), cache.device)
     elif workspace.get_device() != cache.index or not workspace.is_contiguous():
         raise ValueError("workspace is contiguous on the store's GPU")
     st = _lib.fw_cache8_attend(cache._ref, C.byref(c_q), o, lse, status, workspace.data_ptr(), workspace.numel(), handle)

@@ -60,3 +60,29 @@ def test_nothing_evicted_is_the_whole_cache_in_8_bits(example, fmt):
                 extra = 2.0 ** -24 * scale * float(q64[0].abs().sum(1).max()) * q.abs().amax(1)
                 check_rows(r["decoded"][i][2 * h:2 * h + 2], None, want, 2.0 ** -11, extra)
             i += 1
+
+
+def test_buffers_of_a_call_on_another_stream():
+    """The outputs and the workspace that a call makes come from the memory of the stream that it runs on."""
+    from paper_2608_25230_gb300 import fw
+
+    def stream_of(ptr):
+        for seg in torch.cuda.memory_snapshot():
+            if seg["address"] <= ptr < seg["address"] + seg["total_size"]:
+                return seg["stream"]
+
+    side = torch.cuda.Stream()
+    q = torch.randn(40, 4, 64, device="cuda").to(torch.bfloat16)
+    bounds = torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+    want = fw.prompt_attention(q, q[:, :2], q[:, :2], bounds)
+    cache = fw.cache8_empty(torch.arange(121, device="cuda") * 20, 2400, 64)
+    qd = torch.randn(60, 1, 2, 64, device="cuda").to(torch.bfloat16)
+    torch.cuda.synchronize()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = [fw.prompt_attention(q, q[:, :2], q[:, :2], bounds, stream=side), fw.cache8_attend(cache, qd, kv_heads=2, stream=side)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(outs[0]["o"], want["o"]) and torch.equal(outs[0]["lse"], want["lse"])
+    for out in outs:
+        for x in out.values():
+            assert stream_of(x.data_ptr()) == side.cuda_stream
+    torch.cuda.synchronize()

@@ -176,3 +176,46 @@ def test_status_and_workspace_elsewhere_are_refused(fw, monkeypatch):
     fw.cache8_append(Stand(), K, K, status=t(2, dtype=i32))
     fw.cache8_attend(Stand(), q, kv_heads=2, out=outs, workspace=t(256, dtype=u8))
     assert [c[0] for c in lib.calls] == ["fw_cache8_append", "fw_cache8_attend"]
+
+
+def test_buffers_made_for_another_stream_come_from_its_memory(fw, monkeypatch):
+    """What a call with stream= makes for itself is allocated on that stream: a block that the current stream has freed may
+    still be in use there.  Outputs, which the caller reads, are recorded on the current stream."""
+    import contextlib
+
+    lib, side, made, recorded, inside = StandInLibrary(), StandInStream(0, 5), [], [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        inside.append(stream)
+        yield
+        inside.pop()
+
+    empty = torch.empty
+
+    def noted(*args, **kw):
+        made.append(inside[-1] if inside else None)
+        return empty(*args, **kw)
+
+    monkeypatch.setattr(fw, "_lib", lib)
+    monkeypatch.setattr(fw, "_current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: "current")
+    monkeypatch.setattr(torch, "empty", noted)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: recorded.append(s))
+
+    class Stand:
+        cells, d, device, index, _ref = 2, 64, torch.device("cpu"), 0, None
+
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(On)
+
+    fw.prompt_attention(t(5, 8, 64), t(5, 2, 64), t(5, 2, 64), t(2, dtype=torch.int32), stream=side)
+    assert made == [side] * 3 and recorded == ["current"] * 3
+    made.clear(), recorded.clear()
+    fw.cache8_attend(Stand(), t(1, 1, 4, 64), kv_heads=2, stream=side)
+    assert made == [side] * 4 and recorded == ["current"] * 3  # (the workspace is used on that stream only)
+    made.clear(), recorded.clear()
+    monkeypatch.setattr(fw, "_current_raw", lambda index: 0)
+    fw.cache8_attend(Stand(), t(1, 1, 4, 64), kv_heads=2)
+    assert made == [None] * 4 and not recorded and not inside
