@@ -490,13 +490,8 @@ fw_status fw_prompt_attention(const fw_prompt *p, void *o, float *lse, int32_t *
 {
     const fw_status st = check_prompt(p);
     if (st != FW_OK) return st;
-    cudaStream_t s = (cudaStream_t)stream;
-    if (p->total_q == 0) {
-        if (status) FW_CUDA_CHECK(cudaMemsetAsync(status, 0, (size_t)p->num_seqs * 4, s));
-        return FW_OK;
-    }
-    if (!o || !aligned(o, 16)) return FW_ERR_INVALID_ARG;
-    return prompt_attention(*p, o, lse, status, s);
+    if (p->total_q > 0 && (!o || !aligned(o, 16))) return FW_ERR_INVALID_ARG;
+    return prompt_attention(*p, o, lse, status, (cudaStream_t)stream);
 }
 
 fw_status fw_cache8_compact(const fw_cache8 *c, const void *K, const void *V, int32_t T, int64_t cell_stride,

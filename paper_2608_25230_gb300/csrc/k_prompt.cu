@@ -217,6 +217,13 @@ __device__ __forceinline__ bool seq_ok(const PromptArgs &a, int s)
     return q0 >= 0 && q1 >= q0 && q1 <= a.total_q && k0 >= 0 && k1 >= k0 && k1 <= a.total_k;
 }
 
+// The sequences' statuses where there are no query rows, and so nothing else to do.
+__global__ void __launch_bounds__(256) k_prompt_status(const PromptArgs a)
+{
+    const int s = blockIdx.x * 256 + threadIdx.x;
+    if (s < a.num_seqs) a.status[s] = seq_ok(a, s) ? FW_OK : FW_ERR_INVALID_ARG;
+}
+
 template <int D, int TILES>
 __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
     k_prompt(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -714,6 +721,12 @@ fw_status launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap
 
 fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *status, cudaStream_t s)
 {
+    if (p.total_q == 0) {
+        PromptArgs a{};
+        a.cu_q = p.cu_q, a.cu_k = p.cu_k, a.total_k = p.total_k, a.num_seqs = p.num_seqs, a.status = status;
+        if (status) FW_LAUNCH(k_prompt_status, ((unsigned)p.num_seqs + 255u) / 256u, 256, 0, s, a);
+        return FW_OK;
+    }
     const int group = p.q_heads / p.kv_heads, TT = 128 / group;
     int sms = 0;
     const fw_status st = device_sms(&sms);

@@ -230,3 +230,16 @@ def test_prompt_unseen_values_with_keys_split(fw, d):
         assert not bool(torch.isfinite(o[first:, :2, 5]).any())
         rest = [c for c in range(d) if c != 5]
         assert torch.equal(o[first:, :2][..., rest], co[first:, :2][..., rest])
+
+
+@pytest.mark.parametrize("cu_q,cu_k", [([0, 0, 0], [0, 5, 9]), ([0, 1, 0], [0, 5, 9]), ([0, 0, 0], [0, 9, 5]), ([0, 0, 0], [0, 5, 10]),
+                                       ([-1, 0, 0], [0, 5, 9]), ([0, 0, 0], [-2, 5, 9])])
+def test_prompt_bounds_are_reported_without_any_rows_too(fw, cu_q, cu_k):
+    """No query rows at all: the sequences' bounds are looked at all the same."""
+    q = torch.ones(0, 4, 64, dtype=torch.bfloat16, device="cuda")
+    kv = torch.ones(9, 2, 64, dtype=torch.bfloat16, device="cuda")
+    a, b = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (cu_q, cu_k))
+    out = fw.prompt_attention(q, kv, kv, a, b)
+    torch.cuda.synchronize()
+    bad = [not (0 <= a0 <= a1 <= 0 and 0 <= b0 <= b1 <= 9) for a0, a1, b0, b1 in zip(cu_q, cu_q[1:], cu_k, cu_k[1:])]
+    assert out["status"].tolist() == [fw.FW_ERR_INVALID_ARG if x else 0 for x in bad]
