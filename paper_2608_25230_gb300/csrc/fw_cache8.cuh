@@ -53,7 +53,7 @@ template <int FMT> __device__ __forceinline__ int scale_exponent(uint32_t a)
     return max(-120, (int)(a >> 7) - 127 - up + ((a & 0x7f) > mant ? 1 : 0));
 }
 
-// bf16 bits of the largest code times 2^e, M 2^e (-120 <= e <= 119)
+// bf16 bits of the largest code times 2^e, M 2^e (-120 <= e <= 119, or 121 for int8)
 template <int FMT> __device__ __forceinline__ uint32_t top_code_bits(int e)
 {
     return FMT == FW_CACHE8_E4M3 ? (uint32_t)(e + 8 + 127) << 7 | 0x60u : (uint32_t)(e + 6 + 127) << 7 | 0x7eu;
@@ -68,15 +68,16 @@ __device__ __forceinline__ uint32_t piece_top(const uint4 &x, uint32_t top)
 }
 __device__ __forceinline__ uint32_t top_of(uint32_t pair) { return max(pair & 0xffffu, pair >> 16); }
 
-// 8 values with their NaN put to 0 and their infinities to the largest magnitude `lim` (bf16 bits).
-__device__ __forceinline__ uint4 finite_piece(const uint4 &x, uint32_t lim)
+// 8 values times 2^-down, with their NaN put to 0 and their infinities to the magnitude `lim` (bf16 bits).  What falls below
+// bf16's range may come out as anything below 2^-126.
+__device__ __forceinline__ uint4 finite_piece(const uint4 &x, uint32_t lim, int down)
 {
     uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int sh = 16 * (i & 1);
         const uint32_t b = (w[i >> 1] >> sh) & 0xffffu, mag = b & 0x7fffu;
-        const uint32_t y = mag > 0x7f80u ? 0u : mag == 0x7f80u ? (b & 0x8000u) | lim : b;
+        const uint32_t y = mag > 0x7f80u ? 0u : (b & 0x8000u) | (mag == 0x7f80u ? lim : (uint32_t)max((int)mag - (down << 7), 0));
         w[i >> 1] = (w[i >> 1] & ~(0xffffu << sh)) | y << sh;
     }
     return make_uint4(w[0], w[1], w[2], w[3]);

@@ -44,6 +44,7 @@ __device__ __forceinline__ bool quantise_block(const Store &s, int64_t row, int 
     using L = Lay<D, T>;
     const int tid = threadIdx.x, col = tid % L::LPR, r0 = tid / L::LPR;
     uint32_t top[2];
+    int down[2] = {0, 0};  // octaves by which x was brought down
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
         uint32_t t = 0;
@@ -65,7 +66,7 @@ __device__ __forceinline__ bool quantise_block(const Store &s, int64_t row, int 
         for (int kv = 0; kv < 2; ++kv) {
             uint32_t t = 0;
 #pragma unroll
-            for (int i = 0; i < L::N; ++i) t = piece_top(finite_piece(x[kv][i], 0u), t);
+            for (int i = 0; i < L::N; ++i) t = piece_top(finite_piece(x[kv][i], 0u, 0), t);
             t = __reduce_max_sync(FW_FULL, top_of(t));
             __syncthreads();
             if ((tid & 31) == 0) s_max[kv][tid >> 5] = t;
@@ -73,15 +74,18 @@ __device__ __forceinline__ bool quantise_block(const Store &s, int64_t row, int 
             top[kv] = 0;
 #pragma unroll
             for (int w = 0; w < L::WARPS; ++w) top[kv] = max(top[kv], s_max[kv][w]);
+            // (the largest code times the largest scales is no number: such a block is encoded some octaves lower)
+            const int e = scale_exponent<FMT>(top[kv]);
+            down[kv] = e > 100 ? 100 : 0;
 #pragma unroll
-            for (int i = 0; i < L::N; ++i) x[kv][i] = finite_piece(x[kv][i], top_code_bits<FMT>(scale_exponent<FMT>(top[kv])));
+            for (int i = 0; i < L::N; ++i) x[kv][i] = finite_piece(x[kv][i], top_code_bits<FMT>(e - down[kv]), down[kv]);
         }
     }
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
         const int e = scale_exponent<FMT>(top[kv]);
         if (tid == 0) s.scale(kv)[row / BR] = pow2f(e);
-        const float inv = pow2f(-e);
+        const float inv = pow2f(down[kv] - e);
         uint8_t *codes = s.codes(kv) + row * D;
 #pragma unroll
         for (int i = 0; i < L::N; ++i)

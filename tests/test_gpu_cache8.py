@@ -506,3 +506,28 @@ def test_compact_offsets_out_of_order_among_many_cells(fw, bad):
     assert cache.counts.tolist() == want
     for h in [h for h in range(0, cells, 61) if want[h]] + [h for b in bad for h in (b - 3, b - 2, b + 1, b + 2) if h < cells and want[h]]:
         check_cell(cache, h, 0, K[h, pos[int(o[h]):int(o[h + 1])].long()])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("top", [1.0, 2.0 ** 100, 2.9e38, 3.0e38, 3.3895313892515355e38])
+def test_infinities_beside_the_largest_values(fw, fmt, top):
+    """Infinities become the largest code of their sign and NaN 0 whatever the block's scale is, in the compaction and in an
+    append."""
+    gen = torch.Generator("cuda").manual_seed(17)
+    d, n = 64, 40
+    K = ((torch.rand(1, n, d, generator=gen, device="cuda") * 2 - 1) * top).to(torch.bfloat16)
+    K[0, 0, 0] = K[0, 35, 1] = top
+    K[0, 3, 5], K[0, 31, 63], K[0, 7, 7], K[0, 36, 8], K[0, 39, 9] = (float(x) for x in ("inf", "-inf", "nan", "-inf", "nan"))
+    caches = [fw.cache8_empty(off([n]), n, d, fmt=fmt) for _ in range(2)]
+    st = torch.empty(2, dtype=torch.int32, device="cuda")
+    fw.cache8_compact(caches[0], K, K, off([n]), torch.arange(n, dtype=torch.int32, device="cuda"), status=st[:1])
+    fw.cache8_append(caches[1], K[:, :32].contiguous(), K[:, :32].contiguous())
+    fw.cache8_append(caches[1], K[:, 32:].contiguous(), K[:, 32:].contiguous(), status=st[1:])
+    torch.cuda.synchronize()
+    assert st.tolist() == [fw.FW_ERR_NONFINITE] * 2
+    for b in (0, 32):
+        val, sc = quantise64(K[0, b:b + 32], fmt)
+        for c in caches:
+            at = int(c.base[0]) + b
+            for codes, scales in ((c.k, c.k_scale), (c.v, c.v_scale)):
+                assert float(scales[at // 32]) == sc and torch.equal(codes[at:at + val.shape[0]].double(), val)
