@@ -416,8 +416,8 @@ fw_status fw_prompt_attention(const fw_prompt *p, void *o, float *lse, int32_t *
  * is at most 448 * 2^e (e4m3) or 127 * 2^e (int8); a code is the value times
  * 2^-e rounded to nearest, ties to even.  (A power of two: the product is exact,
  * so a code does not depend on how it is computed, e4m3 loses nothing by it, and
- * every stored value is a bf16 number; but for codes times the scales from 2^119
- * (e4m3) or 2^121 (int8) on that reach 2^128, which read as infinite.)  The bf16 rows of a cell's open block stay
+ * every stored value is a bf16 number; but a code of a block with the scale 2^120
+ * (e4m3) or 2^122 (int8) may stand for 2^128 or more, which reads as infinite.)  The bf16 rows of a cell's open block stay
  * in a ring of FW_CACHE8_TAIL rows (row r in slot r % FW_CACHE8_TAIL), so each
  * block is quantised from the originals, however its rows came in, and counts[h]
  * may be set back by up to FW_CACHE8_BLOCK appended rows (a draft that was not
