@@ -58,10 +58,11 @@ struct PromptArgs {
 };
 
 template <int D, int TILES> struct PCfg {
+    static_assert(D == 128 || TILES == 1, "two tiles a CTA: d = 128 only");
     static constexpr int NB = D / 64;              // 128-byte boxes across d
     static constexpr int QT = 128 * D * 2;         // bytes of a tile of queries
     static constexpr int KT = PK * D * 2;          // bytes of a tile of keys or values
-    static constexpr int STAGES = D == 64 && TILES == 2 ? 8 : 5;
+    static constexpr int STAGES = 5;
     static constexpr size_t SMEM = 1024 + TILES * QT + (size_t)STAGES * KT;
     // Parts of a block of scores: with two, the next part's product runs under the softmax of this one (d = 128,
     // 16,384 tokens x 32 heads: 1.46 ms in one part, 1.37 in two).
@@ -72,7 +73,7 @@ template <int D, int TILES> struct PCfg {
     // the softmax's warps, then those of the copies, the products, the guard, and of the other tile's products
     static constexpr int W_COPY = 4 * TILES, W_MMA = W_COPY + 1, W_GUARD = W_COPY + 2, W_MMA1 = W_COPY + 3;
     static constexpr int THREADS = 32 * (W_COPY + 4);
-    static constexpr int CTAS = D == 64 && TILES == 1 ? 2 : 1;  // per SM
+    static constexpr int CTAS = D == 64 ? 2 : 1;   // per SM
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -241,7 +242,8 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
 
     // (by a shuffle, so that the compiler knows the warp's role for the same in all lanes)
     const int tid = threadIdx.x, lane = tid & 31, wid = __shfl_sync(FW_FULL, tid >> 5, 0);
-    const int part = blockIdx.x % a.parts, item = blockIdx.x / a.parts;
+    const bool split = TILES == 1 && a.parts > 1;  // (a CTA of two tiles has all their keys)
+    const int part = split ? blockIdx.x % a.parts : 0, item = split ? blockIdx.x / a.parts : blockIdx.x;
     const int slot = a.slots - 1 - item / a.kv_heads, hk = item % a.kv_heads;
     const int TT = a.TT, ST = TILES * TT;  // tokens of a tile and of a slot
 
@@ -311,11 +313,9 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
     nb[1] = TILES == 2 && tiles == 2 ? (max(0, lk - lq + min(t0 + ST, lq)) + PK - 1) / PK : 0;
     int J = max(nb[0], nb[1]), jm = seen0 / PK;  // blocks from jm on are not seen in full by every row
     int j0 = 0;                                  // this CTA's part: blocks j0 .. j0 + J, counted from j0 below
-    if (a.parts > 1) {
+    if (split) {
         j0 = J * part / a.parts;
-        const int j1 = J * (part + 1) / a.parts;
-        for (int t = 0; t < 2; ++t) nb[t] = max(0, min(nb[t], j1) - j0);
-        J = j1 - j0;
+        J = nb[0] = J * (part + 1) / a.parts - j0;
         jm = min(max(jm - j0, 0), J);
     }
     const int kb = k0 + j0 * PK;  // the part's first key row
@@ -577,11 +577,7 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
             const bool odd = *(volatile int *)&s_odd != 0;
             const int64_t row = (int64_t)(q0 + tok) * a.q_heads + hk * a.group + r % a.group;
             // (of a part: as it is, the parts' sums come later)
-            const float inv = !ok ? NAN : a.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-            if (a.parts > 1 && ok && J > 0) {  // both tiles' products are done with the memory the parts are left in
-                ok = tc::mbar_wait(&drained[t], 0, P_WAIT) && (tiles == 1 || tc::mbar_wait(&drained[t ^ 1], 0, P_WAIT));
-                if (!__all_sync(FW_FULL, ok)) ok = false;
-            }
+            const float inv = !ok ? NAN : split ? 1.f : l == 0.f ? 0.f : 1.f / l;
             // The rows go out by way of the tile's queries' memory (the products have read them), a warp's 32 rows its
             // own: whole rows a store.  (A row a lane: 32 lines an instruction, 6,200 clocks for a CTA's rows.)
             constexpr int PCS = D / 8;  // 16-byte pieces of a row
@@ -609,8 +605,8 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
                         }
                     }
                 }
-                if (a.parts > 1) {
-                    float4 *dst = reinterpret_cast<float4 *>(sKV) + (t * 128 + r) * (D / 4);
+                if (split) {  // (the products are done with the ring's memory)
+                    float4 *dst = reinterpret_cast<float4 *>(sKV) + r * (D / 4);
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         dst[(i / 4 + e) ^ (r & 7)] = make_float4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
@@ -623,25 +619,25 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
                                    pack_bf16(y[8 * e + 4], y[8 * e + 5]), pack_bf16(y[8 * e + 6], y[8 * e + 7]));
             }
             __syncwarp();
-            if (a.parts > 1) reinterpret_cast<float2 *>(sQ)[t * 128 + r] = make_float2(ref, ok ? l : NAN);
+            if (split) reinterpret_cast<float2 *>(sQ)[r] = make_float2(ref, ok ? l : NAN);
 #pragma unroll 8
-            for (int p = 0; a.parts == 1 && p < 32; p += 32 / PCS) {
+            for (int p = 0; !split && p < 32; p += 32 / PCS) {
                 const int k = p + lane / PCS, c = lane % PCS;
                 const int64_t to = __shfl_sync(FW_FULL, live ? row : -1, k);
                 if (to >= 0) reinterpret_cast<uint4 *>(a.o + to * D)[c] = stage[k * PCS + (c ^ (k & 7))];
             }
-            if (live && a.lse && a.parts == 1)
+            if (live && a.lse && !split)
                 a.lse[row] = !ok ? NAN : l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
         }
     }
     tc::fence_before_sync();
     __syncthreads();
-    if (a.parts > 1) {
+    if (split) {
         // The parts of every row joined over the cluster: a CTA takes every parts-th row, a warp a row at a time.
         cluster_sync();
-        for (int r = part + a.parts * wid; r < tiles * 128; r += a.parts * (PT / 32)) {
-            const int i = r & 127, tok = t0 + (r >> 7) * TT + i / a.group;
-            if (i >= TT * a.group || tok >= lq) continue;
+        for (int r = part + a.parts * wid; r < 128; r += a.parts * (PT / 32)) {
+            const int tok = t0 + r / a.group;
+            if (r >= TT * a.group || tok >= lq) continue;
             // (columns 4 lane .. of 32 lanes, or 2 lane ..: one piece of 16 bytes, or half of one)
             const float *src = reinterpret_cast<float *>(sKV) + r * D +
                                (D == 128 ? 4 * (lane ^ (r & 7)) : 4 * ((lane >> 1) ^ (r & 7)) + 2 * (lane & 1));
@@ -670,7 +666,7 @@ __global__ void __launch_bounds__(PCfg<D, TILES>::THREADS, PCfg<D, TILES>::CTAS)
                 for (int e = 0; e < D / 32; ++e) y[e] = fmaf(f, x[p][e], y[e]);
             }
             const float inv = L == 0.f ? 0.f : 1.f / L;
-            const int64_t row = (int64_t)(q0 + tok) * a.q_heads + hk * a.group + i % a.group;
+            const int64_t row = (int64_t)(q0 + tok) * a.q_heads + hk * a.group + r % a.group;
             uint32_t *dst = reinterpret_cast<uint32_t *>(a.o + row * D + lane * (D / 32));
 #pragma unroll
             for (int e = 0; e < D / 32; e += 2) dst[e / 2] = pack_bf16(L == 0.f ? 0.f : y[e] * inv, L == 0.f ? 0.f : y[e + 1] * inv);
@@ -739,6 +735,7 @@ fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *sta
     // joining costs several blocks' time, so only from SPLIT blocks on average on, and MIN_PART or more to a part
     // (one sequence, 8 x 4 heads, d = 128: 17 rows against 16,384 keys 130 us whole, 24 in 8 parts; 256 against 2,048
     // 28.4 whole, 26.3 in 2; d = 64, 128 against 1,024 16.2 whole, 19.1 in 2).
+    // (Of two tiles a CTA there are more than half as many CTAs as SMs, so that their keys are never split.)
     const int64_t blocks = p.total_k / ((int64_t)p.num_seqs * PK);
     int parts = 1;
     while (blocks >= SPLIT && parts < MAX_PARTS && slots * p.kv_heads * parts * 2 <= sms && blocks >= MIN_PART * parts * 2)
@@ -755,8 +752,8 @@ fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *sta
     const PromptArgs a{p.cu_q,  p.cu_k,     p.total_q, p.total_k, p.num_seqs, p.q_heads, p.kv_heads,
                        group,   (int)slots, TT, parts, (const uint16_t *)p.v, p.v_row,   p.v_head,
                        p.scale * 1.4426950408889634f, (uint16_t *)o, lse,  status};
-    if (p.d == 128) return tiles == 1 ? launch<128, 1>(mq, mk, mv, a, s) : launch<128, 2>(mq, mk, mv, a, s);
-    return tiles == 1 ? launch<64, 1>(mq, mk, mv, a, s) : launch<64, 2>(mq, mk, mv, a, s);
+    if (p.d == 64) return launch<64, 1>(mq, mk, mv, a, s);
+    return tiles == 1 ? launch<128, 1>(mq, mk, mv, a, s) : launch<128, 2>(mq, mk, mv, a, s);
 }
 
 }  // namespace fw
