@@ -243,3 +243,71 @@ def test_prompt_bounds_are_reported_without_any_rows_too(fw, cu_q, cu_k):
     torch.cuda.synchronize()
     bad = [not (0 <= a0 <= a1 <= 0 and 0 <= b0 <= b1 <= 9) for a0, a1, b0, b1 in zip(cu_q, cu_q[1:], cu_k, cu_k[1:])]
     assert out["status"].tolist() == [fw.FW_ERR_INVALID_ARG if x else 0 for x in bad]
+
+
+def fills_two_tiles(hk, g, lq):
+    """Whether the CTAs of two tiles fill more than half of the SMs (with d = 128 they are taken then)."""
+    return (sum(lq) // (2 * (128 // g)) + len(lq)) * hk * 2 > torch.cuda.get_device_properties(0).multi_processor_count
+
+
+@pytest.mark.parametrize("hk,g", [(8, 1), (8, 3), (4, 7)])
+def test_prompt_two_tiles_a_cta_rows_and_groups(fw, hk, g):
+    """Rows that see nothing in the first tile of a CTA, in both and in part of one, sequences without keys, groups that do not
+    divide a tile."""
+    lens = [(300, 120), (900, 400), (513, 0), (1200, 1200), (40, 39), (0, 7), (257, 258), (700, 900)]
+    lq, lk = [a for a, _ in lens], [b for _, b in lens]
+    assert fills_two_tiles(hk, g, lq)
+    gen = torch.Generator("cuda").manual_seed(10 * hk + g)
+    q, k, v = rand(gen, sum(lq), hk * g, 128, amp=1.5), rand(gen, sum(lk), hk, 128), rand(gen, sum(lk), hk, 128)
+    out = fw.prompt_attention(q, k, v, cu(lq), cu(lk))
+    torch.cuda.synchronize()
+    check(out, q, k, v, lens, 1 / math.sqrt(128))
+
+
+@pytest.mark.parametrize("hk,g", [(8, 1), (8, 3)])
+def test_prompt_two_tiles_a_cta_large_logits(fw, hk, g):
+    """The running maximum moves by hundreds from block to block, both ways."""
+    gen = torch.Generator("cuda").manual_seed(15)
+    T = 2700
+    assert fills_two_tiles(hk, g, [T])
+    q, k, v = rand(gen, T, hk * g, 128), rand(gen, T, hk, 128), rand(gen, T, hk, 128)
+    ramp = torch.linspace(-60, 60, T, device="cuda")[:, None, None].to(torch.bfloat16)
+    q[..., 0] = 8
+    for sgn in (1, -1):
+        kk = k.clone()
+        kk[..., :1] = sgn * ramp
+        out = fw.prompt_attention(q, kk, v, cu([T]), scale=1.0)
+        torch.cuda.synchronize()
+        check(out, q, kk, v, [(T, T)], 1.0, rows=300)
+
+
+@pytest.mark.parametrize("hk,g", [(8, 1), (8, 3)])
+def test_prompt_two_tiles_a_cta_unseen_values(fw, hk, g):
+    """Values that are not finite, at keys that some rows of a CTA do not see: up to three blocks of them with one head a
+    key head, whose CTAs hold 256 tokens."""
+    gen = torch.Generator("cuda").manual_seed(19)
+    lens = [(1300, 1300), (700, 900), (1000, 1000)]
+    lq, lk = [a for a, _ in lens], [b for _, b in lens]
+    assert fills_two_tiles(hk, g, lq)
+    q, k, v = rand(gen, sum(lq), hk * g, 128), rand(gen, sum(lk), hk, 128), rand(gen, sum(lk), hk, 128)
+    clean = fw.prompt_attention(q, k, v, cu(lq), cu(lk))
+    torch.cuda.synchronize()
+    check(clean, q, k, v, lens, 1 / math.sqrt(128), rows=100)
+    nan, inf = float("nan"), float("inf")
+    for seq, at, bad in ((0, 130, nan), (0, 255, inf), (0, 256, -inf), (1, 201, nan), (1, 330, inf), (1, 455, nan), (1, 456, -inf),
+                         (2, 511, nan), (2, 999, inf), (2, 0, nan)):
+        y = v.clone()
+        y[sum(lk[:seq]) + at, 1, 77] = bad
+        out = fw.prompt_attention(q, k, y, cu(lq), cu(lk))
+        torch.cuda.synchronize()
+        first = sum(lq[:seq]) + max(0, at - (lk[seq] - lq[seq]))  # rows that see it: first .. end of the sequence's
+        end = sum(lq[:seq + 1])
+        o, co = out["o"], clean["o"]
+        assert torch.equal(o[:first], co[:first]) and torch.equal(o[end:], co[end:])
+        hit, was = o[first:end], co[first:end]
+        heads = torch.arange(hk * g, device="cuda") // g == 1
+        assert torch.equal(hit[:, ~heads], was[:, ~heads])
+        cols = torch.arange(128, device="cuda") != 77
+        assert torch.equal(hit[:, heads][..., cols], was[:, heads][..., cols])
+        assert not bool(torch.isfinite(hit[:, heads][..., 77]).any())
+        assert torch.equal(out["lse"], clean["lse"])
