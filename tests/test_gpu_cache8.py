@@ -531,3 +531,22 @@ def test_infinities_beside_the_largest_values(fw, fmt, top):
             at = int(c.base[0]) + b
             for codes, scales in ((c.k, c.k_scale), (c.v, c.v_scale)):
                 assert float(scales[at // 32]) == sc and torch.equal(codes[at:at + val.shape[0]].double(), val)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m", [1, 3])
+def test_attend_on_a_part_of_a_large_store(fw, d, m):
+    """A layer's cells within a store whose other cells hold most of the rows, and the same cells in a store of their own."""
+    gen = torch.Generator("cuda").manual_seed(d + m)
+    counts = [3000, 17, 0, 2900, 3100, 64, 1, 2048]
+    whole = filled(fw, gen, [70000] + counts + [40000], d, "e4m3")
+    part = whole.part(1, 8)
+    lo, hi = int(whole.base[1]), int(whole.base[9])
+    own = fw.Cache8(fmt="e4m3", k=whole.k[lo:hi].clone(), v=whole.v[lo:hi].clone(), k_scale=whole.k_scale[lo // 32:hi // 32].clone(),
+                    v_scale=whole.v_scale[lo // 32:hi // 32].clone(), k_tail=part.k_tail.clone(), v_tail=part.v_tail.clone(),
+                    base=part.base - lo, capacity=part.capacity.clone(), counts=part.counts.clone())
+    q = (1.5 * torch.randn(1, m, 32, d, generator=gen, device="cuda")).to(torch.bfloat16)
+    for cache in (part, own):
+        out = fw.cache8_attend(cache, q, kv_heads=8)
+        torch.cuda.synchronize()
+        check_attend(cache, q, out, 8, float(torch.tensor(1 / math.sqrt(d), dtype=torch.float32)))
