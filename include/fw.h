@@ -417,18 +417,18 @@ fw_status fw_prompt_attention(const fw_prompt *p, void *o, float *lse, int32_t *
  * 2^-e rounded to nearest, ties to even.  (A power of two: the product is exact,
  * so a code does not depend on how it is computed, e4m3 loses nothing by it, and
  * every stored value is a bf16 number; but a code of a block with the scale 2^120
- * (e4m3) or 2^122 (int8) may stand for 2^128 or more, which reads as infinite.)  The bf16 rows of a cell's open block stay
- * in a ring of FW_CACHE8_TAIL rows (row r in slot r % FW_CACHE8_TAIL), so each
- * block is quantised from the originals, however its rows came in, and counts[h]
- * may be set back by up to FW_CACHE8_BLOCK appended rows (a draft that was not
- * accepted).  Infinities become the largest code of their sign and NaN 0; the
+ * (e4m3) or 2^122 (int8) may stand for 2^128 or more, which reads as infinite.)
+ * The bf16 rows of a cell's open block stay in a ring of FW_CACHE8_TAIL rows (row r
+ * in slot r % FW_CACHE8_TAIL), so each block is quantised from the originals, however
+ * its rows came in, and counts[h] may be set back by up to FW_CACHE8_BLOCK appended
+ * rows (a draft that was not accepted).  Infinities become the largest code of their sign and NaN 0; the
  * cell's status says so (FW_ERR_NONFINITE).
  * Per-cell status [cells] of the calls below (may be NULL): FW_OK;
  * FW_ERR_INVALID_ARG where base is no multiple of FW_CACHE8_BLOCK, the cell's rows
  * leave the store or its count (its offsets) is out of range, FW_ERR_WORKSPACE
  * where the rows do not fit the cell's capacity: such a cell is left as it was
  * (fw_cache8_compact: with a count of 0, fw_cache8_attend: its outputs those of an
- * empty cell).  A kept position out of range stores a row of zeros, with
+ * empty cell), and all others are served.  A kept position out of range stores a row of zeros, with
  * FW_ERR_INVALID_ARG. */
 #define FW_CACHE8_BLOCK 32
 #define FW_CACHE8_TAIL 64
@@ -478,7 +478,8 @@ typedef struct {
 /* o: device bf16 [sequences][m][kv_heads * group][d], 16-byte aligned; lse: device
  * fp32 of the same rows (may be NULL).  Products in fp16 (codes are exact there;
  * queries keep their 8 bits within 2^-24 of a row's largest; weights keep 11 bits),
- * sums and softmax in fp32.  The result does not depend on the order in which
+ * sums and softmax in fp32, the weights of a sum up to 2^14 before it is divided: values
+ * of 2^114 / n and more in n rows can overflow (fw_prompt_attention: 2^120 / n).  The result does not depend on the order in which
  * blocks run. */
 fw_status fw_cache8_attend(const fw_cache8 *c, const fw_cache8_query *q, void *o, float *lse, int32_t *status,
                            void *workspace, size_t workspace_bytes, void *stream);

@@ -135,17 +135,17 @@ __global__ void __launch_bounds__(256) k_cache8_status(const CompactArgs a)
     if (h < a.s.cells) a.status[h] = compact_cell(a, h, o0, base, n);
 }
 
-// The kept rows of all cells, block by block.  Bound: memory, the kept rows read (scattered rows
-// of 2 d bytes) and the codes written.  Cell h's blocks are the slots from offsets[h] / 32 + h on,
-// room for all of them (and one at least) without a prefix sum; a CTA takes a run of consecutive
-// slots, finds its first one's cell by a search over the offsets and goes on from there.  All of a
-// block's reads, keys and values, are under way at once (16 KB at d = 128), and the next block's
-// positions with them.  The first CTAs write the cells' counts and look at their offsets: the slots hold every cell's
-// blocks only if all offsets ascend within [0, total].  Where they do not, the first of these CTAs that sees it takes every
-// block of every cell that is in order itself, one after another (about a microsecond a block; what the walk writes of
-// them is the same), so that a cell's offsets concern no other cell.  256 cells x 32,768 rows to an eighth, d = 128: 133 us, 6.1 TB/s of rows read and codes
-// written, 90 % of the measured copy rate (3.4 ms a CTA per cell, 180 us with an unpacked search for the largest magnitude,
-// which left the integer pipe at 65 %).
+// The kept rows of all cells, block by block.  Bound: memory, the kept rows read (scattered rows of 2 d bytes) and the
+// codes written.  Cell h's blocks are the slots from offsets[h] / 32 + h on, room for all of them (and one at least)
+// without a prefix sum; a CTA takes a run of consecutive slots, finds its first one's cell by a search over the offsets
+// and goes on from there.  All of a block's reads, keys and values, are under way at once (16 KB at d = 128), and the
+// next block's positions with them.  The first CTAs write the cells' counts and look at their offsets: the slots hold
+// every cell's blocks only if all offsets ascend within [0, total].  Where they do not, the first of these CTAs that
+// sees it takes every block of every cell that is in order itself, one after another (about a microsecond a block; what
+// the walk writes of them is the same), so that a cell's offsets concern no other cell.  256 cells x 32,768 rows to an
+// eighth, d = 128: 133 to 139 us, 5.8 to 6.1 TB/s of rows read and codes written, 86 to 90 % of the measured copy rate
+// (3.4 ms a CTA per cell, 180 us with an unpacked search for the largest magnitude, which left the integer pipe at 65
+// %).
 template <int D, int FMT>
 __global__ void __launch_bounds__(Lay<D, compact_threads(D)>::THREADS, compact_ctas(D)) k_cache8_compact(const CompactArgs a)
 {
@@ -273,7 +273,8 @@ __device__ __forceinline__ bool append_block(const AppendArgs &a, int h, int64_t
     return quantise_block<D, FMT, AT>(a.s, base + b, min(BR, end - b), x, s_max);
 }
 
-// Bound: latency, one read of the rows, a barrier and the write (256 cells x 1 row and 512 x 7: about 3 us).
+// Bound: latency, one read of the rows, a barrier and the write (256 cells x 1 row and 512 x 7: 4.6 to
+// 5.0 us).
 // Appends of up to ONE_CTA rows: a CTA per cell takes the one or two blocks they touch, writes the ring and
 // the count.  (The rows of the ring that it reads are fewer than 32 before the new ones: no slot of
 // theirs is written.)
@@ -298,7 +299,8 @@ template <int D, int FMT> __global__ void __launch_bounds__(Lay<D, AT>::THREADS)
 }
 
 // Longer appends: a CTA per cell and block, then the ring and the counts by a second launch (one
-// CTA per cell would take its blocks one after another, about a microsecond each).
+// CTA per cell would take its blocks one after another, about a microsecond each).  d = 128, no status: 256 cells x 64 rows
+// 6.9 us, x 512 rows 17 us; 8 cells x 2,048 rows 5.6 us.
 __global__ void __launch_bounds__(256) k_cache8_append_status(const AppendArgs a)
 {
     const int h = blockIdx.x * 256 + threadIdx.x;

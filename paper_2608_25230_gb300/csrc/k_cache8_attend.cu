@@ -779,7 +779,8 @@ __global__ void __launch_bounds__(AT, 1)
 static_assert(FEW == 8 && AW == 8, "a warp per row of 8, eight states to join");
 
 // Query rows of a CTA: as few tiles of 8 as hold them, as far as registers go (a second round over
-// the store costs its fetches and products again).
+// the store costs its fetches and products again: 64 cells of 4,096 rows, d = 128, 4 query rows 20 us, 20 in two rounds 34,
+// 40 in three 48, 128 in eight 105).
 int row_tile(const fw_cache8 &c, const fw_cache8_query &q)
 {
     const int rows = q.group * q.m;
@@ -793,7 +794,10 @@ constexpr int warps_of(int d, int RT) { return d == 64 && RT == 8 ? 16 : 8; }
 // CTAs of a cell where the cells are few and hold little at most, so that a cluster each is faster, else 0.  (Per-layer
 // calls, d = 128, clusters against ranges: 8 cells of 4,096 rows 7.2 us against 10.7; 16 cells in 8 each, whose clusters of
 // whole SMs do not all find them at once, 12.9 against 11.9, of 1,000 rows in 4 each 7.1 against 10.3, of 3,300 13.6 against
-// 11.6; 48 cells of 500 in 2 each 7.4 against 13.2, of 2,000 16.8 against 15.4: the longest cell decides.)
+// 11.6; 48 cells of 500 in 2 each 7.4 against 13.2, of 2,000 16.8 against 15.4: the longest cell decides.)  What the host
+// knows of the lengths is the store's rows over the call's cells: the mean where the store holds nothing else, more where
+// the cells are a part of a larger one.  A layer of a large store therefore takes ranges: 8 cells of 4,096 rows of 256,
+// 10.6 us (7.9 in a store of their own; codes from memory in both).
 int cluster_of(const fw_cache8 &c, int tiles)
 {
     struct Rule {

@@ -4,8 +4,8 @@
 //   x_j = scale q_i . k_j,  o_i = sum_j softmax_j(x) v_j,  lse_i = log sum_j e^x_j.
 //
 // Bound: the tensor cores (two products of 128 x 128 x d per block of 128 keys): 16,384 tokens x 32 heads
-// (8 KV heads), d = 128: 1.36 ms, 1.61 PFLOP/s, 93 % of what the card sustains in bf16 products under its power
-// limit.  With d = 64 the exponentials and the hand-overs between the warps weigh twice as much: 8,192 tokens x 32 heads
+// (8 KV heads), d = 128: 1.33 to 1.44 ms from box to box, 1.53 to 1.65 PFLOP/s, 89 to 96 % of what the card sustains in
+// bf16 products under its power limit.  With d = 64 the exponentials and the hand-overs between the warps weigh twice as much: 8,192 tokens x 32 heads
 // 291 us, 0.94 PFLOP/s.  The weights are rounded to bf16 for the second product, which wants both its operands of one
 // type; sums and statistics are of the unrounded ones.
 // The query heads of a KV head are rows of the same product, so a tile of 128 rows
@@ -25,8 +25,9 @@
 // Slots are the tokens of a CTA's tiles: sequence i's are numbered from
 // floor(cu_q[i] / slot) + i on, which leaves room for all of them without a prefix
 // sum; a CTA finds its sequence by a search over cu_q.  Where there are few slots, a cluster of CTAs takes the
-// blocks of one, and its rows' parts are joined through distributed shared memory.  The last slots, whose rows
-// see the most keys, come first.
+// blocks of one, and its rows' parts are joined through distributed shared memory.  Slots are taken from the last
+// to the first: a sequence's last rows, which see the most keys, come first (of packed sequences the last one does, however
+// short it is).
 #include <cuda_bf16.h>
 
 #include "fw_internal.h"
@@ -734,7 +735,8 @@ fw_status prompt_attention(const fw_prompt &p, void *o, float *lse, int32_t *sta
     // Few rows against long keys: the keys of a slot split over a cluster, as long as the CTAs fit the SMs once.  The
     // joining costs several blocks' time, so only from SPLIT blocks on average on, and MIN_PART or more to a part
     // (one sequence, 8 x 4 heads, d = 128: 17 rows against 16,384 keys 130 us whole, 24 in 8 parts; 256 against 2,048
-    // 28.4 whole, 26.3 in 2; d = 64, 128 against 1,024 16.2 whole, 19.1 in 2).
+    // 28.4 whole, 26.3 in 2; d = 64, 128 against 1,024 16.2 whole, 19.1 in 2).  The host knows the lengths' mean alone: a long
+    // sequence among short ones is not split (16 of one token on 8 KV heads, 128 keys each but one with 16,384: 127 us).
     // (Of two tiles a CTA there are more than half as many CTAs as SMs, so that their keys are never split.)
     const int64_t blocks = p.total_k / ((int64_t)p.num_seqs * PK);
     int parts = 1;
