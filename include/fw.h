@@ -486,6 +486,136 @@ fw_status fw_cache8_attend(const fw_cache8 *c, const fw_cache8_query *q, void *o
 /* Workspace bytes (0 for arguments fw_cache8_attend refuses). */
 size_t fw_cache8_attend_workspace(const fw_cache8 *c, const fw_cache8_query *q);
 
+/* A cache of bf16 rows in pages, for cells (KV heads of sequences) whose lengths are
+ * unlike, known to the GPU alone, grow by appends and shrink by eviction (Sec. 4's
+ * ragged per-head storage, which decode keeps appending to), and that share what
+ * they have in common.  Cell h fills counts[h] rows; row r lies in row r % page_rows
+ * of the page table[h][r / page_rows] of the pool.  The first held[h] entries of its
+ * table are its own to use (as many as its rows need, or more: counts[h] may be set back,
+ * a draft that was not accepted, and the next rows take its place); what stands behind
+ * them means nothing.  refs[p] entries name page p; bit p % 32 of free_bits[p / 32] says
+ * that none does.  A cell writes only to pages that it alone names.
+ * Pages are handed out by the calls themselves: free ones in ascending order from
+ * *next on, round the end, to cells in their order and to a cell's entries in theirs;
+ * *next is then the page behind the last one.  Which pages a call hands out depends
+ * on these books alone.  Pages that a call gives back are free for the calls behind it.
+ * A new cache: counts, held, refs and *next zero, the bits of all pages set.
+ * Calls that change one pool's books run one after another (on one stream, or ordered by
+ * the caller), those on parts of it too.
+ * Per-cell status [cells] of the calls below (may be NULL): FW_OK; FW_ERR_INVALID_ARG
+ * where held[h] or counts[h] is out of range or a page of the cell that the call needs is
+ * no page of the pool; FW_ERR_WORKSPACE where its rows need more than max_pages
+ * entries, or more pages than are left free for it (a cell that what is left does not hold, and
+ * every cell behind it that needs a page, get none).  Such a cell is left as it
+ * was, and all others are served. */
+typedef struct {
+    int32_t cells;
+    int32_t d;               /* 64 or 128                                            */
+    int32_t page_rows;       /* 16, 32, 64 or 128                                    */
+    int32_t num_pages;       /* pages of the pool; fewer than 2^31 rows in all       */
+    int32_t max_pages;       /* entries of a cell's table; cells * max_pages < 2^31  */
+    void *k, *v;             /* device bf16 [num_pages][page_rows][d], 16-byte aligned */
+    int32_t *table;          /* device [cells][max_pages]                            */
+    int32_t *held, *counts;  /* device [cells]                                       */
+    int32_t *refs;           /* device [num_pages]                                   */
+    uint32_t *free_bits;     /* device [ceil(num_pages / 32)]                        */
+    int32_t *next;           /* device [1]                                           */
+} fw_pages;
+
+/* New rows for every cell: m each.  Cells are (sequence, KV head), the head fastest;
+ * column c of row i of cell (b, h) at b * k_seq + i * k_tok + h * k_head + c of k, and
+ * so for v.  Strides in elements, multiples of 8. */
+typedef struct {
+    int32_t kv_heads;        /* cells = sequences x kv_heads                         */
+    int32_t m;
+    const void *k, *v;       /* device bf16, 16-byte aligned                         */
+    int64_t k_seq, k_tok, k_head, v_seq, v_tok, v_head;
+} fw_pages_new;
+/* Appends them behind each cell's rows and adds m to counts.  Pages are taken where rows go
+ * beyond the held ones, and for each page to be written that another entry names too:
+ * the cell gets one of its own, with the rows that it had there. */
+fw_status fw_pages_append(const fw_pages *p, const fw_pages_new *rows, int32_t *status, void *workspace,
+                          size_t workspace_bytes, void *stream);
+/* Workspace bytes of an append of m rows per cell (0 for arguments fw_pages_append refuses). */
+size_t fw_pages_append_workspace(const fw_pages *p, int32_t m);
+
+/* Cell h gets the rows kept_pos[offsets[h] .. offsets[h+1]) in that order (what
+ * fw_contour_alloc gives), in pages taken for them, and gives the pages that it held back:
+ *   - of K and V: device bf16, row t of cell h at h * cell_stride + t * row_stride
+ *     elements (positive multiples of 8), T rows per cell, 16-byte aligned;
+ *   - K and V both NULL: of the cell's own rows (T and the strides are not looked at).
+ * total: the entries that kept_pos holds (at least offsets[cells]).  A kept position out of
+ * range stores a row of zeros, with FW_ERR_INVALID_ARG; so does an offset out of order or
+ * beyond total, whose cell is left as it was. */
+fw_status fw_pages_compact(const fw_pages *p, const void *K, const void *V, int32_t T, int64_t cell_stride,
+                           int64_t row_stride, const int64_t *offsets, const int32_t *kept_pos, int64_t total,
+                           int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+/* Workspace bytes (0 for arguments fw_pages_compact refuses). */
+size_t fw_pages_compact_workspace(const fw_pages *p, int64_t total);
+
+/* Cell h becomes what cell src[h] was before the call: it gives its own pages back and names
+ * the other's (those that its rows fill), no row is copied.  src[h] = h: unchanged (held and
+ * all); src[h] < 0: emptied, which is how a sequence's pages are freed.  Beams that fork and change
+ * places are one call.  src: device [cells]; src[h] >= cells: FW_ERR_INVALID_ARG. */
+fw_status fw_pages_fork(const fw_pages *p, const int32_t *src, int32_t *status, void *workspace,
+                        size_t workspace_bytes, void *stream);
+/* Workspace bytes (0 for arguments fw_pages_fork refuses). */
+size_t fw_pages_fork_workspace(const fw_pages *p);
+
+/* Attention over the pages for the m last tokens of every sequence (m = 1: a decode
+ * step; their own rows are in the cache).  With n = counts[h], token i sees the cell's
+ * rows j < n - m + 1 + i: o = sum_j softmax_j(scale q . k_j) v_j; o = 0, lse = -inf where
+ * nothing is seen.  A page that is no page of the pool has no part (its rows are not seen),
+ * with FW_ERR_INVALID_ARG; a cell whose count is out of range is taken as empty, with
+ * the same. */
+typedef struct {
+    int32_t kv_heads;        /* cells = sequences x kv_heads                         */
+    int32_t group;           /* query heads per KV head                              */
+    int32_t m;               /* tokens per sequence                                  */
+    int32_t longest;         /* a host-side bound on counts, 0 where there is none: it
+                                chooses how the work is split, and no row is left out
+                                where it is wrong                                    */
+    const void *q;           /* device bf16, 16-byte aligned: as fw_cache8_query's   */
+    int64_t q_seq, q_tok, q_head; /* strides in elements, multiples of 8             */
+    float scale;             /* > 0                                                  */
+} fw_pages_query;
+/* o: device bf16 [sequences][m][kv_heads * group][d], 16-byte aligned; lse: device fp32
+ * of the same rows (may be NULL).  status [cells] also FW_ERR_TIMEOUT, where a
+ * bounded wait gave up (the rows concerned are NaN).  The same call gives the same bits. */
+fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, float *lse, int32_t *status,
+                          void *workspace, size_t workspace_bytes, void *stream);
+/* Workspace bytes (0 for arguments fw_pages_attend refuses). */
+size_t fw_pages_attend_workspace(const fw_pages *p, const fw_pages_query *q);
+
+/* What the attention calls above take, out of a projection's queries and keys, in one
+ * pass: the norm of each head, then the rotation by the token's position.
+ *   norm (eps >= 0):  y = x / sqrt(mean_c x_c^2 + eps) * w,   else y = x;
+ *   rotation: with f < rot / 2, angle = pos[row] * inv_freq[f], the columns (a, b) =
+ *   (f, rot / 2 + f), or (2f, 2f + 1) if interleaved, become
+ *   (y_a cos - y_b sin, y_b cos + y_a sin); columns from rot on stay y.
+ * Angles are exact to 2^-26 of a turn while |pos| * max(|inv_freq|, 2) <= 2^38; all
+ * else in fp32, rounded once to bf16.  An output may be its own input (the same address and
+ * strides), but share no memory otherwise.  (The paper has no counterpart: its models' queries
+ * and keys come so into the caches that it evicts from.) */
+typedef struct {
+    int64_t rows;            /* tokens                                               */
+    int32_t q_heads, kv_heads; /* kv_heads may be 0 (no keys)                        */
+    int32_t d;               /* a multiple of 16, at most 256                        */
+    int32_t rot;             /* columns that are rotated: a multiple of 16, 0 .. d   */
+    int32_t interleaved;     /* 0 or 1                                               */
+    int32_t w_dtype;         /* fw_dtype of the weights                              */
+    float eps;               /* negative: no norm                                    */
+    const void *q, *k;       /* device bf16, 16-byte aligned: column c of head h of row
+                                r at r * q_row + h * q_head + c                      */
+    void *q_out, *k_out;
+    const void *q_weight, *k_weight; /* device [d], 16-byte aligned; NULL: ones      */
+    const int32_t *pos;      /* device [rows]                                        */
+    const float *inv_freq;   /* device [rot / 2]                                     */
+    int64_t q_row, q_head, k_row, k_head;                 /* strides in elements,    */
+    int64_t q_out_row, q_out_head, k_out_row, k_out_head; /* multiples of 8, the outputs' positive */
+} fw_rotation;
+fw_status fw_qk_rotate(const fw_rotation *r, void *stream);
+
 /* Largest cells accepted by fw_contour_alloc_noalloc. */
 #define FW_CONTOUR_NOALLOC_MAX_CELLS 4096
 

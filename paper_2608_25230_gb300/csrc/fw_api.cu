@@ -145,6 +145,73 @@ static fw_status check_cache8_query(const fw_cache8 *c, const fw_cache8_query *q
     return FW_OK;
 }
 
+static bool multiple_of_8(int64_t x) { return x % 8 == 0 && x > -((int64_t)1 << 38) && x < ((int64_t)1 << 38); }
+
+static fw_status check_pages(const fw_pages *p)
+{
+    if (!p || p->cells < 1 || p->num_pages < 1 || p->max_pages < 1) return FW_ERR_INVALID_ARG;
+    if (!p->k || !p->v || !p->table || !p->held || !p->counts || !p->refs || !p->free_bits || !p->next)
+        return FW_ERR_INVALID_ARG;
+    if (!aligned(p->k, 16) || !aligned(p->v, 16)) return FW_ERR_INVALID_ARG;
+    if (p->d != 64 && p->d != 128) return FW_ERR_UNSUPPORTED;
+    if (p->page_rows != 16 && p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return FW_ERR_UNSUPPORTED;
+    if (p->cells > (1 << 24) || (int64_t)p->num_pages * p->page_rows >= ((int64_t)1 << 31) ||
+        (int64_t)p->cells * p->max_pages >= ((int64_t)1 << 31) || (int64_t)p->max_pages * p->page_rows >= ((int64_t)1 << 31))
+        return FW_ERR_UNSUPPORTED;
+    return FW_OK;
+}
+
+static fw_status check_pages_append(const fw_pages *p, int m)
+{
+    const fw_status st = check_pages(p);
+    if (st != FW_OK) return st;
+    if (m < 1) return FW_ERR_INVALID_ARG;
+    // (the rows of all cells are numbered in 32 bits)
+    return ((int64_t)m + 2 * p->page_rows) * p->cells >= ((int64_t)1 << 31) ? FW_ERR_UNSUPPORTED : FW_OK;
+}
+
+static fw_status check_pages_compact(const fw_pages *p, int64_t total)
+{
+    const fw_status st = check_pages(p);
+    if (st != FW_OK) return st;
+    return total < 0 ? FW_ERR_INVALID_ARG : total >= ((int64_t)1 << 35) ? FW_ERR_UNSUPPORTED : FW_OK;
+}
+
+static fw_status check_pages_query(const fw_pages *p, const fw_pages_query *q)
+{
+    const fw_status st = check_pages(p);
+    if (st != FW_OK) return st;
+    if (!q || q->kv_heads < 1 || q->group < 1 || q->m < 1 || q->longest < 0 || p->cells % q->kv_heads != 0 ||
+        !(q->scale > 0.f) || !(q->scale < 1e30f))
+        return FW_ERR_INVALID_ARG;
+    if ((int64_t)q->group * q->m > 65535) return FW_ERR_UNSUPPORTED;
+    if (!q->q || !aligned(q->q, 16) || !multiple_of_8(q->q_seq) || !multiple_of_8(q->q_tok) || !multiple_of_8(q->q_head))
+        return FW_ERR_INVALID_ARG;
+    return FW_OK;
+}
+
+static fw_status check_rotation(const fw_rotation *r)
+{
+    if (!r || r->rows < 0 || r->q_heads < 1 || r->kv_heads < 0 || r->d < 1 || r->rot < 0 || r->rot > r->d)
+        return FW_ERR_INVALID_ARG;
+    if (r->interleaved != 0 && r->interleaved != 1) return FW_ERR_INVALID_ARG;
+    if (r->w_dtype != FW_F32 && r->w_dtype != FW_BF16) return FW_ERR_INVALID_ARG;
+    if (r->d % 16 != 0 || r->d > 256 || r->rot % 16 != 0) return FW_ERR_UNSUPPORTED;
+    if (r->rows >= ((int64_t)1 << 31) || r->q_heads > 65536 || r->kv_heads > 65536) return FW_ERR_UNSUPPORTED;
+    if (!(r->eps < 1e30f) || (r->eps < 0.f && (r->q_weight || r->k_weight))) return FW_ERR_INVALID_ARG;
+    if (!aligned(r->q_weight, 16) || !aligned(r->k_weight, 16)) return FW_ERR_INVALID_ARG;
+    if (r->rows == 0) return FW_OK;
+    if (r->rot > 0 && (!r->pos || !r->inv_freq)) return FW_ERR_INVALID_ARG;
+    // (an input may be repeated by a stride of 0, an output's rows may not be one)
+    if (!r->q || !r->q_out || !aligned(r->q, 16) || !aligned(r->q_out, 16) || !multiple_of_8(r->q_row) ||
+        !multiple_of_8(r->q_head) || !good_stride(r->q_out_row) || !good_stride(r->q_out_head))
+        return FW_ERR_INVALID_ARG;
+    if (r->kv_heads > 0 && (!r->k || !r->k_out || !aligned(r->k, 16) || !aligned(r->k_out, 16) || !multiple_of_8(r->k_row) ||
+                            !multiple_of_8(r->k_head) || !good_stride(r->k_out_row) || !good_stride(r->k_out_head)))
+        return FW_ERR_INVALID_ARG;
+    return FW_OK;
+}
+
 static fw_status check_rows(const fw_rows *r, RowsDev &R)
 {
     if (!r) return FW_ERR_INVALID_ARG;
@@ -531,6 +598,80 @@ fw_status fw_cache8_attend(const fw_cache8 *c, const fw_cache8_query *q, void *o
     const size_t need = cache8_attend_workspace(*c, *q);
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return FW_ERR_WORKSPACE;
     return cache8_attend(*c, *q, o, lse, status, workspace, (cudaStream_t)stream);
+}
+
+size_t fw_pages_append_workspace(const fw_pages *p, int32_t m)
+{
+    return check_pages_append(p, m) == FW_OK ? pages_append_workspace(*p, m) : 0;
+}
+
+fw_status fw_pages_append(const fw_pages *p, const fw_pages_new *r, int32_t *status, void *workspace,
+                          size_t workspace_bytes, void *stream)
+{
+    if (!r) return FW_ERR_INVALID_ARG;
+    const fw_status st = check_pages_append(p, r->m);
+    if (st != FW_OK) return st;
+    if (r->kv_heads < 1 || p->cells % r->kv_heads != 0 || !r->k || !r->v || !aligned(r->k, 16) || !aligned(r->v, 16))
+        return FW_ERR_INVALID_ARG;
+    for (const int64_t x : {r->k_seq, r->k_tok, r->k_head, r->v_seq, r->v_tok, r->v_head})
+        if (!multiple_of_8(x)) return FW_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < pages_append_workspace(*p, r->m)) return FW_ERR_WORKSPACE;
+    return pages_append(*p, *r, status, workspace, (cudaStream_t)stream);
+}
+
+size_t fw_pages_compact_workspace(const fw_pages *p, int64_t total)
+{
+    return check_pages_compact(p, total) == FW_OK ? pages_compact_workspace(*p, total) : 0;
+}
+
+fw_status fw_pages_compact(const fw_pages *p, const void *K, const void *V, int32_t T, int64_t cell_stride,
+                           int64_t row_stride, const int64_t *offsets, const int32_t *kept_pos, int64_t total,
+                           int32_t *status, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const fw_status st = check_pages_compact(p, total);
+    if (st != FW_OK) return st;
+    if (!offsets || (total > 0 && !kept_pos) || (!K) != (!V)) return FW_ERR_INVALID_ARG;
+    if (K && (T < 1 || !aligned(K, 16) || !aligned(V, 16) || !good_stride(cell_stride) || !good_stride(row_stride)))
+        return FW_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < pages_compact_workspace(*p, total))
+        return FW_ERR_WORKSPACE;
+    return pages_compact(*p, K, V, T, cell_stride, row_stride, offsets, kept_pos, total, status, workspace,
+                         (cudaStream_t)stream);
+}
+
+size_t fw_pages_fork_workspace(const fw_pages *p) { return check_pages(p) == FW_OK ? pages_fork_workspace(*p) : 0; }
+
+fw_status fw_pages_fork(const fw_pages *p, const int32_t *src, int32_t *status, void *workspace, size_t workspace_bytes,
+                        void *stream)
+{
+    const fw_status st = check_pages(p);
+    if (st != FW_OK) return st;
+    if (!src) return FW_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < pages_fork_workspace(*p)) return FW_ERR_WORKSPACE;
+    return pages_fork(*p, src, status, workspace, (cudaStream_t)stream);
+}
+
+size_t fw_pages_attend_workspace(const fw_pages *p, const fw_pages_query *q)
+{
+    return check_pages_query(p, q) == FW_OK ? pages_attend_workspace(*p, *q) : 0;
+}
+
+fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, float *lse, int32_t *status,
+                          void *workspace, size_t workspace_bytes, void *stream)
+{
+    const fw_status st = check_pages_query(p, q);
+    if (st != FW_OK) return st;
+    if (!o || !aligned(o, 16)) return FW_ERR_INVALID_ARG;
+    const size_t need = pages_attend_workspace(*p, *q);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return FW_ERR_WORKSPACE;
+    return pages_attend(*p, *q, o, lse, status, workspace, (cudaStream_t)stream);
+}
+
+fw_status fw_qk_rotate(const fw_rotation *r, void *stream)
+{
+    const fw_status st = check_rotation(r);
+    if (st != FW_OK) return st;
+    return r->rows == 0 ? FW_OK : qk_rotate(*r, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -114,6 +114,20 @@ size_t cache8_attend_workspace(const fw_cache8 &c, const fw_cache8_query &q);
 fw_status cache8_attend(const fw_cache8 &c, const fw_cache8_query &q, void *o, float *lse, int32_t *status, void *ws,
                         cudaStream_t s);
 
+// The cache in pages, its attention, and the rotation of queries and keys.
+size_t pages_append_workspace(const fw_pages &p, int m);
+fw_status pages_append(const fw_pages &p, const fw_pages_new &r, int32_t *status, void *ws, cudaStream_t s);
+size_t pages_compact_workspace(const fw_pages &p, int64_t total);
+fw_status pages_compact(const fw_pages &p, const void *K, const void *V, int T, int64_t cell_stride, int64_t row_stride,
+                        const int64_t *offsets, const int32_t *kept_pos, int64_t total, int32_t *status, void *ws,
+                        cudaStream_t s);
+size_t pages_fork_workspace(const fw_pages &p);
+fw_status pages_fork(const fw_pages &p, const int32_t *src, int32_t *status, void *ws, cudaStream_t s);
+size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q);
+fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, float *lse, int32_t *status, void *ws,
+                       cudaStream_t s);
+fw_status qk_rotate(const fw_rotation &r, cudaStream_t s);
+
 // A TMA map of a 2-D bf16 tensor [rows][cols] (cols innermost, row stride
 // cols * 2 bytes) read in boxes of box_rows x 64 elements with the 128-byte
 // swizzle.  False if the driver's encoder is unavailable or refuses the map.

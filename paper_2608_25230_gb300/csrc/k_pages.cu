@@ -1,0 +1,494 @@
+// k_pages.cu -- a cache of bf16 rows in pages: appends, compaction, forks.
+//
+// Every call changes the books (tables, counts, how many entries name a page, which pages are
+// free) so that the result depends on the books before it alone, not on the order in which CTAs
+// run: pages are handed out by one CTA (k_pages_plan) by sums over the cells in their order, and
+// what runs in parallel counts entries up or down by integer atomics, whose order changes
+// nothing.  A page that comes back is free for the calls behind, so the pages of a call are never
+// read and handed out at once.
+//
+// Bound: append: latency (two launches); compaction: memory, every kept row read and written
+// once; fork: the tables' entries and their pages' counts, latency for small ones.
+#include <algorithm>
+
+#include "fw_pages.cuh"
+
+namespace fw {
+namespace {
+
+using namespace pages;
+
+constexpr int UR = 16;           // rows that a warp copies at a time; no page holds less
+constexpr int MW = 8;            // warps of a CTA of the copying kernels
+constexpr int PT = 1024;         // threads of the plan's CTA
+constexpr int WORDS = 4;         // words of the free bits that one of them looks at a time
+
+// ------------------------------------------------------------------ the plan
+struct AppendArgs {
+    Pages s;
+    int m, kv_heads;
+    const uint16_t *k, *v;
+    int64_t k_seq, k_tok, k_head, v_seq, v_tok, v_head;
+    int32_t *status;
+    int32_t *first;  // workspace: [cells + 1] where each cell's pages stand in the list
+    int32_t *list;   // workspace: the pages that are handed out (then those that they replace)
+    int2 *plan;      // workspace: [cells] (rows before, -1 where the cell takes none; page to copy from or -1)
+};
+
+struct CompactArgs {
+    Pages s;
+    const uint16_t *K, *V;  // null: the cells' own rows
+    int T;
+    int64_t cell_stride, row_stride;
+    const int64_t *offsets;
+    const int32_t *kept_pos;
+    int64_t total;
+    int32_t *status;
+    int32_t *first, *list;  // workspace, as above
+    int32_t *granted;       // workspace: pages handed out
+};
+
+// Whether entry i of a cell's table, which new rows touch, needs a page: those behind the held ones, and
+// those that another entry names too.
+__device__ __forceinline__ bool append_needs(const Pages &s, const int32_t *row, int held, int i)
+{
+    return i >= held || s.refs[row[i]] > 1;
+}
+// Pages that a cell needs, with its status.
+__device__ __forceinline__ int cell_need(const AppendArgs &a, int h, fw_status &st)
+{
+    int n, held;
+    st = cell_rows(a.s, h, n, held);
+    if (st != FW_OK) return 0;
+    const int i0 = n / a.s.P;
+    const int64_t i1 = ((int64_t)n + a.m - 1) / a.s.P;
+    if (i1 >= a.s.width) {
+        st = FW_ERR_WORKSPACE;
+        return 0;
+    }
+    const int32_t *row = a.s.row(h);
+    int need = 0;
+    for (int i = i0; i <= (int)i1; ++i) {
+        if (i < held && !a.s.is_page(row[i])) {
+            st = FW_ERR_INVALID_ARG;
+            return 0;
+        }
+        need += append_needs(a.s, row, held, i);
+    }
+    return need;
+}
+__device__ __forceinline__ int cell_need(const CompactArgs &a, int h, fw_status &st)
+{
+    int n, held;
+    st = cell_rows(a.s, h, n, held);
+    const int64_t o0 = a.offsets[h], o1 = a.offsets[h + 1];
+    if (o0 < 0 || o1 < o0 || o1 > a.total) st = FW_ERR_INVALID_ARG;
+    if (st == FW_OK && (o1 - o0 + a.s.P - 1) / a.s.P > a.s.width) st = FW_ERR_WORKSPACE;
+    return st == FW_OK ? (int)((o1 - o0 + a.s.P - 1) / a.s.P) : 0;
+}
+// Rows that a cell of the compaction gets, or -1 where it is left as it was.  (Reads what the plan read, and
+// what it wrote: the books' first change comes behind the last reader.)
+__device__ __forceinline__ int compact_rows(const CompactArgs &a, int h, fw_status &st)
+{
+    cell_need(a, h, st);
+    if (st != FW_OK || (a.first[h + 1] > a.first[h] && a.first[h + 1] > *a.granted)) return -1;
+    return (int)(a.offsets[h + 1] - a.offsets[h]);
+}
+
+// Exclusive sum over the CTA's threads; `all`: the sum of all.
+__device__ __forceinline__ int scan_cta(int x, int &all, int (&s_scan)[32])
+{
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    int incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(FW_FULL, incl, o);
+        if (lane >= o) incl += y;
+    }
+    __syncthreads();  // (s_scan is free again)
+    if (lane == 31) s_scan[wid] = incl;
+    __syncthreads();
+    const int mine = s_scan[lane];
+    const int before = __reduce_add_sync(FW_FULL, lane < wid ? mine : 0);
+    all = __reduce_add_sync(FW_FULL, mine);
+    return before + incl - x;
+}
+
+// One CTA: what every cell needs, the free pages for it, and for appends the books.
+template <typename Args> __global__ void __launch_bounds__(PT) k_pages_plan(const Args a)
+{
+    constexpr bool APPEND = sizeof(Args) == sizeof(AppendArgs);
+    static_assert(sizeof(AppendArgs) != sizeof(CompactArgs), "told apart by their size");
+    __shared__ int s_scan[32], s_granted;
+    const Pages &s = a.s;
+    const int tid = threadIdx.x;
+    if (tid == 0) s_granted = 0;
+
+    int want = 0;
+    for (int b = 0; b < s.cells; b += PT) {
+        const int h = b + tid;
+        fw_status st = FW_OK;
+        const int need = h < s.cells ? cell_need(a, h, st) : 0;
+        int all;
+        const int at = want + scan_cta(need, all, s_scan);
+        if (h < s.cells) {
+            a.first[h] = at;
+            if (a.status) a.status[h] = st;
+            if constexpr (APPEND) a.plan[h] = make_int2(st == FW_OK ? s.counts[h] : -1, -1);
+        }
+        want += all;
+    }
+    if (tid == 0) a.first[s.cells] = want;
+
+    // The first `want` free pages from *next on: the words of the bits in a circle, the first one's lower
+    // part last.
+    const int words = (s.N + 31) / 32, got_most = min(want, s.N);
+    const int start = s.is_page(*s.next) ? *s.next : 0, w0 = start / 32;
+    int found = 0;
+    for (int b = 0; b <= words && found < got_most; b += PT * WORDS) {
+        uint32_t x[WORDS];
+        int pop = 0;
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const int t = b + tid * WORDS + i, w = w0 + t < words ? w0 + t : w0 + t - words;
+            x[i] = 0;
+            if (t <= words) {
+                x[i] = s.bits[w];
+                if (t == 0) x[i] &= ~0u << (start % 32);
+                if (t == words) x[i] &= ~(~0u << (start % 32));
+                if (w == words - 1 && s.N % 32 != 0) x[i] &= ~(~0u << (s.N % 32));
+            }
+            pop += __popc(x[i]);
+        }
+        int all;
+        int at = found + scan_cta(pop, all, s_scan);
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const int t = b + tid * WORDS + i, w = w0 + t < words ? w0 + t : w0 + t - words;
+            while (x[i] && at < got_most) {
+                a.list[at++] = w * 32 + __ffs(x[i]) - 1;
+                x[i] &= x[i] - 1;
+            }
+        }
+        found = min(found + all, got_most);
+    }
+    __syncthreads();
+
+    // Which cells it is enough for.
+    for (int h = tid; h < s.cells; h += PT) {
+        const int to = a.first[h + 1];
+        if (to == a.first[h]) continue;
+        if (to <= found) {
+            atomicMax(&s_granted, to);
+        } else {
+            if (a.status) a.status[h] = FW_ERR_WORKSPACE;
+            if constexpr (APPEND) a.plan[h].x = -1;
+        }
+    }
+    __syncthreads();
+    const int granted = s_granted;
+    for (int t = tid; t < granted; t += PT) {
+        const int page = a.list[t];
+        s.refs[page] = 1;
+        atomicAnd(&s.bits[page / 32], ~(1u << (page % 32)));
+        if (t == granted - 1) *s.next = page + 1 < s.N ? page + 1 : 0;
+    }
+    if constexpr (!APPEND) {
+        if (tid == 0) *a.granted = granted;
+    } else {
+        __syncthreads();
+        for (int h = tid; h < s.cells; h += PT) {
+            const int n = a.plan[h].x;
+            if (n < 0) continue;
+            const int held = s.held[h], i0 = n / s.P, i1 = (n + a.m - 1) / s.P;
+            int32_t *row = s.row(h);
+            int at = a.first[h];
+            for (int i = i0; i <= i1; ++i) {
+                if (!append_needs(s, row, held, i)) continue;
+                const int was = i < held ? row[i] : -1;
+                row[i] = a.list[at];
+                a.list[at++] = was;
+                if (i == i0 && n % s.P != 0) a.plan[h].y = was;
+            }
+            s.held[h] = max(held, i1 + 1);
+            s.counts[h] = n + a.m;
+        }
+        __syncthreads();
+        // (behind all readings of refs)
+        for (int t = tid; t < granted; t += PT) {
+            const int was = a.list[t];
+            if (was >= 0 && atomicSub(&s.refs[was], 1) == 1) atomicOr(&s.bits[was / 32], 1u << (was % 32));
+        }
+    }
+}
+
+// ------------------------------------------------------------------- copying
+// UR rows of keys and of values by a warp, all reads under way at once: row i of `rows` from
+// k_of(i), v_of(i) (null: zeros) to the rows behind kd, vd.
+template <int D, typename F>
+__device__ __forceinline__ void copy_rows(uint16_t *kd, uint16_t *vd, int lo, int hi, int lane, F source)
+{
+    constexpr int LPR = D / 8, RS = 32 / LPR, N = UR / RS;
+    const int col = lane % LPR * 8, r0 = lane / LPR;
+    uint4 x[2][N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = r0 + RS * i;
+        const uint16_t *k, *v;
+        source(r, k, v);  // (every lane: it may shuffle)
+        const bool in = r >= lo && r < hi && k;
+        x[0][i] = in ? __ldcs(reinterpret_cast<const uint4 *>(k + col)) : make_uint4(0, 0, 0, 0);
+        x[1][i] = in ? __ldcs(reinterpret_cast<const uint4 *>(v + col)) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = r0 + RS * i;
+        if (r >= lo && r < hi) {
+            *reinterpret_cast<uint4 *>(kd + r * D + col) = x[0][i];
+            *reinterpret_cast<uint4 *>(vd + r * D + col) = x[1][i];
+        }
+    }
+}
+
+// New rows to their pages, and those of a page that was shared to the cell's own: a warp per cell and UR rows.
+template <int D> __global__ void __launch_bounds__(32 * MW) k_pages_append(const AppendArgs a, int units)
+{
+    const Pages &s = a.s;
+    const int lane = threadIdx.x & 31, id = blockIdx.x * MW + (threadIdx.x >> 5);
+    const int h = id / units;
+    if (h >= s.cells) return;
+    const int n = a.plan[h].x, from = a.plan[h].y;
+    if (n < 0) return;
+    const int64_t begin = (from >= 0 ? n / s.P * s.P : n / UR * UR) + (int64_t)(id - h * units) * UR;
+    const int end = n + a.m;
+    if (begin >= end) return;
+    const int r0 = (int)begin;
+    const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
+    const int64_t to = ((int64_t)s.row(h)[r0 / s.P] * s.P + r0 % s.P) * D, old = ((int64_t)from * s.P + r0 % s.P) * D;
+    copy_rows<D>(s.k + to, s.v + to, max(0, from >= 0 ? 0 : n - r0), min(UR, end - r0), lane,
+                 [&](int r, const uint16_t *&k, const uint16_t *&v) {
+                     const int64_t i = (int64_t)r0 + r - n;
+                     k = i >= 0 ? a.k + seq * a.k_seq + i * a.k_tok + hk * a.k_head : s.k + old + r * D;
+                     v = i >= 0 ? a.v + seq * a.v_seq + i * a.v_tok + hk * a.v_head : s.v + old + r * D;
+                 });
+}
+
+// The kept rows to the pages that were taken for them: the list's pages, UR rows a warp, consecutive ones to a warp.
+template <int D, bool OWN> __global__ void __launch_bounds__(32 * MW) k_pages_move(const CompactArgs a)
+{
+    const Pages &s = a.s;
+    const int lane = threadIdx.x & 31, warps = gridDim.x * MW, id = blockIdx.x * MW + (threadIdx.x >> 5), per = s.P / UR;
+    const int64_t units = (int64_t)*a.granted * per, run = (units + warps - 1) / warps;
+    const int64_t u0 = id * run, u1 = min(u0 + run, units);
+    if (u0 >= u1) return;
+    // the cell of the first: the last one whose pages start at or before it, 32 probes at a time
+    int lo = 0, hi = s.cells;
+    do {
+        const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+        const unsigned hit = __ballot_sync(FW_FULL, i < hi && a.first[min(i, hi - 1)] <= u0 / per);
+        lo += max(__popc(hit) - 1, 0) * step;
+        hi = min(lo + step, hi);
+    } while (hi - lo > 1);
+    int h = lo;
+    for (int64_t u = u0; u < u1; ++u) {
+        const int g = (int)(u / per);
+        while (a.first[h + 1] <= g) ++h;
+        const int64_t o0 = a.offsets[h];
+        const int j0 = (int)(u - (int64_t)a.first[h] * per) * UR, n = (int)(a.offsets[h + 1] - o0);
+        if (j0 >= n) continue;
+        const int rows = min(UR, n - j0);
+        int64_t at = -1;  // lane r: where row r comes from
+        if (lane < rows) {
+            const int pos = a.kept_pos[o0 + j0 + lane];
+            if constexpr (OWN) {
+                const int page = pos >= 0 && pos < s.counts[h] ? s.row(h)[pos / s.P] : -1;
+                at = s.is_page(page) ? ((int64_t)page * s.P + pos % s.P) * D : -1;
+            } else {
+                at = pos >= 0 && pos < a.T ? h * a.cell_stride + pos * a.row_stride : -1;
+            }
+        }
+        const bool off = __any_sync(FW_FULL, lane < rows && at < 0);
+        if (off && lane == 0 && a.status) atomicMax(a.status + h, FW_ERR_INVALID_ARG);
+        const int64_t to = ((int64_t)a.list[g] * s.P + j0 % s.P) * D;
+        copy_rows<D>(s.k + to, s.v + to, 0, rows, lane, [&](int r, const uint16_t *&k, const uint16_t *&v) {
+            const int64_t f = __shfl_sync(FW_FULL, at, r);
+            k = f >= 0 ? (OWN ? s.k : a.K) + f : nullptr;
+            v = f >= 0 ? (OWN ? s.v : a.V) + f : nullptr;
+        });
+    }
+}
+
+// Entries of a cell that go: their pages are named by one less.
+__device__ __forceinline__ void give_back(const Pages &s, const int32_t *row, int held)
+{
+    for (int i = threadIdx.x; i < held; i += blockDim.x) {
+        const int page = row[i];
+        if (s.is_page(page) && atomicSub(&s.refs[page], 1) == 1) atomicOr(&s.bits[page / 32], 1u << (page % 32));
+    }
+}
+
+// The cells' new tables, and the pages that they held given back: a CTA per cell.
+__global__ void __launch_bounds__(128) k_pages_swap(const CompactArgs a)
+{
+    const Pages &s = a.s;
+    const int h = blockIdx.x;
+    fw_status st;
+    const int n = compact_rows(a, h, st);
+    if (n < 0) return;
+    int32_t *row = s.row(h);
+    give_back(s, row, s.held[h]);
+    __syncthreads();  // every thread has read the books
+    const int need = (n + s.P - 1) / s.P;
+    for (int i = threadIdx.x; i < need; i += blockDim.x) row[i] = a.list[a.first[h] + i];
+    if (threadIdx.x == 0) {
+        s.held[h] = need;
+        s.counts[h] = n;
+    }
+}
+
+// --------------------------------------------------------------------- forks
+struct ForkArgs {
+    Pages s;
+    const int32_t *src;
+    int32_t *status;
+    int32_t *rows;   // workspace: [cells][width] the new tables
+    int32_t *count;  // workspace: [cells] the new counts, -1 where a cell stays as it is
+};
+
+// The tables that cells take over, whose pages one more entry names then: a CTA per cell.
+__global__ void __launch_bounds__(128) k_pages_fork(const ForkArgs a)
+{
+    const Pages &s = a.s;
+    const int h = blockIdx.x, from = a.src[h];
+    int n, held;
+    fw_status st = cell_rows(s, h, n, held);
+    bool bad = false;
+    int rows = -1;
+    if (from >= s.cells) st = FW_ERR_INVALID_ARG;
+    if (st == FW_OK && from != h) {
+        rows = 0;
+        if (from >= 0) st = cell_rows(s, from, rows, held);
+        if (st == FW_OK && rows > 0) {
+            const int need = (rows + s.P - 1) / s.P;
+            const int32_t *row = s.row(from);
+            int32_t *to = a.rows + (int64_t)h * s.width;
+            for (int i = threadIdx.x; i < need; i += blockDim.x) {
+                to[i] = row[i];
+                bad |= !s.is_page(row[i]);
+            }
+            bad = __syncthreads_or(bad);
+            if (bad)
+                st = FW_ERR_INVALID_ARG;
+            else
+                for (int i = threadIdx.x; i < need; i += blockDim.x) atomicAdd(&s.refs[to[i]], 1);
+        }
+    }
+    if (threadIdx.x == 0) {
+        a.count[h] = st == FW_OK ? rows : -1;
+        if (a.status) a.status[h] = st;
+    }
+}
+// Their old pages given back, behind all that took some over.
+__global__ void __launch_bounds__(128) k_pages_fork_end(const ForkArgs a)
+{
+    const Pages &s = a.s;
+    const int h = blockIdx.x, n = a.count[h];
+    if (n < 0) return;
+    int32_t *row = s.row(h);
+    give_back(s, row, s.held[h]);
+    __syncthreads();
+    const int need = (n + s.P - 1) / s.P;
+    for (int i = threadIdx.x; i < need; i += blockDim.x) row[i] = a.rows[(int64_t)h * s.width + i];
+    if (threadIdx.x == 0) {
+        s.held[h] = need;
+        s.counts[h] = n;
+    }
+}
+
+size_t append_list(const fw_pages &p, int m)
+{
+    const int64_t touched = ((int64_t)m + p.page_rows - 2) / p.page_rows + 1;
+    return (size_t)std::min<int64_t>(p.num_pages, touched * p.cells);
+}
+size_t compact_list(const fw_pages &p, int64_t total)
+{
+    // (offsets out of order may name the same positions for several cells)
+    const int64_t each = std::min<int64_t>(p.max_pages, (total + p.page_rows - 1) / p.page_rows);
+    return (size_t)std::min<int64_t>(p.num_pages, each * p.cells);
+}
+
+}  // namespace
+
+size_t pages_append_workspace(const fw_pages &p, int m)
+{
+    return align256(((size_t)p.cells + 1) * 4) + align256((size_t)p.cells * 8) + align256(append_list(p, m) * 4);
+}
+
+fw_status pages_append(const fw_pages &p, const fw_pages_new &r, int32_t *status, void *ws, cudaStream_t st)
+{
+    uint8_t *w = (uint8_t *)ws;
+    AppendArgs a{view(p), r.m, r.kv_heads, (const uint16_t *)r.k, (const uint16_t *)r.v, r.k_seq, r.k_tok, r.k_head,
+                 r.v_seq, r.v_tok, r.v_head, status, (int32_t *)w, nullptr, nullptr};
+    w += align256(((size_t)p.cells + 1) * 4);
+    a.plan = (int2 *)w;
+    a.list = (int32_t *)(w + align256((size_t)p.cells * 8));
+    const int units = (p.page_rows - 1 + r.m + UR - 1) / UR;
+    const unsigned grid = (unsigned)(((int64_t)p.cells * units + MW - 1) / MW);
+    FW_LAUNCH(k_pages_plan<AppendArgs>, 1, PT, 0, st, a);
+    if (p.d == 128)
+        FW_LAUNCH(k_pages_append<128>, grid, 32 * MW, 0, st, a, units);
+    else
+        FW_LAUNCH(k_pages_append<64>, grid, 32 * MW, 0, st, a, units);
+    return FW_OK;
+}
+
+size_t pages_compact_workspace(const fw_pages &p, int64_t total)
+{
+    return align256(((size_t)p.cells + 1) * 4) + 256 + align256(compact_list(p, total) * 4);
+}
+
+fw_status pages_compact(const fw_pages &p, const void *K, const void *V, int T, int64_t cell_stride, int64_t row_stride,
+                        const int64_t *offsets, const int32_t *kept_pos, int64_t total, int32_t *status, void *ws,
+                        cudaStream_t s)
+{
+    int sms = 0;
+    const fw_status st = device_sms(&sms);
+    if (st != FW_OK) return st;
+    uint8_t *w = (uint8_t *)ws;
+    CompactArgs a{view(p), (const uint16_t *)K, (const uint16_t *)V, T, cell_stride, row_stride, offsets, kept_pos, total,
+                  status, (int32_t *)w, nullptr, nullptr};
+    w += align256(((size_t)p.cells + 1) * 4);
+    a.granted = (int32_t *)w;
+    a.list = (int32_t *)(w + 256);
+    FW_LAUNCH(k_pages_plan<CompactArgs>, 1, PT, 0, s, a);
+    const unsigned grid = (unsigned)sms * 4;
+    if (K) {
+        if (p.d == 128)
+            FW_LAUNCH((k_pages_move<128, false>), grid, 32 * MW, 0, s, a);
+        else
+            FW_LAUNCH((k_pages_move<64, false>), grid, 32 * MW, 0, s, a);
+    } else {
+        if (p.d == 128)
+            FW_LAUNCH((k_pages_move<128, true>), grid, 32 * MW, 0, s, a);
+        else
+            FW_LAUNCH((k_pages_move<64, true>), grid, 32 * MW, 0, s, a);
+    }
+    FW_LAUNCH(k_pages_swap, (unsigned)p.cells, 128, 0, s, a);
+    return FW_OK;
+}
+
+size_t pages_fork_workspace(const fw_pages &p)
+{
+    return align256((size_t)p.cells * 4) + align256((size_t)p.cells * p.max_pages * 4);
+}
+
+fw_status pages_fork(const fw_pages &p, const int32_t *src, int32_t *status, void *ws, cudaStream_t s)
+{
+    uint8_t *w = (uint8_t *)ws;
+    const ForkArgs a{view(p), src, status, (int32_t *)(w + align256((size_t)p.cells * 4)), (int32_t *)w};
+    FW_LAUNCH(k_pages_fork, (unsigned)p.cells, 128, 0, s, a);
+    FW_LAUNCH(k_pages_fork_end, (unsigned)p.cells, 128, 0, s, a);
+    return FW_OK;
+}
+
+}  // namespace fw

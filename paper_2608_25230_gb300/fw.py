@@ -68,6 +68,44 @@ class FwCache8Query(C.Structure):
                 ("q_tok", C.c_int64), ("q_head", C.c_int64), ("scale", C.c_float)]
 
 
+class FwPages(C.Structure):
+    _fields_ = [("cells", C.c_int32), ("d", C.c_int32), ("page_rows", C.c_int32), ("num_pages", C.c_int32),
+                ("max_pages", C.c_int32), ("k", vp), ("v", vp), ("table", vp), ("held", vp), ("counts", vp), ("refs", vp),
+                ("free_bits", vp), ("next", vp)]
+
+
+class FwPagesNew(C.Structure):
+    _fields_ = [("kv_heads", C.c_int32), ("m", C.c_int32), ("k", vp), ("v", vp), ("k_seq", C.c_int64), ("k_tok", C.c_int64),
+                ("k_head", C.c_int64), ("v_seq", C.c_int64), ("v_tok", C.c_int64), ("v_head", C.c_int64)]
+
+
+class FwPagesQuery(C.Structure):
+    _fields_ = [("kv_heads", C.c_int32), ("group", C.c_int32), ("m", C.c_int32), ("longest", C.c_int32), ("q", vp),
+                ("q_seq", C.c_int64), ("q_tok", C.c_int64), ("q_head", C.c_int64), ("scale", C.c_float)]
+
+
+class FwRotation(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32), ("rot", C.c_int32),
+                ("interleaved", C.c_int32), ("w_dtype", C.c_int32), ("eps", C.c_float), ("q", vp), ("k", vp), ("q_out", vp),
+                ("k_out", vp), ("q_weight", vp), ("k_weight", vp), ("pos", vp), ("inv_freq", vp), ("q_row", C.c_int64),
+                ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64), ("q_out_row", C.c_int64),
+                ("q_out_head", C.c_int64), ("k_out_row", C.c_int64), ("k_out_head", C.c_int64)]
+
+
+_lib.fw_pages_append.argtypes = [C.POINTER(FwPages), C.POINTER(FwPagesNew), vp, vp, C.c_size_t, vp]
+_lib.fw_pages_append_workspace.argtypes = [C.POINTER(FwPages), C.c_int32]
+_lib.fw_pages_append_workspace.restype = C.c_size_t
+_lib.fw_pages_compact.argtypes = [C.POINTER(FwPages), vp, vp, C.c_int32, C.c_int64, C.c_int64, vp, vp, C.c_int64, vp, vp,
+                                  C.c_size_t, vp]
+_lib.fw_pages_compact_workspace.argtypes = [C.POINTER(FwPages), C.c_int64]
+_lib.fw_pages_compact_workspace.restype = C.c_size_t
+_lib.fw_pages_fork.argtypes = [C.POINTER(FwPages), vp, vp, vp, C.c_size_t, vp]
+_lib.fw_pages_fork_workspace.argtypes = [C.POINTER(FwPages)]
+_lib.fw_pages_fork_workspace.restype = C.c_size_t
+_lib.fw_pages_attend.argtypes = [C.POINTER(FwPages), C.POINTER(FwPagesQuery), vp, vp, vp, vp, C.c_size_t, vp]
+_lib.fw_pages_attend_workspace.argtypes = [C.POINTER(FwPages), C.POINTER(FwPagesQuery)]
+_lib.fw_pages_attend_workspace.restype = C.c_size_t
+_lib.fw_qk_rotate.argtypes = [C.POINTER(FwRotation), vp]
 _lib.fw_prompt_attention.argtypes = [C.POINTER(FwPrompt), vp, vp, vp, vp]
 _lib.fw_cache8_compact.argtypes = [C.POINTER(FwCache8), vp, vp, C.c_int32, C.c_int64, C.c_int64, vp, vp, C.c_int64, vp,
                                    vp]
@@ -127,7 +165,8 @@ _lib.fw_status_string.restype = C.c_char_p
 _lib.fw_launch_count.restype = C.c_uint64
 for _f in ("fw_dense_and_topk_gap", "fw_swap_refine", "fw_best_subset", "fw_contour_alloc", "fw_ragged_compact",
            "fw_group_vote", "fw_pool_best_subset", "fw_sync_status", "fw_prompt_attention", "fw_cache8_compact",
-           "fw_cache8_append", "fw_cache8_attend"):
+           "fw_cache8_append", "fw_cache8_attend", "fw_pages_append", "fw_pages_compact", "fw_pages_fork", "fw_pages_attend",
+           "fw_qk_rotate"):
     getattr(_lib, _f).restype = C.c_int
 
 
@@ -736,6 +775,269 @@ def cache8_attend(cache: Cache8, q: torch.Tensor, *, kv_heads: int, scale: float
     if st != FW_OK:
         raise FwError(st, "fw_cache8_attend")
     return out
+
+
+class Pages:
+    """A cache of bf16 rows in pages (fw_pages) over the caller's tensors: the pool k, v [pages][16, 32, 64 or 128][d], and
+    int32 books: table [cells][entries], held and counts [cells], refs [pages], free [ceil(pages / 32)] and next [1]."""
+
+    def __init__(self, *, k, v, table, held, counts, refs, free, next):
+        _need(k.dim() == 3 and k.dtype == v.dtype == torch.bfloat16 and k.shape == v.shape,
+              "k and v are bfloat16 [pages][page_rows][d]")
+        num, rows, d = k.shape
+        _need(num >= 1 and rows in (16, 32, 64, 128) and d in (64, 128), "pages of 16, 32, 64 or 128 rows of 64 or 128")
+        _need(table.dim() == 2 and table.shape[0] >= 1 and table.shape[1] >= 1, "table is [cells][entries]")
+        cells, width = table.shape
+        _need(held.numel() == counts.numel() == cells and refs.numel() == num and free.numel() == (num + 31) // 32 and
+              next.numel() == 1, "held and counts are [cells], refs [pages], free [ceil(pages / 32)], next [1]")
+        self.tensors = (k, v, table, held, counts, refs, free, next)
+        _need(all(t.dtype == torch.int32 for t in self.tensors[2:]), "the books are int32")
+        _need(all(t.is_contiguous() for t in self.tensors), "the tensors are contiguous")
+        _one_device(*self.tensors)
+        self.k, self.v, self.table, self.held, self.counts, self.refs, self.free, self.next = self.tensors
+        self.page_rows, self.num_pages, self.max_pages = rows, num, width
+        self.d, self.cells, self.device, self.index, self.book = d, cells, k.device, k.get_device(), None
+        self.c = FwPages(cells, d, rows, num, width, *(t.data_ptr() for t in self.tensors))
+        self._ref = C.byref(self.c)
+
+    def part(self, first: int, cells: int) -> "Pages":
+        """The cells first .. first + cells (a layer's, say) as a cache of their own over the same pool."""
+        _need(0 <= first and cells >= 1 and first + cells <= self.cells, "cells within the cache's")
+        cut = slice(first, first + cells)
+        return Pages(k=self.k, v=self.v, table=self.table[cut], held=self.held[cut], counts=self.counts[cut],
+                     refs=self.refs, free=self.free, next=self.next)
+
+
+def pages_empty(cells: int, num_pages: int, d: int, *, max_pages: int, page_rows: int = 32, device="cuda") -> Pages:
+    """A new cache: a pool of num_pages pages and tables of max_pages entries.  All its books lie in one tensor, `book`: a
+    copy of that takes a step back, as long as no page that it handed out or gave back has been written since."""
+    sizes = dict(next=1, counts=cells, held=cells, table=cells * max_pages, refs=num_pages, free=(num_pages + 31) // 32)
+    book = torch.zeros(sum((n + 3) // 4 * 4 for n in sizes.values()), dtype=torch.int32, device=device)
+    at, b = 0, {}
+    for name, n in sizes.items():
+        b[name] = book[at:at + n]
+        at += (n + 3) // 4 * 4
+    b["table"] = b["table"].view(cells, max_pages)
+    b["free"].fill_(-1)
+    pool = dict(dtype=torch.bfloat16, device=device)
+    p = Pages(k=torch.empty(num_pages, page_rows, d, **pool), v=torch.empty(num_pages, page_rows, d, **pool), **b)
+    p.book = book
+    return p
+
+
+def _pages_ws(workspace, nbytes, pages, stream):
+    """(pointer, bytes, what keeps it alive) of a call's workspace: the caller's, checked, or a new one."""
+    if workspace is None:
+        with _made_on(stream):
+            workspace = _ws(nbytes(), pages.device)
+    elif workspace.get_device() != pages.index or not workspace.is_contiguous():
+        raise ValueError("workspace is contiguous on the cache's GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def pages_append_workspace(pages: Pages, m: int) -> torch.Tensor:
+    """A workspace for pages_append calls of up to m rows a cell (fw_pages_append_workspace)."""
+    _on_current(pages.index)
+    return _ws(_lib.fw_pages_append_workspace(pages._ref, m), pages.device)
+
+
+def pages_append(pages: Pages, new_k: torch.Tensor, new_v: torch.Tensor, *, status: torch.Tensor = None, workspace=None,
+                 stream=None):
+    """fw_pages_append: new_k, new_v (bf16 [sequences][m][kv_heads][d], any strides that are multiples of 8 with d
+    contiguous) behind the rows of the cells [sequences][kv_heads].  A workspace (pages_append_workspace) serves one call at a
+    time."""
+    seqs, m, heads, d = new_k.shape
+    if new_k.dtype is not torch.bfloat16 or new_v.dtype is not torch.bfloat16 or new_v.shape != new_k.shape:
+        raise ValueError("new_k and new_v are bfloat16 [sequences][m][kv_heads][d]")
+    if m < 1 or heads < 1 or seqs * heads != pages.cells or d != pages.d:
+        raise ValueError("sequences x kv_heads is the cache's cells, d the cache's, and there is a row")
+    (k0, k1, k2, k3), (v0, v1, v2, v3) = new_k.stride(), new_v.stride()
+    if k3 != 1 or v3 != 1:
+        raise ValueError("d is the contiguous axis of new_k and new_v")
+    if not new_k.get_device() == new_v.get_device() == pages.index:
+        raise ValueError("the tensors of a call are on the cache's GPU")
+    handle = _raw_stream(stream, pages.index)
+    # (strides of axes of one entry, which torch leaves open)
+    if seqs == 1:
+        k0 = v0 = 0
+    if m == 1:
+        k1 = v1 = 0
+    if heads == 1:
+        k2 = v2 = 0
+    rows = FwPagesNew(heads, m, new_k.data_ptr(), new_v.data_ptr(), k0, k1, k2, v0, v1, v2)
+    ws, size, _keep = _pages_ws(workspace, lambda: _lib.fw_pages_append_workspace(pages._ref, m), pages, stream)
+    st = _lib.fw_pages_append(pages._ref, C.byref(rows), _status_ptr(status, pages), ws, size, handle)
+    if st != FW_OK:
+        raise FwError(st, "fw_pages_append")
+
+
+def pages_compact_workspace(pages: Pages, total: int) -> torch.Tensor:
+    """A workspace for pages_compact and pages_keep calls of up to `total` kept positions (fw_pages_compact_workspace)."""
+    _on_current(pages.index)
+    return _ws(_lib.fw_pages_compact_workspace(pages._ref, total), pages.device)
+
+
+def _pages_compact(pages, K, V, T, cs, rs, offsets, kept_pos, status, workspace, stream):
+    if offsets.dtype is not torch.int64 or offsets.numel() != pages.cells + 1 or kept_pos.dtype is not torch.int32 or not (
+            offsets.is_contiguous() and kept_pos.is_contiguous()):
+        raise ValueError("offsets is contiguous int64 [cells + 1], kept_pos contiguous int32")
+    if not offsets.get_device() == kept_pos.get_device() == pages.index:
+        raise ValueError("the tensors of a call are on the cache's GPU")
+    handle, total = _raw_stream(stream, pages.index), kept_pos.numel()
+    ws, size, _keep = _pages_ws(workspace, lambda: _lib.fw_pages_compact_workspace(pages._ref, total), pages, stream)
+    st = _lib.fw_pages_compact(pages._ref, K, V, T, cs, rs, offsets.data_ptr(), kept_pos.data_ptr(), total,
+                               _status_ptr(status, pages), ws, size, handle)
+    if st != FW_OK:
+        raise FwError(st, "fw_pages_compact")
+
+
+def pages_compact(pages: Pages, K: torch.Tensor, V: torch.Tensor, offsets: torch.Tensor, kept_pos: torch.Tensor, *,
+                  status: torch.Tensor = None, workspace=None, stream=None):
+    """fw_pages_compact: the kept rows of K, V (bf16 [cells][T][d], equal strides that are multiples of 8, d contiguous)
+    become the cells' rows, in pages taken for them; those that the cells held are given back.  A workspace
+    (pages_compact_workspace) serves one call at a time."""
+    cells, T, d = K.shape
+    if K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16 or V.shape != K.shape or cells != pages.cells or \
+            d != pages.d:
+        raise ValueError("K and V are bfloat16 [cells][T][d], as the cache's")
+    (cs, rs, one), (vcs, vrs, vone) = K.stride(), V.stride()
+    if cells == 1:
+        cs = vcs = T * d
+    if T == 1:
+        rs = vrs = d
+    if one != 1 or vone != 1 or cs != vcs or rs != vrs:
+        raise ValueError("K and V have equal strides and d contiguous")
+    if not K.get_device() == V.get_device() == pages.index:
+        raise ValueError("the tensors of a call are on the cache's GPU")
+    _pages_compact(pages, K.data_ptr(), V.data_ptr(), T, cs, rs, offsets, kept_pos, status, workspace, stream)
+
+
+def pages_keep(pages: Pages, offsets: torch.Tensor, kept_pos: torch.Tensor, *, status: torch.Tensor = None, workspace=None,
+               stream=None):
+    """fw_pages_compact of the cells' own rows: cell h keeps its rows kept_pos[offsets[h]:offsets[h + 1]], in that order."""
+    _pages_compact(pages, None, None, 0, 0, 0, offsets, kept_pos, status, workspace, stream)
+
+
+def pages_fork_workspace(pages: Pages) -> torch.Tensor:
+    """A workspace for pages_fork calls (fw_pages_fork_workspace)."""
+    _on_current(pages.index)
+    return _ws(_lib.fw_pages_fork_workspace(pages._ref), pages.device)
+
+
+def pages_fork(pages: Pages, src: torch.Tensor, *, status: torch.Tensor = None, workspace=None, stream=None):
+    """fw_pages_fork: cell h becomes what cell src[h] was (int32 [cells]; itself: unchanged, negative: emptied), sharing its
+    pages.  A workspace (pages_fork_workspace) serves one call at a time."""
+    if src.dtype is not torch.int32 or src.numel() != pages.cells or not src.is_contiguous() or src.get_device() != pages.index:
+        raise ValueError("src is contiguous int32 [cells] on the cache's GPU")
+    handle = _raw_stream(stream, pages.index)
+    ws, size, _keep = _pages_ws(workspace, lambda: _lib.fw_pages_fork_workspace(pages._ref), pages, stream)
+    st = _lib.fw_pages_fork(pages._ref, src.data_ptr(), _status_ptr(status, pages), ws, size, handle)
+    if st != FW_OK:
+        raise FwError(st, "fw_pages_fork")
+
+
+def _pages_query(pages, q, kv_heads, scale, longest):
+    seqs, m, hq, d = q.shape
+    s0, s1, s2, one = q.stride()
+    if q.dtype is not torch.bfloat16 or one != 1 or d != pages.d:
+        raise ValueError("q is bfloat16 [sequences][m][heads][d], d contiguous and the cache's")
+    if kv_heads < 1 or hq % kv_heads or seqs * kv_heads != pages.cells:
+        raise ValueError("sequences x kv_heads is the cache's cells, heads a multiple of kv_heads")
+    # (strides of axes of one entry, which torch leaves open)
+    return FwPagesQuery(kv_heads, hq // kv_heads, m, longest, q.data_ptr(), s0 if seqs > 1 else d, s1 if m > 1 else d,
+                        s2 if hq > 1 else d, 1.0 / math.sqrt(d) if scale is None else scale)
+
+
+def pages_attend_workspace(pages: Pages, q: torch.Tensor, *, kv_heads: int, longest: int = 0) -> torch.Tensor:
+    """A workspace for pages_attend calls with queries of q's shape and this `longest` (fw_pages_attend_workspace)."""
+    c_q = _pages_query(pages, q, kv_heads, None, longest)
+    _on_current(pages.index)
+    return _ws(_lib.fw_pages_attend_workspace(pages._ref, C.byref(c_q)), pages.device)
+
+
+def pages_attend(pages: Pages, q: torch.Tensor, *, kv_heads: int, scale: float = None, longest: int = 0, out=None,
+                 workspace=None, stream=None):
+    """fw_pages_attend.  q: bf16 [sequences][m][q_heads][d] (strides multiples of 8, d contiguous), the queries of each
+    sequence's last m tokens; the cells are [sequences][kv_heads].  longest: a bound on the cells' rows where the caller has one
+    (it chooses how the work is split).  Returns a dict of o (bf16, as q), lse (fp32 [sequences][m][q_heads]) and status
+    [cells]; such a dict passed as out is written instead.  A workspace (pages_attend_workspace) serves one call at a time."""
+    c_q = _pages_query(pages, q, kv_heads, scale, longest)
+    if q.get_device() != pages.index:
+        raise ValueError("q is on the cache's GPU")
+    handle = _raw_stream(stream, pages.index)
+    o, lse, status, out = _attention_out(out, q, pages.cells, stream)
+    ws, size, _keep = _pages_ws(workspace, lambda: _lib.fw_pages_attend_workspace(pages._ref, C.byref(c_q)), pages, stream)
+    st = _lib.fw_pages_attend(pages._ref, C.byref(c_q), o, lse, status, ws, size, handle)
+    if st != FW_OK:
+        raise FwError(st, "fw_pages_attend")
+    return out
+
+
+def _rotation_strides(x, what):
+    rows, heads, d = x.shape
+    r, h, one = x.stride()
+    if one != 1:
+        raise ValueError(f"d is the contiguous axis of {what}")
+    # (strides of axes of one entry, which torch leaves open)
+    h = h if heads > 1 else d
+    return (r if rows > 1 else heads * d), h
+
+
+def qk_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, *,
+              q_weight: torch.Tensor = None, k_weight: torch.Tensor = None, eps: float = None, interleaved: bool = False,
+              out=None, stream=None):
+    """fw_qk_rotate.  q, k: bf16 [rows][heads][d] (strides multiples of 8, d contiguous; k None: queries alone); positions:
+    int32 [rows]; inv_freq: float32 [rot / 2].  eps None: no norm; else each head is normed, with q_weight and k_weight ([d],
+    bfloat16 or float32, both alike) where they are given.  Returns (q, k) rotated; such a pair passed as out (the inputs
+    themselves, if wished) is written instead."""
+    bf16, both = torch.bfloat16, [x for x in (q, k) if x is not None]
+    if any(x.dtype is not bf16 or x.dim() != 3 for x in both) or (k is not None and (k.shape[0], k.shape[2]) != (
+            q.shape[0], q.shape[2])):
+        raise ValueError("q and k are bfloat16 [rows][heads][d], rows and d alike")
+    rows, hq, d = q.shape
+    if positions.dtype is not torch.int32 or positions.shape != (rows,) or inv_freq.dtype is not torch.float32 or \
+            inv_freq.dim() != 1 or not (positions.is_contiguous() and inv_freq.is_contiguous()):
+        raise ValueError("positions is contiguous int32 [rows], inv_freq contiguous float32 [rot / 2]")
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    if weights and eps is None:
+        raise ValueError("weights belong to a norm: eps is given with them")
+    if any(w.shape != (d,) or not w.is_contiguous() or w.dtype not in (bf16, torch.float32) or w.dtype != weights[0].dtype
+           for w in weights):
+        raise ValueError("q_weight and k_weight are contiguous [d], both bfloat16 or both float32")
+    if eps is not None and not eps >= 0:
+        raise ValueError("eps is not negative")
+    index = q.get_device()
+    if any(t.get_device() != index for t in (*both, positions, inv_freq, *weights)) or index < 0:
+        raise ValueError("the tensors of a call are on one GPU")
+    handle = _raw_stream(stream, index)
+    if out is None:
+        with _made_on(stream):
+            out = tuple(None if x is None else torch.empty(x.shape, dtype=bf16, device=x.device) for x in (q, k))
+        if stream is not None:  # the caller reads them on the current one
+            for t in out:
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream(q.device))
+    else:
+        for x, y in zip((q, k), out):
+            if x is not None and (y is None or y.shape != x.shape or y.dtype is not bf16 or y.get_device() != index):
+                raise ValueError("out is (q, k) of the inputs' shapes, bfloat16 on their GPU")
+    qo, ko = out
+    none = (None, 0, 0)
+    (qp, qr, qh), (qop, qor, qoh), (kp, kr, kh), (kop, kor, koh) = (
+        none if x is None else (x.data_ptr(), *_rotation_strides(x, w))
+        for x, w in ((q, "q"), (qo, "out's q"), (k, "k"), (None if k is None else ko, "out's k")))
+    r = FwRotation(rows, hq, 0 if k is None else k.shape[1], d, 2 * inv_freq.numel(), int(bool(interleaved)),
+                   FW_BF16 if weights and weights[0].dtype is bf16 else FW_F32, -1.0 if eps is None else eps, qp, kp, qop, kop,
+                   _raw(q_weight), _raw(k_weight), positions.data_ptr(), inv_freq.data_ptr() or None, qr, qh, kr, kh, qor, qoh,
+                   kor, koh)
+    st = _lib.fw_qk_rotate(C.byref(r), handle)
+    if st != FW_OK:
+        raise FwError(st, "fw_qk_rotate")
+    return out
+
+
+def _raw(t):
+    return None if t is None else t.data_ptr()
 
 
 def raw():
