@@ -185,6 +185,8 @@ static fw_status check_pages_query(const fw_pages *p, const fw_pages_query *q)
         !(q->scale > 0.f) || !(q->scale < 1e30f))
         return FW_ERR_INVALID_ARG;
     if ((int64_t)q->group * q->m > 65535) return FW_ERR_UNSUPPORTED;
+    // (blocks of 16 rows are numbered over all cells)
+    if ((int64_t)p->cells * p->max_pages * (p->page_rows / 16) >= ((int64_t)1 << 31)) return FW_ERR_UNSUPPORTED;
     if (!q->q || !aligned(q->q, 16) || !multiple_of_8(q->q_seq) || !multiple_of_8(q->q_tok) || !multiple_of_8(q->q_head))
         return FW_ERR_INVALID_ARG;
     return FW_OK;

@@ -2,106 +2,957 @@
 // of m sees the rows j < n - m + 1 + i:
 //   x_j = scale (q . k_j),  o = sum_j softmax_j(x) v_j,  lse = log sum_j e^x_j.
 //
-// A CTA per cell and query row, a running maximum and sum per warp, joined at the end.
+// Bound: the rows' bytes, each read once from memory.  Two ways over the cells:
+//   few short cells (k_pages_attend_few): a cluster of CTAs per cell, its blocks dealt out to all their
+//   warps, whose states are joined through (distributed) shared memory;
+//   many (k_pages_attend): the blocks of all cells in a row are divided evenly over the teams of
+//   the GPU, whatever the cells' lengths, so a team takes the end of one cell, whole cells and the
+//   start of another, and waits for no other; the parts of cells that several teams share go to the
+//   workspace, and a second kernel, launched behind the first one's tail, joins them in their order.
+// A team is a warp, or where the query rows do not fit one warp's registers 2, 4 or 8 warps, which read the same
+// blocks against other query rows.  It fetches its blocks by TMA into a ring of its own, through page
+// numbers that its first warp has read 32 blocks ahead.
+//
+// A block is 16 rows, so it lies in one page whatever the pages' size.  Against 8 query rows, transposed on the
+// warp-wide bf16 tensor instructions (a few query rows cannot fill a tcgen05 tile, and the stream
+// of rows leaves the slower instructions mostly idle): S^T = K Q^T, then O^T += V^T P^T.  The weights enter as the sum
+// of two bf16 numbers, the upper half of the fp32 weight's bits and what that leaves, so that 16
+// bits of each count; both are positive where the weight is, so that an infinite value stays one.
 #include <algorithm>
 
 #include <cuda_bf16.h>
 
 #include "fw_pages.cuh"
+#include "tc_sm100.cuh"
 
 namespace fw {
 namespace {
 
 using namespace pages;
 
-constexpr int AW = 4;
+constexpr int BR = 16;                 // rows of a block
+constexpr uint32_t A_WAIT = 1u << 22;  // polls before a wait gives up
 
 struct AttendArgs {
     Pages s;
     int kv_heads, group, m;
+    uint32_t group_inv;  // 2^32 / group + 1 (0 for a group of 1)
     const uint16_t *q;
     int64_t q_seq, q_tok, q_head;
-    float scale;
+    float scale2;  // scale * log2(e)
     uint16_t *o;
     float *lse;
     int32_t *status;
+    int G, teams;      // CTAs along the blocks, and their teams
+    int cluster;       // CTAs of a cell (few cells)
+    int32_t *start;    // workspace: [cells] first block of each cell
+    int32_t *plan;     // workspace: blocks per team
+    int32_t *flags;    // workspace: [teams][2] statuses of parts
+    float2 *part_ml;   // workspace: [tiles of rows][teams][2][rows of a tile] (max, sum)
+    float *part_o;     // workspace: the same with D columns, column 8 i + g at g D / 8 + i
 };
 
-template <int D> __global__ void __launch_bounds__(32 * AW) k_pages_attend(const AttendArgs a)
+// r / group for a query row r: both are below 2^16, so the product's upper half is exact
+__device__ __forceinline__ int token_of(const AttendArgs &a, int r) { return a.group_inv ? __umulhi(r, a.group_inv) : r; }
+
+// Blocks of a cell (0 where the cell is not valid), and its status.
+__device__ __forceinline__ int cell_blocks(const Pages &s, int h, int &n, fw_status &st)
+{
+    int held;
+    st = cell_rows(s, h, n, held);
+    if (st != FW_OK) n = 0;
+    return (n + BR - 1) / BR;
+}
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a word at this CTA's shared address p, as CTA `rank` of the cluster has it
+__device__ __forceinline__ uint32_t remote_u(const void *p, int rank)
+{
+    uint32_t v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.u32 %0, [a];\n\t}"
+                 : "=r"(v)
+                 : "r"(tc::smem_u32(p)), "r"(rank)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ float remote(const float *p, int rank) { return __uint_as_float(remote_u(p, rank)); }
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+        "%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <bool TRANS> __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
+{
+    if constexpr (TRANS)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(addr)
+                     : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(addr)
+                     : "memory");
+}
+// A box of BR rows and both halves of their columns: [half][row][64], rows swizzled over 128 bytes.
+__device__ __forceinline__ void tma_load_rows(void *dst, const void *tmap, int32_t row, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2}], "
+        "[%4];" ::"r"(tc::smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(0), "r"(row), "r"(tc::smem_u32(bar))
+        : "memory");
+}
+
+// Teams of TW warps whose warps hold NT tiles of 8 query rows.
+template <int D, int NT, int TW> struct Cfg {
+    static constexpr int W = D == 64 && NT == 1 ? 16 : 8;  // warps of a CTA
+    static constexpr int TEAMS = W / TW;
+    static constexpr int TILE = BR * D * 2;                // bytes of a block's keys, or values
+    static constexpr int STAGES = 196608 / (2 * TILE) / TEAMS;
+    static constexpr int RING = TEAMS * STAGES * 2 * TILE;
+    static constexpr size_t SMEM = 1024 + RING;
+    static constexpr int RT = TW * 8 * NT;                 // query rows of a team
+};
+
+// Byte offset of piece x (16 bytes, 8 columns) of row r in a tile.
+__device__ __forceinline__ int piece(int r, int x) { return (x >> 3) * (BR * 128) + r * 128 + (((x ^ r) & 7) << 4); }
+
+// A team's ring of blocks.  Its first warp fetches; with more warps each says that it has read a block.
+template <int D, int STAGES, int TW> struct Ring {
+    static constexpr int TILE = BR * D * 2;
+    uint8_t *mem;
+    uint64_t *full, *empty;
+    int32_t *page;  // of the stages' blocks, -1: none
+    int issued = 0, used = 0;
+    bool ok = true;
+
+    __device__ void init(int lane, int member)
+    {
+        if (member == 0)
+            for (int i = lane; i < STAGES; i += 32) {
+                tc::mbar_init(&full[i], 1);
+                if (TW > 1) tc::mbar_init(&empty[i], TW);
+            }
+        tc::mbar_init_fence();
+    }
+    // block of BR rows from row `at` of page `pg` (the first warp)
+    __device__ void fetch(const CUtensorMap *tmK, const CUtensorMap *tmV, const Pages &s, int pg, int at, int lane)
+    {
+        const int st = issued % STAGES;
+        if (TW > 1 && issued >= STAGES && ok) ok = tc::mbar_wait(&empty[st], (issued / STAGES - 1) & 1, A_WAIT);
+        if (!ok) return;
+        if (lane == 0) {
+            const bool is = s.is_page(pg);
+            page[st] = is ? pg : -1;
+            if (is) {
+                const int row = pg * s.P + at;
+                tc::mbar_arrive_expect_tx(&full[st], 2 * TILE);
+                tma_load_rows(mem + st * 2 * TILE, tmK, row, &full[st]);
+                tma_load_rows(mem + st * 2 * TILE + TILE, tmV, row, &full[st]);
+            } else {
+                tc::mbar_arrive(&full[st]);
+            }
+        }
+        ++issued;
+    }
+    // the next block's stage, or -1 where the wait gave up
+    __device__ int next()
+    {
+        const int st = used % STAGES;
+        if (ok) ok = tc::mbar_wait(&full[st], (used / STAGES) & 1, A_WAIT);
+        if (!ok) return -1;
+        ++used;
+        return st;
+    }
+    // a block has been read by every lane
+    __device__ void release(int st, int lane)
+    {
+        __syncwarp();
+        if (TW > 1 && lane == 0) tc::mbar_arrive(&empty[st]);
+    }
+    // copies still under way land before the CTA's memory goes
+    __device__ void drain()
+    {
+        for (; used < issued; ++used) tc::mbar_wait(&full[used % STAGES], (used / STAGES) & 1, A_WAIT);
+    }
+};
+
+// The pages of a walk over blocks first, first + step, ...: 32 of them at a time, one a lane.
+struct Window {
+    int from, pages;
+    // (a block's entry lies in the table whatever its number, the pages are looked at when they are fetched)
+    __device__ void load(const Pages &s, int h, int first, int step, int lane)
+    {
+        from = first;
+        const int64_t e = ((int64_t)first + (int64_t)lane * step) * BR / s.P;
+        pages = s.row(h)[e < s.width ? (int)e : s.width - 1];
+    }
+    __device__ int at(int i) const { return __shfl_sync(FW_FULL, pages, i); }
+};
+
+// A warp's queries and running softmax over blocks of one cell, NT tiles of 8 query rows.
+template <int D, int NT> struct Rows {
+    static constexpr int MT = D / 16;  // 16-column tiles of the output, and steps of the first product
+    uint32_t qf[NT][MT][2];            // row g of each 8, columns 2c, 2c + 1 (and 8 behind them) of each 16
+    float O[NT][MT][4], mx[NT][2], l[NT][2];
+
+    __device__ __forceinline__ void read(const AttendArgs &a, int seq, int hk, int row0, int lane)
+    {
+        const int g = lane >> 2, c = lane & 3, rows = a.group * a.m;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int r = row0 + 8 * t + g, i = token_of(a, r);
+            const uint16_t *src = a.q + seq * a.q_seq + i * a.q_tok + (int64_t)(hk * a.group + r - i * a.group) * a.q_head + 2 * c;
+#pragma unroll
+            for (int k = 0; k < MT; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    qf[t][k][e] = r < rows ? *reinterpret_cast<const uint32_t *>(src + 16 * k + 8 * e) : 0;
+        }
+    }
+    __device__ __forceinline__ void start()
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) mx[t][e] = -INFINITY, l[t][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[t][i][e] = 0.f;
+        }
+    }
+
+    // One block, rows BR blk .. of a cell of n, whose tile of keys lies at tk, the values' behind it.
+    __device__ __forceinline__ void block(const AttendArgs &a, const uint8_t *tk, int blk, int n, int row0, int lane)
+    {
+        const int g = lane >> 2, c = lane & 3;
+        const uint32_t ak = tc::smem_u32(tk), av = ak + BR * D * 2;
+        // S^T: keys g, g + 8 of rows 2c, 2c + 1
+        float S[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) S[t][z] = 0.f;
+        const int lr = lane & 7, lm = lane >> 3;  // the row and the matrix that a lane's address is for
+#pragma unroll
+        for (int k = 0; k < MT; ++k) {
+            uint32_t x[4];  // keys 0 .. 7, 8 .. 15 of the step's first 8 columns, then of the others
+            ldmatrix4<false>(x, ak + piece(lr + 8 * (lm & 1), 2 * k + (lm >> 1)));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma(S[t], x, qf[t][k][0], qf[t][k][1]);
+        }
+        const int j0 = blk * BR, all = n - a.m + 1;  // rows that every query sees
+        const bool masked = j0 + BR > all;
+        bool grew = false;
+        float al[NT][2];
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x0 = S[t][e] * a.scale2, x1 = S[t][2 + e] * a.scale2;
+                if (masked) {
+                    const int seen = all + token_of(a, row0 + 8 * t + 2 * c + e);
+                    if (j0 + g >= min(seen, n)) x0 = -INFINITY;
+                    if (j0 + 8 + g >= min(seen, n)) x1 = -INFINITY;
+                }
+                float top = fmaxf(x0, x1);
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 16));
+                const float old = mx[t][e], now = fmaxf(old, top);
+                grew |= now > old;
+                al[t][e] = now > old ? ex2(old - now) : 1.f;  // (0 where nothing was seen before)
+                mx[t][e] = now;
+                const float ref = now == -INFINITY ? 0.f : now;
+                S[t][e] = ex2(x0 - ref);
+                S[t][2 + e] = ex2(x1 - ref);
+                l[t][e] = fmaf(l[t][e], al[t][e], S[t][e] + S[t][2 + e]);
+            }
+            // the weights' upper halves and what they leave, a little at least where there is a weight
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                const float p0 = S[t][2 * z], p1 = S[t][2 * z + 1];
+                const float r0 = p0 - __uint_as_float(__float_as_uint(p0) & 0xffff0000u);
+                const float r1 = p1 - __uint_as_float(__float_as_uint(p1) & 0xffff0000u);
+                ph[t][z] = transpose8x8(__byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632));
+                pl[t][z] = transpose8x8(pack_bf16(p0 > 0.f ? fmaxf(r0, 0x1p-126f) : p0, p1 > 0.f ? fmaxf(r1, 0x1p-126f) : p1));
+            }
+        }
+        if (__any_sync(FW_FULL, grew)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) O[t][i][e] *= al[t][e & 1];
+        }
+        // O^T += V^T P^T: columns g, g + 8 of each 16, keys 2c, 2c + 1 and 8 behind them
+        uint32_t in0 = ~0u, in1 = ~0u;
+        bool odd = false;
+        if (masked) {
+            // rows behind the count hold anything
+            in0 = (j0 + 2 * c < n ? 0xffffu : 0u) | (j0 + 2 * c + 1 < n ? 0xffff0000u : 0u);
+            in1 = (j0 + 2 * c + 8 < n ? 0xffffu : 0u) | (j0 + 2 * c + 9 < n ? 0xffff0000u : 0u);
+            if (a.m > 1) odd = unseen_odd(tk + BR * D * 2, max(0, all - j0), min(BR, n - j0), lane);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            uint32_t x[4];  // keys 0 .. 7 of the tile's first 8 columns and of the others, then keys 8 .. 15
+            ldmatrix4<true>(x, av + piece(lr + 8 * (lm >> 1), 2 * i + (lm & 1)));
+            if (masked) {
+                x[0] &= in0, x[1] &= in0, x[2] &= in1, x[3] &= in1;
+                if (odd) {
+                    const int f = all - j0 - 2 * c;  // keys from here on are not seen by all
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) x[z] = finite_from(x[z], f - 8 * (z >> 1));
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                mma(O[t][i], x, ph[t][0], ph[t][1]);
+                mma(O[t][i], x, pl[t][0], pl[t][1]);
+            }
+        }
+        if (odd) add_odd(a, tk + BR * D * 2, S, j0, all, n, row0, lane);
+    }
+
+    // Whether rows [lo, hi) of a tile of values, which some queries do not see, hold any that are not finite: a
+    // weight of 0 times one of those is NaN.  (The last m - 1 rows of a cell, so a block or a few.)
+    __device__ static bool unseen_odd(const uint8_t *tv, int lo, int hi, int lane)
+    {
+        bool odd = false;
+        for (int p = lo * (D / 8) + lane; p < hi * (D / 8); p += 32) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(tv + piece(p / (D / 8), p % (D / 8)));
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+        }
+        return __any_sync(FW_FULL, odd);
+    }
+    // A pair of keys' values with 0 in the place of those that are not finite, of the keys from `f` on.
+    __device__ static uint32_t finite_from(uint32_t x, int f)
+    {
+        if (f <= 0 && (x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+        if (f <= 1 && (x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+        return x;
+    }
+    // What they give the rows that do see them.
+    __device__ void add_odd(const AttendArgs &a, const uint8_t *tv, const float (&P)[NT][4], int j0, int all, int n, int row0,
+                            int lane)
+    {
+        const int g = lane >> 2, c = lane & 3;
+        for (int key = max(0, all - j0); key < min(BR, n - j0); ++key) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float p = __shfl_sync(FW_FULL, key < 8 ? P[t][e] : P[t][2 + e], (key & 7) * 4 + c);
+                    if (j0 + key >= all + token_of(a, row0 + 8 * t + 2 * c + e)) continue;
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const float v = bf16_to_f32(*reinterpret_cast<const uint16_t *>(tv + piece(key, 2 * i + z) + 2 * g));
+                            if (!isfinite(v)) O[t][i][2 * z + e] += p * v;
+                        }
+                }
+        }
+    }
+
+    // The sums over all lanes of a row.
+    __device__ __forceinline__ void close()
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[t][e];
+                sum += __shfl_xor_sync(FW_FULL, sum, 4);
+                sum += __shfl_xor_sync(FW_FULL, sum, 8);
+                sum += __shfl_xor_sync(FW_FULL, sum, 16);
+                l[t][e] = sum;
+            }
+    }
+};
+
+// Index of query row r of cell (seq, hk) in the outputs.
+__device__ __forceinline__ int64_t out_row(const AttendArgs &a, int seq, int hk, int r)
+{
+    const int i = token_of(a, r);
+    return ((int64_t)seq * a.m + i) * a.kv_heads * a.group + hk * a.group + (r - i * a.group);
+}
+// lse of a row with running maximum mx and sum l of 2^(x - mx)
+__device__ __forceinline__ float lse_of(float mx, float l) { return l == 0.f ? -INFINITY : (mx + log2f(l)) * 0.6931471805599453f; }
+
+template <int D, int NT, int TW>
+__global__ void __launch_bounds__(32 * Cfg<D, NT, TW>::W, 1)
+    k_pages_attend(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
+{
+    using C = Cfg<D, NT, TW>;
+    constexpr int W = C::W, AT = 32 * W, TEAMS = C::TEAMS, MT = D / 16, RT = C::RT;
+    extern __shared__ uint8_t smraw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
+    __shared__ __align__(8) uint64_t full[TEAMS][C::STAGES], empty[TEAMS][C::STAGES];
+    __shared__ int32_t s_page[TEAMS][C::STAGES];
+    __shared__ int s_scan[W], s_h0[TEAMS], s_b0[TEAMS], s_n0[TEAMS];  // (s_*0: where each team's range begins)
+
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int team = wid / TW, member = wid % TW;
+    const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT + member * 8 * NT, rows = a.group * a.m;
+    const Pages &s = a.s;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    Ring<D, C::STAGES, TW> ring;
+    ring.mem = sm + team * C::STAGES * 2 * C::TILE;
+    ring.full = full[team];
+    ring.empty = empty[team];
+    ring.page = s_page[team];
+    ring.init(lane, member);
+
+    // ---- the blocks of all cells, divided evenly over the teams of all CTAs
+    const int per = (s.cells + AT - 1) / AT;
+    const int h_lo = min(tid * per, s.cells), h_hi = min(h_lo + per, s.cells);
+    int mine = 0, nb_lo = 0, n_lo = 0;
+    for (int h = h_lo; h < h_hi; ++h) {
+        int n;
+        fw_status st;
+        const int nb = cell_blocks(s, h, n, st);
+        if (h == h_lo) nb_lo = nb, n_lo = n;
+        mine += nb;
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(FW_FULL, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) s_scan[wid] = incl;
+    __syncthreads();
+    int total = 0, before = incl - mine;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w < wid) before += s_scan[w];
+        total += s_scan[w];
+    }
+    // consecutive ranges go to different CTAs; at least four blocks each, so that there is less to join
+    const int quota = max((total + a.G * TEAMS - 1) / (a.G * TEAMS), 4);
+    {
+        int at = before;
+        for (int h = h_lo; h < h_hi; ++h) {
+            int n = n_lo;
+            fw_status st;
+            const int nb = h == h_lo ? nb_lo : cell_blocks(s, h, n, st);
+            // the teams of this CTA whose ranges begin in the cell
+            for (int w = 0; w < TEAMS; ++w) {
+                const int64_t u = (int64_t)(w * a.G + cta) * quota;
+                if (u >= at && u < (int64_t)at + nb) {
+                    s_h0[w] = h;
+                    s_b0[w] = (int)(u - at);
+                    s_n0[w] = n;
+                }
+            }
+            if (cta == 0 && tile == 0) a.start[h] = at;
+            at += nb;
+        }
+        if (cta == 0 && tile == 0 && tid == 0) *a.plan = quota;
+    }
+    __syncthreads();
+    const int gw = team * a.G + cta;
+    const int64_t first = (int64_t)gw * quota;
+    if (first >= total) return;
+    int u = (int)first;
+    const int u1 = (int)min(first + quota, (int64_t)total);
+
+    // the team's producer: its next block to fetch, by cell
+    int pu = u, ph = s_h0[team], pb = s_b0[team], pn = s_n0[team], pnb = (pn + BR - 1) / BR;
+    fw_status pst;
+    Window win;
+    win.from = -64;
+    auto fetch = [&]() {
+        if (pu >= u1) return;
+        while (pb >= pnb && ph + 1 < s.cells) {  // (a block is left, so a cell holds it)
+            pb -= pnb;
+            pnb = cell_blocks(s, ++ph, pn, pst);
+            win.from = -64;
+        }
+        if (pb - win.from >= 32 || win.from < 0) win.load(s, ph, pb, 1, lane);
+        ring.fetch(&tmK, &tmV, s, win.at(pb - win.from), pb * BR % s.P, lane);
+        ++pu;
+        ++pb;
+    };
+    Rows<D, NT> R;
+    R.read(a, ph / a.kv_heads, ph % a.kv_heads, row0, lane);
+    if (member == 0) {
+#pragma unroll 1
+        for (int i = 0; i < C::STAGES - (TW > 1 ? 1 : 0); ++i) fetch();  // (with more warps a stage behind, so that the first
+    }                                                                   // does not wait for the others at every block)
+
+    int h = s_h0[team], b = s_b0[team];  // the segment: blocks of one cell
+    while (u < u1) {
+        int n = s_n0[team];
+        fw_status st;
+        int nb = u == (int)first ? (n + BR - 1) / BR : cell_blocks(s, h, n, st);
+        while (b >= nb && h + 1 < s.cells) {  // cells without rows, and the next cell
+            b -= nb;
+            nb = cell_blocks(s, ++h, n, st);
+        }
+        if (b >= nb) break;  // (never, unless the counts change under the call)
+        const int bend = min(nb, b + (u1 - u));
+        const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
+        if (u != (int)first) R.read(a, seq, hk, row0, lane);
+        R.start();
+        bool bad = false;
+#pragma unroll 1
+        for (int blk = b; blk < bend; ++blk) {
+            const int stage = ring.next();
+            if (stage < 0) break;
+            if (s_page[team][stage] >= 0)
+                R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
+            else
+                bad = true;
+            ring.release(stage, lane);
+            if (member == 0) fetch();
+        }
+        R.close();
+        const bool whole = b == 0 && bend == nb;
+        const int seg = u == (int)first ? 0 : 1;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float sum[2], inv[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                sum[e] = ring.ok ? R.l[t][e] : NAN;
+                inv[e] = sum[e] == 0.f ? 0.f : 1.f / sum[e];
+            }
+            if (whole) {
+                const int r = row0 + 8 * t + g;
+                uint16_t *dst = a.o + out_row(a, seq, hk, r) * D + 2 * c;
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const uint32_t x = transpose8x8(pack_bf16(R.O[t][i][2 * z] * inv[0], R.O[t][i][2 * z + 1] * inv[1]));
+                        if (r < rows) *reinterpret_cast<uint32_t *>(dst + 16 * i + 8 * z) = x;
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = row0 + 8 * t + 2 * c + e;
+                if (r >= rows) continue;
+                if (whole) {
+                    if (a.lse && g == 0) a.lse[out_row(a, seq, hk, r)] = lse_of(R.mx[t][e], sum[e]);
+                } else {
+                    const int64_t at = (((int64_t)tile * a.teams + gw) * 2 + seg) * RT + member * 8 * NT + 8 * t + 2 * c + e;
+                    if (g == 0) a.part_ml[at] = make_float2(R.mx[t][e], sum[e]);
+                    float4 *dst = reinterpret_cast<float4 *>(a.part_o + at * D + g * (D / 8));
+#pragma unroll
+                    for (int i = 0; i < MT; i += 2)
+                        dst[i / 2] = make_float4(R.O[t][i][e], R.O[t][i][2 + e], R.O[t][i + 1][e], R.O[t][i + 1][2 + e]);
+                }
+            }
+        }
+        if (tile == 0 && member == 0 && lane == 0) {
+            const int code = !ring.ok ? FW_ERR_TIMEOUT : bad ? FW_ERR_INVALID_ARG : FW_OK;
+            if (!whole)
+                a.flags[gw * 2 + seg] = code;
+            else if (a.status)
+                a.status[h] = code;
+        }
+        u += bend - b;
+        b = bend;
+    }
+    if (member == 0) ring.drain();
+}
+
+// The parts of a cell that several teams share, joined in their order; empty cells' outputs.  Each of a CTA's JW warps
+// takes a row, or (SPREAD) all of them one row's parts, where there are few rows and so the parts may be many.
+constexpr int JW = 8;
+template <int D, bool SPREAD> __global__ void __launch_bounds__(32 * JW) k_pages_join(const AttendArgs a, int RT)
 {
     constexpr int E = D / 32;
-    const Pages &s = a.s;
-    __shared__ float s_m[AW], s_l[AW], s_o[AW][D];
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, rows = a.group * a.m;
-    const int h = blockIdx.x, r = blockIdx.y, i = r / a.group, g = r - i * a.group;
-    const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
-    int n, held;
-    const fw_status st = cell_rows(s, h, n, held);
-    if (st != FW_OK) n = 0;
-    const int seen = max(0, n - a.m + 1 + i);
-    const uint16_t *q = a.q + seq * a.q_seq + i * a.q_tok + (int64_t)(hk * a.group + g) * a.q_head;
-    float qf[E], acc[E], M = -INFINITY, L = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) qf[e] = bf16_to_f32(q[lane + 32 * e]), acc[e] = 0.f;
-    bool bad = st != FW_OK;
-    for (int j = wid; j < n; j += AW) {
-        const int page = s.row(h)[j / s.P];
-        if (!s.is_page(page)) {
-            bad = true;
-            continue;
-        }
-        if (j >= seen) continue;
-        const int64_t at = ((int64_t)page * s.P + j % s.P) * D + lane;
-        float x = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x = fmaf(qf[e], bf16_to_f32(s.k[at + 32 * e]), x);
-        x = warp_sum(x) * a.scale;
-        const float now = fmaxf(M, x), ref = now == -INFINITY ? 0.f : now;
-        const float old = expf(M - ref), w = expf(x - ref);
-        L = L * old + w;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = acc[e] * old + w * bf16_to_f32(s.v[at + 32 * e]);
-        M = now;
+    __shared__ float s_o[SPREAD ? JW : 1][D];
+    __shared__ float2 s_ml[JW];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int h = blockIdx.x, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int r = SPREAD ? blockIdx.y : blockIdx.y * JW + wid;
+    int n;
+    fw_status st;
+    const int nb = cell_blocks(a.s, h, n, st), quota = *a.plan, s = a.start[h];
+    const int w0 = s / quota, w1 = nb > 0 ? (s + nb - 1) / quota + 1 : w0;  // the cell's teams
+    if (w1 == w0 + 1) return;
+    if (r >= a.group * a.m) return;  // (SPREAD: no row of the grid is)
+    const int64_t tile0 = (int64_t)(r / RT) * a.teams;
+    auto seg_of = [&](int p) { return p == w0 && s > p * quota ? 1 : 0; };
+    auto part_at = [&](int p) { return ((tile0 + p) * 2 + seg_of(p)) * RT + r % RT; };
+    if (r == 0 && a.status && (!SPREAD || wid == 0)) {
+        int code = st;
+        for (int p = w0 + lane; p < w1; p += 32) code = max(code, a.flags[p * 2 + seg_of(p)]);
+        code = __reduce_max_sync(FW_FULL, code);
+        if (lane == 0) a.status[h] = code;
     }
-    if (lane == 0) s_m[wid] = M, s_l[wid] = L;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s_o[wid][lane + 32 * e] = acc[e];
-    bad = __syncthreads_or(bad);
-    if (wid != 0) return;
-    M = -INFINITY;
-    for (int w = 0; w < AW; ++w) M = fmaxf(M, s_m[w]);
-    L = 0.f;
+    // this warp's parts: 32 maxima and sums at a time, then their columns
+    const int all = w1 - w0, each = SPREAD ? (all + JW - 1) / JW : all;
+    const int p0 = SPREAD ? w0 + min(wid * each, all) : w0, p1 = min(p0 + each, w1);
+    float M = -INFINITY, L = 0.f, acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    for (int w = 0; w < AW; ++w) {
-        const float f = M == -INFINITY ? 0.f : expf(s_m[w] - M);
-        L += f * s_l[w];
+    for (int q = p0; q < p1; q += 32) {
+        // (the columns of B parts are asked for before the maxima are looked at, and B at a time after that)
+        constexpr int B = 64 / E;
+        const int cnt = min(32, p1 - q);
+        const float2 ml = lane < cnt ? a.part_ml[part_at(q + lane)] : make_float2(-INFINITY, 0.f);
+        float f = 0.f;
+        for (int i = 0; i < cnt; i += B) {
+            float x[B][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += f * s_o[w][lane + 32 * e];
+            for (int u = 0; u < B; ++u) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[u][e] = 0.f;
+                if (i + u < cnt) {
+                    const float *src = a.part_o + part_at(q + i + u) * D + lane * E;
+                    if constexpr (E == 4) {
+                        const float4 y = *reinterpret_cast<const float4 *>(src);
+                        x[u][0] = y.x, x[u][1] = y.y, x[u][2] = y.z, x[u][3] = y.w;
+                    } else {
+                        const float2 y = *reinterpret_cast<const float2 *>(src);
+                        x[u][0] = y.x, x[u][1] = y.y;
+                    }
+                }
+            }
+            if (i == 0) {
+                const float now = fmaxf(M, warp_max(ml.x)), old = M == now ? 1.f : ex2(M - now);
+                f = ml.x == now ? 1.f : ex2(ml.x - now);
+                M = now;
+                L = fmaf(L, old, warp_sum(f * ml.y));
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] *= old;
+            }
+#pragma unroll
+            for (int u = 0; u < B; ++u) {
+                const float g = __shfl_sync(FW_FULL, f, i + u);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(g, x[u][e], acc[e]);  // (a part that is not there is 0, its factor 0 or 1)
+            }
+        }
     }
-    const int64_t out = ((int64_t)seq * a.m + i) * a.kv_heads * a.group + hk * a.group + g;
+    if constexpr (SPREAD) {
+        if (lane == 0) s_ml[wid] = make_float2(M, L);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(L == 0.f ? 0.f : acc[e] / L));
-    if (lane == 0 && a.lse) a.lse[out] = L == 0.f ? -INFINITY : M + logf(L);
-    if (lane == 0 && a.status && r == rows - 1) a.status[h] = bad ? FW_ERR_INVALID_ARG : FW_OK;
+        for (int e = 0; e < E; ++e) s_o[wid][lane * E + e] = acc[e];
+        __syncthreads();
+        if (wid != 0) return;
+        const float2 ml = lane < JW ? s_ml[lane] : make_float2(-INFINITY, 0.f);
+        M = warp_max(ml.x);
+        const float f = ml.x == M ? 1.f : ex2(ml.x - M);
+        L = warp_sum(f * ml.y);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < JW; ++w) {
+            const float g = __shfl_sync(FW_FULL, f, w);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(g, s_o[w][lane * E + e], acc[e]);
+        }
+    }
+    const int seq = h / a.kv_heads;
+    const int64_t out = out_row(a, seq, h - seq * a.kv_heads, r);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int at = lane * E + e, col = at % (D / 8) * 8 + at / (D / 8);
+        a.o[out * D + col] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
+    }
+    if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
+}
+
+// Eight states of a row joined: their (maximum, sum) and E of a lane's columns.
+template <int E, typename FM, typename FO>
+__device__ __forceinline__ void join8(FM ml_of, FO o_of, float &M, float &L, float (&acc)[E])
+{
+    float2 ml[8];
+    M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) ml[w] = ml_of(w), M = fmaxf(M, ml[w].x);
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        const float f = ml[w].x == M ? 1.f : ex2(ml[w].x - M);
+        L = fmaf(f, ml[w].y, L);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(f, o_of(w, e), acc[e]);
+    }
+}
+
+// A cluster of up to FEW CTAs per cell and tile of rows, its blocks dealt out to their warps one by one.
+constexpr int FEW = 8, FW = 8;
+template <int D, int NT>
+__global__ void __launch_bounds__(32 * FW, 1)
+    k_pages_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
+{
+    using C = Cfg<D, 2, 1>;  // (8 warps)
+    static_assert(C::W == FW && FEW == 8 && FW == 8, "a warp per row of 8, eight states to join");
+    constexpr int MT = D / 16, RT = 8 * NT, E = D / 32, LDO = D + 4;
+    extern __shared__ uint8_t smraw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
+    float *s_o = reinterpret_cast<float *>(sm);  // [FW][8][LDO], in the rings' place when these are done
+    static_assert(FW * 8 * LDO * 4 <= C::RING, "the states fit the rings");
+    __shared__ __align__(8) uint64_t full[FW][C::STAGES];
+    __shared__ int32_t s_page[FW][C::STAGES];
+    __shared__ float2 s_ml[FW][8];
+    __shared__ float2 s_pml[8];
+    __shared__ int s_code;
+
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int h = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, row0 = blockIdx.y * RT, rows = a.group * a.m;
+    const Pages &s = a.s;
+    const int first = rank + a.cluster * wid, step = a.cluster * FW;  // (the first blocks go to different CTAs)
+    Window win;
+    win.load(s, h, first, step, lane);  // (beside the counts)
+    int n;
+    fw_status st;
+    const int nb = cell_blocks(s, h, n, st);
+    if (tid == 0) s_code = st;
+    Ring<D, C::STAGES, 1> ring;
+    ring.mem = sm + wid * C::STAGES * 2 * C::TILE;
+    ring.full = full[wid];
+    ring.page = s_page[wid];
+    ring.init(lane, 0);
+    __syncthreads();
+    int pb = first;
+    auto fetch = [&]() {
+        if (pb >= nb) return;
+        int i = (pb - win.from) / step;
+        if (i >= 32) win.load(s, h, pb, step, lane), i = 0;
+        ring.fetch(&tmK, &tmV, s, win.at(i), pb * BR % s.P, lane);
+        pb += step;
+    };
+    const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
+    Rows<D, NT> R;
+    R.read(a, seq, hk, row0, lane);
+#pragma unroll 1
+    for (int i = 0; i < C::STAGES; ++i) fetch();
+    R.start();
+    bool bad = false;
+#pragma unroll 1
+    for (int blk = first; blk < nb; blk += step) {
+        const int stage = ring.next();
+        if (stage < 0) break;
+        if (s_page[wid][stage] >= 0)
+            R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
+        else
+            bad = true;
+        ring.release(stage, lane);
+        fetch();
+    }
+    R.close();
+    ring.drain();
+    const int code = !ring.ok ? FW_ERR_TIMEOUT : bad ? FW_ERR_INVALID_ARG : FW_OK;
+    if (lane == 0 && code != FW_OK) atomicMax(&s_code, code);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (t > 0 && row0 + 8 * t >= rows) break;
+        // ---- the warps' rows joined in the CTA, a warp per row
+        if (t > 0)
+            cluster_sync();  // (the rows before have been read)
+        else
+            __syncthreads();  // (the rings have been read)
+        if (g == 0) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s_ml[wid][2 * c + e] = make_float2(R.mx[t][e], ring.ok ? R.l[t][e] : NAN);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) s_o[(wid * 8 + 2 * c + e) * LDO + 16 * i + 8 * z + g] = R.O[t][i][2 * z + e];
+        __syncthreads();
+        float M, L, acc[E];
+        join8<E>([&](int w) { return s_ml[w][wid]; }, [&](int w, int e) { return s_o[(w * 8 + wid) * LDO + lane + 32 * e]; }, M, L,
+                 acc);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_o[wid * LDO + lane + 32 * e] = acc[e];  // (its row in the first warp's place)
+        if (lane == 0) s_pml[wid] = make_float2(M, L);
+        cluster_sync();
+        // ---- and over the cluster's CTAs: rows dealt out to them and their warps
+        const int r8 = rank + a.cluster * wid, r = row0 + 8 * t + r8;
+        if (r8 < 8 && r < rows) {
+            join8<E>([&](int w) { return w < a.cluster ? make_float2(remote(&s_pml[r8].x, w), remote(&s_pml[r8].y, w))
+                                                      : make_float2(-INFINITY, 0.f); },
+                     [&](int w, int e) { return w < a.cluster ? remote(&s_o[r8 * LDO + lane + 32 * e], w) : 0.f; }, M, L, acc);
+            const int64_t out = out_row(a, seq, hk, r);
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
+            if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
+        }
+        if (t == 0 && rank == 0 && blockIdx.y == 0 && wid == FW - 1 && a.status) {
+            const int codes = __reduce_max_sync(FW_FULL, lane < a.cluster ? (int)remote_u(&s_code, lane) : 0);
+            if (lane == 0) a.status[h] = codes;
+        }
+    }
+    cluster_sync();  // no CTA leaves while another reads its rows
+}
+
+// CTAs of a cell where the cells are few and hold little at most, so that a cluster each is faster, else 0.
+int cluster_of(const fw_pages &p, const fw_pages_query &q, int tiles)
+{
+    struct Rule {
+        int ctas;
+        int64_t cells, rows;
+    };
+    if (q.longest == 0) return 0;
+    for (const Rule &r : {Rule{8, 14, 8192}, Rule{4, 36, 2560}, Rule{2, 72, 1280}})
+        if ((int64_t)p.cells * tiles <= r.cells && q.longest <= r.rows) return r.ctas;
+    return 0;
+}
+
+struct Plan {
+    int few;  // CTAs of a cell's cluster, or 0
+    int G, NT, TW, teams, RT, tiles;
+    size_t start, plan, flags, ml, o, bytes;
+};
+void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
+{
+    int sms = 0;
+    if (device_sms(&sms) != FW_OK) sms = 152;  // no device: the size query still answers
+    const int rows = q.group * q.m;
+    x.NT = rows <= 8 ? 1 : 2;
+    x.TW = 1;
+    while (x.TW < 8 && x.TW * 8 * x.NT < rows) x.TW *= 2;
+    x.start = x.plan = x.flags = x.ml = x.o = x.bytes = 0;
+    x.few = cluster_of(p, q, (rows + 8 * x.NT - 1) / (8 * x.NT));
+    if (x.few) x.TW = 1;
+    x.RT = x.TW * 8 * x.NT;
+    x.tiles = (rows + x.RT - 1) / x.RT;
+    if (x.few) return;
+    x.G = std::max(1, sms / x.tiles);  // one wave
+    x.teams = x.G * ((p.d == 64 && x.NT == 1 ? 16 : 8) / x.TW);
+    x.plan = align256((size_t)p.cells * 4);
+    x.flags = x.plan + 256;
+    x.ml = x.flags + align256((size_t)x.teams * 8);
+    const size_t parts = (size_t)x.tiles * x.teams * 2 * x.RT;
+    x.o = x.ml + align256(parts * 8);
+    x.bytes = x.o + align256(parts * p.d * 4);
+}
+
+template <typename K>
+fw_status launch(K kernel, int grid, int tiles, int cluster, int threads, size_t smem, const CUtensorMap &mk,
+                 const CUtensorMap &mv, const AttendArgs &a, std::atomic<uint64_t> &done, cudaStream_t s)
+{
+    const fw_status st = big_smem((const void *)kernel, smem, done);
+    if (st != FW_OK) return st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)tiles);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mk, mv, a);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
+}
+template <int D, int NT, int TW>
+fw_status launch_ranges(const Plan &x, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
+{
+    using C = Cfg<D, NT, TW>;
+    static std::atomic<uint64_t> done{0};
+    return launch(k_pages_attend<D, NT, TW>, x.G, x.tiles, 0, 32 * C::W, C::SMEM, mk, mv, a, done, s);
+}
+template <int D, int NT>
+fw_status launch_few(const Plan &x, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
+{
+    static std::atomic<uint64_t> done{0};
+    return launch(k_pages_attend_few<D, NT>, cells * x.few, x.tiles, x.few, 32 * FW, Cfg<D, 2, 1>::SMEM, mk, mv, a, done, s);
+}
+template <int D>
+fw_status attend(const Plan &x, int cells, int rows, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a,
+                 cudaStream_t s)
+{
+    if (x.few) return x.NT == 1 ? launch_few<D, 1>(x, cells, mk, mv, a, s) : launch_few<D, 2>(x, cells, mk, mv, a, s);
+    const fw_status st = x.NT == 1   ? launch_ranges<D, 1, 1>(x, mk, mv, a, s)
+                         : x.TW == 1 ? launch_ranges<D, 2, 1>(x, mk, mv, a, s)
+                         : x.TW == 2 ? launch_ranges<D, 2, 2>(x, mk, mv, a, s)
+                         : x.TW == 4 ? launch_ranges<D, 2, 4>(x, mk, mv, a, s)
+                                     : launch_ranges<D, 2, 8>(x, mk, mv, a, s);
+    if (st != FW_OK) return st;
+    // the joining kernel starts as the first one's CTAs leave
+    const bool spread = (int64_t)cells * rows <= 2 * x.G;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)cells, (unsigned)(spread ? rows : (rows + JW - 1) / JW));
+    cfg.blockDim = dim3(32 * JW);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = spread ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true>, a, x.RT)
+                                 : cudaLaunchKernelEx(&cfg, k_pages_join<D, false>, a, x.RT);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }
 
 }  // namespace
 
-size_t pages_attend_workspace(const fw_pages &, const fw_pages_query &) { return 0; }
+size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q)
+{
+    Plan x;
+    plan_of(p, q, x);
+    return x.bytes;
+}
 
-fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, float *lse, int32_t *status, void *,
+fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, float *lse, int32_t *status, void *ws,
                        cudaStream_t s)
 {
-    const AttendArgs a{view(p), q.kv_heads, q.group, q.m, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head, q.scale,
-                       (uint16_t *)o, lse, status};
-    const dim3 grid((unsigned)p.cells, (unsigned)(q.group * q.m));
-    if (p.d == 128)
-        FW_LAUNCH(k_pages_attend<128>, grid, 32 * AW, 0, s, a);
-    else
-        FW_LAUNCH(k_pages_attend<64>, grid, 32 * AW, 0, s, a);
-    return FW_OK;
+    Plan x;
+    plan_of(p, q, x);
+    // (rows of the pool as the second axis, the halves of their columns as the third)
+    const int rows = p.num_pages * p.page_rows, halves = p.d / 64;
+    CUtensorMap mk, mv;
+    if (!make_tma_heads_bf16(&mk, p.k, 64, rows, halves, p.d, 64, BR, halves) ||
+        !make_tma_heads_bf16(&mv, p.v, 64, rows, halves, p.d, 64, BR, halves))
+        return FW_ERR_CUDA;
+    uint8_t *w = (uint8_t *)ws;
+    const uint32_t inv = q.group > 1 ? (uint32_t)(((uint64_t)1 << 32) / q.group + 1) : 0;
+    const AttendArgs a{view(p), q.kv_heads, q.group, q.m, inv, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
+                       q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, x.few ? 0 : x.G, x.few ? 0 : x.teams, x.few,
+                       (int32_t *)(w + x.start), (int32_t *)(w + x.plan), (int32_t *)(w + x.flags), (float2 *)(w + x.ml),
+                       (float *)(w + x.o)};
+    return p.d == 128 ? attend<128>(x, p.cells, q.group * q.m, mk, mv, a, s) : attend<64>(x, p.cells, q.group * q.m, mk, mv, a, s);
 }
 
 }  // namespace fw
