@@ -110,13 +110,11 @@ template <bool TRANS> __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4]
     if constexpr (TRANS)
         asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                     : "r"(addr)
-                     : "memory");
+                     : "r"(addr));
     else
         asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                     : "r"(addr)
-                     : "memory");
+                     : "r"(addr));
 }
 // A box of BR rows and both halves of their columns: [half][row][64], rows swizzled over 128 bytes.
 __device__ __forceinline__ void tma_load_rows(void *dst, const void *tmap, int32_t row, uint64_t *bar)
@@ -219,7 +217,12 @@ struct Window {
 template <int D, int NT> struct Rows {
     static constexpr int MT = D / 16;  // 16-column tiles of the output, and steps of the first product
     uint32_t qf[NT][MT][2];            // row g of each 8, columns 2c, 2c + 1 (and 8 behind them) of each 16
-    float O[NT][MT][4], mx[NT][2], l[NT][2];
+    // The weights are 2^(x - ref), ref[t][e] a maximum of row 2c + e as it was at some block, 0 where nothing was
+    // seen yet (mx has -inf there): it follows the maximum once a weight would pass 2^UP, so most blocks
+    // need no maximum over the lanes and no rescaling.
+    static constexpr float UP = 8.f;
+    float O[NT][MT][4], mx[NT][2], ref[NT][2], l[NT][2];
+    bool settled;  // every row has seen something
 
     __device__ __forceinline__ void read(const AttendArgs &a, int seq, int hk, int row0, int lane)
     {
@@ -237,10 +240,11 @@ template <int D, int NT> struct Rows {
     }
     __device__ __forceinline__ void start()
     {
+        settled = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) mx[t][e] = -INFINITY, l[t][e] = 0.f;
+            for (int e = 0; e < 2; ++e) mx[t][e] = -INFINITY, ref[t][e] = l[t][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -253,65 +257,78 @@ template <int D, int NT> struct Rows {
     {
         const int g = lane >> 2, c = lane & 3;
         const uint32_t ak = tc::smem_u32(tk), av = ak + BR * D * 2;
-        // S^T: keys g, g + 8 of rows 2c, 2c + 1
-        float S[NT][4];
+        // S^T: keys g, g + 8 of rows 2c, 2c + 1, in two sums, so that fewer products wait for one another
+        float S[NT][4], S2[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) S[t][z] = 0.f;
+            for (int z = 0; z < 4; ++z) S[t][z] = S2[t][z] = 0.f;
         const int lr = lane & 7, lm = lane >> 3;  // the row and the matrix that a lane's address is for
 #pragma unroll
         for (int k = 0; k < MT; ++k) {
             uint32_t x[4];  // keys 0 .. 7, 8 .. 15 of the step's first 8 columns, then of the others
             ldmatrix4<false>(x, ak + piece(lr + 8 * (lm & 1), 2 * k + (lm >> 1)));
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mma(S[t], x, qf[t][k][0], qf[t][k][1]);
+            for (int t = 0; t < NT; ++t) mma(k & 1 ? S2[t] : S[t], x, qf[t][k][0], qf[t][k][1]);
         }
+        uint32_t V[MT][4];  // keys 0 .. 7 of a tile's first 8 columns and of the others, then keys 8 .. 15
+#pragma unroll
+        for (int i = 0; i < MT; ++i) ldmatrix4<true>(V[i], av + piece(lr + 8 * (lm >> 1), 2 * i + (lm & 1)));
         const int j0 = blk * BR, all = n - a.m + 1;  // rows that every query sees
         const bool masked = j0 + BR > all;
-        bool grew = false;
-        float al[NT][2];
-        uint32_t ph[NT][2], pl[NT][2];
+        bool over = !settled;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float x0 = S[t][e] * a.scale2, x1 = S[t][2 + e] * a.scale2;
-                if (masked) {
-                    const int seen = all + token_of(a, row0 + 8 * t + 2 * c + e);
-                    if (j0 + g >= min(seen, n)) x0 = -INFINITY;
-                    if (j0 + 8 + g >= min(seen, n)) x1 = -INFINITY;
-                }
-                float top = fmaxf(x0, x1);
-                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 4));
-                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 8));
-                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 16));
-                const float old = mx[t][e], now = fmaxf(old, top);
-                grew |= now > old;
-                al[t][e] = now > old ? ex2(old - now) : 1.f;  // (0 where nothing was seen before)
-                mx[t][e] = now;
-                const float ref = now == -INFINITY ? 0.f : now;
-                S[t][e] = ex2(x0 - ref);
-                S[t][2 + e] = ex2(x1 - ref);
-                l[t][e] = fmaf(l[t][e], al[t][e], S[t][e] + S[t][2 + e]);
-            }
-            // the weights' upper halves and what they leave, a little at least where there is a weight
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                const float p0 = S[t][2 * z], p1 = S[t][2 * z + 1];
-                const float r0 = p0 - __uint_as_float(__float_as_uint(p0) & 0xffff0000u);
-                const float r1 = p1 - __uint_as_float(__float_as_uint(p1) & 0xffff0000u);
-                ph[t][z] = transpose8x8(__byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632));
-                pl[t][z] = transpose8x8(pack_bf16(p0 > 0.f ? fmaxf(r0, 0x1p-126f) : p0, p1 > 0.f ? fmaxf(r1, 0x1p-126f) : p1));
+                for (int z = e; z < 4; z += 2) S[t][z] += S2[t][z];
+                if (masked) {
+                    const int seen = min(all + token_of(a, row0 + 8 * t + 2 * c + e), n);
+                    if (j0 + g >= seen) S[t][e] = -INFINITY;
+                    if (j0 + 8 + g >= seen) S[t][2 + e] = -INFINITY;
+                }
+                over |= fmaf(fmaxf(S[t][e], S[t][2 + e]), a.scale2, -ref[t][e]) > UP;
             }
-        }
-        if (__any_sync(FW_FULL, grew)) {
+        if (__any_sync(FW_FULL, over)) {
+            settled = true;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(S[t][e], S[t][2 + e]);
+                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 16)) * a.scale2;
+                    // (a row moves by its own scores alone, whatever the rows beside it do)
+                    const float old = mx[t][e], now = old == -INFINITY || top > old + UP ? top : old;
+                    const float al = now > old ? ex2(old - now) : 1.f;  // (0 where nothing was seen before)
+                    mx[t][e] = now;
+                    ref[t][e] = now == -INFINITY ? 0.f : now;
+                    settled = settled && now > -INFINITY;
+                    l[t][e] *= al;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) O[t][i][e] *= al[t][e & 1];
+                    for (int i = 0; i < MT; ++i) O[t][i][e] *= al, O[t][i][2 + e] *= al;
+                }
+            settled = __all_sync(FW_FULL, settled);
+        }
+        // the weights' upper halves and what they leave, with 2^-22 of the weight more, so that it is 0 only where the
+        // weight is
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float r[4];
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                const float p = S[t][z] = ex2(fmaf(S[t][z], a.scale2, -ref[t][z & 1]));
+                r[z] = fmaf(p, 0x1p-22f, p - __uint_as_float(__float_as_uint(p) & 0xffff0000u));
+                l[t][z & 1] += p;
+            }
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                ph[t][z] = transpose8x8(__byte_perm(__float_as_uint(S[t][2 * z]), __float_as_uint(S[t][2 * z + 1]), 0x7632));
+                pl[t][z] = transpose8x8(pack_bf16(r[2 * z], r[2 * z + 1]));
+            }
         }
         // O^T += V^T P^T: columns g, g + 8 of each 16, keys 2c, 2c + 1 and 8 behind them
         uint32_t in0 = ~0u, in1 = ~0u;
@@ -322,23 +339,22 @@ template <int D, int NT> struct Rows {
             in1 = (j0 + 2 * c + 8 < n ? 0xffffu : 0u) | (j0 + 2 * c + 9 < n ? 0xffff0000u : 0u);
             if (a.m > 1) odd = unseen_odd(tk + BR * D * 2, max(0, all - j0), min(BR, n - j0), lane);
         }
+        if (masked) {
+            const int f = all - j0 - 2 * c;  // keys from here on are not seen by all
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            uint32_t x[4];  // keys 0 .. 7 of the tile's first 8 columns and of the others, then keys 8 .. 15
-            ldmatrix4<true>(x, av + piece(lr + 8 * (lm >> 1), 2 * i + (lm & 1)));
-            if (masked) {
-                x[0] &= in0, x[1] &= in0, x[2] &= in1, x[3] &= in1;
-                if (odd) {
-                    const int f = all - j0 - 2 * c;  // keys from here on are not seen by all
+            for (int i = 0; i < MT; ++i) {
+                V[i][0] &= in0, V[i][1] &= in0, V[i][2] &= in1, V[i][3] &= in1;
+                if (odd)
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) x[z] = finite_from(x[z], f - 8 * (z >> 1));
-                }
+                    for (int z = 0; z < 4; ++z) V[i][z] = finite_from(V[i][z], f - 8 * (z >> 1));
             }
+        }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                mma(O[t][i], x, ph[t][0], ph[t][1]);
-                mma(O[t][i], x, pl[t][0], pl[t][1]);
-            }
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) mma(O[t][i], V[i], ph[t][0], ph[t][1]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) mma(O[t][i], V[i], pl[t][0], pl[t][1]);
         }
         if (odd) add_odd(a, tk + BR * D * 2, S, j0, all, n, row0, lane);
     }
