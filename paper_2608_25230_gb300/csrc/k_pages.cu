@@ -10,6 +10,7 @@
 // Bound: append: latency (two launches); compaction: memory, every kept row read and written
 // once; fork: the tables' entries and their pages' counts, latency for small ones.
 #include <algorithm>
+#include <type_traits>
 
 #include "fw_pages.cuh"
 
@@ -21,7 +22,7 @@ using namespace pages;
 constexpr int UR = 16;           // rows that a warp copies at a time; no page holds less
 constexpr int MW = 8;            // warps of a CTA of the copying kernels
 constexpr int PT = 1024;         // threads of the plan's CTA
-constexpr int WORDS = 4;         // words of the free bits that one of them looks at a time
+constexpr int WORDS = 4;         // words of the free bits that one of them asks for at a time
 
 // ------------------------------------------------------------------ the plan
 struct AppendArgs {
@@ -77,6 +78,35 @@ __device__ __forceinline__ int cell_need(const AppendArgs &a, int h, fw_status &
     }
     return need;
 }
+// The same by a warp, a lane per entry (a thread takes half a microsecond for each).
+__device__ __forceinline__ int cell_need_warp(const AppendArgs &a, int h, fw_status &st)
+{
+    const int lane = threadIdx.x & 31;
+    int n, held;
+    st = cell_rows(a.s, h, n, held);
+    if (st != FW_OK) return 0;
+    const int i0 = n / a.s.P;
+    const int64_t i1 = ((int64_t)n + a.m - 1) / a.s.P;
+    if (i1 >= a.s.width) {
+        st = FW_ERR_WORKSPACE;
+        return 0;
+    }
+    const int32_t *row = a.s.row(h);
+    int need = 0;
+    bool bad = false;
+#pragma unroll 4
+    for (int i = i0 + lane; i <= (int)i1; i += 32) {
+        if (i < held && !a.s.is_page(row[i]))
+            bad = true;
+        else
+            need += append_needs(a.s, row, held, i);
+    }
+    if (__any_sync(FW_FULL, bad)) {
+        st = FW_ERR_INVALID_ARG;
+        return 0;
+    }
+    return __reduce_add_sync(FW_FULL, need);
+}
 __device__ __forceinline__ int cell_need(const CompactArgs &a, int h, fw_status &st)
 {
     int n, held;
@@ -93,6 +123,17 @@ __device__ __forceinline__ int compact_rows(const CompactArgs &a, int h, fw_stat
     cell_need(a, h, st);
     if (st != FW_OK || (a.first[h + 1] > a.first[h] && a.first[h + 1] > *a.granted)) return -1;
     return (int)(a.offsets[h + 1] - a.offsets[h]);
+}
+
+// A free page's first entry, and an entry that goes.
+__device__ __forceinline__ void take(const Pages &s, int page)
+{
+    s.refs[page] = 1;
+    atomicAnd(&s.bits[page / 32], ~(1u << (page % 32)));
+}
+__device__ __forceinline__ void give(const Pages &s, int page)
+{
+    if (atomicSub(&s.refs[page], 1) == 1) atomicOr(&s.bits[page / 32], 1u << (page % 32));
 }
 
 // Exclusive sum over the CTA's threads; `all`: the sum of all.
@@ -114,43 +155,30 @@ __device__ __forceinline__ int scan_cta(int x, int &all, int (&s_scan)[32])
     return before + incl - x;
 }
 
-// One CTA: what every cell needs, the free pages for it, and for appends the books.
-template <typename Args> __global__ void __launch_bounds__(PT) k_pages_plan(const Args a)
+// What follows a kernel in a call starts as soon as its CTAs find room, and waits for it here.
+__device__ __forceinline__ void wait_for_the_one_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_the_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// One CTA: what every cell needs, the free pages for it, and for appends the books.  WIDE: a warp per cell instead of a
+// thread, for appends that touch several pages a cell.
+template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_pages_plan(const Args a)
 {
-    constexpr bool APPEND = sizeof(Args) == sizeof(AppendArgs);
-    static_assert(sizeof(AppendArgs) != sizeof(CompactArgs), "told apart by their size");
+    constexpr bool APPEND = std::is_same<Args, AppendArgs>::value;
     __shared__ int s_scan[32], s_granted;
     const Pages &s = a.s;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    let_the_next_start();
     if (tid == 0) s_granted = 0;
 
-    int want = 0;
-    for (int b = 0; b < s.cells; b += PT) {
-        const int h = b + tid;
-        fw_status st = FW_OK;
-        const int need = h < s.cells ? cell_need(a, h, st) : 0;
-        int all;
-        const int at = want + scan_cta(need, all, s_scan);
-        if (h < s.cells) {
-            a.first[h] = at;
-            if (a.status) a.status[h] = st;
-            if constexpr (APPEND) a.plan[h] = make_int2(st == FW_OK ? s.counts[h] : -1, -1);
-        }
-        want += all;
-    }
-    if (tid == 0) a.first[s.cells] = want;
-
-    // The first `want` free pages from *next on: the words of the bits in a circle, the first one's lower
-    // part last.
-    const int words = (s.N + 31) / 32, got_most = min(want, s.N);
-    const int start = s.is_page(*s.next) ? *s.next : 0, w0 = start / 32;
-    int found = 0;
-    for (int b = 0; b <= words && found < got_most; b += PT * WORDS) {
-        uint32_t x[WORDS];
-        int pop = 0;
+    // The free bits from *next on, in a circle, the first word's lower part last; the first ones are asked for before
+    // the cells are looked at.
+    const int words = (s.N + 31) / 32, next = *s.next, start = s.is_page(next) ? next : 0, w0 = start / 32;
+    uint32_t x[WORDS];
+    auto word_of = [&](int t) { return w0 + t < words ? w0 + t : w0 + t - words; };
+    auto look = [&](int b) {
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) {
-            const int t = b + tid * WORDS + i, w = w0 + t < words ? w0 + t : w0 + t - words;
+            const int t = b + i * PT + tid, w = word_of(t);
             x[i] = 0;
             if (t <= words) {
                 x[i] = s.bits[w];
@@ -158,19 +186,53 @@ template <typename Args> __global__ void __launch_bounds__(PT) k_pages_plan(cons
                 if (t == words) x[i] &= ~(~0u << (start % 32));
                 if (w == words - 1 && s.N % 32 != 0) x[i] &= ~(~0u << (s.N % 32));
             }
-            pop += __popc(x[i]);
         }
-        int all;
-        int at = found + scan_cta(pop, all, s_scan);
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            const int t = b + tid * WORDS + i, w = w0 + t < words ? w0 + t : w0 + t - words;
-            while (x[i] && at < got_most) {
-                a.list[at++] = w * 32 + __ffs(x[i]) - 1;
-                x[i] &= x[i] - 1;
+    };
+    look(0);
+
+    if constexpr (WIDE) {
+        for (int h = wid; h < s.cells; h += PT / 32) {
+            fw_status st = FW_OK;
+            const int need = cell_need_warp(a, h, st);
+            if (lane == 0) {
+                a.first[h] = need;
+                if (a.status) a.status[h] = st;
+                a.plan[h] = make_int2(st == FW_OK ? s.counts[h] : -1, -1);
             }
         }
-        found = min(found + all, got_most);
+        __syncthreads();
+    }
+    int want = 0;
+    for (int b = 0; b < s.cells; b += PT) {
+        const int h = b + tid;
+        fw_status st = FW_OK;
+        const int need = h >= s.cells ? 0 : WIDE ? a.first[h] : cell_need(a, h, st);
+        int all;
+        const int at = want + scan_cta(need, all, s_scan);
+        if (h < s.cells) {
+            a.first[h] = at;
+            if constexpr (!WIDE) {
+                if (a.status) a.status[h] = st;
+                if constexpr (APPEND) a.plan[h] = make_int2(st == FW_OK ? s.counts[h] : -1, -1);
+            }
+        }
+        want += all;
+    }
+    if (tid == 0) a.first[s.cells] = want;
+
+    // The first `want` free pages: a word of the bits a thread, which writes its pages one after another.
+    const int got_most = min(want, s.N);
+    int found = 0;
+    for (int b = 0; b <= words && found < got_most; b += PT * WORDS) {
+        if (b > 0) look(b);
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            if (b + i * PT > words || found >= got_most) break;
+            int all, at = found + scan_cta(__popc(x[i]), all, s_scan);
+            const int w = word_of(b + i * PT + tid) * 32;
+            for (uint32_t y = x[i]; y && at < got_most; y &= y - 1) a.list[at++] = w + __ffs(y) - 1;
+            found = min(found + all, got_most);
+        }
     }
     __syncthreads();
 
@@ -187,37 +249,43 @@ template <typename Args> __global__ void __launch_bounds__(PT) k_pages_plan(cons
     }
     __syncthreads();
     const int granted = s_granted;
-    for (int t = tid; t < granted; t += PT) {
-        const int page = a.list[t];
-        s.refs[page] = 1;
-        atomicAnd(&s.bits[page / 32], ~(1u << (page % 32)));
-        if (t == granted - 1) *s.next = page + 1 < s.N ? page + 1 : 0;
+    if (tid == 0 && granted > 0) {
+        const int last = a.list[granted - 1];
+        *s.next = last + 1 < s.N ? last + 1 : 0;
     }
     if constexpr (!APPEND) {
         if (tid == 0) *a.granted = granted;
     } else {
+        for (int t = tid; t < granted; t += PT) take(s, a.list[t]);
         __syncthreads();
-        for (int h = tid; h < s.cells; h += PT) {
+        for (int h = WIDE ? wid : tid; h < s.cells; h += WIDE ? PT / 32 : PT) {
             const int n = a.plan[h].x;
             if (n < 0) continue;
             const int held = s.held[h], i0 = n / s.P, i1 = (n + a.m - 1) / s.P;
             int32_t *row = s.row(h);
             int at = a.first[h];
-            for (int i = i0; i <= i1; ++i) {
-                if (!append_needs(s, row, held, i)) continue;
-                const int was = i < held ? row[i] : -1;
-                row[i] = a.list[at];
-                a.list[at++] = was;
-                if (i == i0 && n % s.P != 0) a.plan[h].y = was;
+            for (int b = i0; b <= i1; b += WIDE ? 32 : 1) {
+                const int i = WIDE ? b + lane : b;
+                const bool needs = i <= i1 && append_needs(s, row, held, i);
+                const unsigned some = WIDE ? __ballot_sync(FW_FULL, needs) : needs;
+                if (needs) {
+                    const int was = i < held ? row[i] : -1, to = at + (WIDE ? __popc(some & ((1u << lane) - 1)) : 0);
+                    row[i] = a.list[to];
+                    a.list[to] = was;
+                    if (i == i0 && n % s.P != 0) a.plan[h].y = was;
+                }
+                at += __popc(some);
             }
-            s.held[h] = max(held, i1 + 1);
-            s.counts[h] = n + a.m;
+            if (!WIDE || lane == 0) {
+                s.held[h] = max(held, i1 + 1);
+                s.counts[h] = n + a.m;
+            }
         }
         __syncthreads();
         // (behind all readings of refs)
         for (int t = tid; t < granted; t += PT) {
             const int was = a.list[t];
-            if (was >= 0 && atomicSub(&s.refs[was], 1) == 1) atomicOr(&s.bits[was / 32], 1u << (was % 32));
+            if (was >= 0) give(s, was);
         }
     }
 }
@@ -255,6 +323,7 @@ template <int D> __global__ void __launch_bounds__(32 * MW) k_pages_append(const
 {
     const Pages &s = a.s;
     const int lane = threadIdx.x & 31, id = blockIdx.x * MW + (threadIdx.x >> 5);
+    wait_for_the_one_before();
     const int h = id / units;
     if (h >= s.cells) return;
     const int n = a.plan[h].x, from = a.plan[h].y;
@@ -278,6 +347,8 @@ template <int D, bool OWN> __global__ void __launch_bounds__(32 * MW) k_pages_mo
 {
     const Pages &s = a.s;
     const int lane = threadIdx.x & 31, warps = gridDim.x * MW, id = blockIdx.x * MW + (threadIdx.x >> 5), per = s.P / UR;
+    let_the_next_start();
+    wait_for_the_one_before();
     const int64_t units = (int64_t)*a.granted * per, run = (units + warps - 1) / warps;
     const int64_t u0 = id * run, u1 = min(u0 + run, units);
     if (u0 >= u1) return;
@@ -323,7 +394,7 @@ __device__ __forceinline__ void give_back(const Pages &s, const int32_t *row, in
 {
     for (int i = threadIdx.x; i < held; i += blockDim.x) {
         const int page = row[i];
-        if (s.is_page(page) && atomicSub(&s.refs[page], 1) == 1) atomicOr(&s.bits[page / 32], 1u << (page % 32));
+        if (s.is_page(page)) give(s, page);
     }
 }
 
@@ -333,13 +404,18 @@ __global__ void __launch_bounds__(128) k_pages_swap(const CompactArgs a)
     const Pages &s = a.s;
     const int h = blockIdx.x;
     fw_status st;
+    wait_for_the_one_before();
     const int n = compact_rows(a, h, st);
     if (n < 0) return;
     int32_t *row = s.row(h);
     give_back(s, row, s.held[h]);
     __syncthreads();  // every thread has read the books
     const int need = (n + s.P - 1) / s.P;
-    for (int i = threadIdx.x; i < need; i += blockDim.x) row[i] = a.list[a.first[h] + i];
+    for (int i = threadIdx.x; i < need; i += blockDim.x) {
+        const int page = a.list[a.first[h] + i];
+        row[i] = page;
+        take(s, page);
+    }
     if (threadIdx.x == 0) {
         s.held[h] = need;
         s.counts[h] = n;
@@ -359,6 +435,7 @@ struct ForkArgs {
 __global__ void __launch_bounds__(128) k_pages_fork(const ForkArgs a)
 {
     const Pages &s = a.s;
+    let_the_next_start();
     const int h = blockIdx.x, from = a.src[h];
     int n, held;
     fw_status st = cell_rows(s, h, n, held);
@@ -392,6 +469,7 @@ __global__ void __launch_bounds__(128) k_pages_fork(const ForkArgs a)
 __global__ void __launch_bounds__(128) k_pages_fork_end(const ForkArgs a)
 {
     const Pages &s = a.s;
+    wait_for_the_one_before();
     const int h = blockIdx.x, n = a.count[h];
     if (n < 0) return;
     int32_t *row = s.row(h);
@@ -403,6 +481,24 @@ __global__ void __launch_bounds__(128) k_pages_fork_end(const ForkArgs a)
         s.held[h] = need;
         s.counts[h] = n;
     }
+}
+
+// Launches what follows in a call.
+template <typename... P, typename... A>
+fw_status launch_after(void (*kernel)(P...), unsigned grid, int threads, cudaStream_t s, const A &...args)
+{
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }
 
 size_t append_list(const fw_pages &p, int m)
@@ -434,12 +530,13 @@ fw_status pages_append(const fw_pages &p, const fw_pages_new &r, int32_t *status
     a.list = (int32_t *)(w + align256((size_t)p.cells * 8));
     const int units = (p.page_rows - 1 + r.m + UR - 1) / UR;
     const unsigned grid = (unsigned)(((int64_t)p.cells * units + MW - 1) / MW);
-    FW_LAUNCH(k_pages_plan<AppendArgs>, 1, PT, 0, st, a);
-    if (p.d == 128)
-        FW_LAUNCH(k_pages_append<128>, grid, 32 * MW, 0, st, a, units);
+    // (4 cells x 509 rows, 33 pages each: a warp per cell 3 us, a thread 10)
+    if (r.m > 3 * p.page_rows)
+        FW_LAUNCH((k_pages_plan<AppendArgs, true>), 1, PT, 0, st, a);
     else
-        FW_LAUNCH(k_pages_append<64>, grid, 32 * MW, 0, st, a, units);
-    return FW_OK;
+        FW_LAUNCH((k_pages_plan<AppendArgs, false>), 1, PT, 0, st, a);
+    return p.d == 128 ? launch_after(k_pages_append<128>, grid, 32 * MW, st, a, units)
+                      : launch_after(k_pages_append<64>, grid, 32 * MW, st, a, units);
 }
 
 size_t pages_compact_workspace(const fw_pages &p, int64_t total)
@@ -460,21 +557,12 @@ fw_status pages_compact(const fw_pages &p, const void *K, const void *V, int T, 
     w += align256(((size_t)p.cells + 1) * 4);
     a.granted = (int32_t *)w;
     a.list = (int32_t *)(w + 256);
-    FW_LAUNCH(k_pages_plan<CompactArgs>, 1, PT, 0, s, a);
+    FW_LAUNCH((k_pages_plan<CompactArgs, false>), 1, PT, 0, s, a);
     const unsigned grid = (unsigned)sms * 4;
-    if (K) {
-        if (p.d == 128)
-            FW_LAUNCH((k_pages_move<128, false>), grid, 32 * MW, 0, s, a);
-        else
-            FW_LAUNCH((k_pages_move<64, false>), grid, 32 * MW, 0, s, a);
-    } else {
-        if (p.d == 128)
-            FW_LAUNCH((k_pages_move<128, true>), grid, 32 * MW, 0, s, a);
-        else
-            FW_LAUNCH((k_pages_move<64, true>), grid, 32 * MW, 0, s, a);
-    }
-    FW_LAUNCH(k_pages_swap, (unsigned)p.cells, 128, 0, s, a);
-    return FW_OK;
+    const fw_status moved = launch_after(K ? p.d == 128 ? k_pages_move<128, false> : k_pages_move<64, false>
+                                         : p.d == 128 ? k_pages_move<128, true> : k_pages_move<64, true>,
+                                         grid, 32 * MW, s, a);
+    return moved == FW_OK ? launch_after(k_pages_swap, (unsigned)p.cells, 128, s, a) : moved;
 }
 
 size_t pages_fork_workspace(const fw_pages &p)
@@ -487,8 +575,7 @@ fw_status pages_fork(const fw_pages &p, const int32_t *src, int32_t *status, voi
     uint8_t *w = (uint8_t *)ws;
     const ForkArgs a{view(p), src, status, (int32_t *)(w + align256((size_t)p.cells * 4)), (int32_t *)w};
     FW_LAUNCH(k_pages_fork, (unsigned)p.cells, 128, 0, s, a);
-    FW_LAUNCH(k_pages_fork_end, (unsigned)p.cells, 128, 0, s, a);
-    return FW_OK;
+    return launch_after(k_pages_fork_end, (unsigned)p.cells, 128, s, a);
 }
 
 }  // namespace fw

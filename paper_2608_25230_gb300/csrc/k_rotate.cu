@@ -15,7 +15,13 @@
 namespace fw {
 namespace {
 
-constexpr int RW = 8;  // warps of a CTA
+constexpr int RW = 8;      // warps of a CTA
+constexpr int AHEAD = 4;   // chunks of heads that a warp has asked for ahead of the one that it works on
+
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 
 struct RotateArgs {
     int64_t rows;
@@ -51,28 +57,112 @@ __device__ __forceinline__ uint64_t turns_of(float x)
     return b >> 31 ? 0 - t : t;
 }
 
-template <int LPL> __global__ void __launch_bounds__(32 * RW) k_qk_rotate(const RotateArgs a)
+// Two fp32 numbers side by side, and operations on both at once.
+__device__ __forceinline__ uint64_t pack2(float x, float y)
 {
-    constexpr int HP = 32 / LPL, PER = 8 / HP > 0 ? 8 / HP : 1;  // heads at a time; frequencies that a lane works out
-    __shared__ float s_w[2][256];
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, p = lane % LPL, hl = lane / LPL;
-    if (a.eps >= 0.f) {
-        for (int i = tid; i < 2 * a.d; i += 32 * RW) {
-            const int kv = i >= a.d, c = i - kv * a.d;
-            s_w[kv][c] = !a.w[kv] ? 1.f
-                         : a.w_bf16 ? bf16_to_f32(static_cast<const uint16_t *>(a.w[kv])[c])
-                                    : static_cast<const float *>(a.w[kv])[c];
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t swap2(uint64_t v)
+{
+    float x, y;
+    unpack2(v, x, y);
+    return pack2(y, x);
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t to_bf16x2(uint64_t v)
+{
+    float x, y;
+    unpack2(v, x, y);
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+    return r;
+}
+
+// 8 weights from `at` on, in pairs.
+__device__ __forceinline__ void weights8(const RotateArgs &a, int kv, int at, uint64_t (&w)[4])
+{
+    if (!a.w[kv]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2(1.f, 1.f);
+    } else if (a.w_bf16) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.w[kv]) + at);
+        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float4 x = reinterpret_cast<const float4 *>(static_cast<const float *>(a.w[kv]) + at)[i];
+            w[2 * i] = pack2(x.x, x.y), w[2 * i + 1] = pack2(x.z, x.w);
         }
-        __syncthreads();
     }
+}
+
+template <int LPL, bool INTER> __global__ void __launch_bounds__(32 * RW, 3) k_qk_rotate(const RotateArgs a)
+{
+    constexpr int HP = 32 / LPL, PER = 8 / HP;  // heads at a time; frequencies that a lane works out
+    __shared__ uint4 s_x[RW][AHEAD + 1][2][32];  // a lane's own pieces: no lane reads another's
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, p = lane % LPL, hl = lane / LPL;
     const int64_t id = (int64_t)blockIdx.x * RW + wid;
     const int64_t row = id / a.split;
-    if (row >= a.rows) return;
     const int part = (int)(id - row * a.split);
+    if (row >= a.rows) return;
 
     const bool rotated = 16 * p < a.rot, there = 16 * p < a.d;
-    const int at0 = rotated && !a.interleaved ? 8 * p : 16 * p;
-    const int at1 = rotated && !a.interleaved ? a.rot / 2 + 8 * p : 16 * p + 8;
+    const int at0 = rotated && !INTER ? 8 * p : 16 * p;
+    const int at1 = rotated && !INTER ? a.rot / 2 + 8 * p : 16 * p + 8;
+    // chunks of HP heads: the queries' heads, then the keys'
+    const int chunks_q = (a.q_heads + HP - 1) / HP, chunks = chunks_q + (a.kv_heads + HP - 1) / HP;
+    const uint32_t mem = (uint32_t)__cvta_generic_to_shared(&s_x[wid][0][0][lane]);
+    constexpr int SLOT = sizeof(s_x[0][0]), HALF = SLOT / 2;
+    if (!there) {
+#pragma unroll
+        for (int i = 0; i <= AHEAD; ++i) s_x[wid][i][0][lane] = s_x[wid][i][1][lane] = make_uint4(0, 0, 0, 0);
+    }
+    // The next chunk to be asked for: its head of this lane and where that lies.
+    int next = part, next_slot = 0, head = 0, heads_of = 0;
+    const uint16_t *src = nullptr;
+    auto seek = [&](int kv) {
+        head = (next - (kv ? chunks_q : 0)) * HP + hl;
+        heads_of = !there ? 0 : kv ? a.kv_heads : a.q_heads;
+        src = (kv ? a.k + row * a.k_row + head * a.k_head : a.q + row * a.q_row + head * a.q_head) + at0;
+    };
+    seek(part >= chunks_q);
+    auto load = [&]() {
+        if (next < chunks) {
+            if (head < heads_of) {
+                copy_async16(mem + next_slot, src);
+                copy_async16(mem + next_slot + HALF, src + (at1 - at0));
+            }
+            const bool was_q = next < chunks_q;
+            next += a.split;
+            if (was_q && next >= chunks_q) {
+                seek(1);
+            } else {
+                head += a.split * HP;
+                src += a.split * HP * (was_q ? a.q_head : a.k_head);
+            }
+        }
+        next_slot = next_slot == AHEAD * SLOT ? 0 : next_slot + SLOT;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // (a row's first heads are under way before its angles are worked out)
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load();
     float cs[8], sn[8];
     if (a.rot > 0) {
         const int64_t pos = a.pos[row];
@@ -90,69 +180,86 @@ template <int LPL> __global__ void __launch_bounds__(32 * RW) k_qk_rotate(const 
             cs[i] = __shfl_sync(FW_FULL, c[i % PER], (i / PER) * LPL + p);
             sn[i] = __shfl_sync(FW_FULL, s[i % PER], (i / PER) * LPL + p);
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) cs[i] = 1.f, sn[i] = 0.f;
     }
-    const int chunks_q = (a.q_heads + HP - 1) / HP, chunks = chunks_q + (a.kv_heads + HP - 1) / HP;
-    auto load = [&](int ch, uint4 (&x)[2]) {
-        const bool kv = ch >= chunks_q;
-        const int h = (kv ? ch - chunks_q : ch) * HP + hl;
-        x[0] = x[1] = make_uint4(0, 0, 0, 0);
-        if (ch < chunks && there && h < (kv ? a.kv_heads : a.q_heads)) {
-            const uint16_t *src = kv ? a.k + row * a.k_row + h * a.k_head : a.q + row * a.q_row + h * a.q_head;
-            x[0] = *reinterpret_cast<const uint4 *>(src + at0);
-            x[1] = *reinterpret_cast<const uint4 *>(src + at1);
-        }
-    };
-    uint4 next[2];
-    load(part, next);
-    for (int ch = part; ch < chunks; ch += a.split) {
-        const bool kv = ch >= chunks_q;
-        const int h = (kv ? ch - chunks_q : ch) * HP + hl;
-        const uint32_t w[8] = {next[0].x, next[0].y, next[0].z, next[0].w, next[1].x, next[1].y, next[1].z, next[1].w};
-        float y[16];
+    const float inv_d = 1.f / (float)a.d;
+    int slot = 0, ch = part;
+    for (int kv = 0; kv < 2; ++kv) {
+        const int first = kv ? chunks_q : 0, end = kv ? chunks : chunks_q, heads = kv ? a.kv_heads : a.q_heads;
+        if (ch >= end) continue;
+        // Factors of a pair's columns, the weights in them: with y the head's values (before its root mean square),
+        // half apart: out_a = y_a A_a - y_b B_b, out_b = y_b A_b + y_a B_a; neighbours: (y_0, y_1) A + (y_1, y_0) B.
+        uint64_t A[2][4], B[2][4];
+        if (there) {
+            weights8(a, kv, at0, A[0]);
+            weights8(a, kv, at1, A[1]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            y[2 * i] = __uint_as_float(w[i] << 16);
-            y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-        load(ch + a.split, next);
-        if (a.eps >= 0.f) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sum = fmaf(y[i], y[i], sum);
-#pragma unroll
-            for (int o = LPL / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(FW_FULL, sum, o);
-            const float inv = rsqrtf(sum / (float)a.d + a.eps);
-            const float *wt = s_w[kv];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] *= inv * (there ? wt[(i < 8 ? at0 : at1 - 8) + i] : 0.f);
+            for (int i = 0; i < 4; ++i) A[0][i] = A[1][i] = 0;
         }
         if (rotated) {
-            if (a.interleaved) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float u = y[2 * i], v = y[2 * i + 1];
-                    y[2 * i] = u * cs[i] - v * sn[i];
-                    y[2 * i + 1] = v * cs[i] + u * sn[i];
-                }
-            } else {
+            for (int z = 0; z < 2; ++z)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float u = y[i], v = y[8 + i];
-                    y[i] = u * cs[i] - v * sn[i];
-                    y[8 + i] = v * cs[i] + u * sn[i];
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (INTER) {
+                        const int f = 4 * z + i;
+                        B[z][i] = mul2(swap2(A[z][i]), pack2(-sn[f], sn[f]));
+                        A[z][i] = mul2(A[z][i], pack2(cs[f], cs[f]));
+                    } else {
+                        const uint64_t s = z ? pack2(-sn[2 * i], -sn[2 * i + 1]) : pack2(sn[2 * i], sn[2 * i + 1]);
+                        B[z][i] = mul2(A[z][i], s);
+                        A[z][i] = mul2(A[z][i], pack2(cs[2 * i], cs[2 * i + 1]));
+                    }
                 }
-            }
         }
-        if (there && h < (kv ? a.kv_heads : a.q_heads)) {
-            uint32_t r[8];
+        int h = (ch - first) * HP + hl;
+        uint16_t *dst = (kv ? a.k_out + row * a.k_out_row + h * a.k_out_head : a.q_out + row * a.q_out_row + h * a.q_out_head) + at0;
+        const int64_t step = a.split * HP * (kv ? a.k_out_head : a.q_out_head);
+        const int mine = there ? heads : 0;
+        for (; ch < end; ch += a.split, h += a.split * HP, dst += step) {
+            load();
+            asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+            uint64_t y[2][4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
-                r[i] = *reinterpret_cast<const uint32_t *>(&b);
+            for (int z = 0; z < 2; ++z) {
+                const uint4 x = s_x[wid][slot][z][lane];
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[z][i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
             }
-            uint16_t *dst = kv ? a.k_out + row * a.k_out_row + h * a.k_out_head : a.q_out + row * a.q_out_row + h * a.q_out_head;
-            *reinterpret_cast<uint4 *>(dst + at0) = make_uint4(r[0], r[1], r[2], r[3]);
-            *reinterpret_cast<uint4 *>(dst + at1) = make_uint4(r[4], r[5], r[6], r[7]);
+            slot = slot == AHEAD ? 0 : slot + 1;
+            uint64_t inv = pack2(1.f, 1.f);
+            if (a.eps >= 0.f) {
+                uint64_t sum2 = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum2 = fma2(y[i >> 2][i & 3], y[i >> 2][i & 3], sum2);
+                float s0, s1;
+                unpack2(sum2, s0, s1);
+                s0 += s1;
+#pragma unroll
+                for (int o = LPL / 2; o > 0; o >>= 1) s0 += __shfl_xor_sync(FW_FULL, s0, o);
+                const float r = rsqrtf(fmaf(s0, inv_d, a.eps));
+                inv = pack2(r, r);
+            }
+            uint32_t out[2][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint64_t u = mul2(y[0][i], A[0][i]), v = mul2(y[1][i], A[1][i]);
+                if (rotated) {
+                    u = fma2(INTER ? swap2(y[0][i]) : y[1][i], INTER ? B[0][i] : B[1][i], u);
+                    v = fma2(INTER ? swap2(y[1][i]) : y[0][i], INTER ? B[1][i] : B[0][i], v);
+                }
+                out[0][i] = to_bf16x2(mul2(u, inv));
+                out[1][i] = to_bf16x2(mul2(v, inv));
+            }
+            if (h < mine) {
+                *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0][0], out[0][1], out[0][2], out[0][3]);
+                *reinterpret_cast<uint4 *>(dst + (at1 - at0)) = make_uint4(out[1][0], out[1][1], out[1][2], out[1][3]);
+            }
         }
     }
 }
@@ -162,7 +269,11 @@ template <int LPL> fw_status launch(RotateArgs &a, int sms, cudaStream_t s)
     constexpr int HP = 32 / LPL;
     const int chunks = (a.q_heads + HP - 1) / HP + (a.kv_heads + HP - 1) / HP;
     a.split = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, (int64_t)sms * 32 / a.rows));
-    FW_LAUNCH(k_qk_rotate<LPL>, (unsigned)((a.rows * a.split + RW - 1) / RW), 32 * RW, 0, s, a);
+    const unsigned grid = (unsigned)((a.rows * a.split + RW - 1) / RW);
+    if (a.interleaved)
+        FW_LAUNCH((k_qk_rotate<LPL, true>), grid, 32 * RW, 0, s, a);
+    else
+        FW_LAUNCH((k_qk_rotate<LPL, false>), grid, 32 * RW, 0, s, a);
     return FW_OK;
 }
 

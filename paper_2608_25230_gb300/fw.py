@@ -973,13 +973,13 @@ def pages_attend(pages: Pages, q: torch.Tensor, *, kv_heads: int, scale: float =
     return out
 
 
-def _rotation_strides(x, what):
-    rows, heads, d = x.shape
+def _rotation_strides(x, rows, heads, d):
     r, h, one = x.stride()
     if one != 1:
-        raise ValueError(f"d is the contiguous axis of {what}")
+        raise ValueError("d is the contiguous axis of q, k and the outputs")
     # (strides of axes of one entry, which torch leaves open)
-    h = h if heads > 1 else d
+    if heads == 1:
+        h = d
     return (r if rows > 1 else heads * d), h
 
 
@@ -990,54 +990,58 @@ def qk_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_fre
     int32 [rows]; inv_freq: float32 [rot / 2].  eps None: no norm; else each head is normed, with q_weight and k_weight ([d],
     bfloat16 or float32, both alike) where they are given.  Returns (q, k) rotated; such a pair passed as out (the inputs
     themselves, if wished) is written instead."""
-    bf16, both = torch.bfloat16, [x for x in (q, k) if x is not None]
-    if any(x.dtype is not bf16 or x.dim() != 3 for x in both) or (k is not None and (k.shape[0], k.shape[2]) != (
-            q.shape[0], q.shape[2])):
-        raise ValueError("q and k are bfloat16 [rows][heads][d], rows and d alike")
+    bf16, f32 = torch.bfloat16, torch.float32
     rows, hq, d = q.shape
-    if positions.dtype is not torch.int32 or positions.shape != (rows,) or inv_freq.dtype is not torch.float32 or \
+    if q.dtype is not bf16 or (k is not None and (k.dtype is not bf16 or k.dim() != 3 or k.shape[0] != rows or k.shape[2] != d)):
+        raise ValueError("q and k are bfloat16 [rows][heads][d], rows and d alike")
+    if positions.dtype is not torch.int32 or positions.shape != (rows,) or inv_freq.dtype is not f32 or \
             inv_freq.dim() != 1 or not (positions.is_contiguous() and inv_freq.is_contiguous()):
         raise ValueError("positions is contiguous int32 [rows], inv_freq contiguous float32 [rot / 2]")
-    weights = [w for w in (q_weight, k_weight) if w is not None]
-    if weights and eps is None:
-        raise ValueError("weights belong to a norm: eps is given with them")
-    if any(w.shape != (d,) or not w.is_contiguous() or w.dtype not in (bf16, torch.float32) or w.dtype != weights[0].dtype
-           for w in weights):
-        raise ValueError("q_weight and k_weight are contiguous [d], both bfloat16 or both float32")
+    dev = q.get_device()
+    if dev < 0 or positions.get_device() != dev or inv_freq.get_device() != dev or (k is not None and k.get_device() != dev):
+        raise ValueError("the tensors of a call are on one GPU")
+    w_dtype = None
+    for w in (q_weight, k_weight):
+        if w is not None:
+            if eps is None:
+                raise ValueError("weights belong to a norm: eps is given with them")
+            if w.shape != (d,) or not w.is_contiguous() or w.dtype not in (bf16, f32) or w_dtype not in (None, w.dtype):
+                raise ValueError("q_weight and k_weight are contiguous [d], both bfloat16 or both float32")
+            if w.get_device() != dev:
+                raise ValueError("the tensors of a call are on one GPU")
+            w_dtype = w.dtype
     if eps is not None and not eps >= 0:
         raise ValueError("eps is not negative")
-    index = q.get_device()
-    if any(t.get_device() != index for t in (*both, positions, inv_freq, *weights)) or index < 0:
-        raise ValueError("the tensors of a call are on one GPU")
-    handle = _raw_stream(stream, index)
+    handle = _raw_stream(stream, dev)
     if out is None:
         with _made_on(stream):
-            out = tuple(None if x is None else torch.empty(x.shape, dtype=bf16, device=x.device) for x in (q, k))
+            out = (torch.empty(q.shape, dtype=bf16, device=q.device),
+                   None if k is None else torch.empty(k.shape, dtype=bf16, device=q.device))
         if stream is not None:  # the caller reads them on the current one
             for t in out:
                 if t is not None:
                     t.record_stream(torch.cuda.current_stream(q.device))
+        qo, ko = out
     else:
-        for x, y in zip((q, k), out):
-            if x is not None and (y is None or y.shape != x.shape or y.dtype is not bf16 or y.get_device() != index):
-                raise ValueError("out is (q, k) of the inputs' shapes, bfloat16 on their GPU")
-    qo, ko = out
-    none = (None, 0, 0)
-    (qp, qr, qh), (qop, qor, qoh), (kp, kr, kh), (kop, kor, koh) = (
-        none if x is None else (x.data_ptr(), *_rotation_strides(x, w))
-        for x, w in ((q, "q"), (qo, "out's q"), (k, "k"), (None if k is None else ko, "out's k")))
-    r = FwRotation(rows, hq, 0 if k is None else k.shape[1], d, 2 * inv_freq.numel(), int(bool(interleaved)),
-                   FW_BF16 if weights and weights[0].dtype is bf16 else FW_F32, -1.0 if eps is None else eps, qp, kp, qop, kop,
-                   _raw(q_weight), _raw(k_weight), positions.data_ptr(), inv_freq.data_ptr() or None, qr, qh, kr, kh, qor, qoh,
-                   kor, koh)
+        qo, ko = out
+        if qo.shape != q.shape or qo.dtype is not bf16 or qo.get_device() != dev or (k is not None and (
+                ko is None or ko.shape != k.shape or ko.dtype is not bf16 or ko.get_device() != dev)):
+            raise ValueError("out is (q, k) of the inputs' shapes, bfloat16 on their GPU")
+    qr, qh = _rotation_strides(q, rows, hq, d)
+    qor, qoh = _rotation_strides(qo, rows, hq, d)
+    hk = kp = kop = kr = kh = kor = koh = 0
+    if k is not None:
+        hk, kp, kop = k.shape[1], k.data_ptr(), ko.data_ptr()
+        kr, kh = _rotation_strides(k, rows, hk, d)
+        kor, koh = _rotation_strides(ko, rows, hk, d)
+    r = FwRotation(rows, hq, hk, d, 2 * inv_freq.shape[0], 1 if interleaved else 0, FW_BF16 if w_dtype is bf16 else FW_F32,
+                   -1.0 if eps is None else eps, q.data_ptr(), kp, qo.data_ptr(), kop,
+                   None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+                   positions.data_ptr(), inv_freq.data_ptr(), qr, qh, kr, kh, qor, qoh, kor, koh)
     st = _lib.fw_qk_rotate(C.byref(r), handle)
     if st != FW_OK:
         raise FwError(st, "fw_qk_rotate")
     return out
-
-
-def _raw(t):
-    return None if t is None else t.data_ptr()
 
 
 def raw():
