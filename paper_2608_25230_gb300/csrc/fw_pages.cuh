@@ -24,11 +24,15 @@ inline Pages view(const fw_pages &p)
 }
 
 // A cell's rows and entries, checked against its table.
+__device__ __forceinline__ fw_status cell_rows_ok(const Pages &s, int n, int held)
+{
+    return held < 0 || held > s.width || n < 0 || n > (int64_t)held * s.P ? FW_ERR_INVALID_ARG : FW_OK;
+}
 __device__ __forceinline__ fw_status cell_rows(const Pages &s, int h, int &n, int &held)
 {
     n = s.counts[h];
     held = s.held[h];
-    return held < 0 || held > s.width || n < 0 || n > (int64_t)held * s.P ? FW_ERR_INVALID_ARG : FW_OK;
+    return cell_rows_ok(s, n, held);
 }
 
 }  // namespace pages
