@@ -608,8 +608,8 @@ __global__ void __launch_bounds__(32 * Cfg<D, NT, TW>::W, 1)
 
 // The parts of a cell that several teams share, joined in their order; empty cells' outputs.  Each of a CTA's JW warps
 // takes a row, or (SPREAD) all of them one row's parts, where there are few rows and so the parts may be many.
-constexpr int JW = 8;
-template <int D, bool SPREAD> __global__ void __launch_bounds__(32 * JW) k_pages_join(const AttendArgs a, int RT)
+constexpr int JW = 4;
+template <int D, bool SPREAD> __global__ void __launch_bounds__(32 * JW, 5) k_pages_join(const AttendArgs a, int RT)
 {
     constexpr int E = D / 32;
     __shared__ float s_o[SPREAD ? JW : 1][D];
@@ -640,7 +640,7 @@ template <int D, bool SPREAD> __global__ void __launch_bounds__(32 * JW) k_pages
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
     for (int q = p0; q < p1; q += 32) {
         // (the columns of B parts are asked for before the maxima are looked at, and B at a time after that)
-        constexpr int B = 64 / E;
+        constexpr int B = 32 / E;
         const int cnt = min(32, p1 - q);
         const float2 ml = lane < cnt ? a.part_ml[part_at(q + lane)] : make_float2(-INFINITY, 0.f);
         float f = 0.f;
@@ -726,40 +726,43 @@ __device__ __forceinline__ void join8(FM ml_of, FO o_of, float &M, float &L, flo
     }
 }
 
-// A cluster of up to FEW CTAs per cell and tile of rows, its blocks dealt out to their warps one by one.
+// A cluster of up to FEW CTAs per cell and tile of rows, its blocks dealt out to their teams one by one.
 constexpr int FEW = 8, FW = 8;
-template <int D, int NT>
+template <int D, int NT, int TW>
 __global__ void __launch_bounds__(32 * FW, 1)
     k_pages_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
 {
-    using C = Cfg<D, 2, 1>;  // (8 warps)
+    using C = Cfg<D, 2, TW>;  // (8 warps, whatever NT is)
     static_assert(C::W == FW && FEW == 8 && FW == 8, "a warp per row of 8, eight states to join");
-    constexpr int MT = D / 16, RT = 8 * NT, E = D / 32, LDO = D + 4;
+    constexpr int MT = D / 16, RT = TW * 8 * NT, E = D / 32, LDO = D + 4, TEAMS = C::TEAMS, STAGES = C::STAGES;
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
     float *s_o = reinterpret_cast<float *>(sm);  // [FW][8][LDO], in the rings' place when these are done
     static_assert(FW * 8 * LDO * 4 <= C::RING, "the states fit the rings");
-    __shared__ __align__(8) uint64_t full[FW][C::STAGES];
-    __shared__ int32_t s_page[FW][C::STAGES];
+    __shared__ __align__(8) uint64_t full[TEAMS][STAGES], empty[TEAMS][STAGES];
+    __shared__ int32_t s_page[TEAMS][STAGES];
     __shared__ float2 s_ml[FW][8];
-    __shared__ float2 s_pml[8];
+    __shared__ float2 s_pml[TW * 8];
     __shared__ int s_code;
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int h = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, row0 = blockIdx.y * RT, rows = a.group * a.m;
+    const int team = wid / TW, member = wid % TW;
+    const int h = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, rows = a.group * a.m;
+    const int tile0 = blockIdx.y * RT, row0 = tile0 + member * 8 * NT;
     const Pages &s = a.s;
-    const int first = rank + a.cluster * wid, step = a.cluster * FW;  // (the first blocks go to different CTAs)
+    const int first = rank + a.cluster * team, step = a.cluster * TEAMS;  // (the first blocks go to different CTAs)
     Window win;
     win.load(s, h, first, step, lane);  // (beside the counts)
     int n;
     fw_status st;
     const int nb = cell_blocks(s, h, n, st);
     if (tid == 0) s_code = st;
-    Ring<D, C::STAGES, 1> ring;
-    ring.mem = sm + wid * C::STAGES * 2 * C::TILE;
-    ring.full = full[wid];
-    ring.page = s_page[wid];
-    ring.init(lane, 0);
+    Ring<D, STAGES, TW> ring;
+    ring.mem = sm + team * STAGES * 2 * C::TILE;
+    ring.full = full[team];
+    ring.empty = empty[team];
+    ring.page = s_page[team];
+    ring.init(lane, member);
     __syncthreads();
     int pb = first;
     auto fetch = [&]() {
@@ -772,20 +775,22 @@ __global__ void __launch_bounds__(32 * FW, 1)
     const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
     Rows<D, NT> R;
     R.read(a, seq, hk, row0, lane);
+    if (member == 0) {
 #pragma unroll 1
-    for (int i = 0; i < C::STAGES; ++i) fetch();
+        for (int i = 0; i < STAGES - (TW > 1 ? 1 : 0); ++i) fetch();
+    }
     R.start();
     bool bad = false;
 #pragma unroll 1
     for (int blk = first; blk < nb; blk += step) {
         const int stage = ring.next();
         if (stage < 0) break;
-        if (s_page[wid][stage] >= 0)
+        if (s_page[team][stage] >= 0)
             R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
         else
             bad = true;
         ring.release(stage, lane);
-        fetch();
+        if (member == 0) fetch();
     }
     R.close();
     ring.drain();
@@ -793,8 +798,8 @@ __global__ void __launch_bounds__(32 * FW, 1)
     if (lane == 0 && code != FW_OK) atomicMax(&s_code, code);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        if (t > 0 && row0 + 8 * t >= rows) break;
-        // ---- the warps' rows joined in the CTA, a warp per row
+        if (t > 0 && tile0 + 8 * t >= rows) break;
+        // ---- the teams' rows joined in the CTA, a warp per row of the members' 8
         if (t > 0)
             cluster_sync();  // (the rows before have been read)
         else
@@ -811,18 +816,22 @@ __global__ void __launch_bounds__(32 * FW, 1)
                 for (int z = 0; z < 2; ++z) s_o[(wid * 8 + 2 * c + e) * LDO + 16 * i + 8 * z + g] = R.O[t][i][2 * z + e];
         __syncthreads();
         float M, L, acc[E];
-        join8<E>([&](int w) { return s_ml[w][wid]; }, [&](int w, int e) { return s_o[(w * 8 + wid) * LDO + lane + 32 * e]; }, M, L,
-                 acc);
 #pragma unroll
-        for (int e = 0; e < E; ++e) s_o[wid * LDO + lane + 32 * e] = acc[e];  // (its row in the first warp's place)
-        if (lane == 0) s_pml[wid] = make_float2(M, L);
+        for (int k = 0; k < TW; ++k) {  // row wid of member k's
+            join8<E>([&](int w) { return w < TEAMS ? s_ml[w * TW + k][wid] : make_float2(-INFINITY, 0.f); },
+                     [&](int w, int e) { return w < TEAMS ? s_o[((w * TW + k) * 8 + wid) * LDO + lane + 32 * e] : 0.f; }, M, L, acc);
+#pragma unroll
+            for (int e = 0; e < E; ++e) s_o[(k * 8 + wid) * LDO + lane + 32 * e] = acc[e];  // (in the first team's place)
+            if (lane == 0) s_pml[k * 8 + wid] = make_float2(M, L);
+        }
         cluster_sync();
         // ---- and over the cluster's CTAs: rows dealt out to them and their warps
-        const int r8 = rank + a.cluster * wid, r = row0 + 8 * t + r8;
-        if (r8 < 8 && r < rows) {
-            join8<E>([&](int w) { return w < a.cluster ? make_float2(remote(&s_pml[r8].x, w), remote(&s_pml[r8].y, w))
+        for (int x = rank + a.cluster * wid; x < TW * 8; x += a.cluster * FW) {
+            const int r = tile0 + (x >> 3) * 8 * NT + 8 * t + (x & 7);
+            if (r >= rows) continue;
+            join8<E>([&](int w) { return w < a.cluster ? make_float2(remote(&s_pml[x].x, w), remote(&s_pml[x].y, w))
                                                       : make_float2(-INFINITY, 0.f); },
-                     [&](int w, int e) { return w < a.cluster ? remote(&s_o[r8 * LDO + lane + 32 * e], w) : 0.f; }, M, L, acc);
+                     [&](int w, int e) { return w < a.cluster ? remote(&s_o[x * LDO + lane + 32 * e], w) : 0.f; }, M, L, acc);
             const int64_t out = out_row(a, seq, hk, r);
             const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
@@ -838,17 +847,29 @@ __global__ void __launch_bounds__(32 * FW, 1)
     cluster_sync();  // no CTA leaves while another reads its rows
 }
 
-// CTAs of a cell where the cells are few and hold little at most, so that a cluster each is faster, else 0.
-int cluster_of(const fw_pages &p, const fw_pages_query &q, int tiles)
+// CTAs of a cell's cluster where that is the faster way, else 0 (ranges).  Both ways' times in us, from sweeps of cells of
+// unlike lengths (the longest about twice the mean, which the host does not know).  Ranges: two launches, the sums
+// over the cells, the joining, and the blocks of all over the GPU.  Clusters: a launch, and the longest cell's blocks over
+// its CTAs, which share the memory with all others at first and have their SMs' whole rate at the end.
+int cluster_of(const fw_pages &p, const fw_pages_query &q, int NT, int TW, int tiles, int sms)
 {
-    struct Rule {
-        int ctas;
-        int64_t cells, rows;
-    };
     if (q.longest == 0) return 0;
-    for (const Rule &r : {Rule{8, 14, 8192}, Rule{4, 36, 2560}, Rule{2, 72, 1280}})
-        if ((int64_t)p.cells * tiles <= r.cells && q.longest <= r.rows) return r.ctas;
-    return 0;
+    // an SM's time for a block of 16 rows: 91 GB/s for one tile of query rows, products for more
+    const double per = (p.d == 128 ? 1.0 : 0.5) * (NT == 1 ? 0.09 : 0.15 * TW);
+    const double memory = BR * p.d * 4 / 6.7e6;  // and the memory's
+    const double blocks = (q.longest + BR - 1) / BR, all = 0.5 * blocks * p.cells * tiles;
+    struct Rule {
+        int ctas, clusters;  // that find room at once
+    };
+    int best = 0;
+    double least = 12.0 + std::max(all * per / sms, all * memory / tiles);
+    for (const Rule &r : {Rule{8, 14}, Rule{4, 36}, Rule{2, 72}, Rule{1, 152}}) {
+        const int64_t clusters = (int64_t)p.cells * tiles, waves = (clusters + r.clusters - 1) / r.clusters;
+        const double at_once = (double)std::min<int64_t>(clusters, r.clusters) * r.ctas * memory / tiles;
+        const double t = waves * (5.5 + blocks / r.ctas * 0.5 * (per + std::max(per, at_once)));
+        if (t < least) best = r.ctas, least = t;
+    }
+    return best;
 }
 
 struct Plan {
@@ -865,10 +886,9 @@ void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
     x.TW = 1;
     while (x.TW < 8 && x.TW * 8 * x.NT < rows) x.TW *= 2;
     x.start = x.plan = x.flags = x.ml = x.o = x.bytes = 0;
-    x.few = cluster_of(p, q, (rows + 8 * x.NT - 1) / (8 * x.NT));
-    if (x.few) x.TW = 1;
     x.RT = x.TW * 8 * x.NT;
     x.tiles = (rows + x.RT - 1) / x.RT;
+    x.few = cluster_of(p, q, x.NT, x.TW, x.tiles, sms);
     if (x.few) return;
     x.G = std::max(1, sms / x.tiles);  // one wave
     x.teams = x.G * ((p.d == 64 && x.NT == 1 ? 16 : 8) / x.TW);
@@ -908,25 +928,30 @@ fw_status launch_ranges(const Plan &x, const CUtensorMap &mk, const CUtensorMap 
     static std::atomic<uint64_t> done{0};
     return launch(k_pages_attend<D, NT, TW>, x.G, x.tiles, 0, 32 * C::W, C::SMEM, mk, mv, a, done, s);
 }
-template <int D, int NT>
+template <int D, int NT, int TW>
 fw_status launch_few(const Plan &x, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
 {
     static std::atomic<uint64_t> done{0};
-    return launch(k_pages_attend_few<D, NT>, cells * x.few, x.tiles, x.few, 32 * FW, Cfg<D, 2, 1>::SMEM, mk, mv, a, done, s);
+    return launch(k_pages_attend_few<D, NT, TW>, cells * x.few, x.tiles, x.few, 32 * FW, Cfg<D, 2, TW>::SMEM, mk, mv, a, done, s);
+}
+template <int D, int NT, int TW>
+fw_status launch_one(const Plan &x, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
+{
+    return x.few ? launch_few<D, NT, TW>(x, cells, mk, mv, a, s) : launch_ranges<D, NT, TW>(x, mk, mv, a, s);
 }
 template <int D>
 fw_status attend(const Plan &x, int cells, int rows, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a,
                  cudaStream_t s)
 {
-    if (x.few) return x.NT == 1 ? launch_few<D, 1>(x, cells, mk, mv, a, s) : launch_few<D, 2>(x, cells, mk, mv, a, s);
-    const fw_status st = x.NT == 1   ? launch_ranges<D, 1, 1>(x, mk, mv, a, s)
-                         : x.TW == 1 ? launch_ranges<D, 2, 1>(x, mk, mv, a, s)
-                         : x.TW == 2 ? launch_ranges<D, 2, 2>(x, mk, mv, a, s)
-                         : x.TW == 4 ? launch_ranges<D, 2, 4>(x, mk, mv, a, s)
-                                     : launch_ranges<D, 2, 8>(x, mk, mv, a, s);
+    const fw_status st = x.NT == 1   ? launch_one<D, 1, 1>(x, cells, mk, mv, a, s)
+                         : x.TW == 1 ? launch_one<D, 2, 1>(x, cells, mk, mv, a, s)
+                         : x.TW == 2 ? launch_one<D, 2, 2>(x, cells, mk, mv, a, s)
+                         : x.TW == 4 ? launch_one<D, 2, 4>(x, cells, mk, mv, a, s)
+                                     : launch_one<D, 2, 8>(x, cells, mk, mv, a, s);
+    if (x.few) return st;
     if (st != FW_OK) return st;
     // the joining kernel starts as the first one's CTAs leave
-    const bool spread = (int64_t)cells * rows <= 2 * x.G;
+    const bool spread = x.teams >= 4 * cells && (int64_t)cells * rows <= 16 * x.G;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
