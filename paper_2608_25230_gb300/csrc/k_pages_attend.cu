@@ -126,16 +126,20 @@ __device__ __forceinline__ void tma_load_rows(void *dst, const void *tmap, int32
         : "memory");
 }
 
-// Teams of TW warps whose warps hold NT tiles of 8 query rows.
-template <int D, int NT, int TW> struct Cfg {
-    static constexpr int W = D == 64 && NT == 1 ? 16 : 8;  // warps of a CTA
+// CTAs of W warps in teams of TW.
+template <int D, int TW, int W> struct Cfg {
     static constexpr int TEAMS = W / TW;
-    static constexpr int TILE = BR * D * 2;                // bytes of a block's keys, or values
+    static constexpr int TILE = BR * D * 2;  // bytes of a block's keys, or values
     static constexpr int STAGES = 196608 / (2 * TILE) / TEAMS;
     static constexpr int RING = TEAMS * STAGES * 2 * TILE;
     static constexpr size_t SMEM = 1024 + RING;
-    static constexpr int RT = TW * 8 * NT;                 // query rows of a team
+    static constexpr int RT = TW * 8;  // query rows of a team
+    // blocks under way: with more warps one less than there is room for, so that the first warp does not wait for the others
+    // at every block
+    static constexpr int AHEAD = STAGES - (TW > 1 ? 1 : 0);
 };
+__host__ __device__ constexpr int range_warps(int D, int TW) { return TW > 1 ? 12 : D == 64 ? 16 : 8; }
+__host__ __device__ constexpr int few_warps(int TW) { return TW > 1 ? 12 : 8; }
 
 // Byte offset of piece x (16 bytes, 8 columns) of row r in a tile.
 __device__ __forceinline__ int piece(int r, int x) { return (x >> 3) * (BR * 128) + r * 128 + (((x ^ r) & 7) << 4); }
@@ -213,43 +217,37 @@ struct Window {
     __device__ int at(int i) const { return __shfl_sync(FW_FULL, pages, i); }
 };
 
-// A warp's queries and running softmax over blocks of one cell, NT tiles of 8 query rows.
-template <int D, int NT> struct Rows {
+// A warp's 8 query rows and their running softmax over blocks of one cell.
+template <int D> struct Rows {
     static constexpr int MT = D / 16;  // 16-column tiles of the output, and steps of the first product
-    uint32_t qf[NT][MT][2];            // row g of each 8, columns 2c, 2c + 1 (and 8 behind them) of each 16
-    // The weights are 2^(x - ref), ref[t][e] a maximum of row 2c + e as it was at some block, 0 where nothing was
+    uint32_t qf[MT][2];            // row g of each 8, columns 2c, 2c + 1 (and 8 behind them) of each 16
+    // The weights are 2^(x - ref), ref[e] a maximum of row 2c + e as it was at some block, 0 where nothing was
     // seen yet (mx has -inf there): it follows the maximum once a weight would pass 2^UP, so most blocks
     // need no maximum over the lanes and no rescaling.
     static constexpr float UP = 8.f;
-    float O[NT][MT][4], mx[NT][2], ref[NT][2], l[NT][2];
+    float O[MT][4], mx[2], ref[2], l[2];
     bool settled;  // every row has seen something
 
     __device__ __forceinline__ void read(const AttendArgs &a, int seq, int hk, int row0, int lane)
     {
         const int g = lane >> 2, c = lane & 3, rows = a.group * a.m;
+        const int r = row0 + g, i = token_of(a, r);
+        const uint16_t *src = a.q + seq * a.q_seq + i * a.q_tok + (int64_t)(hk * a.group + r - i * a.group) * a.q_head + 2 * c;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int r = row0 + 8 * t + g, i = token_of(a, r);
-            const uint16_t *src = a.q + seq * a.q_seq + i * a.q_tok + (int64_t)(hk * a.group + r - i * a.group) * a.q_head + 2 * c;
+        for (int k = 0; k < MT; ++k)
 #pragma unroll
-            for (int k = 0; k < MT; ++k)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    qf[t][k][e] = r < rows ? *reinterpret_cast<const uint32_t *>(src + 16 * k + 8 * e) : 0;
-        }
+            for (int e = 0; e < 2; ++e)
+                qf[k][e] = r < rows ? *reinterpret_cast<const uint32_t *>(src + 16 * k + 8 * e) : 0;
     }
     __device__ __forceinline__ void start()
     {
         settled = false;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int e = 0; e < 2; ++e) mx[e] = -INFINITY, ref[e] = l[e] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) mx[t][e] = -INFINITY, ref[t][e] = l[t][e] = 0.f;
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) O[t][i][e] = 0.f;
-        }
+            for (int e = 0; e < 4; ++e) O[i][e] = 0.f;
     }
 
     // One block, rows BR blk .. of a cell of n, whose tile of keys lies at tk, the values' behind it.
@@ -258,18 +256,15 @@ template <int D, int NT> struct Rows {
         const int g = lane >> 2, c = lane & 3;
         const uint32_t ak = tc::smem_u32(tk), av = ak + BR * D * 2;
         // S^T: keys g, g + 8 of rows 2c, 2c + 1, in two sums, so that fewer products wait for one another
-        float S[NT][4], S2[NT][4];
+        float S[4], S2[4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int z = 0; z < 4; ++z) S[t][z] = S2[t][z] = 0.f;
+        for (int z = 0; z < 4; ++z) S[z] = S2[z] = 0.f;
         const int lr = lane & 7, lm = lane >> 3;  // the row and the matrix that a lane's address is for
 #pragma unroll
         for (int k = 0; k < MT; ++k) {
             uint32_t x[4];  // keys 0 .. 7, 8 .. 15 of the step's first 8 columns, then of the others
             ldmatrix4<false>(x, ak + piece(lr + 8 * (lm & 1), 2 * k + (lm >> 1)));
-#pragma unroll
-            for (int t = 0; t < NT; ++t) mma(k & 1 ? S2[t] : S[t], x, qf[t][k][0], qf[t][k][1]);
+            mma(k & 1 ? S2 : S, x, qf[k][0], qf[k][1]);
         }
         uint32_t V[MT][4];  // keys 0 .. 7 of a tile's first 8 columns and of the others, then keys 8 .. 15
 #pragma unroll
@@ -278,57 +273,50 @@ template <int D, int NT> struct Rows {
         const bool masked = j0 + BR > all;
         bool over = !settled;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int z = e; z < 4; z += 2) S[t][z] += S2[t][z];
-                if (masked) {
-                    const int seen = min(all + token_of(a, row0 + 8 * t + 2 * c + e), n);
-                    if (j0 + g >= seen) S[t][e] = -INFINITY;
-                    if (j0 + 8 + g >= seen) S[t][2 + e] = -INFINITY;
-                }
-                over |= fmaf(fmaxf(S[t][e], S[t][2 + e]), a.scale2, -ref[t][e]) > UP;
+            for (int z = e; z < 4; z += 2) S[z] += S2[z];
+            if (masked) {
+                const int seen = min(all + token_of(a, row0 + 2 * c + e), n);
+                if (j0 + g >= seen) S[e] = -INFINITY;
+                if (j0 + 8 + g >= seen) S[2 + e] = -INFINITY;
             }
+            over |= fmaf(fmaxf(S[e], S[2 + e]), a.scale2, -ref[e]) > UP;
+        }
         if (__any_sync(FW_FULL, over)) {
             settled = true;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int e = 0; e < 2; ++e) {
+                float top = fmaxf(S[e], S[2 + e]);
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 16)) * a.scale2;
+                // (a row moves by its own scores alone, whatever the rows beside it do)
+                const float old = mx[e], now = old == -INFINITY || top > old + UP ? top : old;
+                const float al = now > old ? ex2(old - now) : 1.f;  // (0 where nothing was seen before)
+                mx[e] = now;
+                ref[e] = now == -INFINITY ? 0.f : now;
+                settled = settled && now > -INFINITY;
+                l[e] *= al;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float top = fmaxf(S[t][e], S[t][2 + e]);
-                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 4));
-                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 8));
-                    top = fmaxf(top, __shfl_xor_sync(FW_FULL, top, 16)) * a.scale2;
-                    // (a row moves by its own scores alone, whatever the rows beside it do)
-                    const float old = mx[t][e], now = old == -INFINITY || top > old + UP ? top : old;
-                    const float al = now > old ? ex2(old - now) : 1.f;  // (0 where nothing was seen before)
-                    mx[t][e] = now;
-                    ref[t][e] = now == -INFINITY ? 0.f : now;
-                    settled = settled && now > -INFINITY;
-                    l[t][e] *= al;
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) O[t][i][e] *= al, O[t][i][2 + e] *= al;
-                }
+                for (int i = 0; i < MT; ++i) O[i][e] *= al, O[i][2 + e] *= al;
+            }
             settled = __all_sync(FW_FULL, settled);
         }
         // the weights' upper halves and what they leave, with 2^-22 of the weight more, so that it is 0 only where the
         // weight is
-        uint32_t ph[NT][2], pl[NT][2];
+        uint32_t ph[2], pl[2];
+        float r[4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float r[4];
+        for (int z = 0; z < 4; ++z) {
+            const float p = S[z] = ex2(fmaf(S[z], a.scale2, -ref[z & 1]));
+            r[z] = fmaf(p, 0x1p-22f, p - __uint_as_float(__float_as_uint(p) & 0xffff0000u));
+            l[z & 1] += p;
+        }
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
-                const float p = S[t][z] = ex2(fmaf(S[t][z], a.scale2, -ref[t][z & 1]));
-                r[z] = fmaf(p, 0x1p-22f, p - __uint_as_float(__float_as_uint(p) & 0xffff0000u));
-                l[t][z & 1] += p;
-            }
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                ph[t][z] = transpose8x8(__byte_perm(__float_as_uint(S[t][2 * z]), __float_as_uint(S[t][2 * z + 1]), 0x7632));
-                pl[t][z] = transpose8x8(pack_bf16(r[2 * z], r[2 * z + 1]));
-            }
+        for (int z = 0; z < 2; ++z) {
+            ph[z] = transpose8x8(__byte_perm(__float_as_uint(S[2 * z]), __float_as_uint(S[2 * z + 1]), 0x7632));
+            pl[z] = transpose8x8(pack_bf16(r[2 * z], r[2 * z + 1]));
         }
         // O^T += V^T P^T: columns g, g + 8 of each 16, keys 2c, 2c + 1 and 8 behind them
         uint32_t in0 = ~0u, in1 = ~0u;
@@ -350,12 +338,9 @@ template <int D, int NT> struct Rows {
             }
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int i = 0; i < MT; ++i) mma(O[i], V[i], ph[0], ph[1]);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) mma(O[t][i], V[i], ph[t][0], ph[t][1]);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) mma(O[t][i], V[i], pl[t][0], pl[t][1]);
-        }
+        for (int i = 0; i < MT; ++i) mma(O[i], V[i], pl[0], pl[1]);
         if (odd) add_odd(a, tk + BR * D * 2, S, j0, all, n, row0, lane);
     }
 
@@ -380,25 +365,23 @@ template <int D, int NT> struct Rows {
         return x;
     }
     // What they give the rows that do see them.
-    __device__ void add_odd(const AttendArgs &a, const uint8_t *tv, const float (&P)[NT][4], int j0, int all, int n, int row0,
+    __device__ void add_odd(const AttendArgs &a, const uint8_t *tv, const float (&P)[4], int j0, int all, int n, int row0,
                             int lane)
     {
         const int g = lane >> 2, c = lane & 3;
         for (int key = max(0, all - j0); key < min(BR, n - j0); ++key) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int e = 0; e < 2; ++e) {
+                const float p = __shfl_sync(FW_FULL, key < 8 ? P[e] : P[2 + e], (key & 7) * 4 + c);
+                if (j0 + key >= all + token_of(a, row0 + 2 * c + e)) continue;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float p = __shfl_sync(FW_FULL, key < 8 ? P[t][e] : P[t][2 + e], (key & 7) * 4 + c);
-                    if (j0 + key >= all + token_of(a, row0 + 8 * t + 2 * c + e)) continue;
+                for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i)
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const float v = bf16_to_f32(*reinterpret_cast<const uint16_t *>(tv + piece(key, 2 * i + z) + 2 * g));
-                            if (!isfinite(v)) O[t][i][2 * z + e] += p * v;
-                        }
-                }
+                    for (int z = 0; z < 2; ++z) {
+                        const float v = bf16_to_f32(*reinterpret_cast<const uint16_t *>(tv + piece(key, 2 * i + z) + 2 * g));
+                        if (!isfinite(v)) O[i][2 * z + e] += p * v;
+                    }
+            }
         }
     }
 
@@ -406,15 +389,13 @@ template <int D, int NT> struct Rows {
     __device__ __forceinline__ void close()
     {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float sum = l[t][e];
-                sum += __shfl_xor_sync(FW_FULL, sum, 4);
-                sum += __shfl_xor_sync(FW_FULL, sum, 8);
-                sum += __shfl_xor_sync(FW_FULL, sum, 16);
-                l[t][e] = sum;
-            }
+        for (int e = 0; e < 2; ++e) {
+            float sum = l[e];
+            sum += __shfl_xor_sync(FW_FULL, sum, 4);
+            sum += __shfl_xor_sync(FW_FULL, sum, 8);
+            sum += __shfl_xor_sync(FW_FULL, sum, 16);
+            l[e] = sum;
+        }
     }
 };
 
@@ -427,12 +408,13 @@ __device__ __forceinline__ int64_t out_row(const AttendArgs &a, int seq, int hk,
 // lse of a row with running maximum mx and sum l of 2^(x - mx)
 __device__ __forceinline__ float lse_of(float mx, float l) { return l == 0.f ? -INFINITY : (mx + log2f(l)) * 0.6931471805599453f; }
 
-template <int D, int NT, int TW>
-__global__ void __launch_bounds__(32 * Cfg<D, NT, TW>::W, 1)
+template <int D, int TW>
+__global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
     k_pages_attend(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
 {
-    using C = Cfg<D, NT, TW>;
-    constexpr int W = C::W, AT = 32 * W, TEAMS = C::TEAMS, MT = D / 16, RT = C::RT;
+    constexpr int W = range_warps(D, TW), AT = 32 * W;
+    using C = Cfg<D, TW, W>;
+    constexpr int TEAMS = C::TEAMS, MT = D / 16, RT = C::RT;
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
     __shared__ __align__(8) uint64_t full[TEAMS][C::STAGES], empty[TEAMS][C::STAGES];
@@ -441,7 +423,7 @@ __global__ void __launch_bounds__(32 * Cfg<D, NT, TW>::W, 1)
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
     const int team = wid / TW, member = wid % TW;
-    const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT + member * 8 * NT, rows = a.group * a.m;
+    const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT + member * 8, rows = a.group * a.m;
     const Pages &s = a.s;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Ring<D, C::STAGES, TW> ring;
@@ -522,12 +504,12 @@ __global__ void __launch_bounds__(32 * Cfg<D, NT, TW>::W, 1)
         ++pu;
         ++pb;
     };
-    Rows<D, NT> R;
+    Rows<D> R;
     R.read(a, ph / a.kv_heads, ph % a.kv_heads, row0, lane);
     if (member == 0) {
 #pragma unroll 1
-        for (int i = 0; i < C::STAGES - (TW > 1 ? 1 : 0); ++i) fetch();  // (with more warps a stage behind, so that the first
-    }                                                                   // does not wait for the others at every block)
+        for (int i = 0; i < C::AHEAD; ++i) fetch();
+    }
 
     int h = s_h0[team], b = s_b0[team];  // the segment: blocks of one cell
     while (u < u1) {
@@ -548,49 +530,46 @@ __global__ void __launch_bounds__(32 * Cfg<D, NT, TW>::W, 1)
         for (int blk = b; blk < bend; ++blk) {
             const int stage = ring.next();
             if (stage < 0) break;
-            if (s_page[team][stage] >= 0)
-                R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
-            else
+            if (s_page[team][stage] < 0)
                 bad = true;
+            else if (row0 < rows)
+                R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
             ring.release(stage, lane);
             if (member == 0) fetch();
         }
         R.close();
         const bool whole = b == 0 && bend == nb;
         const int seg = u == (int)first ? 0 : 1;
+        float sum[2], inv[2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float sum[2], inv[2];
+        for (int e = 0; e < 2; ++e) {
+            sum[e] = ring.ok ? R.l[e] : NAN;
+            inv[e] = sum[e] == 0.f ? 0.f : 1.f / sum[e];
+        }
+        if (whole) {
+            const int r = row0 + g;
+            uint16_t *dst = a.o + out_row(a, seq, hk, r) * D + 2 * c;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                sum[e] = ring.ok ? R.l[t][e] : NAN;
-                inv[e] = sum[e] == 0.f ? 0.f : 1.f / sum[e];
-            }
-            if (whole) {
-                const int r = row0 + 8 * t + g;
-                uint16_t *dst = a.o + out_row(a, seq, hk, r) * D + 2 * c;
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const uint32_t x = transpose8x8(pack_bf16(R.O[t][i][2 * z] * inv[0], R.O[t][i][2 * z + 1] * inv[1]));
-                        if (r < rows) *reinterpret_cast<uint32_t *>(dst + 16 * i + 8 * z) = x;
-                    }
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = row0 + 8 * t + 2 * c + e;
-                if (r >= rows) continue;
-                if (whole) {
-                    if (a.lse && g == 0) a.lse[out_row(a, seq, hk, r)] = lse_of(R.mx[t][e], sum[e]);
-                } else {
-                    const int64_t at = (((int64_t)tile * a.teams + gw) * 2 + seg) * RT + member * 8 * NT + 8 * t + 2 * c + e;
-                    if (g == 0) a.part_ml[at] = make_float2(R.mx[t][e], sum[e]);
-                    float4 *dst = reinterpret_cast<float4 *>(a.part_o + at * D + g * (D / 8));
-#pragma unroll
-                    for (int i = 0; i < MT; i += 2)
-                        dst[i / 2] = make_float4(R.O[t][i][e], R.O[t][i][2 + e], R.O[t][i + 1][e], R.O[t][i + 1][2 + e]);
+                for (int z = 0; z < 2; ++z) {
+                    const uint32_t x = transpose8x8(pack_bf16(R.O[i][2 * z] * inv[0], R.O[i][2 * z + 1] * inv[1]));
+                    if (r < rows) *reinterpret_cast<uint32_t *>(dst + 16 * i + 8 * z) = x;
                 }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = row0 + 2 * c + e;
+            if (r >= rows) continue;
+            if (whole) {
+                if (a.lse && g == 0) a.lse[out_row(a, seq, hk, r)] = lse_of(R.mx[e], sum[e]);
+            } else {
+                const int64_t at = (((int64_t)tile * a.teams + gw) * 2 + seg) * RT + member * 8 + 2 * c + e;
+                if (g == 0) a.part_ml[at] = make_float2(R.mx[e], sum[e]);
+                float4 *dst = reinterpret_cast<float4 *>(a.part_o + at * D + g * (D / 8));
+#pragma unroll
+                for (int i = 0; i < MT; i += 2)
+                    dst[i / 2] = make_float4(R.O[i][e], R.O[i][2 + e], R.O[i + 1][e], R.O[i + 1][2 + e]);
             }
         }
         if (tile == 0 && member == 0 && lane == 0) {
@@ -707,18 +686,19 @@ template <int D, bool SPREAD> __global__ void __launch_bounds__(32 * JW, 5) k_pa
     if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
 }
 
-// Eight states of a row joined: their (maximum, sum) and E of a lane's columns.
-template <int E, typename FM, typename FO>
-__device__ __forceinline__ void join8(FM ml_of, FO o_of, float &M, float &L, float (&acc)[E])
+// Up to N states of a row joined: their (maximum, sum) and E of a lane's columns.
+template <int N, int E, typename FM, typename FO>
+__device__ __forceinline__ void join(int n, FM ml_of, FO o_of, float &M, float &L, float (&acc)[E])
 {
-    float2 ml[8];
+    float2 ml[N];
     M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) ml[w] = ml_of(w), M = fmaxf(M, ml[w].x);
+    for (int w = 0; w < N; ++w) ml[w] = w < n ? ml_of(w) : make_float2(-INFINITY, 0.f), M = fmaxf(M, ml[w].x);
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
+    for (int w = 0; w < N; ++w) {
+        if (w >= n) break;
         const float f = ml[w].x == M ? 1.f : ex2(ml[w].x - M);
         L = fmaf(f, ml[w].y, L);
 #pragma unroll
@@ -727,28 +707,28 @@ __device__ __forceinline__ void join8(FM ml_of, FO o_of, float &M, float &L, flo
 }
 
 // A cluster of up to FEW CTAs per cell and tile of rows, its blocks dealt out to their teams one by one.
-constexpr int FEW = 8, FW = 8;
-template <int D, int NT, int TW>
-__global__ void __launch_bounds__(32 * FW, 1)
+constexpr int FEW = 12;
+template <int D, int TW>
+__global__ void __launch_bounds__(32 * few_warps(TW), 1)
     k_pages_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
 {
-    using C = Cfg<D, 2, TW>;  // (8 warps, whatever NT is)
-    static_assert(C::W == FW && FEW == 8 && FW == 8, "a warp per row of 8, eight states to join");
-    constexpr int MT = D / 16, RT = TW * 8 * NT, E = D / 32, LDO = D + 4, TEAMS = C::TEAMS, STAGES = C::STAGES;
+    constexpr int W = few_warps(TW);
+    using C = Cfg<D, TW, W>;
+    constexpr int MT = D / 16, RT = C::RT, E = D / 32, LDO = D + 4, TEAMS = C::TEAMS, STAGES = C::STAGES;
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
-    float *s_o = reinterpret_cast<float *>(sm);  // [FW][8][LDO], in the rings' place when these are done
-    static_assert(FW * 8 * LDO * 4 <= C::RING, "the states fit the rings");
+    float *s_o = reinterpret_cast<float *>(sm);  // [W][8][LDO], in the rings' place when these are done
+    static_assert(W * 8 * LDO * 4 <= C::RING, "the states fit the rings");
     __shared__ __align__(8) uint64_t full[TEAMS][STAGES], empty[TEAMS][STAGES];
     __shared__ int32_t s_page[TEAMS][STAGES];
-    __shared__ float2 s_ml[FW][8];
+    __shared__ float2 s_ml[W][8];
     __shared__ float2 s_pml[TW * 8];
     __shared__ int s_code;
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
     const int team = wid / TW, member = wid % TW;
     const int h = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, rows = a.group * a.m;
-    const int tile0 = blockIdx.y * RT, row0 = tile0 + member * 8 * NT;
+    const int tile0 = blockIdx.y * RT, row0 = tile0 + member * 8;
     const Pages &s = a.s;
     const int first = rank + a.cluster * team, step = a.cluster * TEAMS;  // (the first blocks go to different CTAs)
     Window win;
@@ -773,11 +753,11 @@ __global__ void __launch_bounds__(32 * FW, 1)
         pb += step;
     };
     const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
-    Rows<D, NT> R;
+    Rows<D> R;
     R.read(a, seq, hk, row0, lane);
     if (member == 0) {
 #pragma unroll 1
-        for (int i = 0; i < STAGES - (TW > 1 ? 1 : 0); ++i) fetch();
+        for (int i = 0; i < C::AHEAD; ++i) fetch();
     }
     R.start();
     bool bad = false;
@@ -785,10 +765,10 @@ __global__ void __launch_bounds__(32 * FW, 1)
     for (int blk = first; blk < nb; blk += step) {
         const int stage = ring.next();
         if (stage < 0) break;
-        if (s_page[team][stage] >= 0)
-            R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
-        else
+        if (s_page[team][stage] < 0)
             bad = true;
+        else if (row0 < rows)
+            R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
         ring.release(stage, lane);
         if (member == 0) fetch();
     }
@@ -796,85 +776,111 @@ __global__ void __launch_bounds__(32 * FW, 1)
     ring.drain();
     const int code = !ring.ok ? FW_ERR_TIMEOUT : bad ? FW_ERR_INVALID_ARG : FW_OK;
     if (lane == 0 && code != FW_OK) atomicMax(&s_code, code);
+    // ---- the teams' rows joined in the CTA
+    __syncthreads();  // (the rings have been read)
+    if (g == 0) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        if (t > 0 && tile0 + 8 * t >= rows) break;
-        // ---- the teams' rows joined in the CTA, a warp per row of the members' 8
-        if (t > 0)
-            cluster_sync();  // (the rows before have been read)
-        else
-            __syncthreads();  // (the rings have been read)
-        if (g == 0) {
+        for (int e = 0; e < 2; ++e) s_ml[wid][2 * c + e] = make_float2(R.mx[e], ring.ok ? R.l[e] : NAN);
+    }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) s_ml[wid][2 * c + e] = make_float2(R.mx[t][e], ring.ok ? R.l[t][e] : NAN);
-        }
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int f = 0; f < 4; ++f) s_o[(wid * 8 + 2 * c + (f & 1)) * LDO + 16 * i + 8 * (f >> 1) + g] = R.O[i][f];
+    __syncthreads();
+    float M, L, acc[E];
+    for (int x = wid; x < TW * 8; x += W) {  // row x & 7 of member x >> 3
+        join<TEAMS, E>(TEAMS, [&](int w) { return s_ml[w * TW + (x >> 3)][x & 7]; },
+                       [&](int w, int e) { return s_o[(w * TW * 8 + x) * LDO + lane + 32 * e]; }, M, L, acc);
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+        for (int e = 0; e < E; ++e) s_o[x * LDO + lane + 32 * e] = acc[e];  // (in the first team's place)
+        if (lane == 0) s_pml[x] = make_float2(M, L);
+    }
+    cluster_sync();
+    // ---- and over the cluster's CTAs: rows dealt out to them and their warps
+    for (int x = rank + a.cluster * wid; x < TW * 8; x += a.cluster * W) {
+        const int r = tile0 + x;
+        if (r >= rows) continue;
+        join<FEW, E>(a.cluster, [&](int w) { return make_float2(remote(&s_pml[x].x, w), remote(&s_pml[x].y, w)); },
+                     [&](int w, int e) { return remote(&s_o[x * LDO + lane + 32 * e], w); }, M, L, acc);
+        const int64_t out = out_row(a, seq, hk, r);
+        const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-                for (int z = 0; z < 2; ++z) s_o[(wid * 8 + 2 * c + e) * LDO + 16 * i + 8 * z + g] = R.O[t][i][2 * z + e];
-        __syncthreads();
-        float M, L, acc[E];
-#pragma unroll
-        for (int k = 0; k < TW; ++k) {  // row wid of member k's
-            join8<E>([&](int w) { return w < TEAMS ? s_ml[w * TW + k][wid] : make_float2(-INFINITY, 0.f); },
-                     [&](int w, int e) { return w < TEAMS ? s_o[((w * TW + k) * 8 + wid) * LDO + lane + 32 * e] : 0.f; }, M, L, acc);
-#pragma unroll
-            for (int e = 0; e < E; ++e) s_o[(k * 8 + wid) * LDO + lane + 32 * e] = acc[e];  // (in the first team's place)
-            if (lane == 0) s_pml[k * 8 + wid] = make_float2(M, L);
-        }
-        cluster_sync();
-        // ---- and over the cluster's CTAs: rows dealt out to them and their warps
-        for (int x = rank + a.cluster * wid; x < TW * 8; x += a.cluster * FW) {
-            const int r = tile0 + (x >> 3) * 8 * NT + 8 * t + (x & 7);
-            if (r >= rows) continue;
-            join8<E>([&](int w) { return w < a.cluster ? make_float2(remote(&s_pml[x].x, w), remote(&s_pml[x].y, w))
-                                                      : make_float2(-INFINITY, 0.f); },
-                     [&](int w, int e) { return w < a.cluster ? remote(&s_o[x * LDO + lane + 32 * e], w) : 0.f; }, M, L, acc);
-            const int64_t out = out_row(a, seq, hk, r);
-            const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
-            if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
-        }
-        if (t == 0 && rank == 0 && blockIdx.y == 0 && wid == FW - 1 && a.status) {
-            const int codes = __reduce_max_sync(FW_FULL, lane < a.cluster ? (int)remote_u(&s_code, lane) : 0);
-            if (lane == 0) a.status[h] = codes;
-        }
+        for (int e = 0; e < E; ++e)
+            a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
+        if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
+    }
+    if (rank == 0 && blockIdx.y == 0 && wid == W - 1 && a.status) {
+        const int codes = __reduce_max_sync(FW_FULL, lane < a.cluster ? (int)remote_u(&s_code, lane) : 0);
+        if (lane == 0) a.status[h] = codes;
     }
     cluster_sync();  // no CTA leaves while another reads its rows
+}
+
+// How many clusters of each size find room on the GPU at once, a CTA an SM (GPUs differ in the SMs of their parts), and the
+// sizes.  Sizes above 8 are let in for these kernels.
+constexpr int SIZES = 6, SIZE[SIZES] = {12, 10, 8, 4, 2, 1};
+void clusters_at_once(int (&room)[SIZES])
+{
+    static std::atomic<int> cache[64][SIZES];
+    const int known[SIZES] = {9, 14, 16, 37, 77, 153};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = -1;
+    for (int i = 0; i < SIZES; ++i) {
+        int n = dev >= 0 ? cache[dev][i].load(std::memory_order_relaxed) : known[i];  // (one more than it is)
+        if (n == 0) {
+            const auto kernel = k_pages_attend_few<128, 1>;
+            constexpr size_t smem = Cfg<128, 1, few_warps(1)>::SMEM;
+            cudaLaunchAttribute at[1];
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = (unsigned)SIZE[i];
+            at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)SIZE[i]);
+            cfg.blockDim = dim3(32 * few_warps(1));
+            cfg.dynamicSmemBytes = smem;
+            cfg.attrs = at;
+            cfg.numAttrs = 1;
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+                cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+                cudaGetLastError();  // (sizes that the GPU has no room for are not taken)
+                n = 0;
+            }
+            cache[dev][i].store(++n, std::memory_order_relaxed);
+        }
+        room[i] = n - 1;
+    }
 }
 
 // CTAs of a cell's cluster where that is the faster way, else 0 (ranges).  Both ways' times in us, from sweeps of cells of
 // unlike lengths (the longest about twice the mean, which the host does not know).  Ranges: two launches, the sums
 // over the cells, the joining, and the blocks of all over the GPU.  Clusters: a launch, and the longest cell's blocks over
-// its CTAs, which share the memory with all others at first and have their SMs' whole rate at the end.
-int cluster_of(const fw_pages &p, const fw_pages_query &q, int NT, int TW, int tiles, int sms)
+// its CTAs, which share the memory with all others at first and have their SMs' whole rate at the end.  (d = 128, four query
+// rows, ranges against clusters: 8 cells of up to 8,000 rows 16.3 us against 11.4, 64 of up to 3,000 17.9 against 16.1, of up
+// to 12,000 31 against 40; 64 of up to 50 13 against 6.)
+int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, int sms)
 {
     if (q.longest == 0) return 0;
-    // an SM's time for a block of 16 rows: 91 GB/s for one tile of query rows, products for more
-    const double per = (p.d == 128 ? 1.0 : 0.5) * (NT == 1 ? 0.09 : 0.15 * TW);
+    // an SM's time for a block of 16 rows: 91 GB/s for 8 query rows, products for more
+    const double per = (p.d == 128 ? 1.0 : 0.5) * std::max(0.09, 0.08 * TW);
     const double memory = BR * p.d * 4 / 6.7e6;  // and the memory's
     const double blocks = (q.longest + BR - 1) / BR, all = 0.5 * blocks * p.cells * tiles;
-    struct Rule {
-        int ctas, clusters;  // that find room at once
-    };
-    int best = 0;
+    int best = 0, room[SIZES];
     double least = 12.0 + std::max(all * per / sms, all * memory / tiles);
-    for (const Rule &r : {Rule{8, 14}, Rule{4, 36}, Rule{2, 72}, Rule{1, 152}}) {
-        const int64_t clusters = (int64_t)p.cells * tiles, waves = (clusters + r.clusters - 1) / r.clusters;
-        const double at_once = (double)std::min<int64_t>(clusters, r.clusters) * r.ctas * memory / tiles;
-        const double t = waves * (5.5 + blocks / r.ctas * 0.5 * (per + std::max(per, at_once)));
-        if (t < least) best = r.ctas, least = t;
+    clusters_at_once(room);
+    for (int i = SIZES - 1; i >= 0; --i) {
+        if (room[i] < 1) continue;
+        const int64_t clusters = (int64_t)p.cells * tiles, waves = (clusters + room[i] - 1) / room[i];
+        const double at_once = (double)std::min<int64_t>(clusters, room[i]) * SIZE[i] * memory / tiles;
+        const double t = waves * (5.5 + blocks / SIZE[i] * 0.5 * (per + std::max(per, at_once)));
+        if (t < least - 0.1) best = SIZE[i], least = t;
     }
     return best;
 }
 
 struct Plan {
     int few;  // CTAs of a cell's cluster, or 0
-    int G, NT, TW, teams, RT, tiles;
+    int G, TW, teams, RT, tiles;
     size_t start, plan, flags, ml, o, bytes;
 };
 void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
@@ -882,22 +888,37 @@ void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
     int sms = 0;
     if (device_sms(&sms) != FW_OK) sms = 152;  // no device: the size query still answers
     const int rows = q.group * q.m;
-    x.NT = rows <= 8 ? 1 : 2;
-    x.TW = 1;
-    while (x.TW < 8 && x.TW * 8 * x.NT < rows) x.TW *= 2;
+    // as many warps a team as hold the rows; beyond 48 rows, tiles of 48 or 32, whichever leave fewer warps without rows
+    // (64 x 4,096 rows, d = 128, 64 query rows: two tiles of 32 94 us, one of 96 118)
+    const int need = (rows + 7) / 8;
+    x.TW = need > 6 && (need + 5) / 6 * 6 > (need + 3) / 4 * 4 ? 4 : 6;
+    for (const int tw : {4, 3, 2, 1})
+        if (need <= tw) x.TW = tw;
     x.start = x.plan = x.flags = x.ml = x.o = x.bytes = 0;
-    x.RT = x.TW * 8 * x.NT;
+    x.RT = x.TW * 8;
     x.tiles = (rows + x.RT - 1) / x.RT;
-    x.few = cluster_of(p, q, x.NT, x.TW, x.tiles, sms);
+    x.few = cluster_of(p, q, x.TW, x.tiles, sms);
     if (x.few) return;
     x.G = std::max(1, sms / x.tiles);  // one wave
-    x.teams = x.G * ((p.d == 64 && x.NT == 1 ? 16 : 8) / x.TW);
+    x.teams = x.G * (range_warps(p.d, x.TW) / x.TW);
     x.plan = align256((size_t)p.cells * 4);
     x.flags = x.plan + 256;
     x.ml = x.flags + align256((size_t)x.teams * 8);
     const size_t parts = (size_t)x.tiles * x.teams * 2 * x.RT;
     x.o = x.ml + align256(parts * 8);
     x.bytes = x.o + align256(parts * p.d * 4);
+}
+
+// Lets a kernel have clusters of more than 8 CTAs on the current device, once per device (a bit each).
+fw_status wide_clusters(const void *kernel, std::atomic<uint64_t> &done)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return FW_ERR_CUDA;
+    const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return FW_OK;
+    FW_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return FW_OK;
 }
 
 template <typename K>
@@ -921,33 +942,38 @@ fw_status launch(K kernel, int grid, int tiles, int cluster, int threads, size_t
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }
-template <int D, int NT, int TW>
+template <int D, int TW>
 fw_status launch_ranges(const Plan &x, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
 {
-    using C = Cfg<D, NT, TW>;
+    constexpr int W = range_warps(D, TW);
     static std::atomic<uint64_t> done{0};
-    return launch(k_pages_attend<D, NT, TW>, x.G, x.tiles, 0, 32 * C::W, C::SMEM, mk, mv, a, done, s);
+    return launch(k_pages_attend<D, TW>, x.G, x.tiles, 0, 32 * W, Cfg<D, TW, W>::SMEM, mk, mv, a, done, s);
 }
-template <int D, int NT, int TW>
+template <int D, int TW>
 fw_status launch_few(const Plan &x, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
 {
-    static std::atomic<uint64_t> done{0};
-    return launch(k_pages_attend_few<D, NT, TW>, cells * x.few, x.tiles, x.few, 32 * FW, Cfg<D, 2, TW>::SMEM, mk, mv, a, done, s);
+    constexpr int W = few_warps(TW);
+    static std::atomic<uint64_t> done{0}, wide{0};
+    if (x.few > 8) {
+        const fw_status st = wide_clusters((const void *)k_pages_attend_few<D, TW>, wide);
+        if (st != FW_OK) return st;
+    }
+    return launch(k_pages_attend_few<D, TW>, cells * x.few, x.tiles, x.few, 32 * W, Cfg<D, TW, W>::SMEM, mk, mv, a, done, s);
 }
-template <int D, int NT, int TW>
+template <int D, int TW>
 fw_status launch_one(const Plan &x, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
 {
-    return x.few ? launch_few<D, NT, TW>(x, cells, mk, mv, a, s) : launch_ranges<D, NT, TW>(x, mk, mv, a, s);
+    return x.few ? launch_few<D, TW>(x, cells, mk, mv, a, s) : launch_ranges<D, TW>(x, mk, mv, a, s);
 }
 template <int D>
 fw_status attend(const Plan &x, int cells, int rows, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a,
                  cudaStream_t s)
 {
-    const fw_status st = x.NT == 1   ? launch_one<D, 1, 1>(x, cells, mk, mv, a, s)
-                         : x.TW == 1 ? launch_one<D, 2, 1>(x, cells, mk, mv, a, s)
-                         : x.TW == 2 ? launch_one<D, 2, 2>(x, cells, mk, mv, a, s)
-                         : x.TW == 4 ? launch_one<D, 2, 4>(x, cells, mk, mv, a, s)
-                                     : launch_one<D, 2, 8>(x, cells, mk, mv, a, s);
+    const fw_status st = x.TW == 1   ? launch_one<D, 1>(x, cells, mk, mv, a, s)
+                         : x.TW == 2 ? launch_one<D, 2>(x, cells, mk, mv, a, s)
+                         : x.TW == 3 ? launch_one<D, 3>(x, cells, mk, mv, a, s)
+                         : x.TW == 4 ? launch_one<D, 4>(x, cells, mk, mv, a, s)
+                                     : launch_one<D, 6>(x, cells, mk, mv, a, s);
     if (x.few) return st;
     if (st != FW_OK) return st;
     // the joining kernel starts as the first one's CTAs leave
