@@ -586,9 +586,10 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
 }
 
 // The parts of a cell that several teams share, joined in their order; empty cells' outputs.  Each of a CTA's JW warps
-// takes a row, or (SPREAD) all of them one row's parts, where there are few rows and so the parts may be many.
-constexpr int JW = 4;
-template <int D, bool SPREAD> __global__ void __launch_bounds__(32 * JW, 5) k_pages_join(const AttendArgs a, int RT)
+// takes a row, or (SPREAD) all of them one row's parts, where there are few rows and so the parts may be many: the fewer
+// the rows the more warps (8 cells x 4 rows of 150 parts each, 32,768 rows a cell: 35 us with 4 warps, 26 with 16; 64 cells x 20
+// rows: 21.6 with 4, 27 with 8).  CTAs of 4 are small enough to wait beside the first kernel's.
+template <int D, bool SPREAD, int JW> __global__ void __launch_bounds__(32 * JW, JW == 4 ? 5 : 1) k_pages_join(const AttendArgs a, int RT)
 {
     constexpr int E = D / 32;
     __shared__ float s_o[SPREAD ? JW : 1][D];
@@ -872,7 +873,7 @@ int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, in
         if (room[i] < 1) continue;
         const int64_t clusters = (int64_t)p.cells * tiles, waves = (clusters + room[i] - 1) / room[i];
         const double at_once = (double)std::min<int64_t>(clusters, room[i]) * SIZE[i] * memory / tiles;
-        const double t = waves * (5.5 + blocks / SIZE[i] * 0.5 * (per + std::max(per, at_once)));
+        const double t = waves * (5.2 + 0.1 * SIZE[i] + blocks / SIZE[i] * 0.5 * (per + std::max(per, at_once)));
         if (t < least - 0.1) best = SIZE[i], least = t;
     }
     return best;
@@ -978,6 +979,7 @@ fw_status attend(const Plan &x, int cells, int rows, const CUtensorMap &mk, cons
     if (st != FW_OK) return st;
     // the joining kernel starts as the first one's CTAs leave
     const bool spread = x.teams >= 4 * cells && (int64_t)cells * rows <= 16 * x.G;
+    const int JW = !spread ? 4 : cells * rows <= 64 ? 16 : cells * rows <= 2 * x.G ? 8 : 4;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -987,8 +989,10 @@ fw_status attend(const Plan &x, int cells, int rows, const CUtensorMap &mk, cons
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const cudaError_t e = spread ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true>, a, x.RT)
-                                 : cudaLaunchKernelEx(&cfg, k_pages_join<D, false>, a, x.RT);
+    const cudaError_t e = JW == 16 ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true, 16>, a, x.RT)
+                          : JW == 8 ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true, 8>, a, x.RT)
+                          : spread ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true, 4>, a, x.RT)
+                                   : cudaLaunchKernelEx(&cfg, k_pages_join<D, false, 4>, a, x.RT);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }
