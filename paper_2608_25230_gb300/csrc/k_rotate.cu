@@ -71,18 +71,14 @@ __device__ __forceinline__ uint64_t swap2(uint64_t v)
     unpack2(v, x, y);
     return pack2(y, x);
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
 {
     uint64_t r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+// (a product and -0, which changes nothing, are one instruction)
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { return fma2(a, b, 0x8000000080000000ull); }
 __device__ __forceinline__ uint32_t to_bf16x2(uint64_t v)
 {
     float x, y;
@@ -112,7 +108,7 @@ __device__ __forceinline__ void weights8(const RotateArgs &a, int kv, int at, ui
     }
 }
 
-template <int LPL, bool INTER> __global__ void __launch_bounds__(32 * RW, 3) k_qk_rotate(const RotateArgs a)
+template <int LPL, bool INTER, bool FULL> __global__ void __launch_bounds__(32 * RW, 3) k_qk_rotate(const RotateArgs a)
 {
     constexpr int HP = 32 / LPL, PER = 8 / HP;  // heads at a time; frequencies that a lane works out
     __shared__ uint4 s_x[RW][AHEAD + 1][2][32];  // a lane's own pieces: no lane reads another's
@@ -122,9 +118,13 @@ template <int LPL, bool INTER> __global__ void __launch_bounds__(32 * RW, 3) k_q
     const int part = (int)(id - row * a.split);
     if (row >= a.rows) return;
 
-    const bool rotated = 16 * p < a.rot, there = 16 * p < a.d;
-    const int at0 = rotated && !INTER ? 8 * p : 16 * p;
-    const int at1 = rotated && !INTER ? a.rot / 2 + 8 * p : 16 * p + 8;
+    // A lane's two pieces of 8 columns.  Half apart, they are a pair's, in the rotated columns; neighbours are in one
+    // piece, so any two do.  The lanes' first pieces lie side by side, and so do their second ones, for whole sectors.
+    const bool there = 16 * p < a.d, pair = FULL || 16 * p < a.rot;
+    const int rest = INTER || FULL ? 0 : a.rot, q = INTER || pair ? p : p - a.rot / 16;
+    const int at0 = (INTER || pair ? 0 : rest) + 8 * q;
+    const int at1 = at0 + (INTER ? a.d / 2 : pair ? a.rot / 2 : (a.d - rest) / 2);
+    const bool turn0 = FULL || (INTER ? at0 < a.rot : pair), turn1 = FULL || (INTER ? at1 < a.rot : pair);
     // chunks of HP heads: the queries' heads, then the keys'
     const int chunks_q = (a.q_heads + HP - 1) / HP, chunks = chunks_q + (a.kv_heads + HP - 1) / HP;
     const uint32_t mem = (uint32_t)__cvta_generic_to_shared(&s_x[wid][0][0][lane]);
@@ -169,8 +169,8 @@ template <int LPL, bool INTER> __global__ void __launch_bounds__(32 * RW, 3) k_q
         float c[PER], s[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int f = 8 * p + (hl * PER + i) % 8;
-            const float x = rotated ? a.inv_freq[f] : 0.f;
+            const int j = (hl * PER + i) % 8, f = INTER ? (j < 4 ? at0 : at1) / 2 + j % 4 : 8 * p + j;
+            const float x = f < a.rot / 2 ? a.inv_freq[f] : 0.f;
             // half turns in [-1, 1): the upper 32 bits of the product
             const float h = (float)(int32_t)((uint64_t)pos * turns_of(x) >> 32) * 0x1p-31f;
             sincospif(isfinite(x) ? h : NAN, &s[i], &c[i]);
@@ -199,9 +199,9 @@ template <int LPL, bool INTER> __global__ void __launch_bounds__(32 * RW, 3) k_q
 #pragma unroll
             for (int i = 0; i < 4; ++i) A[0][i] = A[1][i] = 0;
         }
-        if (rotated) {
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
+        for (int z = 0; z < 2; ++z) {
+            if (z ? turn1 : turn0) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if constexpr (INTER) {
@@ -214,6 +214,7 @@ template <int LPL, bool INTER> __global__ void __launch_bounds__(32 * RW, 3) k_q
                         A[z][i] = mul2(A[z][i], pack2(cs[2 * i], cs[2 * i + 1]));
                     }
                 }
+            }
         }
         int h = (ch - first) * HP + hl;
         uint16_t *dst = (kv ? a.k_out + row * a.k_out_row + h * a.k_out_head : a.q_out + row * a.q_out_row + h * a.q_out_head) + at0;
@@ -248,11 +249,10 @@ template <int LPL, bool INTER> __global__ void __launch_bounds__(32 * RW, 3) k_q
             uint32_t out[2][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                // (what is not rotated takes no part of another column, be that no number)
                 uint64_t u = mul2(y[0][i], A[0][i]), v = mul2(y[1][i], A[1][i]);
-                if (rotated) {
-                    u = fma2(INTER ? swap2(y[0][i]) : y[1][i], INTER ? B[0][i] : B[1][i], u);
-                    v = fma2(INTER ? swap2(y[1][i]) : y[0][i], INTER ? B[1][i] : B[0][i], v);
-                }
+                if (turn0) u = fma2(INTER ? swap2(y[0][i]) : y[1][i], INTER ? B[0][i] : B[1][i], u);
+                if (turn1) v = fma2(INTER ? swap2(y[1][i]) : y[0][i], INTER ? B[1][i] : B[0][i], v);
                 out[0][i] = to_bf16x2(mul2(u, inv));
                 out[1][i] = to_bf16x2(mul2(v, inv));
             }
@@ -270,10 +270,15 @@ template <int LPL> fw_status launch(RotateArgs &a, int sms, cudaStream_t s)
     const int chunks = (a.q_heads + HP - 1) / HP + (a.kv_heads + HP - 1) / HP;
     a.split = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, (int64_t)sms * 32 / a.rows));
     const unsigned grid = (unsigned)((a.rows * a.split + RW - 1) / RW);
-    if (a.interleaved)
-        FW_LAUNCH((k_qk_rotate<LPL, true>), grid, 32 * RW, 0, s, a);
+    // (all columns rotated: every lane does the same)
+    if (a.interleaved && a.rot == a.d)
+        FW_LAUNCH((k_qk_rotate<LPL, true, true>), grid, 32 * RW, 0, s, a);
+    else if (a.interleaved)
+        FW_LAUNCH((k_qk_rotate<LPL, true, false>), grid, 32 * RW, 0, s, a);
+    else if (a.rot == a.d)
+        FW_LAUNCH((k_qk_rotate<LPL, false, true>), grid, 32 * RW, 0, s, a);
     else
-        FW_LAUNCH((k_qk_rotate<LPL, false>), grid, 32 * RW, 0, s, a);
+        FW_LAUNCH((k_qk_rotate<LPL, false, false>), grid, 32 * RW, 0, s, a);
     return FW_OK;
 }
 
