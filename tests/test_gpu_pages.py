@@ -223,3 +223,130 @@ def test_bad_books(fw):
     b.p.next.fill_(-5)  # (a place to search from that is none: the first page)
     b.m.next = 0
     b.append(17)
+
+
+@pytest.mark.parametrize("cells,width,N,P,d", [(40, 12, 700, 16, 64), (7, 300, 1700, 16, 64), (33, 600, 3000, 16, 128)])
+def test_forks_of_many_cells_and_long_tables(fw, cells, width, N, P, d):
+    """More cells than one CTA takes, tables longer than what is asked for early."""
+    r = random.Random(f"{cells} {width}")
+    b = Both(fw, cells, N, P, width, d)
+    b.append(min(P * (width - 1), P * N // cells // 2))
+    b.set_counts([r.randint(0, n) for n in b.m.counts])
+    b.append(1)
+    for _ in range(4):
+        b.fork([r.choice([h, r.randrange(cells), r.randrange(cells), -1, cells + 3]) for h in range(cells)])
+        b.append(r.choice([1, P + 1]))
+    b.fork([-1] * cells)
+    assert all(b.m.free)
+
+
+def test_many_cells_in_a_large_pool(fw):
+    """More cells than the plan's CTA has threads, more words of free bits than it asks for at a time, a search round the
+    end."""
+    r = random.Random(3)
+    cells, N, P, width = 2500, 140000, 16, 70
+    b = Both(fw, cells, N, P, width, 64)
+    b.p.next.fill_(N - 1000)
+    b.m.next = N - 1000
+    b.append(3)
+    b.append(200)  # (13 pages more a cell)
+    b.fork([r.choice([h, h, r.randrange(cells), -1]) for h in range(cells)])
+    b.append(1)
+    b.append(700)  # (32,000 pages are in use, these do not all fit)
+    b.set_counts([n // 2 for n in b.m.counts])
+    b.keep(*picks(r, b.m.counts))
+    b.compact(40, *picks(r, [40] * cells))
+    b.append(60)
+
+
+def test_pool_nearly_full(fw):
+    """Free pages far from where the search begins, a few among many words of none."""
+    b = Both(fw, 3, 300000, 16, 100000, 64)
+    b.append(16 * 99990)
+    b.fork([0, 1, 2])
+    b.set_counts([16 * 99990 - 5, 7, 16 * 500])
+    b.append(40)
+    b.fork([0, -1, 2])
+    b.append(16 * 70000)
+    b.append(16 * 30000)
+
+
+def test_calls_in_a_graph(fw):
+    """A captured step (append, fork, keep), replayed: it goes by the books as they are then."""
+    cells, P, d = 6, 16, 64
+    b = Both(fw, cells, 200, P, 12, d)
+    b.append(21)
+    ids = b.idents(cells, 1)
+    k, v = as_rows(ids.view(1, cells, 1).transpose(1, 2), d)
+    src = torch.tensor([0, 0, 2, 3, 2, -1], dtype=torch.int32, device="cuda")
+    off, pos = [0, 3, 5, 5, 9, 9, 9], [0, 2, 20, 1, 19, 0, 1, 2, 3]
+    o, q = torch.tensor(off, device="cuda"), torch.tensor(pos, dtype=torch.int32, device="cuda")
+    st = [torch.empty(cells, dtype=torch.int32, device="cuda") for _ in range(3)]
+    ws = [fw.pages_append_workspace(b.p, 1), fw.pages_fork_workspace(b.p), fw.pages_compact_workspace(b.p, 9)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        fw.pages_append(b.p, k, v, status=st[0], workspace=ws[0])
+        fw.pages_fork(b.p, src, status=st[1], workspace=ws[1])
+        fw.pages_append(b.p, k, v, status=st[2], workspace=ws[0])
+    one = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(one):
+        fw.pages_keep(b.p, o, q, status=b.status, workspace=ws[2])
+    for _ in range(3):
+        for w in ws:
+            w.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        assert st[0].tolist() == b.m.append(1, lambda h, j: int(ids[h, 0]))
+        assert st[1].tolist() == b.m.fork(src.tolist())
+        b.status.copy_(st[2])
+        b.check(b.m.append(1, lambda h, j: int(ids[h, 0])))
+    one.replay()
+    b.check(b.m.compact(off, pos))
+
+
+def test_a_book_put_back_undoes_a_step(fw):
+    b = Both(fw, 4, 60, 32, 5, 128)
+    b.append(40)
+    b.fork([0, 0, 2, 3])
+    before, k, v = b.p.book.clone(), b.p.k.clone(), b.p.v.clone()
+    rows = [[(b.p.table[h, r // 32].item(), r % 32) for r in range(40)] for h in range(4)]
+    new = torch.ones(1, 5, 4, 128, dtype=torch.bfloat16, device="cuda")
+    fw.pages_append(b.p, new, new)
+    b.p.book.copy_(before)
+    torch.cuda.synchronize()
+    for h in range(4):
+        for page, r in rows[h]:
+            assert torch.equal(b.p.k[page, r].view(torch.int16), k[page, r].view(torch.int16))
+            assert torch.equal(b.p.v[page, r].view(torch.int16), v[page, r].view(torch.int16))
+
+
+def test_strides_streams_and_broadcast_rows(fw):
+    """New rows out of wider projections, one row for all, on another stream; a cache of one cell."""
+    gen = torch.Generator("cuda").manual_seed(1)
+    p = fw.pages_empty(6, 40, 64, max_pages=4, page_rows=16)
+    x = torch.randn(3, 7, 10, 64, generator=gen, device="cuda").to(torch.bfloat16)  # [sequences][tokens][heads]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    fw.pages_append(p, x[:, :, 3:5], x[:, :, 5:7], stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    fw.pages_append(p, x[:, 2:3, 8:10].expand(3, 13, 2, 64), x[0, 0, 0].expand(3, 13, 2, 64))
+    torch.cuda.synchronize()
+    assert p.counts.tolist() == [20] * 6
+    for c in range(6):
+        s, h = divmod(c, 2)
+        t = torch.arange(20, device="cuda")
+        k, v = (y[p.table[c].long()[t // 16], t % 16] for y in (p.k, p.v))
+        assert torch.equal(k[:7], x[s, :, 3 + h]) and torch.equal(v[:7], x[s, :, 5 + h])
+        assert torch.equal(k[7:], x[s, 2, 8 + h].expand(13, 64)) and torch.equal(v[7:], x[0, 0, 0].expand(13, 64))
+    one = fw.pages_empty(1, 3, 128, max_pages=3, page_rows=128)
+    y = torch.randn(1, 300, 1, 128, generator=gen, device="cuda").to(torch.bfloat16)
+    fw.pages_append(one, y, y)
+    # a token-major cache's kept rows
+    z = torch.randn(90, 6, 64, generator=gen, device="cuda").to(torch.bfloat16)
+    o = torch.arange(7, device="cuda") * 10
+    pos = torch.arange(60, dtype=torch.int32, device="cuda")
+    fw.pages_compact(p, z.transpose(0, 1), z.transpose(0, 1), o, pos)
+    torch.cuda.synchronize()
+    assert torch.equal(one.k.view(-1, 128)[:300], y[0, :, 0]) and one.counts.tolist() == [300]
+    for c in range(6):
+        assert torch.equal(p.k[p.table[c, 0].long(), :10], z[10 * c:10 * c + 10, c])

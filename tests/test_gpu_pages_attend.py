@@ -286,3 +286,41 @@ def test_without_lse_and_status(fw):
     fw.pages_attend(p, q, kv_heads=1, out=dict(o=o))
     torch.cuda.synchronize()
     assert torch.equal(o, want["o"])
+
+
+@pytest.mark.parametrize("group,m", [(100, 40), (7, 33), (5, 17), (60, 1)])
+def test_many_query_rows(fw, group, m):
+    """Tiles of rows beyond one team's, the last of them nearly empty."""
+    gen = torch.Generator("cuda").manual_seed(group)
+    counts = [33, 400, 5]
+    p = cache_of(fw, gen, counts, 32, 128)
+    q = rand(gen, 3, m, group, 128)
+    for longest in (0, 400):
+        check_all(fw, p, counts, q, 1, longest=longest)
+
+
+def test_rows_that_see_nothing_beside_rows_that_do(fw):
+    """Drafts longer than their cells' rows."""
+    gen = torch.Generator("cuda").manual_seed(4)
+    counts = [1, 3, 0, 16, 17, 30]
+    p = cache_of(fw, gen, counts, 16, 64, fill=float("inf"))
+    for longest in (0, 30):
+        out = check_all(fw, p, counts, rand(gen, 6, 20, 3, 64), 1, longest=longest)
+        assert bool(torch.isneginf(out["lse"][2]).all()) and not bool(out["o"][0, :19].any())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_that_grow_and_are_far_apart(fw, d):
+    """Maxima that move in every block, by little and by much, up and down; rows of equal logits."""
+    gen = torch.Generator("cuda").manual_seed(d)
+    n = 700
+    p = cache_of(fw, gen, [n] * 5, 16, d)
+    q = torch.zeros(5, 1, 2, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 8.0
+    t = torch.arange(n, device="cuda").float()
+    for h, f in enumerate((0.1 * t, -0.1 * t, 40 * torch.sin(t), 0 * t, torch.where(t % 97 == 0, 90.0, -3e38 / 8))):
+        page = p.table[h].long()[torch.arange(n, device="cuda") // 16]
+        p.k[page, torch.arange(n, device="cuda") % 16, 0] = f.to(torch.bfloat16)
+        p.k[page, torch.arange(n, device="cuda") % 16, 1:] = 0
+    for longest in (0, n):
+        check_all(fw, p, [n] * 5, q, 1, scale=1.0, longest=longest)
