@@ -31,9 +31,11 @@ struct AppendArgs {
     const uint16_t *k, *v;
     int64_t k_seq, k_tok, k_head, v_seq, v_tok, v_head;
     int32_t *status;
-    int32_t *first;  // workspace: [cells + 1] where each cell's pages stand in the list
-    int32_t *list;   // workspace: the pages that are handed out (then those that they replace)
-    int2 *plan;      // workspace: [cells] (rows before, -1 where the cell takes none; page to copy from or -1)
+    int32_t *first;    // workspace: [cells + 1] where each cell's pages stand in the list
+    int32_t *list;     // workspace: the pages that are handed out
+    int32_t *was;      // workspace: the pages that they replace, or -1
+    int2 *plan;        // workspace: [cells] (rows before, -1 where the cell takes none; page to copy from or -1)
+    int32_t *granted;  // workspace: pages handed out
 };
 
 struct CompactArgs {
@@ -282,11 +284,8 @@ template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_p
         const int last = a.list[granted - 1];
         *s.next = last + 1 < s.N ? last + 1 : 0;
     }
-    if constexpr (!APPEND) {
-        if (tid == 0) *a.granted = granted;
-    } else {
-        for (int t = tid; t < granted; t += PT) take(s, a.list[t]);
-        __syncthreads();
+    if (tid == 0) *a.granted = granted;
+    if constexpr (APPEND) {
         for (int h = WIDE ? wid : tid; h < s.cells; h += WIDE ? PT / 32 : PT) {
             const int n = a.plan[h].x;
             if (n < 0) continue;
@@ -300,7 +299,7 @@ template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_p
                 if (needs) {
                     const int was = i < held ? row[i] : -1, to = at + (WIDE ? __popc(some & ((1u << lane) - 1)) : 0);
                     row[i] = a.list[to];
-                    a.list[to] = was;
+                    a.was[to] = was;
                     if (i == i0 && n % s.P != 0) a.plan[h].y = was;
                 }
                 at += __popc(some);
@@ -309,12 +308,6 @@ template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_p
                 s.held[h] = max(held, i1 + 1);
                 s.counts[h] = n + a.m;
             }
-        }
-        __syncthreads();
-        // (behind all readings of refs)
-        for (int t = tid; t < granted; t += PT) {
-            const int was = a.list[t];
-            if (was >= 0) give(s, was);
         }
     }
 }
@@ -347,12 +340,22 @@ __device__ __forceinline__ void copy_rows(uint16_t *kd, uint16_t *vd, int lo, in
     }
 }
 
-// New rows to their pages, and those of a page that was shared to the cell's own: a warp per cell and UR rows.
+// New rows to their pages, and those of a page that was shared to the cell's own: a warp per cell and UR rows.  The first
+// BOOK CTAs count the entries that came and went (behind the plan, which goes by how many entries name a page).
+constexpr int BOOK = 4;
 template <int D> __global__ void __launch_bounds__(32 * MW) k_pages_append(const AppendArgs a, int units)
 {
     const Pages &s = a.s;
-    const int lane = threadIdx.x & 31, id = blockIdx.x * MW + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, id = ((int)blockIdx.x - BOOK) * MW + (threadIdx.x >> 5);
     wait_for_the_one_before();
+    if (id < 0) {
+        for (int t = blockIdx.x * 32 * MW + threadIdx.x, n = *a.granted; t < n; t += BOOK * 32 * MW) {
+            const int was = a.was[t];
+            take(s, a.list[t]);
+            if (was >= 0) give(s, was);
+        }
+        return;
+    }
     const int h = id / units;
     if (h >= s.cells) return;
     const int n = a.plan[h].x, from = a.plan[h].y;
@@ -604,19 +607,23 @@ size_t compact_list(const fw_pages &p, int64_t total)
 
 size_t pages_append_workspace(const fw_pages &p, int m)
 {
-    return align256(((size_t)p.cells + 1) * 4) + align256((size_t)p.cells * 8) + align256(append_list(p, m) * 4);
+    return align256(((size_t)p.cells + 1) * 4) + align256((size_t)p.cells * 8) + 2 * align256(append_list(p, m) * 4) + 256;
 }
 
 fw_status pages_append(const fw_pages &p, const fw_pages_new &r, int32_t *status, void *ws, cudaStream_t st)
 {
     uint8_t *w = (uint8_t *)ws;
     AppendArgs a{view(p), r.m, r.kv_heads, (const uint16_t *)r.k, (const uint16_t *)r.v, r.k_seq, r.k_tok, r.k_head,
-                 r.v_seq, r.v_tok, r.v_head, status, (int32_t *)w, nullptr, nullptr};
+                 r.v_seq, r.v_tok, r.v_head, status, (int32_t *)w, nullptr, nullptr, nullptr, nullptr};
     w += align256(((size_t)p.cells + 1) * 4);
     a.plan = (int2 *)w;
-    a.list = (int32_t *)(w + align256((size_t)p.cells * 8));
+    w += align256((size_t)p.cells * 8);
+    a.list = (int32_t *)w;
+    w += align256(append_list(p, r.m) * 4);
+    a.was = (int32_t *)w;
+    a.granted = (int32_t *)(w + align256(append_list(p, r.m) * 4));
     const int units = (p.page_rows - 1 + r.m + UR - 1) / UR;
-    const unsigned grid = (unsigned)(((int64_t)p.cells * units + MW - 1) / MW);
+    const unsigned grid = BOOK + (unsigned)(((int64_t)p.cells * units + MW - 1) / MW);
     // (4 cells x 509 rows, 33 pages each: a warp per cell 3 us, a thread 10)
     if (r.m > 3 * p.page_rows)
         FW_LAUNCH((k_pages_plan<AppendArgs, true>), 1, PT, 0, st, a);
