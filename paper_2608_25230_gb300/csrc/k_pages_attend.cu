@@ -76,22 +76,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ void cluster_sync()
+__device__ __forceinline__ void cluster_arrive()
 {
     __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
-// a word at this CTA's shared address p, as CTA `rank` of the cluster has it
-__device__ __forceinline__ uint32_t remote_u(const void *p, int rank)
+__device__ __forceinline__ void cluster_wait()
 {
-    uint32_t v;
-    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.u32 %0, [a];\n\t}"
-                 : "=r"(v)
-                 : "r"(tc::smem_u32(p)), "r"(rank)
-                 : "memory");
-    return v;
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float remote(const float *p, int rank) { return __uint_as_float(remote_u(p, rank)); }
+// a float to what this CTA has at the shared address p, in CTA `rank` of the cluster
+__device__ __forceinline__ void store_to(const void *p, int rank, float v)
+{
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f32 [a], %2;\n\t}" ::"r"(
+                     tc::smem_u32(p)),
+                 "r"(rank), "f"(v)
+                 : "memory");
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
 {
     uint32_t r;
@@ -709,6 +711,7 @@ __device__ __forceinline__ void join(int n, FM ml_of, FO o_of, float &M, float &
 
 // A cluster of up to FEW CTAs per cell and tile of rows, its blocks dealt out to their teams one by one.
 constexpr int FEW = 12;
+template <int D, int TW> constexpr size_t few_smem() { return Cfg<D, TW, few_warps(TW)>::SMEM + (TW * 8 + FEW) * (D + 4) * 4; }
 template <int D, int TW>
 __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     k_pages_attend_few(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
@@ -718,13 +721,14 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     constexpr int MT = D / 16, RT = C::RT, E = D / 32, LDO = D + 4, TEAMS = C::TEAMS, STAGES = C::STAGES;
     extern __shared__ uint8_t smraw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~(uintptr_t)1023);
-    float *s_o = reinterpret_cast<float *>(sm);  // [W][8][LDO], in the rings' place when these are done
+    float *s_o = reinterpret_cast<float *>(sm);               // [W][8][LDO], in the rings' place when these are done
+    float *s_in = reinterpret_cast<float *>(sm + C::RING);    // [rows of this CTA][cluster][LDO]: the CTAs' states of them
     static_assert(W * 8 * LDO * 4 <= C::RING, "the states fit the rings");
     __shared__ __align__(8) uint64_t full[TEAMS][STAGES], empty[TEAMS][STAGES];
     __shared__ int32_t s_page[TEAMS][STAGES];
     __shared__ float2 s_ml[W][8];
-    __shared__ float2 s_pml[TW * 8];
-    __shared__ int s_code;
+    __shared__ float2 s_mlin[TW * 8 + FEW];
+    __shared__ int s_code, s_codes[FEW];
 
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, c = lane & 3;
     const int team = wid / TW, member = wid % TW;
@@ -738,6 +742,7 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     fw_status st;
     const int nb = cell_blocks(s, h, n, st);
     if (tid == 0) s_code = st;
+    cluster_arrive();  // (waited for before anything is sent: every CTA of the cluster runs then)
     Ring<D, STAGES, TW> ring;
     ring.mem = sm + team * STAGES * 2 * C::TILE;
     ring.full = full[team];
@@ -788,21 +793,26 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
 #pragma unroll
         for (int f = 0; f < 4; ++f) s_o[(wid * 8 + 2 * c + (f & 1)) * LDO + 16 * i + 8 * (f >> 1) + g] = R.O[i][f];
     __syncthreads();
+    // ---- and sent to the CTA of the cluster that joins the row's: rows in turn to the CTAs
+    cluster_wait();
     float M, L, acc[E];
     for (int x = wid; x < TW * 8; x += W) {  // row x & 7 of member x >> 3
+        if (tile0 + x >= rows) break;
         join<TEAMS, E>(TEAMS, [&](int w) { return s_ml[w * TW + (x >> 3)][x & 7]; },
                        [&](int w, int e) { return s_o[(w * TW * 8 + x) * LDO + lane + 32 * e]; }, M, L, acc);
+        const int to = x % a.cluster, slot = x - to + rank;
 #pragma unroll
-        for (int e = 0; e < E; ++e) s_o[x * LDO + lane + 32 * e] = acc[e];  // (in the first team's place)
-        if (lane == 0) s_pml[x] = make_float2(M, L);
+        for (int e = 0; e < E; ++e) store_to(&s_in[slot * LDO + lane + 32 * e], to, acc[e]);
+        if (lane < 2) store_to(lane ? &s_mlin[slot].y : &s_mlin[slot].x, to, lane ? L : M);
     }
-    cluster_sync();
-    // ---- and over the cluster's CTAs: rows dealt out to them and their warps
+    if (tid == 0) store_to(&s_codes[rank], 0, __int_as_float(s_code));
+    cluster_arrive();
+    cluster_wait();
     for (int x = rank + a.cluster * wid; x < TW * 8; x += a.cluster * W) {
-        const int r = tile0 + x;
-        if (r >= rows) continue;
-        join<FEW, E>(a.cluster, [&](int w) { return make_float2(remote(&s_pml[x].x, w), remote(&s_pml[x].y, w)); },
-                     [&](int w, int e) { return remote(&s_o[x * LDO + lane + 32 * e], w); }, M, L, acc);
+        const int r = tile0 + x, slot = x - rank;
+        if (r >= rows) break;
+        join<FEW, E>(a.cluster, [&](int w) { return s_mlin[slot + w]; }, [&](int w, int e) { return s_in[(slot + w) * LDO + lane + 32 * e]; },
+                     M, L, acc);
         const int64_t out = out_row(a, seq, hk, r);
         const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
@@ -811,10 +821,9 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
         if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
     }
     if (rank == 0 && blockIdx.y == 0 && wid == W - 1 && a.status) {
-        const int codes = __reduce_max_sync(FW_FULL, lane < a.cluster ? (int)remote_u(&s_code, lane) : 0);
+        const int codes = __reduce_max_sync(FW_FULL, lane < a.cluster ? s_codes[lane] : 0);
         if (lane == 0) a.status[h] = codes;
     }
-    cluster_sync();  // no CTA leaves while another reads its rows
 }
 
 // How many clusters of each size find room on the GPU at once, a CTA an SM (GPUs differ in the SMs of their parts), and the
@@ -830,7 +839,7 @@ void clusters_at_once(int (&room)[SIZES])
         int n = dev >= 0 ? cache[dev][i].load(std::memory_order_relaxed) : known[i];  // (one more than it is)
         if (n == 0) {
             const auto kernel = k_pages_attend_few<128, 1>;
-            constexpr size_t smem = Cfg<128, 1, few_warps(1)>::SMEM;
+            constexpr size_t smem = few_smem<128, 1>();
             cudaLaunchAttribute at[1];
             at[0].id = cudaLaunchAttributeClusterDimension;
             at[0].val.clusterDim.x = (unsigned)SIZE[i];
@@ -857,7 +866,7 @@ void clusters_at_once(int (&room)[SIZES])
 // unlike lengths (the longest about twice the mean, which the host does not know).  Ranges: two launches, the sums
 // over the cells, the joining, and the blocks of all over the GPU.  Clusters: a launch, and the longest cell's blocks over
 // its CTAs, which share the memory with all others at first and have their SMs' whole rate at the end.  (d = 128, four query
-// rows, ranges against clusters: 8 cells of up to 8,000 rows 16.3 us against 11.4, 64 of up to 3,000 17.9 against 16.1, of up
+// rows, ranges against clusters: 8 cells of up to 8,000 rows 12.9 us against 9.2, 64 of up to 3,000 17.4 against 15.7, of up
 // to 12,000 31 against 40; 64 of up to 50 13 against 6.)
 int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, int sms)
 {
@@ -873,7 +882,7 @@ int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, in
         if (room[i] < 1) continue;
         const int64_t clusters = (int64_t)p.cells * tiles, waves = (clusters + room[i] - 1) / room[i];
         const double at_once = (double)std::min<int64_t>(clusters, room[i]) * SIZE[i] * memory / tiles;
-        const double t = waves * (5.2 + 0.1 * SIZE[i] + blocks / SIZE[i] * 0.5 * (per + std::max(per, at_once)));
+        const double t = waves * (5.0 + 0.1 * SIZE[i] + blocks / SIZE[i] * 0.5 * (per + std::max(per, at_once)));
         if (t < least - 0.1) best = SIZE[i], least = t;
     }
     return best;
@@ -959,7 +968,7 @@ fw_status launch_few(const Plan &x, int cells, const CUtensorMap &mk, const CUte
         const fw_status st = wide_clusters((const void *)k_pages_attend_few<D, TW>, wide);
         if (st != FW_OK) return st;
     }
-    return launch(k_pages_attend_few<D, TW>, cells * x.few, x.tiles, x.few, 32 * W, Cfg<D, TW, W>::SMEM, mk, mv, a, done, s);
+    return launch(k_pages_attend_few<D, TW>, cells * x.few, x.tiles, x.few, 32 * W, few_smem<D, TW>(), mk, mv, a, done, s);
 }
 template <int D, int TW>
 fw_status launch_one(const Plan &x, int cells, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
