@@ -581,7 +581,9 @@ typedef struct {
 } fw_pages_query;
 /* o: device bf16 [sequences][m][kv_heads * group][d], 16-byte aligned; lse: device fp32
  * of the same rows (may be NULL).  status [cells] also FW_ERR_TIMEOUT, where a
- * bounded wait gave up (the rows concerned are NaN).  The same call gives the same bits. */
+ * bounded wait gave up (the rows concerned are NaN).  Products of bf16 with fp32 sums, the
+ * weights as the sum of two bf16 numbers (16 bits of each count) up to 2^8 before a sum is
+ * divided: values of 2^120 / n and more in n rows can overflow.  The same call gives the same bits. */
 fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, float *lse, int32_t *status,
                           void *workspace, size_t workspace_bytes, void *stream);
 /* Workspace bytes (0 for arguments fw_pages_attend refuses). */

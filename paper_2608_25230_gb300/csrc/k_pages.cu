@@ -7,8 +7,10 @@
 // nothing.  A page that comes back is free for the calls behind, so the pages of a call are never
 // read and handed out at once.
 //
-// Bound: append: latency (two launches); compaction: memory, every kept row read and written
-// once; fork: the tables' entries and their pages' counts, latency for small ones.
+// Bound: append: latency, one CTA's sums and searches (5 us) and the copies behind it (a token to 256 cells, a fourth of
+// them just forked: 8.2 us; 509 rows to 32 cells 8.9 us); compaction: memory, every kept row read and written once (256 x 32,768
+// rows of 128 to an eighth: 184 us, 5.9 TB/s, of which the copies take 165 us, 6.5 TB/s; 64 x 7,001 rows in pages to a half:
+// 45 us, the copies 35); fork: the tables' entries and their pages' counts (2,048 cells of 256 pages: 9.8 us; 24 cells 3.3 us).
 #include <algorithm>
 #include <type_traits>
 

@@ -3,21 +3,28 @@
 //   x_j = scale (q . k_j),  o = sum_j softmax_j(x) v_j,  lse = log sum_j e^x_j.
 //
 // Bound: the rows' bytes, each read once from memory.  Two ways over the cells:
-//   few short cells (k_pages_attend_few): a cluster of CTAs per cell, its blocks dealt out to all their
-//   warps, whose states are joined through (distributed) shared memory;
+//   few short cells (k_pages_attend_few): a cluster of up to 12 CTAs per cell, its blocks dealt out to all
+//   their teams, whose states are joined in shared memory and sent to the CTA that joins a row's;
 //   many (k_pages_attend): the blocks of all cells in a row are divided evenly over the teams of
 //   the GPU, whatever the cells' lengths, so a team takes the end of one cell, whole cells and the
 //   start of another, and waits for no other; the parts of cells that several teams share go to the
 //   workspace, and a second kernel, launched behind the first one's tail, joins them in their order.
-// A team is a warp, or where the query rows do not fit one warp's registers 2, 4 or 8 warps, which read the same
-// blocks against other query rows.  It fetches its blocks by TMA into a ring of its own, through page
-// numbers that its first warp has read 32 blocks ahead.
+// A team is a warp for 8 query rows, or 2, 3, 4 or 6 warps, which read the same blocks against other query
+// rows.  It fetches its blocks by TMA into a ring of its own, through page numbers that its first warp
+// has read 32 blocks ahead.  64 x 8 cells of about 16,384 rows, d = 128, 4 query rows: 606 us, 6.75 TB/s, the measured
+// copy rate; 24 x 4 cells of 5,000, 7 query rows 45 us (4.7 TB/s: 3 us to the first blocks, the teams finish up to 8 us
+// apart, 5 us to join); 8 cells of 4,096 8.8 us (latency: 2 us to the first block, 4 blocks a warp, 4 us to join).
+// (Ranges of a CTA each, with its warps' states joined at the end of each cell's share and the parts by the last CTA to come,
+// were faster for many long cells, 128 x 8 of 4,096 326 us against 338, and slower for others, 32 x 8 of 1,024 38 against 34, drafts
+// of 20 rows 56 against 47.)
 //
 // A block is 16 rows, so it lies in one page whatever the pages' size.  Against 8 query rows, transposed on the
 // warp-wide bf16 tensor instructions (a few query rows cannot fill a tcgen05 tile, and the stream
-// of rows leaves the slower instructions mostly idle): S^T = K Q^T, then O^T += V^T P^T.  The weights enter as the sum
-// of two bf16 numbers, the upper half of the fp32 weight's bits and what that leaves, so that 16
-// bits of each count; both are positive where the weight is, so that an infinite value stays one.
+// of rows leaves the slower instructions mostly idle: 13 % of their time with 8 query rows): S^T = K Q^T, then O^T += V^T P^T.
+// The weights enter as the sum of two bf16 numbers, the upper half of the fp32 weight's bits and what that leaves, so that 16
+// bits of each count; both are positive where the weight is, so that an infinite value stays one.  More query rows are bound
+// by the reading of the blocks from shared memory and by issue: an SM takes about 12 tiles of 8 rows x 16 keys a us (64 cells x 4,096 rows: 20
+// query rows 44 us, 32 54, 48 67, 64 94).
 #include <algorithm>
 
 #include <cuda_bf16.h>

@@ -3,9 +3,11 @@
 //   y = x / sqrt(mean_c x_c^2 + eps) * w;  (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
 // with t = pos * inv_freq[f] for the pair f of columns.
 //
-// Bound: memory, every row read and written once.  A lane holds 16 columns of a head, so chosen
-// that a pair's two columns meet in it, and LPL lanes a head; a warp keeps one token's
-// cosines and sines in registers and goes over its heads.
+// Bound: memory, every row read and written once, and near it issue (58 % of the slots): 170 instructions a chunk of heads, 700 a
+// token.  A lane holds 16 columns of a head, so chosen that a pair's two columns meet in it, and LPL lanes a head; a warp keeps
+// one token's cosines and sines, times the weights, in registers and goes over its heads, which it has asked for ahead into
+// shared memory.  16,381 tokens x 40 heads of 128: 54.5 us, 6.2 TB/s (registers alone, one chunk ahead: 67 us); 30,001 x
+// 40 of 64 59 us (a token's 700 instructions weigh twice); 40 tokens x 16 heads 3.1 us.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -16,7 +18,7 @@ namespace fw {
 namespace {
 
 constexpr int RW = 8;      // warps of a CTA
-constexpr int AHEAD = 4;   // chunks of heads that a warp has asked for ahead of the one that it works on
+constexpr int AHEAD = 4;   // chunks of heads that a warp has asked for ahead of the one that it works on (6: 65 us)
 
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void *src)
 {
