@@ -125,6 +125,13 @@ template <bool TRANS> __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4]
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                      : "r"(addr));
 }
+// true for one lane of a warp that is there as a whole
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 // A box of BR rows and both halves of their columns: [half][row][64], rows swizzled over 128 bytes.
 __device__ __forceinline__ void tma_load_rows(void *dst, const void *tmap, int32_t row, uint64_t *bar)
 {
@@ -172,12 +179,12 @@ template <int D, int STAGES, int TW> struct Ring {
         tc::mbar_init_fence();
     }
     // block of BR rows from row `at` of page `pg` (the first warp)
-    __device__ void fetch(const CUtensorMap *tmK, const CUtensorMap *tmV, const Pages &s, int pg, int at, int lane)
+    __device__ void fetch(const CUtensorMap *tmK, const CUtensorMap *tmV, const Pages &s, int pg, int at)
     {
         const int st = issued % STAGES;
         if (TW > 1 && issued >= STAGES && ok) ok = tc::mbar_wait(&empty[st], (issued / STAGES - 1) & 1, A_WAIT);
         if (!ok) return;
-        if (lane == 0) {
+        if (elect_one()) {  // (a copy that lane 0's branch asks for takes three times as long to issue: its operands are not uniform)
             const bool is = s.is_page(pg);
             page[st] = is ? pg : -1;
             if (is) {
@@ -509,7 +516,7 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
             win.from = -64;
         }
         if (pb - win.from >= 32 || win.from < 0) win.load(s, ph, pb, 1, lane);
-        ring.fetch(&tmK, &tmV, s, win.at(pb - win.from), pb * BR % s.P, lane);
+        ring.fetch(&tmK, &tmV, s, win.at(pb - win.from), pb * BR % s.P);
         ++pu;
         ++pb;
     };
@@ -762,7 +769,7 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
         if (pb >= nb) return;
         int i = (pb - win.from) / step;
         if (i >= 32) win.load(s, h, pb, step, lane), i = 0;
-        ring.fetch(&tmK, &tmV, s, win.at(i), pb * BR % s.P, lane);
+        ring.fetch(&tmK, &tmV, s, win.at(i), pb * BR % s.P);
         pb += step;
     };
     const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
