@@ -24,7 +24,7 @@
 // The weights enter as the sum of two bf16 numbers, the upper half of the fp32 weight's bits and what that leaves, so that 16
 // bits of each count; both are positive where the weight is, so that an infinite value stays one.  More query rows are bound
 // by the reading of the blocks from shared memory and by issue: an SM takes about 12 tiles of 8 rows x 16 keys a us (64 cells x 4,096 rows: 20
-// query rows 44 us, 32 54, 48 67, 64 94).
+// query rows 40 us, 32 45, 48 55, 64 73).
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -147,6 +147,7 @@ template <int D, int TW, int W> struct Cfg {
     static constexpr int TEAMS = W / TW;
     static constexpr int TILE = BR * D * 2;  // bytes of a block's keys, or values
     static constexpr int STAGES = 196608 / (2 * TILE) / TEAMS;
+    static_assert(STAGES % TW == 0 || W % TW != 0, "a stage is always filled by the same warp");
     static constexpr int RING = TEAMS * STAGES * 2 * TILE;
     static constexpr size_t SMEM = 1024 + RING;
     static constexpr int RT = TW * 8;  // query rows of a team
@@ -160,17 +161,19 @@ __host__ __device__ constexpr int few_warps(int TW) { return TW > 1 ? 12 : 8; }
 // Byte offset of piece x (16 bytes, 8 columns) of row r in a tile.
 __device__ __forceinline__ int piece(int r, int x) { return (x >> 3) * (BR * 128) + r * 128 + (((x ^ r) & 7) << 4); }
 
-// A team's ring of blocks.  Its first warp fetches; with more warps each says that it has read a block.
+// A team's ring of blocks.  Its warps fetch them in turn (asking for a block takes a warp 0.3 us where many are under way: drafts of
+// 20 rows over 64 cells of 1,537 19.6 us, 21.4 with one that asks for all); with more warps than one each says that it has read a block.
 template <int D, int STAGES, int TW> struct Ring {
     static constexpr int TILE = BR * D * 2;
     uint8_t *mem;
     uint64_t *full, *empty;
     int32_t *page;  // of the stages' blocks, -1: none
-    int issued = 0, used = 0;
+    int mine, used = 0;  // blocks of the team: the next that this warp fetches, and that it reads
     bool ok = true;
 
     __device__ void init(int lane, int member)
     {
+        mine = member;
         if (member == 0)
             for (int i = lane; i < STAGES; i += 32) {
                 tc::mbar_init(&full[i], 1);
@@ -178,11 +181,11 @@ template <int D, int STAGES, int TW> struct Ring {
             }
         tc::mbar_init_fence();
     }
-    // block of BR rows from row `at` of page `pg` (the first warp)
+    // block of BR rows from row `at` of page `pg`
     __device__ void fetch(const CUtensorMap *tmK, const CUtensorMap *tmV, const Pages &s, int pg, int at)
     {
-        const int st = issued % STAGES;
-        if (TW > 1 && issued >= STAGES && ok) ok = tc::mbar_wait(&empty[st], (issued / STAGES - 1) & 1, A_WAIT);
+        const int st = mine % STAGES;
+        if (TW > 1 && mine >= STAGES && ok) ok = tc::mbar_wait(&empty[st], (mine / STAGES - 1) & 1, A_WAIT);
         if (!ok) return;
         if (elect_one()) {  // (a copy that lane 0's branch asks for takes three times as long to issue: its operands are not uniform)
             const bool is = s.is_page(pg);
@@ -196,7 +199,7 @@ template <int D, int STAGES, int TW> struct Ring {
                 tc::mbar_arrive(&full[st]);
             }
         }
-        ++issued;
+        mine += TW;
     }
     // the next block's stage, or -1 where the wait gave up
     __device__ int next()
@@ -216,7 +219,7 @@ template <int D, int STAGES, int TW> struct Ring {
     // copies still under way land before the CTA's memory goes
     __device__ void drain()
     {
-        for (; used < issued; ++used) tc::mbar_wait(&full[used % STAGES], (used / STAGES) & 1, A_WAIT);
+        for (int b = mine - TW; b >= used; b -= TW) tc::mbar_wait(&full[b % STAGES], (b / STAGES) & 1, A_WAIT);
     }
 };
 
@@ -503,29 +506,27 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
     int u = (int)first;
     const int u1 = (int)min(first + quota, (int64_t)total);
 
-    // the team's producer: its next block to fetch, by cell
-    int pu = u, ph = s_h0[team], pb = s_b0[team], pn = s_n0[team], pnb = (pn + BR - 1) / BR;
+    // the warp's next block to fetch, by cell
+    int pu = u + member, ph = s_h0[team], pb = s_b0[team] + member, pn = s_n0[team], pnb = (pn + BR - 1) / BR;
     fw_status pst;
     Window win;
-    win.from = -64;
+    win.from = -1;
     auto fetch = [&]() {
         if (pu >= u1) return;
         while (pb >= pnb && ph + 1 < s.cells) {  // (a block is left, so a cell holds it)
             pb -= pnb;
             pnb = cell_blocks(s, ++ph, pn, pst);
-            win.from = -64;
+            win.from = -1;
         }
-        if (pb - win.from >= 32 || win.from < 0) win.load(s, ph, pb, 1, lane);
-        ring.fetch(&tmK, &tmV, s, win.at(pb - win.from), pb * BR % s.P);
-        ++pu;
-        ++pb;
+        if (win.from < 0 || pb - win.from >= 32 * TW) win.load(s, ph, pb, TW, lane);
+        ring.fetch(&tmK, &tmV, s, win.at((pb - win.from) / TW), pb * BR % s.P);
+        pu += TW;
+        pb += TW;
     };
     Rows<D> R;
     R.read(a, ph / a.kv_heads, ph % a.kv_heads, row0, lane);
-    if (member == 0) {
 #pragma unroll 1
-        for (int i = 0; i < C::AHEAD; ++i) fetch();
-    }
+    for (int i = member; i < C::AHEAD; i += TW) fetch();
 
     int h = s_h0[team], b = s_b0[team];  // the segment: blocks of one cell
     while (u < u1) {
@@ -551,7 +552,7 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
             else if (row0 < rows)
                 R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
             ring.release(stage, lane);
-            if (member == 0) fetch();
+            if (ring.mine < ring.used + C::AHEAD) fetch();
         }
         R.close();
         const bool whole = b == 0 && bend == nb;
@@ -598,7 +599,7 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
         u += bend - b;
         b = bend;
     }
-    if (member == 0) ring.drain();
+    ring.drain();
 }
 
 // The parts of a cell that several teams share, joined in their order; empty cells' outputs.  Each of a CTA's JW warps
@@ -751,7 +752,7 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     const Pages &s = a.s;
     const int first = rank + a.cluster * team, step = a.cluster * TEAMS;  // (the first blocks go to different CTAs)
     Window win;
-    win.load(s, h, first, step, lane);  // (beside the counts)
+    win.load(s, h, first + member * step, step * TW, lane);  // (beside the counts)
     int n;
     fw_status st;
     const int nb = cell_blocks(s, h, n, st);
@@ -764,21 +765,19 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     ring.page = s_page[team];
     ring.init(lane, member);
     __syncthreads();
-    int pb = first;
+    int pb = first + member * step;  // the warp's next block to fetch
     auto fetch = [&]() {
         if (pb >= nb) return;
-        int i = (pb - win.from) / step;
-        if (i >= 32) win.load(s, h, pb, step, lane), i = 0;
+        int i = (pb - win.from) / (step * TW);
+        if (i >= 32) win.load(s, h, pb, step * TW, lane), i = 0;
         ring.fetch(&tmK, &tmV, s, win.at(i), pb * BR % s.P);
-        pb += step;
+        pb += step * TW;
     };
     const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
     Rows<D> R;
     R.read(a, seq, hk, row0, lane);
-    if (member == 0) {
 #pragma unroll 1
-        for (int i = 0; i < C::AHEAD; ++i) fetch();
-    }
+    for (int i = member; i < C::AHEAD; i += TW) fetch();
     R.start();
     bool bad = false;
 #pragma unroll 1
@@ -790,7 +789,7 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
         else if (row0 < rows)
             R.block(a, ring.mem + stage * 2 * C::TILE, blk, n, row0, lane);
         ring.release(stage, lane);
-        if (member == 0) fetch();
+        if (ring.mine < ring.used + C::AHEAD) fetch();
     }
     R.close();
     ring.drain();
