@@ -472,7 +472,7 @@ template <int T, int N> __device__ __forceinline__ void early(const Pages &s, in
 {
     const int32_t *row = s.row(h);
 #pragma unroll
-    for (int k = 0; k < N; ++k) e[k] = t + T * k < s.width ? row[t + T * k] : -1;
+    for (int k = 0; k < N; ++k) e[k] = t + T * k < s.width ? __ldcg(row + t + T * k) : -1;
 }
 // f(i, e) for all n entries of the table that e begins, N a thread at a time: e[k] is entry i + T k, or -1 behind the n-th.
 template <int T, int N, typename F>
@@ -552,9 +552,11 @@ __global__ void __launch_bounds__(KT) k_pages_fork(const ForkArgs a)
 }
 __global__ void __launch_bounds__(KT) k_pages_fork_end(const ForkArgs a)
 {
-    const int h = blockIdx.x, held = a.s.held[h];
+    // (the kernel before changes no table, and what came before that one is in memory; an SM's own cache is up to date only
+    // behind the wait, so these reads go past it)
+    const int h = blockIdx.x, held = __ldcg(a.s.held + h);
     int first[KE];
-    early<KT>(a.s, h, threadIdx.x, first);  // (the kernel before changes no table)
+    early<KT>(a.s, h, threadIdx.x, first);
     wait_for_the_one_before();
     hand_over<KT, KE>(a, h, held, threadIdx.x, first);
 }

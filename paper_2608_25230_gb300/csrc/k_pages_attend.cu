@@ -912,7 +912,7 @@ void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
     if (device_sms(&sms) != FW_OK) sms = 152;  // no device: the size query still answers
     const int rows = q.group * q.m;
     // as many warps a team as hold the rows; beyond 48 rows, tiles of 48 or 32, whichever leave fewer warps without rows
-    // (64 x 4,096 rows, d = 128, 64 query rows: two tiles of 32 94 us, one of 96 118)
+    // (64 x 4,096 rows, d = 128, 64 query rows: two tiles of 32 73 us, one of 96 90)
     const int need = (rows + 7) / 8;
     x.TW = need > 6 && (need + 5) / 6 * 6 > (need + 3) / 4 * 4 ? 4 : 6;
     for (const int tw : {4, 3, 2, 1})
