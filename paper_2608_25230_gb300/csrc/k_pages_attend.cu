@@ -878,24 +878,25 @@ void clusters_at_once(int (&room)[SIZES])
 // CTAs of a cell's cluster where that is the faster way, else 0 (ranges).  Both ways' times in us, from sweeps of cells of
 // unlike lengths (the longest about twice the mean, which the host does not know).  Ranges: two launches, the sums
 // over the cells, the joining, and the blocks of all over the GPU.  Clusters: a launch, and the longest cell's blocks over
-// its CTAs, which share the memory with all others at first and have their SMs' whole rate at the end.  (d = 128, four query
-// rows, ranges against clusters: 8 cells of up to 8,000 rows 12.9 us against 9.2, 64 of up to 3,000 17.4 against 15.7, of up
-// to 12,000 31 against 40; 64 of up to 50 13 against 6.)
+// its CTAs, which share the memory with all others at first and have their SMs' whole rate at the end.  (Of 57 shapes, 8 to 128
+// cells of 300 to 3,000 rows on average, 4 to 64 query rows, it takes the slower way for 2, by 1 to 3 us.  d = 128, 4 query rows,
+// clusters against ranges: 8 cells of 3,000 9.6 us against 12.8, 64 of 300 8.0 against 12.3, of 1,000 14.6 against 15.4, 128 of 3,000 62
+// against 39; 20 query rows, 64 of 3,000: 61 against 34.)
 int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, int sms)
 {
     if (q.longest == 0) return 0;
-    // an SM's time for a block of 16 rows: 91 GB/s for 8 query rows, products for more
-    const double per = (p.d == 128 ? 1.0 : 0.5) * std::max(0.09, 0.08 * TW);
+    // an SM's time for a block of 16 rows
+    const double per = (p.d == 128 ? 1.0 : 0.5) * std::max(0.12, 0.08 * TW);
     const double memory = BR * p.d * 4 / 6.7e6;  // and the memory's
     const double blocks = (q.longest + BR - 1) / BR, all = 0.5 * blocks * p.cells * tiles;
     int best = 0, room[SIZES];
-    double least = 12.0 + std::max(all * per / sms, all * memory / tiles);
+    double least = 11.0 + std::max(all * per / sms, all * memory / tiles);
     clusters_at_once(room);
     for (int i = SIZES - 1; i >= 0; --i) {
         if (room[i] < 1) continue;
         const int64_t clusters = (int64_t)p.cells * tiles, waves = (clusters + room[i] - 1) / room[i];
         const double at_once = (double)std::min<int64_t>(clusters, room[i]) * SIZE[i] * memory / tiles;
-        const double t = waves * (5.0 + 0.1 * SIZE[i] + blocks / SIZE[i] * 0.5 * (per + std::max(per, at_once)));
+        const double t = waves * (5.4 + 0.05 * SIZE[i] + blocks / SIZE[i] * 0.5 * (per + std::max(per, at_once)));
         if (t < least - 0.1) best = SIZE[i], least = t;
     }
     return best;
