@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "fw_chain.cuh"
 #include "fw_pages.cuh"
 
 namespace fw {
@@ -168,10 +169,6 @@ __device__ __forceinline__ int scan_cta(int x, int &all, int (&s_scan)[32])
     return before + incl - x;
 }
 
-// What follows a kernel in a call starts as soon as its CTAs find room, and waits for it here.
-__device__ __forceinline__ void wait_for_the_one_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_the_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // One CTA: what every cell needs, the free pages for it, and for appends the books.  WIDE: a warp per cell instead of a
 // thread, for appends that touch several pages a cell.
 template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_pages_plan(const Args a)
@@ -182,6 +179,7 @@ template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_p
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     let_the_next_start();
     if (tid == 0) s_granted = 0;
+    wait_for_the_one_before();
 
     int n0 = 0, held0 = 0;  // (of the first cells, asked for before anything is waited for)
     if (!WIDE && tid < s.cells) n0 = s.counts[tid], held0 = s.held[tid];
@@ -349,6 +347,7 @@ template <int D> __global__ void __launch_bounds__(32 * MW) k_pages_append(const
 {
     const Pages &s = a.s;
     const int lane = threadIdx.x & 31, id = ((int)blockIdx.x - BOOK) * MW + (threadIdx.x >> 5);
+    let_the_next_start();
     wait_for_the_one_before();
     if (id < 0) {
         for (int t = blockIdx.x * 32 * MW + threadIdx.x, n = *a.granted; t < n; t += BOOK * 32 * MW) {
@@ -440,6 +439,7 @@ __global__ void __launch_bounds__(128) k_pages_swap(const CompactArgs a)
     const Pages &s = a.s;
     const int h = blockIdx.x;
     fw_status st;
+    let_the_next_start();
     wait_for_the_one_before();
     const int n = compact_rows(a, h, st);
     if (n < 0) return;
@@ -547,13 +547,15 @@ template <int T, int N> __device__ __forceinline__ void hand_over(const ForkArgs
 constexpr int KT = 128, KE = 2;
 __global__ void __launch_bounds__(KT) k_pages_fork(const ForkArgs a)
 {
-    let_the_next_start();
+    wait_for_the_one_before();
+    let_the_next_start();  // (which reads tables before its own wait)
     take_over<KT, KE>(a, blockIdx.x, threadIdx.x);
 }
 __global__ void __launch_bounds__(KT) k_pages_fork_end(const ForkArgs a)
 {
     // (the kernel before changes no table, and what came before that one is in memory; an SM's own cache is up to date only
     // behind the wait, so these reads go past it)
+    let_the_next_start();
     const int h = blockIdx.x, held = __ldcg(a.s.held + h);
     int first[KE];
     early<KT>(a.s, h, threadIdx.x, first);
@@ -567,6 +569,8 @@ __global__ void __launch_bounds__(1024, 1) k_pages_fork_one(const ForkArgs a)
 {
     const int h = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool mine = h < a.s.cells;
+    let_the_next_start();
+    wait_for_the_one_before();
     int first[KE], held = 0;
     if (mine) {
         held = a.s.held[h];
@@ -575,24 +579,6 @@ __global__ void __launch_bounds__(1024, 1) k_pages_fork_one(const ForkArgs a)
     }
     __syncthreads();
     if (mine) hand_over<32, KE>(a, h, held, lane, first);
-}
-
-// Launches what follows in a call.
-template <typename... P, typename... A>
-fw_status launch_after(void (*kernel)(P...), unsigned grid, int threads, cudaStream_t s, const A &...args)
-{
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.stream = s;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
 }
 
 size_t append_list(const fw_pages &p, int m)
@@ -629,12 +615,10 @@ fw_status pages_append(const fw_pages &p, const fw_pages_new &r, int32_t *status
     const int units = (p.page_rows - 1 + r.m + UR - 1) / UR;
     const unsigned grid = BOOK + (unsigned)(((int64_t)p.cells * units + MW - 1) / MW);
     // (4 cells x 509 rows, 33 pages each: a warp per cell 3 us, a thread 10)
-    if (r.m > 3 * p.page_rows)
-        FW_LAUNCH((k_pages_plan<AppendArgs, true>), 1, PT, 0, st, a);
-    else
-        FW_LAUNCH((k_pages_plan<AppendArgs, false>), 1, PT, 0, st, a);
-    return p.d == 128 ? launch_after(k_pages_append<128>, grid, 32 * MW, st, a, units)
-                      : launch_after(k_pages_append<64>, grid, 32 * MW, st, a, units);
+    const fw_status planned = launch_chained(r.m > 3 * p.page_rows ? k_pages_plan<AppendArgs, true> : k_pages_plan<AppendArgs, false>,
+                                             dim3(1), PT, 0, 0, st, a);
+    if (planned != FW_OK) return planned;
+    return launch_chained(p.d == 128 ? k_pages_append<128> : k_pages_append<64>, dim3(grid), 32 * MW, 0, 0, st, a, units);
 }
 
 size_t pages_compact_workspace(const fw_pages &p, int64_t total)
@@ -655,12 +639,13 @@ fw_status pages_compact(const fw_pages &p, const void *K, const void *V, int T, 
     w += align256(((size_t)p.cells + 1) * 4);
     a.granted = (int32_t *)w;
     a.list = (int32_t *)(w + 256);
-    FW_LAUNCH((k_pages_plan<CompactArgs, false>), 1, PT, 0, s, a);
     const unsigned grid = (unsigned)sms * 4;
-    const fw_status moved = launch_after(K ? p.d == 128 ? k_pages_move<128, false> : k_pages_move<64, false>
-                                         : p.d == 128 ? k_pages_move<128, true> : k_pages_move<64, true>,
-                                         grid, 32 * MW, s, a);
-    return moved == FW_OK ? launch_after(k_pages_swap, (unsigned)p.cells, 128, s, a) : moved;
+    fw_status done = launch_chained(k_pages_plan<CompactArgs, false>, dim3(1), PT, 0, 0, s, a);
+    if (done == FW_OK)
+        done = launch_chained(K ? p.d == 128 ? k_pages_move<128, false> : k_pages_move<64, false>
+                              : p.d == 128 ? k_pages_move<128, true> : k_pages_move<64, true>,
+                              dim3(grid), 32 * MW, 0, 0, s, a);
+    return done == FW_OK ? launch_chained(k_pages_swap, dim3((unsigned)p.cells), 128, 0, 0, s, a) : done;
 }
 
 size_t pages_fork_workspace(const fw_pages &p)
@@ -672,12 +657,9 @@ fw_status pages_fork(const fw_pages &p, const int32_t *src, int32_t *status, voi
 {
     uint8_t *w = (uint8_t *)ws;
     const ForkArgs a{view(p), src, status, (int32_t *)(w + align256((size_t)p.cells * 4)), (int32_t *)w};
-    if (p.cells <= ONE_CELLS && p.max_pages <= ONE_PAGES) {
-        FW_LAUNCH(k_pages_fork_one, 1, 1024, 0, s, a);
-        return FW_OK;
-    }
-    FW_LAUNCH(k_pages_fork, (unsigned)p.cells, KT, 0, s, a);
-    return launch_after(k_pages_fork_end, (unsigned)p.cells, KT, s, a);
+    if (p.cells <= ONE_CELLS && p.max_pages <= ONE_PAGES) return launch_chained(k_pages_fork_one, dim3(1), 1024, 0, 0, s, a);
+    const fw_status taken = launch_chained(k_pages_fork, dim3((unsigned)p.cells), KT, 0, 0, s, a);
+    return taken == FW_OK ? launch_chained(k_pages_fork_end, dim3((unsigned)p.cells), KT, 0, 0, s, a) : taken;
 }
 
 }  // namespace fw

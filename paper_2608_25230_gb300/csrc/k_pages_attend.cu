@@ -13,7 +13,7 @@
 // rows.  It fetches its blocks by TMA into a ring of its own, through page numbers that its first warp
 // has read 32 blocks ahead.  64 x 8 cells of about 16,384 rows, d = 128, 4 query rows: 606 us, 6.75 TB/s, the measured
 // copy rate; 24 x 4 cells of 5,000, 7 query rows 45 us (4.7 TB/s: 3 us to the first blocks, the teams finish up to 8 us
-// apart, 5 us to join); 8 cells of 4,096 8.8 us (latency: 2 us to the first block, 4 blocks a warp, 4 us to join).
+// apart, 5 us to join); 8 cells of 4,096 8.0 us (latency: 2 us to the first block, 4 blocks a warp, 3 us to join).
 // (Ranges of a CTA each, with its warps' states joined at the end of each cell's share and the parts by the last CTA to come,
 // were faster for many long cells, 128 x 8 of 4,096 326 us against 338, and slower for others, 32 x 8 of 1,024 38 against 34, drafts
 // of 20 rows 56 against 47.)
@@ -29,6 +29,7 @@
 
 #include <cuda_bf16.h>
 
+#include "fw_chain.cuh"
 #include "fw_pages.cuh"
 #include "tc_sm100.cuh"
 
@@ -444,13 +445,14 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
     const int team = wid / TW, member = wid % TW;
     const int cta = blockIdx.x, tile = blockIdx.y, row0 = tile * RT + member * 8, rows = a.group * a.m;
     const Pages &s = a.s;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    let_the_next_start();
     Ring<D, C::STAGES, TW> ring;
     ring.mem = sm + team * C::STAGES * 2 * C::TILE;
     ring.full = full[team];
     ring.empty = empty[team];
     ring.page = s_page[team];
     ring.init(lane, member);
+    wait_for_the_one_before();
 
     // ---- the blocks of all cells, divided evenly over the teams of all CTAs
     const int per = (s.cells + AT - 1) / AT;
@@ -611,7 +613,8 @@ template <int D, bool SPREAD, int JW> __global__ void __launch_bounds__(32 * JW,
     constexpr int E = D / 32;
     __shared__ float s_o[SPREAD ? JW : 1][D];
     __shared__ float2 s_ml[JW];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    let_the_next_start();
+    wait_for_the_one_before();
     const int h = blockIdx.x, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const int r = SPREAD ? blockIdx.y : blockIdx.y * JW + wid;
     int n;
@@ -751,12 +754,7 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     const int tile0 = blockIdx.y * RT, row0 = tile0 + member * 8;
     const Pages &s = a.s;
     const int first = rank + a.cluster * team, step = a.cluster * TEAMS;  // (the first blocks go to different CTAs)
-    Window win;
-    win.load(s, h, first + member * step, step * TW, lane);  // (beside the counts)
-    int n;
-    fw_status st;
-    const int nb = cell_blocks(s, h, n, st);
-    if (tid == 0) s_code = st;
+    let_the_next_start();
     cluster_arrive();  // (waited for before anything is sent: every CTA of the cluster runs then)
     Ring<D, STAGES, TW> ring;
     ring.mem = sm + team * STAGES * 2 * C::TILE;
@@ -764,6 +762,13 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     ring.empty = empty[team];
     ring.page = s_page[team];
     ring.init(lane, member);
+    wait_for_the_one_before();
+    Window win;
+    win.load(s, h, first + member * step, step * TW, lane);  // (beside the counts)
+    int n;
+    fw_status st;
+    const int nb = cell_blocks(s, h, n, st);
+    if (tid == 0) s_code = st;
     __syncthreads();
     int pb = first + member * step;  // the warp's next block to fetch
     auto fetch = [&]() {
@@ -951,20 +956,7 @@ fw_status launch(K kernel, int grid, int tiles, int cluster, int threads, size_t
 {
     const fw_status st = big_smem((const void *)kernel, smem, done);
     if (st != FW_OK) return st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)cluster;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid, (unsigned)tiles);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cfg.attrs = at;
-    cfg.numAttrs = cluster ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mk, mv, a);
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
+    return launch_chained(kernel, dim3((unsigned)grid, (unsigned)tiles), threads, smem, cluster, s, mk, mv, a);
 }
 template <int D, int TW>
 fw_status launch_ranges(const Plan &x, const CUtensorMap &mk, const CUtensorMap &mv, const AttendArgs &a, cudaStream_t s)
@@ -1003,21 +995,10 @@ fw_status attend(const Plan &x, int cells, int rows, const CUtensorMap &mk, cons
     // the joining kernel starts as the first one's CTAs leave
     const bool spread = x.teams >= 4 * cells && (int64_t)cells * rows <= 16 * x.G;
     const int JW = !spread ? 4 : cells * rows <= 64 ? 16 : cells * rows <= 2 * x.G ? 8 : 4;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)cells, (unsigned)(spread ? rows : (rows + JW - 1) / JW));
-    cfg.blockDim = dim3(32 * JW);
-    cfg.stream = s;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    const cudaError_t e = JW == 16 ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true, 16>, a, x.RT)
-                          : JW == 8 ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true, 8>, a, x.RT)
-                          : spread ? cudaLaunchKernelEx(&cfg, k_pages_join<D, true, 4>, a, x.RT)
-                                   : cudaLaunchKernelEx(&cfg, k_pages_join<D, false, 4>, a, x.RT);
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    return e == cudaSuccess ? FW_OK : FW_ERR_CUDA;
+    const dim3 grid((unsigned)cells, (unsigned)(spread ? rows : (rows + JW - 1) / JW));
+    return launch_chained(JW == 16 ? k_pages_join<D, true, 16> : JW == 8 ? k_pages_join<D, true, 8>
+                          : spread ? k_pages_join<D, true, 4> : k_pages_join<D, false, 4>,
+                          grid, 32 * JW, 0, 0, s, a, x.RT);
 }
 
 }  // namespace

@@ -12,7 +12,7 @@
 
 #include <cuda_bf16.h>
 
-#include "fw_internal.h"
+#include "fw_chain.cuh"
 
 namespace fw {
 namespace {
@@ -114,6 +114,8 @@ template <int LPL, bool INTER, bool FULL> __global__ void __launch_bounds__(32 *
 {
     constexpr int HP = 32 / LPL, PER = 8 / HP;  // heads at a time; frequencies that a lane works out
     __shared__ uint4 s_x[RW][AHEAD + 1][2][32];  // a lane's own pieces: no lane reads another's
+    let_the_next_start();
+    wait_for_the_one_before();
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, p = lane % LPL, hl = lane / LPL;
     const int64_t id = (int64_t)blockIdx.x * RW + wid;
     const int64_t row = id / a.split;
@@ -273,15 +275,9 @@ template <int LPL> fw_status launch(RotateArgs &a, int sms, cudaStream_t s)
     a.split = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, (int64_t)sms * 32 / a.rows));
     const unsigned grid = (unsigned)((a.rows * a.split + RW - 1) / RW);
     // (all columns rotated: every lane does the same)
-    if (a.interleaved && a.rot == a.d)
-        FW_LAUNCH((k_qk_rotate<LPL, true, true>), grid, 32 * RW, 0, s, a);
-    else if (a.interleaved)
-        FW_LAUNCH((k_qk_rotate<LPL, true, false>), grid, 32 * RW, 0, s, a);
-    else if (a.rot == a.d)
-        FW_LAUNCH((k_qk_rotate<LPL, false, true>), grid, 32 * RW, 0, s, a);
-    else
-        FW_LAUNCH((k_qk_rotate<LPL, false, false>), grid, 32 * RW, 0, s, a);
-    return FW_OK;
+    return launch_chained(a.interleaved ? a.rot == a.d ? k_qk_rotate<LPL, true, true> : k_qk_rotate<LPL, true, false>
+                          : a.rot == a.d ? k_qk_rotate<LPL, false, true> : k_qk_rotate<LPL, false, false>,
+                          dim3(grid), 32 * RW, 0, 0, s, a);
 }
 
 }  // namespace
