@@ -8,9 +8,9 @@
 // read and handed out at once.
 //
 // Bound: append: latency, one CTA's sums and searches (5 us) and the copies behind it (a token to 256 cells, a fourth of
-// them just forked: 8.2 us; 509 rows to 32 cells 8.9 us); compaction: memory, every kept row read and written once (256 x 32,768
-// rows of 128 to an eighth: 184 us, 5.9 TB/s, of which the copies take 165 us, 6.5 TB/s; 64 x 7,001 rows in pages to a half:
-// 45 us, the copies 35); fork: the tables' entries and their pages' counts (2,048 cells of 256 pages: 9.8 us; 24 cells 3.3 us).
+// them just forked: 8.0 us; 509 rows to 32 cells 8.4 us); compaction: memory, every kept row read and written once (256 x 32,768
+// rows of 128 to an eighth: 183 us, 5.9 TB/s, of which the copies take 165 us, 6.5 TB/s; 64 x 7,001 rows in pages to a half:
+// 45 us, the copies 35); fork: the tables' entries and their pages' counts (2,048 cells of 256 pages: 9.8 us; 24 cells 3.0 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -22,7 +22,7 @@ namespace {
 
 using namespace pages;
 
-constexpr int UR = 16;           // rows that a warp copies at a time; no page holds less
+constexpr int UR = 16;           // (2^4) rows that a warp copies at a time; no page holds less
 constexpr int MW = 8;            // warps of a CTA of the copying kernels
 constexpr int PT = 1024;         // threads of the plan's CTA
 constexpr int WORDS = 4;         // words of the free bits that one of them asks for at a time
@@ -65,8 +65,8 @@ __device__ __forceinline__ int cell_need(const AppendArgs &a, int h, int n, int 
 {
     st = cell_rows_ok(a.s, n, held);
     if (st != FW_OK) return 0;
-    const int i0 = n / a.s.P;
-    const int64_t i1 = ((int64_t)n + a.m - 1) / a.s.P;
+    const int i0 = n >> a.s.lg;
+    const int64_t i1 = ((int64_t)n + a.m - 1) >> a.s.lg;
     if (i1 >= a.s.width) {
         st = FW_ERR_WORKSPACE;
         return 0;
@@ -89,8 +89,8 @@ __device__ __forceinline__ int cell_need_warp(const AppendArgs &a, int h, fw_sta
     int n, held;
     st = cell_rows(a.s, h, n, held);
     if (st != FW_OK) return 0;
-    const int i0 = n / a.s.P;
-    const int64_t i1 = ((int64_t)n + a.m - 1) / a.s.P;
+    const int i0 = n >> a.s.lg;
+    const int64_t i1 = ((int64_t)n + a.m - 1) >> a.s.lg;
     if (i1 >= a.s.width) {
         st = FW_ERR_WORKSPACE;
         return 0;
@@ -116,8 +116,8 @@ __device__ __forceinline__ int cell_need(const CompactArgs &a, int h, int n, int
     st = cell_rows_ok(a.s, n, held);
     const int64_t o0 = a.offsets[h], o1 = a.offsets[h + 1];
     if (o0 < 0 || o1 < o0 || o1 > a.total) st = FW_ERR_INVALID_ARG;
-    if (st == FW_OK && (o1 - o0 + a.s.P - 1) / a.s.P > a.s.width) st = FW_ERR_WORKSPACE;
-    return st == FW_OK ? (int)((o1 - o0 + a.s.P - 1) / a.s.P) : 0;
+    if (st == FW_OK && (o1 - o0 + a.s.P - 1) >> a.s.lg > a.s.width) st = FW_ERR_WORKSPACE;
+    return st == FW_OK ? (int)((o1 - o0 + a.s.P - 1) >> a.s.lg) : 0;
 }
 // Rows that a cell of the compaction gets, or -1 where it is left as it was.  (Reads what the plan read, and
 // what it wrote: the books' first change comes behind the last reader.)
@@ -289,7 +289,7 @@ template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_p
         for (int h = WIDE ? wid : tid; h < s.cells; h += WIDE ? PT / 32 : PT) {
             const int n = a.plan[h].x;
             if (n < 0) continue;
-            const int held = s.held[h], i0 = n / s.P, i1 = (n + a.m - 1) / s.P;
+            const int held = s.held[h], i0 = n >> s.lg, i1 = (n + a.m - 1) >> s.lg;
             int32_t *row = s.row(h);
             int at = a.first[h];
             for (int b = i0; b <= i1; b += WIDE ? 32 : 1) {
@@ -300,7 +300,7 @@ template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_p
                     const int was = i < held ? row[i] : -1, to = at + (WIDE ? __popc(some & ((1u << lane) - 1)) : 0);
                     row[i] = a.list[to];
                     a.was[to] = was;
-                    if (i == i0 && n % s.P != 0) a.plan[h].y = was;
+                    if (i == i0 && (n & (s.P - 1)) != 0) a.plan[h].y = was;
                 }
                 at += __popc(some);
             }
@@ -361,12 +361,13 @@ template <int D> __global__ void __launch_bounds__(32 * MW) k_pages_append(const
     if (h >= s.cells) return;
     const int n = a.plan[h].x, from = a.plan[h].y;
     if (n < 0) return;
-    const int64_t begin = (from >= 0 ? n / s.P * s.P : n / UR * UR) + (int64_t)(id - h * units) * UR;
+    const int64_t begin = (from >= 0 ? n & -s.P : n / UR * UR) + (int64_t)(id - h * units) * UR;
     const int end = n + a.m;
     if (begin >= end) return;
     const int r0 = (int)begin;
     const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
-    const int64_t to = ((int64_t)s.row(h)[r0 / s.P] * s.P + r0 % s.P) * D, old = ((int64_t)from * s.P + r0 % s.P) * D;
+    const int64_t to = (((int64_t)s.row(h)[r0 >> s.lg] << s.lg) + (r0 & (s.P - 1))) * D;
+    const int64_t old = (((int64_t)from << s.lg) + (r0 & (s.P - 1))) * D;
     copy_rows<D>(s.k + to, s.v + to, max(0, from >= 0 ? 0 : n - r0), min(UR, end - r0), lane,
                  [&](int r, const uint16_t *&k, const uint16_t *&v) {
                      const int64_t i = (int64_t)r0 + r - n;
@@ -390,41 +391,42 @@ __device__ __forceinline__ void give_back(const Pages &s, const int32_t *row, in
 template <int D, bool OWN> __global__ void __launch_bounds__(32 * MW) k_pages_move(const CompactArgs a)
 {
     const Pages &s = a.s;
-    const int lane = threadIdx.x & 31, warps = gridDim.x * MW, id = blockIdx.x * MW + (threadIdx.x >> 5), per = s.P / UR;
+    const int lane = threadIdx.x & 31, warps = gridDim.x * MW, id = blockIdx.x * MW + (threadIdx.x >> 5);
+    const int lp = s.lg - 4;  // 2^lp units of a page
     let_the_next_start();
     wait_for_the_one_before();
-    const int64_t units = (int64_t)*a.granted * per, run = (units + warps - 1) / warps;
+    const int64_t units = (int64_t)*a.granted << lp, run = (units + warps - 1) / warps;
     const int64_t u0 = id * run, u1 = min(u0 + run, units);
     if (u0 >= u1) return;
     // the cell of the first: the last one whose pages start at or before it, 32 probes at a time
     int lo = 0, hi = s.cells;
     do {
         const int step = (hi - lo + 31) / 32, i = lo + lane * step;
-        const unsigned hit = __ballot_sync(FW_FULL, i < hi && a.first[min(i, hi - 1)] <= u0 / per);
+        const unsigned hit = __ballot_sync(FW_FULL, i < hi && a.first[min(i, hi - 1)] <= u0 >> lp);
         lo += max(__popc(hit) - 1, 0) * step;
         hi = min(lo + step, hi);
     } while (hi - lo > 1);
     int h = lo;
     for (int64_t u = u0; u < u1; ++u) {
-        const int g = (int)(u / per);
+        const int g = (int)(u >> lp);
         while (a.first[h + 1] <= g) ++h;
         const int64_t o0 = a.offsets[h];
-        const int j0 = (int)(u - (int64_t)a.first[h] * per) * UR, n = (int)(a.offsets[h + 1] - o0);
+        const int j0 = (int)(u - ((int64_t)a.first[h] << lp)) * UR, n = (int)(a.offsets[h + 1] - o0);
         if (j0 >= n) continue;
         const int rows = min(UR, n - j0);
         int64_t at = -1;  // lane r: where row r comes from
         if (lane < rows) {
             const int pos = a.kept_pos[o0 + j0 + lane];
             if constexpr (OWN) {
-                const int page = pos >= 0 && pos < s.counts[h] ? s.row(h)[pos / s.P] : -1;
-                at = s.is_page(page) ? ((int64_t)page * s.P + pos % s.P) * D : -1;
+                const int page = pos >= 0 && pos < s.counts[h] ? s.row(h)[pos >> s.lg] : -1;
+                at = s.is_page(page) ? (((int64_t)page << s.lg) + (pos & (s.P - 1))) * D : -1;
             } else {
                 at = pos >= 0 && pos < a.T ? h * a.cell_stride + pos * a.row_stride : -1;
             }
         }
         const bool off = __any_sync(FW_FULL, lane < rows && at < 0);
         if (off && lane == 0 && a.status) atomicMax(a.status + h, FW_ERR_INVALID_ARG);
-        const int64_t to = ((int64_t)a.list[g] * s.P + j0 % s.P) * D;
+        const int64_t to = (((int64_t)a.list[g] << s.lg) + (j0 & (s.P - 1))) * D;
         copy_rows<D>(s.k + to, s.v + to, 0, rows, lane, [&](int r, const uint16_t *&k, const uint16_t *&v) {
             const int64_t f = __shfl_sync(FW_FULL, at, r);
             k = f >= 0 ? (OWN ? s.k : a.K) + f : nullptr;
@@ -446,7 +448,7 @@ __global__ void __launch_bounds__(128) k_pages_swap(const CompactArgs a)
     int32_t *row = s.row(h);
     give_back(s, row, s.held[h], threadIdx.x, blockDim.x);
     __syncthreads();  // every thread has read the books
-    const int need = (n + s.P - 1) / s.P;
+    const int need = (n + s.P - 1) >> s.lg;
     for (int i = threadIdx.x; i < need; i += blockDim.x) {
         const int page = a.list[a.first[h] + i];
         row[i] = page;
@@ -500,7 +502,7 @@ template <int T, int N> __device__ __forceinline__ void take_over(const ForkArgs
     if (from >= s.cells) st = FW_ERR_INVALID_ARG;
     if (st == FW_OK && other) {
         st = cell_rows(s, from, rows, held);
-        const int need = st == FW_OK ? (rows + s.P - 1) / s.P : 0;
+        const int need = st == FW_OK ? (rows + s.P - 1) >> s.lg : 0;
         int32_t *to = a.rows + (int64_t)h * s.width;
         bool bad = false;
         entries<T, N>(s, from, need, t, first, [&](int i, const int (&e)[N]) {
@@ -533,7 +535,7 @@ template <int T, int N> __device__ __forceinline__ void hand_over(const ForkArgs
     if (n < 0) return;
     entries<T, N>(s, h, held, t, first, [&](int, const int (&e)[N]) { give_all(s, e); });
     any_of<T>(false);  // (every thread has read the old entries)
-    const int need = (n + s.P - 1) / s.P;
+    const int need = (n + s.P - 1) >> s.lg;
     int32_t *row = s.row(h);
 #pragma unroll 4
     for (int i = t; i < need; i += T) row[i] = a.rows[(int64_t)h * s.width + i];

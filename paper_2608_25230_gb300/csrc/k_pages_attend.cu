@@ -10,10 +10,10 @@
 //   start of another, and waits for no other; the parts of cells that several teams share go to the
 //   workspace, and a second kernel, launched behind the first one's tail, joins them in their order.
 // A team is a warp for 8 query rows, or 2, 3, 4 or 6 warps, which read the same blocks against other query
-// rows.  It fetches its blocks by TMA into a ring of its own, through page numbers that its first warp
-// has read 32 blocks ahead.  64 x 8 cells of about 16,384 rows, d = 128, 4 query rows: 606 us, 6.75 TB/s, the measured
+// rows.  It fetches its blocks by TMA into a ring of its own, through page numbers that its warps
+// have read 32 blocks ahead.  64 x 8 cells of about 16,384 rows, d = 128, 4 query rows: 601 us, 6.8 TB/s, the measured
 // copy rate; 24 x 4 cells of 5,000, 7 query rows 45 us (4.7 TB/s: 3 us to the first blocks, the teams finish up to 8 us
-// apart, 5 us to join); 8 cells of 4,096 8.0 us (latency: 2 us to the first block, 4 blocks a warp, 3 us to join).
+// apart, 5 us to join); 8 cells of 4,096 7.4 us (latency: 2 us to the first block, 4 blocks a warp, 3 us to join).
 // (Ranges of a CTA each, with its warps' states joined at the end of each cell's share and the parts by the last CTA to come,
 // were faster for many long cells, 128 x 8 of 4,096 326 us against 338, and slower for others, 32 x 8 of 1,024 38 against 34, drafts
 // of 20 rows 56 against 47.)
@@ -152,8 +152,8 @@ template <int D, int TW, int W> struct Cfg {
     static constexpr int RING = TEAMS * STAGES * 2 * TILE;
     static constexpr size_t SMEM = 1024 + RING;
     static constexpr int RT = TW * 8;  // query rows of a team
-    // blocks under way: with more warps one less than there is room for, so that the first warp does not wait for the others
-    // at every block
+    // blocks under way: with more warps one less than there is room for, so that the warp that asks does not wait for the
+    // others at every block
     static constexpr int AHEAD = STAGES - (TW > 1 ? 1 : 0);
 };
 __host__ __device__ constexpr int range_warps(int D, int TW) { return TW > 1 ? 12 : D == 64 ? 16 : 8; }
@@ -188,11 +188,11 @@ template <int D, int STAGES, int TW> struct Ring {
         const int st = mine % STAGES;
         if (TW > 1 && mine >= STAGES && ok) ok = tc::mbar_wait(&empty[st], (mine / STAGES - 1) & 1, A_WAIT);
         if (!ok) return;
-        if (elect_one()) {  // (a copy that lane 0's branch asks for takes three times as long to issue: its operands are not uniform)
+        if (elect_one()) {  // (8 cells of 4,096 rows: 8.5 us, 8.8 where lane 0 asks)
             const bool is = s.is_page(pg);
             page[st] = is ? pg : -1;
             if (is) {
-                const int row = pg * s.P + at;
+                const int row = (pg << s.lg) + at;
                 tc::mbar_arrive_expect_tx(&full[st], 2 * TILE);
                 tma_load_rows(mem + st * 2 * TILE, tmK, row, &full[st]);
                 tma_load_rows(mem + st * 2 * TILE + TILE, tmV, row, &full[st]);
@@ -231,7 +231,7 @@ struct Window {
     __device__ void load(const Pages &s, int h, int first, int step, int lane)
     {
         from = first;
-        const int64_t e = ((int64_t)first + (int64_t)lane * step) * BR / s.P;
+        const int64_t e = ((int64_t)first + (int64_t)lane * step) * BR >> s.lg;
         pages = s.row(h)[e < s.width ? (int)e : s.width - 1];
     }
     __device__ int at(int i) const { return __shfl_sync(FW_FULL, pages, i); }
@@ -521,7 +521,7 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
             win.from = -1;
         }
         if (win.from < 0 || pb - win.from >= 32 * TW) win.load(s, ph, pb, TW, lane);
-        ring.fetch(&tmK, &tmV, s, win.at((pb - win.from) / TW), pb * BR % s.P);
+        ring.fetch(&tmK, &tmV, s, win.at((pb - win.from) / TW), pb * BR & (s.P - 1));
         pu += TW;
         pb += TW;
     };
@@ -775,7 +775,7 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
         if (pb >= nb) return;
         int i = (pb - win.from) / (step * TW);
         if (i >= 32) win.load(s, h, pb, step * TW, lane), i = 0;
-        ring.fetch(&tmK, &tmV, s, win.at(i), pb * BR % s.P);
+        ring.fetch(&tmK, &tmV, s, win.at(i), pb * BR & (s.P - 1));
         pb += step * TW;
     };
     const int seq = h / a.kv_heads, hk = h - seq * a.kv_heads;
