@@ -480,7 +480,8 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
         total += s_scan[w];
     }
     // consecutive ranges go to different CTAs; at least four blocks each, so that there is less to join
-    const int quota = max((total + a.G * TEAMS - 1) / (a.G * TEAMS), 4);
+    // (the blocks of all cells may be just below 2^31)
+    const int quota = max((int)(((int64_t)total + a.G * TEAMS - 1) / (a.G * TEAMS)), 4);
     {
         int at = before;
         for (int h = h_lo; h < h_hi; ++h) {
@@ -509,12 +510,12 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
     const int u1 = (int)min(first + quota, (int64_t)total);
 
     // the warp's next block to fetch, by cell
-    int pu = u + member, ph = s_h0[team], pb = s_b0[team] + member, pn = s_n0[team], pnb = (pn + BR - 1) / BR;
+    int left = u1 - u - member, ph = s_h0[team], pb = s_b0[team] + member, pn = s_n0[team], pnb = (pn + BR - 1) / BR;
     fw_status pst;
     Window win;
     win.from = -1;
     auto fetch = [&]() {
-        if (pu >= u1) return;
+        if (left <= 0) return;
         while (pb >= pnb && ph + 1 < s.cells) {  // (a block is left, so a cell holds it)
             pb -= pnb;
             pnb = cell_blocks(s, ++ph, pn, pst);
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
         }
         if (win.from < 0 || pb - win.from >= 32 * TW) win.load(s, ph, pb, TW, lane);
         ring.fetch(&tmK, &tmV, s, win.at((pb - win.from) / TW), pb * BR & (s.P - 1));
-        pu += TW;
+        left -= TW;
         pb += TW;
     };
     Rows<D> R;

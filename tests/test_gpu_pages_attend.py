@@ -324,3 +324,23 @@ def test_logits_that_grow_and_are_far_apart(fw, d):
         p.k[page, torch.arange(n, device="cuda") % 16, 1:] = 0
     for longest in (0, n):
         check_all(fw, p, [n] * 5, q, 1, scale=1.0, longest=longest)
+
+
+def test_as_many_blocks_as_are_numbered(fw):
+    """Tables that name few pages over and over: all cells' blocks of 16 rows together are 2^31 - 128, so that a share of them
+    rounded up passes 2^31.  Every weight is 1 and every value 0 or 1, so all sums of a team (14 million rows) are whole
+    numbers below 2^24, exact in 32 bits.  About 2,432 of these in 16 cells are joined by 153 sums each, 2^-24 off relative, so
+    o, whose values 2^-6 apart are bf16 numbers, is exact, and lse off by 2^-24 * 153, a step of the logarithm to base 2 of
+    about 31 (2^-19) and two roundings at 21.5: below 2^-15."""
+    cells, P, d, width, N = 16, 128, 64, (1 << 24) - 1, 64
+    table = (torch.arange(width, device="cuda", dtype=torch.int32) % N).expand(cells, width).contiguous()
+    r, c = torch.arange(P, device="cuda")[:, None], torch.arange(d, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    p = fw.Pages(k=rand(torch.Generator("cuda").manual_seed(1), N, P, d), v=(r % 64 <= c).to(torch.bfloat16).expand(N, P, d).contiguous(),
+                 table=table, held=torch.full((cells,), width, **i32), counts=torch.full((cells,), width * P, **i32),
+                 refs=torch.ones(N, **i32), free=torch.zeros(2, **i32), next=torch.zeros(1, **i32))
+    out = fw.pages_attend(p, torch.zeros(cells, 1, 1, d, dtype=torch.bfloat16, device="cuda"), kv_heads=1)
+    torch.cuda.synchronize()
+    assert not bool(out["status"].any())
+    assert torch.equal(out["o"].double(), ((c + 1) / 64).double().expand_as(out["o"]))
+    assert bool(((out["lse"].double() - math.log(width * P)).abs() < 2.0 ** -15).all())
