@@ -894,7 +894,9 @@ int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, in
     // an SM's time for a block of 16 rows
     const double per = (p.d == 128 ? 1.0 : 0.5) * std::max(0.12, 0.08 * TW);
     const double memory = BR * p.d * 4 / 6.7e6;  // and the memory's
-    const double blocks = (q.longest + BR - 1) / BR, all = 0.5 * blocks * p.cells * tiles;
+    // (no cell has more rows than its table)
+    const int64_t longest = std::min<int64_t>(q.longest, (int64_t)p.max_pages * p.page_rows);
+    const double blocks = (double)((longest + BR - 1) / BR), all = 0.5 * blocks * p.cells * tiles;
     int best = 0, room[SIZES];
     double least = 11.0 + std::max(all * per / sms, all * memory / tiles);
     clusters_at_once(room);

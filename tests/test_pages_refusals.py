@@ -99,6 +99,16 @@ def test_the_library_refuses_on_the_host(fw):
     assert fw.launch_count() == before
 
 
+def test_a_bound_beyond_the_tables_is_theirs(fw):
+    """The way over the cells for a `longest` that no table holds, up to the largest number, is the one for full tables: here ranges,
+    which want a workspace (clusters would not)."""
+    for d, pages, cells in ((64, 200, 100), (128, 5000, 300)):
+        c = cache(fw, d=d, max_pages=pages, cells=cells)
+        for longest in (16 * pages, 16 * pages + 1, 1 << 30, (1 << 31) - 16, (1 << 31) - 15, (1 << 31) - 1):
+            q = C.byref(fw.FwPagesQuery(kv_heads=2, group=4, m=1, longest=longest, q=P, q_seq=512, q_tok=512, q_head=64, scale=0.125))
+            assert fw._lib.fw_pages_attend(c, q, P, P, P, None, 0, None) == fw.FW_ERR_WORKSPACE, longest
+
+
 def bf(*shape, kind=torch.Tensor):
     return torch.zeros(*shape, dtype=torch.bfloat16).as_subclass(kind)
 
