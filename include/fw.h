@@ -581,13 +581,19 @@ typedef struct {
 } fw_pages_query;
 /* o: device bf16 [sequences][m][kv_heads * group][d], 16-byte aligned; lse: device fp32
  * of the same rows (may be NULL).  status [cells] also FW_ERR_TIMEOUT, where a
- * bounded wait gave up (the rows concerned are NaN).  Products of bf16 with fp32 sums, the
+ * bounded wait gave up (the rows concerned are NaN), whichever rows these are.  Products of bf16 with fp32 sums, the
  * weights as the sum of two bf16 numbers (16 bits of each count) up to 2^8 before a sum is
  * divided: values of 2^120 / n and more in n rows can overflow.  The same call gives the same bits. */
 fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, float *lse, int32_t *status,
                           void *workspace, size_t workspace_bytes, void *stream);
 /* Workspace bytes (0 for arguments fw_pages_attend refuses). */
 size_t fw_pages_attend_workspace(const fw_pages *p, const fw_pages_query *q);
+
+/* Test aid, not part of the path: in all of the process's fw_pages_attend calls from now on (a captured call stays as it was
+ * captured) the warps that take the `warp`-th 8 query rows of the `tile`-th tile of a cell's act as if their first wait for rows
+ * had given up.  Query rows are numbered token by token, within one by head of the group; a tile is all of them, or where there
+ * are more than 48, 32 or 48.  A negative number: none, as at the start. */
+void fw_pages_attend_give_up(int32_t tile, int32_t warp);
 
 /* What the attention calls above take, out of a projection's queries and keys, in one
  * pass: the norm of each head, then the rotation by the token's position.

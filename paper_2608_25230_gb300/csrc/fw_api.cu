@@ -669,6 +669,8 @@ fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, f
     return pages_attend(*p, *q, o, lse, status, workspace, (cudaStream_t)stream);
 }
 
+void fw_pages_attend_give_up(int32_t tile, int32_t warp) { pages_attend_give_up(tile, warp); }
+
 fw_status fw_qk_rotate(const fw_rotation *r, void *stream)
 {
     const fw_status st = check_rotation(r);

@@ -126,6 +126,7 @@ fw_status pages_fork(const fw_pages &p, const int32_t *src, int32_t *status, voi
 size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q);
 fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, float *lse, int32_t *status, void *ws,
                        cudaStream_t s);
+void pages_attend_give_up(int tile, int warp);
 fw_status qk_rotate(const fw_rotation &r, cudaStream_t s);
 
 // A TMA map of a 2-D bf16 tensor [rows][cols] (cols innermost, row stride

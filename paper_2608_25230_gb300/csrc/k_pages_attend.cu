@@ -26,6 +26,7 @@
 // by the reading of the blocks from shared memory and by issue: an SM takes about 12 tiles of 8 rows x 16 keys a us (64 cells x 4,096 rows: 20
 // query rows 40 us, 32 45, 48 55, 64 73).
 #include <algorithm>
+#include <climits>
 
 #include <cuda_bf16.h>
 
@@ -53,9 +54,12 @@ struct AttendArgs {
     int32_t *status;
     int G, teams;      // CTAs along the blocks, and their teams
     int cluster;       // CTAs of a cell (few cells)
+    int tiles;         // of query rows
+    int give_tile, give_warp;  // (tests) the warp of every team that is as if its waits had given up; -1: none
     int32_t *start;    // workspace: [cells] first block of each cell
     int32_t *plan;     // workspace: blocks per team
-    int32_t *flags;    // workspace: [teams][2] statuses of parts
+    int32_t *flags;    // workspace: [teams][2] statuses of parts, but for waits that gave up
+    int32_t *failed;   // workspace: [tiles of rows][teams][warps of a team] the cell from which on a warp's waits gave up
     float2 *part_ml;   // workspace: [tiles of rows][teams][2][rows of a tile] (max, sum)
     float *part_o;     // workspace: the same with D columns, column 8 i + g at g D / 8 + i
 };
@@ -532,6 +536,11 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
     for (int i = member; i < C::AHEAD; i += TW) fetch();
 
     int h = s_h0[team], b = s_b0[team];  // the segment: blocks of one cell
+    // the cell where the warp's waits give up: its rows are NaN there and in all cells behind
+    auto gave = [&](int cell) {
+        if (a.status && lane == 0) a.failed[((int64_t)tile * a.teams + gw) * TW + member] = row0 < rows ? cell : INT_MAX;
+    };
+    gave(INT_MAX);
     while (u < u1) {
         int n = s_n0[team];
         fw_status st;
@@ -546,6 +555,8 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
         if (u != (int)first) R.read(a, seq, hk, row0, lane);
         R.start();
         bool bad = false;
+        const bool was = ring.ok;
+        if (tile == a.give_tile && member == a.give_warp) ring.ok = false;
 #pragma unroll 1
         for (int blk = b; blk < bend; ++blk) {
             const int stage = ring.next();
@@ -592,8 +603,9 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
                     dst[i / 2] = make_float4(R.O[i][e], R.O[i][2 + e], R.O[i + 1][e], R.O[i + 1][2 + e]);
             }
         }
+        if (was && !ring.ok) gave(h);
         if (tile == 0 && member == 0 && lane == 0) {
-            const int code = !ring.ok ? FW_ERR_TIMEOUT : bad ? FW_ERR_INVALID_ARG : FW_OK;
+            const int code = bad ? FW_ERR_INVALID_ARG : FW_OK;
             if (!whole)
                 a.flags[gw * 2 + seg] = code;
             else if (a.status)
@@ -608,7 +620,8 @@ __global__ void __launch_bounds__(32 * range_warps(D, TW), 1)
 // The parts of a cell that several teams share, joined in their order; empty cells' outputs.  Each of a CTA's JW warps
 // takes a row, or (SPREAD) all of them one row's parts, where there are few rows and so the parts may be many: the fewer
 // the rows the more warps (8 cells x 4 rows of 150 parts each, 32,768 rows a cell: 35 us with 4 warps, 26 with 16; 64 cells x 20
-// rows: 21.6 with 4, 27 with 8).  CTAs of 4 are small enough to wait beside the first kernel's.
+// rows: 21.6 with 4, 27 with 8).  CTAs of 4 are small enough to wait beside the first kernel's.  Where statuses are asked for, a
+// cell's last CTA sees to its.
 template <int D, bool SPREAD, int JW> __global__ void __launch_bounds__(32 * JW, JW == 4 ? 5 : 1) k_pages_join(const AttendArgs a, int RT)
 {
     constexpr int E = D / 32;
@@ -622,17 +635,27 @@ template <int D, bool SPREAD, int JW> __global__ void __launch_bounds__(32 * JW,
     fw_status st;
     const int nb = cell_blocks(a.s, h, n, st), quota = *a.plan, s = a.start[h];
     const int w0 = s / quota, w1 = nb > 0 ? (s + nb - 1) / quota + 1 : w0;  // the cell's teams
-    if (w1 == w0 + 1) return;
-    if (r >= a.group * a.m) return;  // (SPREAD: no row of the grid is)
-    const int64_t tile0 = (int64_t)(r / RT) * a.teams;
+    const bool whole = w1 == w0 + 1;
     auto seg_of = [&](int p) { return p == w0 && s > p * quota ? 1 : 0; };
-    auto part_at = [&](int p) { return ((tile0 + p) * 2 + seg_of(p)) * RT + r % RT; };
-    if (r == 0 && a.status && (!SPREAD || wid == 0)) {
+    if (a.status && blockIdx.y == gridDim.y - 1) {
+        // the cell's status: whether any warp of any tile gave up in it, and where it has parts, theirs
+        if (wid != 0) return;
         int code = st;
-        for (int p = w0 + lane; p < w1; p += 32) code = max(code, a.flags[p * 2 + seg_of(p)]);
+        if (!whole)
+#pragma unroll 4
+            for (int p = w0 + lane; p < w1; p += 32) code = max(code, a.flags[p * 2 + seg_of(p)]);
+        const int each = (w1 - w0) * (RT / 8);
+#pragma unroll 4
+        for (int i = lane; i < each * a.tiles; i += 32)
+            if (a.failed[((int64_t)(i / each) * a.teams + w0) * (RT / 8) + i % each] <= h) code = max(code, FW_ERR_TIMEOUT);
         code = __reduce_max_sync(FW_FULL, code);
-        if (lane == 0) a.status[h] = code;
+        if (lane == 0 && (!whole || code != FW_OK)) a.status[h] = code;
+        return;
     }
+    if (whole) return;
+    if (r >= a.group * a.m) return;  // (SPREAD: none is)
+    const int64_t tile0 = (int64_t)(r / RT) * a.teams;
+    auto part_at = [&](int p) { return ((tile0 + p) * 2 + seg_of(p)) * RT + r % RT; };
     // this warp's parts: 32 maxima and sums at a time, then their columns
     const int all = w1 - w0, each = SPREAD ? (all + JW - 1) / JW : all;
     const int p0 = SPREAD ? w0 + min(wid * each, all) : w0, p1 = min(p0 + each, w1);
@@ -786,6 +809,7 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
     for (int i = member; i < C::AHEAD; i += TW) fetch();
     R.start();
     bool bad = false;
+    if ((int)blockIdx.y == a.give_tile && member == a.give_warp && first < nb) ring.ok = false;
 #pragma unroll 1
     for (int blk = first; blk < nb; blk += step) {
         const int stage = ring.next();
@@ -839,10 +863,20 @@ __global__ void __launch_bounds__(32 * few_warps(TW), 1)
             a.o[out * D + lane + 32 * e] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[e] * inv));
         if (a.lse && lane == 0) a.lse[out] = lse_of(M, L);
     }
-    if (rank == 0 && blockIdx.y == 0 && wid == W - 1 && a.status) {
+    if (rank == 0 && wid == W - 1 && a.status) {
         const int codes = __reduce_max_sync(FW_FULL, lane < a.cluster ? s_codes[lane] : 0);
-        if (lane == 0) a.status[h] = codes;
+        if (lane == 0 && gridDim.y == 1) a.status[h] = codes;
+        if (lane == 0 && gridDim.y > 1 && codes != FW_OK) atomicMax(a.status + h, codes);
     }
+}
+
+// The statuses that the clusters of several tiles raise (0.65 us in front of them; a single tile's cluster writes its cell's status).
+__global__ void __launch_bounds__(128) k_pages_clear_status(const AttendArgs a)
+{
+    const int h = blockIdx.x * 128 + threadIdx.x;
+    let_the_next_start();
+    wait_for_the_one_before();
+    if (h < a.s.cells) a.status[h] = FW_OK;
 }
 
 // How many clusters of each size find room on the GPU at once, a CTA an SM (GPUs differ in the SMs of their parts), and the
@@ -913,7 +947,7 @@ int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, in
 struct Plan {
     int few;  // CTAs of a cell's cluster, or 0
     int G, TW, teams, RT, tiles;
-    size_t start, plan, flags, ml, o, bytes;
+    size_t start, plan, flags, failed, ml, o, bytes;
 };
 void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
 {
@@ -926,7 +960,7 @@ void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
     x.TW = need > 6 && (need + 5) / 6 * 6 > (need + 3) / 4 * 4 ? 4 : 6;
     for (const int tw : {4, 3, 2, 1})
         if (need <= tw) x.TW = tw;
-    x.start = x.plan = x.flags = x.ml = x.o = x.bytes = 0;
+    x.start = x.plan = x.flags = x.failed = x.ml = x.o = x.bytes = 0;
     x.RT = x.TW * 8;
     x.tiles = (rows + x.RT - 1) / x.RT;
     x.few = cluster_of(p, q, x.TW, x.tiles, sms);
@@ -935,7 +969,8 @@ void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
     x.teams = x.G * (range_warps(p.d, x.TW) / x.TW);
     x.plan = align256((size_t)p.cells * 4);
     x.flags = x.plan + 256;
-    x.ml = x.flags + align256((size_t)x.teams * 8);
+    x.failed = x.flags + align256((size_t)x.teams * 8);
+    x.ml = x.failed + align256((size_t)x.tiles * x.teams * x.TW * 4);
     const size_t parts = (size_t)x.tiles * x.teams * 2 * x.RT;
     x.o = x.ml + align256(parts * 8);
     x.bytes = x.o + align256(parts * p.d * 4);
@@ -977,6 +1012,10 @@ fw_status launch_few(const Plan &x, int cells, const CUtensorMap &mk, const CUte
         const fw_status st = wide_clusters((const void *)k_pages_attend_few<D, TW>, wide);
         if (st != FW_OK) return st;
     }
+    if (x.tiles > 1 && a.status) {
+        const fw_status st = launch_chained(k_pages_clear_status, dim3((unsigned)((cells + 127) / 128)), 128, 0, 0, s, a);
+        if (st != FW_OK) return st;
+    }
     return launch(k_pages_attend_few<D, TW>, cells * x.few, x.tiles, x.few, 32 * W, few_smem<D, TW>(), mk, mv, a, done, s);
 }
 template <int D, int TW>
@@ -998,13 +1037,17 @@ fw_status attend(const Plan &x, int cells, int rows, const CUtensorMap &mk, cons
     // the joining kernel starts as the first one's CTAs leave
     const bool spread = x.teams >= 4 * cells && (int64_t)cells * rows <= 16 * x.G;
     const int JW = !spread ? 4 : cells * rows <= 64 ? 16 : cells * rows <= 2 * x.G ? 8 : 4;
-    const dim3 grid((unsigned)cells, (unsigned)(spread ? rows : (rows + JW - 1) / JW));
+    const dim3 grid((unsigned)cells, (unsigned)(spread ? rows : (rows + JW - 1) / JW) + (a.status ? 1 : 0));
     return launch_chained(JW == 16 ? k_pages_join<D, true, 16> : JW == 8 ? k_pages_join<D, true, 8>
                           : spread ? k_pages_join<D, true, 4> : k_pages_join<D, false, 4>,
                           grid, 32 * JW, 0, 0, s, a, x.RT);
 }
 
+std::atomic<int64_t> g_give_up{-1};  // tile << 32 | warp
+
 }  // namespace
+
+void pages_attend_give_up(int tile, int warp) { g_give_up.store(tile < 0 || warp < 0 ? -1 : (int64_t)tile << 32 | warp); }
 
 size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q)
 {
@@ -1026,10 +1069,11 @@ fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, floa
         return FW_ERR_CUDA;
     uint8_t *w = (uint8_t *)ws;
     const uint32_t inv = q.group > 1 ? (uint32_t)(((uint64_t)1 << 32) / q.group + 1) : 0;
+    const int64_t give = g_give_up.load(std::memory_order_relaxed);
     const AttendArgs a{view(p), q.kv_heads, q.group, q.m, inv, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
                        q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, x.few ? 0 : x.G, x.few ? 0 : x.teams, x.few,
-                       (int32_t *)(w + x.start), (int32_t *)(w + x.plan), (int32_t *)(w + x.flags), (float2 *)(w + x.ml),
-                       (float *)(w + x.o)};
+                       x.tiles, (int)(give >> 32), (int)give, (int32_t *)(w + x.start), (int32_t *)(w + x.plan),
+                       (int32_t *)(w + x.flags), (int32_t *)(w + x.failed), (float2 *)(w + x.ml), (float *)(w + x.o)};
     return p.d == 128 ? attend<128>(x, p.cells, q.group * q.m, mk, mv, a, s) : attend<64>(x, p.cells, q.group * q.m, mk, mv, a, s);
 }
 

@@ -106,6 +106,8 @@ _lib.fw_pages_fork_workspace.restype = C.c_size_t
 _lib.fw_pages_attend.argtypes = [C.POINTER(FwPages), C.POINTER(FwPagesQuery), vp, vp, vp, vp, C.c_size_t, vp]
 _lib.fw_pages_attend_workspace.argtypes = [C.POINTER(FwPages), C.POINTER(FwPagesQuery)]
 _lib.fw_pages_attend_workspace.restype = C.c_size_t
+_lib.fw_pages_attend_give_up.argtypes = [C.c_int32, C.c_int32]
+_lib.fw_pages_attend_give_up.restype = None
 _lib.fw_qk_rotate.argtypes = [vp, vp]
 _ROTATION = struct.Struct("@q6if4x16q")  # FwRotation's fields: packed in a quarter of the time that setting them takes (2 us)
 assert _ROTATION.size == C.sizeof(FwRotation)

@@ -344,3 +344,35 @@ def test_as_many_blocks_as_are_numbered(fw):
     assert not bool(out["status"].any())
     assert torch.equal(out["o"].double(), ((c + 1) / 64).double().expand_as(out["o"]))
     assert bool(((out["lse"].double() - math.log(width * P)).abs() < 2.0 ** -15).all())
+
+
+@pytest.mark.parametrize("d,group,m,tile,warp,rows", [
+    (128, 4, 1, 0, 0, range(0, 4)), (64, 5, 2, 0, 0, range(0, 8)), (64, 5, 2, 0, 1, range(8, 10)), (128, 4, 5, 0, 2, range(16, 20)),
+    (64, 20, 1, 0, 1, range(8, 16)), (64, 30, 1, 0, 3, range(24, 30)), (128, 12, 5, 0, 3, range(24, 32)),
+    (128, 12, 5, 1, 0, range(32, 40)), (128, 12, 5, 1, 3, range(56, 60)), (64, 45, 2, 1, 5, range(88, 90))])
+def test_a_wait_that_gives_up_shows(fw, d, group, m, tile, warp, rows):
+    """Whichever warp of whichever tile gives up: its rows are NaN, its cells' statuses say so, and all else is as it was.  (As if a
+    wait had given up: no wait runs out.  Cells are so short that no other warp waits for what this one would have asked for.)"""
+    gen = torch.Generator("cuda").manual_seed(group)
+    counts = [40, 0, 16, 17, 70, 48, 33, 1, 90, 0, 64, 5]
+    p = cache_of(fw, gen, counts, 16, d)
+    q = rand(gen, 12, m, group, d)
+    p.table[4, 1] = -1  # (a page that is none beside it)
+    mine = torch.tensor([r in rows for r in range(m * group)], device="cuda").view(m, group)
+    for longest in (0, 90):
+        want = fw.pages_attend(p, q, kv_heads=1, longest=longest)
+        fw.raw().fw_pages_attend_give_up(tile, warp)
+        try:
+            out = fw.pages_attend(p, q, kv_heads=1, longest=longest)
+        finally:
+            fw.raw().fw_pages_attend_give_up(-1, -1)
+        again = fw.pages_attend(p, q, kv_heads=1, longest=longest)
+        torch.cuda.synchronize()
+        assert want["status"].tolist() == [fw.FW_ERR_INVALID_ARG if h == 4 else 0 for h in range(12)]
+        assert out["status"].tolist() == [fw.FW_ERR_TIMEOUT if n else 0 for n in counts]
+        hit = mine & (torch.tensor(counts, device="cuda")[:, None, None] > 0)
+        assert bool(torch.isnan(out["o"][hit]).all()) and bool(torch.isnan(out["lse"][hit]).all())
+        assert torch.equal(out["o"][~hit].view(torch.int16), want["o"][~hit].view(torch.int16))
+        assert torch.equal(out["lse"][~hit], want["lse"][~hit])
+        for x in ("o", "lse", "status"):
+            assert torch.equal(again[x], want[x])
