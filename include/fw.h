@@ -586,7 +586,7 @@ typedef struct {
  * divided: values of 2^120 / n and more in n rows can overflow.  The same call gives the same bits. */
 fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, float *lse, int32_t *status,
                           void *workspace, size_t workspace_bytes, void *stream);
-/* Workspace bytes (0 for arguments fw_pages_attend refuses). */
+/* Workspace bytes, for every `longest` (0 for arguments fw_pages_attend refuses). */
 size_t fw_pages_attend_workspace(const fw_pages *p, const fw_pages_query *q);
 
 /* Test aid, not part of the path: in all of the process's fw_pages_attend calls from now on (a captured call stays as it was

@@ -655,7 +655,7 @@ fw_status fw_pages_fork(const fw_pages *p, const int32_t *src, int32_t *status, 
 
 size_t fw_pages_attend_workspace(const fw_pages *p, const fw_pages_query *q)
 {
-    return check_pages_query(p, q) == FW_OK ? pages_attend_workspace(*p, *q) : 0;
+    return check_pages_query(p, q) == FW_OK ? pages_attend_workspace(*p, *q, true) : 0;
 }
 
 fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, float *lse, int32_t *status,
@@ -664,7 +664,7 @@ fw_status fw_pages_attend(const fw_pages *p, const fw_pages_query *q, void *o, f
     const fw_status st = check_pages_query(p, q);
     if (st != FW_OK) return st;
     if (!o || !aligned(o, 16)) return FW_ERR_INVALID_ARG;
-    const size_t need = pages_attend_workspace(*p, *q);
+    const size_t need = pages_attend_workspace(*p, *q, false);
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return FW_ERR_WORKSPACE;
     return pages_attend(*p, *q, o, lse, status, workspace, (cudaStream_t)stream);
 }

@@ -123,7 +123,8 @@ fw_status pages_compact(const fw_pages &p, const void *K, const void *V, int T, 
                         cudaStream_t s);
 size_t pages_fork_workspace(const fw_pages &p);
 fw_status pages_fork(const fw_pages &p, const int32_t *src, int32_t *status, void *ws, cudaStream_t s);
-size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q);
+// any_longest: for every `longest`; else what this call needs (clusters need none).
+size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q, bool any_longest);
 fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, float *lse, int32_t *status, void *ws,
                        cudaStream_t s);
 void pages_attend_give_up(int tile, int warp);

@@ -947,7 +947,7 @@ int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, in
 struct Plan {
     int few;  // CTAs of a cell's cluster, or 0
     int G, TW, teams, RT, tiles;
-    size_t start, plan, flags, failed, ml, o, bytes;
+    size_t start, plan, flags, failed, ml, o, bytes;  // (of ranges, whichever way is taken: a workspace serves both)
 };
 void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
 {
@@ -960,11 +960,10 @@ void plan_of(const fw_pages &p, const fw_pages_query &q, Plan &x)
     x.TW = need > 6 && (need + 5) / 6 * 6 > (need + 3) / 4 * 4 ? 4 : 6;
     for (const int tw : {4, 3, 2, 1})
         if (need <= tw) x.TW = tw;
-    x.start = x.plan = x.flags = x.failed = x.ml = x.o = x.bytes = 0;
+    x.start = 0;
     x.RT = x.TW * 8;
     x.tiles = (rows + x.RT - 1) / x.RT;
     x.few = cluster_of(p, q, x.TW, x.tiles, sms);
-    if (x.few) return;
     x.G = std::max(1, sms / x.tiles);  // one wave
     x.teams = x.G * (range_warps(p.d, x.TW) / x.TW);
     x.plan = align256((size_t)p.cells * 4);
@@ -1049,11 +1048,11 @@ std::atomic<int64_t> g_give_up{-1};  // tile << 32 | warp
 
 void pages_attend_give_up(int tile, int warp) { g_give_up.store(tile < 0 || warp < 0 ? -1 : (int64_t)tile << 32 | warp); }
 
-size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q)
+size_t pages_attend_workspace(const fw_pages &p, const fw_pages_query &q, bool any_longest)
 {
     Plan x;
     plan_of(p, q, x);
-    return x.bytes;
+    return any_longest || !x.few ? x.bytes : 0;
 }
 
 fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, float *lse, int32_t *status, void *ws,
@@ -1071,7 +1070,7 @@ fw_status pages_attend(const fw_pages &p, const fw_pages_query &q, void *o, floa
     const uint32_t inv = q.group > 1 ? (uint32_t)(((uint64_t)1 << 32) / q.group + 1) : 0;
     const int64_t give = g_give_up.load(std::memory_order_relaxed);
     const AttendArgs a{view(p), q.kv_heads, q.group, q.m, inv, (const uint16_t *)q.q, q.q_seq, q.q_tok, q.q_head,
-                       q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, x.few ? 0 : x.G, x.few ? 0 : x.teams, x.few,
+                       q.scale * 1.4426950408889634f, (uint16_t *)o, lse, status, x.G, x.teams, x.few,
                        x.tiles, (int)(give >> 32), (int)give, (int32_t *)(w + x.start), (int32_t *)(w + x.plan),
                        (int32_t *)(w + x.flags), (int32_t *)(w + x.failed), (float2 *)(w + x.ml), (float *)(w + x.o)};
     return p.d == 128 ? attend<128>(x, p.cells, q.group * q.m, mk, mv, a, s) : attend<64>(x, p.cells, q.group * q.m, mk, mv, a, s);

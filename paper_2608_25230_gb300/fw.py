@@ -955,7 +955,7 @@ def _pages_query(pages, q, kv_heads, scale, longest):
 
 
 def pages_attend_workspace(pages: Pages, q: torch.Tensor, *, kv_heads: int, longest: int = 0) -> torch.Tensor:
-    """A workspace for pages_attend calls with queries of q's shape and this `longest` (fw_pages_attend_workspace)."""
+    """A workspace for pages_attend calls with queries of q's shape, whatever their `longest` (fw_pages_attend_workspace)."""
     c_q = _pages_query(pages, q, kv_heads, None, longest)
     _on_current(pages.index)
     return _ws(_lib.fw_pages_attend_workspace(pages._ref, C.byref(c_q)), pages.device)

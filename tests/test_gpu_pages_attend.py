@@ -277,6 +277,17 @@ def test_side_streams_and_graphs(fw):
             check_cell(p, h, n, x, o, 2, 0.125)
 
 
+def test_a_kept_workspace_and_a_bound_that_grows(fw):
+    """A workspace made at the first step, whose bound asks for clusters, serves the steps whose bound asks for ranges."""
+    gen = torch.Generator("cuda").manual_seed(9)
+    counts = [300] * 64
+    p = cache_of(fw, gen, counts, 16, 128, width=2000)
+    q = rand(gen, 64, 1, 4, 128)
+    ws = fw.pages_attend_workspace(p, q, kv_heads=1, longest=300)
+    for longest in (300, 600, 3000, 32000, 0):
+        check_all(fw, p, counts, q, 1, longest=longest, workspace=ws)
+
+
 def test_without_lse_and_status(fw):
     gen = torch.Generator("cuda").manual_seed(7)
     p = cache_of(fw, gen, [90, 0, 3], 32, 64)

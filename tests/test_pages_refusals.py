@@ -109,6 +109,15 @@ def test_a_bound_beyond_the_tables_is_theirs(fw):
             assert fw._lib.fw_pages_attend(c, q, P, P, P, None, 0, None) == fw.FW_ERR_WORKSPACE, longest
 
 
+def test_an_attention_workspace_serves_every_bound(fw):
+    for d, cells, group, m in ((64, 8, 4, 1), (128, 64, 4, 5), (128, 2, 16, 4)):
+        c, size = cache(fw, d=d, max_pages=5000, cells=cells), set()
+        for longest in (0, 1, 100, 3000, 80000, (1 << 31) - 1):
+            q = fw.FwPagesQuery(kv_heads=2, group=group, m=m, longest=longest, q=P, q_seq=512, q_tok=512, q_head=64, scale=0.125)
+            size.add(fw._lib.fw_pages_attend_workspace(c, C.byref(q)))
+        assert len(size) == 1 and min(size) > 0, size
+
+
 def bf(*shape, kind=torch.Tensor):
     return torch.zeros(*shape, dtype=torch.bfloat16).as_subclass(kind)
 
