@@ -170,3 +170,31 @@ def test_on_a_side_stream_and_in_a_graph(fw):
     torch.cuda.synchronize()
     check(out[0], rotate64(q, None, 1e-6, pos, f, False))
     check(out[1], rotate64(k, None, 1e-6, pos, f, False))
+
+
+@pytest.mark.parametrize("rows,hq,hk,d,rot", [(5003, 32, 8, 128, 128), (5003, 7, 3, 256, 96), (5000, 3, 50, 48, 48), (1500, 40, 9, 64, 64),
+                                              (1500, 41, 7, 208, 208), (700, 64, 9, 128, 32), (6001, 29, 0, 128, 0),
+                                              (2501, 33, 15, 80, 16)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_warps_that_take_many_heads(fw, rows, hq, hk, d, rot, interleaved):
+    """So many tokens that a warp takes several chunks of a token's heads, all or every 2nd to 7th of up to 25: the heads that it asks
+    for ahead come round in their places, and it goes over from queries to keys, with full and ragged chunks, not in place and in
+    place."""
+    gen = torch.Generator("cuda").manual_seed(rows + d)
+    q, k = packed(gen, rows, hq, hk, d)
+    base = q._base
+    pos = torch.randint(-5000, 1 << 20, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    f = freqs(rot)
+    w = [torch.randn(d, generator=gen, device="cuda") for _ in "qk"]
+    for eps, (wq, wk) in ((1e-6, w), (None, (None, None))):
+        want = [rotate64(x, y, eps, pos, f, interleaved) for x, y in ((q, wq), (k, wk))]
+        args = dict(q_weight=wq, k_weight=wk if hk else None, eps=eps, interleaved=interleaved)
+        a, b = fw.qk_rotate(q, k if hk else None, pos, f, **args)
+        torch.cuda.synchronize()
+        check(a, want[0])
+        if hk:
+            check(b, want[1])
+    values = base[:, hq + hk:].clone()
+    fw.qk_rotate(q, k if hk else None, pos, f, out=(q, k if hk else None), **args)
+    torch.cuda.synchronize()
+    assert torch.equal(q, a) and (not hk or torch.equal(k, b)) and torch.equal(base[:, hq + hk:], values)
