@@ -3,8 +3,9 @@
 // A kernel launched by launch_chained() may find its CTAs on the GPU as soon as all CTAs of the kernel before have started
 // and said so (or left), whoever's it is; it sets up what needs no memory, and waits for that kernel's end, and so for
 // all before it, in wait_for_the_one_before().  Every thread calls that before it reads or writes global memory, and no thread
-// leaves without: a kernel that ended without having waited would let the next one pass its own wait too soon.  A decode
-// step's rotation, append and attention in a graph: 8 cells of 512 rows 13.2 us (14.3 launched one after another), of 4,096
+// leaves without: a kernel that ended without having waited would let the next one pass its own wait too soon.  One kernel reads
+// before its wait, k_pages_fork_end: tables that the kernel before it, k_pages_fork, does not change, and that all kernels before
+// that one are done with, since it lets the next start only behind its own wait.  A decode step's rotation, append and attention in a graph: 8 cells of 512 rows 13.2 us (14.3 launched one after another), of 4,096
 // 17.1 (18.2), 64 of 1,024 20.3 (21.3).
 #pragma once
 

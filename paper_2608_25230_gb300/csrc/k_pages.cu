@@ -555,8 +555,8 @@ __global__ void __launch_bounds__(KT) k_pages_fork(const ForkArgs a)
 }
 __global__ void __launch_bounds__(KT) k_pages_fork_end(const ForkArgs a)
 {
-    // (the kernel before changes no table, and what came before that one is in memory; an SM's own cache is up to date only
-    // behind the wait, so these reads go past it)
+    // (the kernel before, k_pages_fork, changes no table, and has waited for what came before it, which so is in memory; an SM's own
+    // cache is up to date only behind the wait, so these reads go past it)
     let_the_next_start();
     const int h = blockIdx.x, held = __ldcg(a.s.held + h);
     int first[KE];
