@@ -507,7 +507,7 @@ size_t fw_cache8_attend_workspace(const fw_cache8 *c, const fw_cache8_query *q);
  * no page of the pool; FW_ERR_WORKSPACE where its rows need more than max_pages
  * entries, or more pages than are left free for it (a cell that what is left does not hold, and
  * every cell behind it that needs a page, get none).  Such a cell is left as it
- * was, and all others are served. */
+ * was (but for a kept row's page, see fw_pages_compact), and all others are served. */
 typedef struct {
     int32_t cells;
     int32_t d;               /* 64 or 128                                            */
@@ -544,9 +544,10 @@ size_t fw_pages_append_workspace(const fw_pages *p, int32_t m);
  *   - of K and V: device bf16, row t of cell h at h * cell_stride + t * row_stride
  *     elements (positive multiples of 8), T rows per cell, 16-byte aligned;
  *   - K and V both NULL: of the cell's own rows (T and the strides are not looked at).
- * total: the entries that kept_pos holds (at least offsets[cells]).  A kept position out of
- * range stores a row of zeros, with FW_ERR_INVALID_ARG; so does an offset out of order or
- * beyond total, whose cell is left as it was. */
+ * total: the entries that kept_pos holds (at least offsets[cells]).  A kept position that has no
+ * row, out of range or on an entry of the cell's own that is no page of the pool, stores a row of zeros, with
+ * FW_ERR_INVALID_ARG: the cell's other rows are kept and its old pages given back all the same.  An offset out of
+ * order or beyond total gives FW_ERR_INVALID_ARG too, and its cell is left as it was. */
 fw_status fw_pages_compact(const fw_pages *p, const void *K, const void *V, int32_t T, int64_t cell_stride,
                            int64_t row_stride, const int64_t *offsets, const int32_t *kept_pos, int64_t total,
                            int32_t *status, void *workspace, size_t workspace_bytes, void *stream);

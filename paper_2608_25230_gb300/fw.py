@@ -920,7 +920,8 @@ def pages_compact(pages: Pages, K: torch.Tensor, V: torch.Tensor, offsets: torch
 
 def pages_keep(pages: Pages, offsets: torch.Tensor, kept_pos: torch.Tensor, *, status: torch.Tensor = None, workspace=None,
                stream=None):
-    """fw_pages_compact of the cells' own rows: cell h keeps its rows kept_pos[offsets[h]:offsets[h + 1]], in that order."""
+    """fw_pages_compact of the cells' own rows: cell h keeps its rows kept_pos[offsets[h]:offsets[h + 1]], in that order.  A kept
+    row whose table entry is no page becomes zeros, with a status; the others are kept."""
     _pages_compact(pages, None, None, 0, 0, 0, offsets, kept_pos, status, workspace, stream)
 
 

@@ -225,6 +225,32 @@ def test_bad_books(fw):
     b.append(17)
 
 
+def test_kept_rows_on_an_entry_that_is_no_page(fw):
+    """They become zeros, with a status; the cell's other rows are kept, its good pages are given back, other cells are served."""
+    P, d, n = 16, 64, 40
+    p = fw.pages_empty(3, 20, d, max_pages=4, page_rows=P)
+    ids = torch.arange(1, 3 * n + 1, device="cuda").view(1, 3, n).transpose(1, 2)
+    fw.pages_append(p, *as_rows(ids, d))
+    k, v = (x[0].transpose(0, 1) for x in as_rows(ids, d))  # [cells][rows][d]
+    gone = int(p.table[1, 1])
+    p.table[1, 1] = 20
+    status = torch.full((3,), -1, dtype=torch.int32, device="cuda")
+    pos = [0, 39, 3, 15, 16, 31, 32, 5]
+    off = torch.tensor([0, 2, 6, 8], device="cuda")
+    fw.pages_keep(p, off, torch.tensor(pos, dtype=torch.int32, device="cuda"), status=status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [fw.FW_OK, fw.FW_ERR_INVALID_ARG, fw.FW_OK]
+    assert p.counts.tolist() == [2, 4, 2] and p.held.tolist() == [1, 1, 1]
+    for h in range(3):
+        for j, t in enumerate(pos[int(off[h]):int(off[h + 1])]):
+            page = int(p.table[h, 0])
+            for pool, want in ((p.k, k), (p.v, v)):
+                row = torch.zeros_like(want[h, t]) if h == 1 and t // P == 1 else want[h, t]
+                assert torch.equal(pool[page, j].view(torch.int16), row.view(torch.int16))
+    # all that the books named but the three new pages is free again; the page that an entry named no more is nobody's
+    assert [i for i, x in enumerate(p.refs.tolist()) if x] == sorted([gone] + p.table[:, 0].tolist())
+
+
 @pytest.mark.parametrize("cells,width,N,P,d", [(40, 12, 700, 16, 64), (7, 300, 1700, 16, 64), (33, 600, 3000, 16, 128)])
 def test_forks_of_many_cells_and_long_tables(fw, cells, width, N, P, d):
     """More cells than one CTA takes, tables longer than what is asked for early."""
