@@ -564,8 +564,9 @@ __global__ void __launch_bounds__(KT) k_pages_fork_end(const ForkArgs a)
     wait_for_the_one_before();
     hand_over<KT, KE>(a, h, held, threadIdx.x, first);
 }
-// Few cells of short tables: both by one CTA, a warp per cell.  It takes the GPU as long (24 cells of up to 40 pages: 3.3 us, 3.8 in two
-// launches; 32 of 20: 3.6, 3.3), the host 2 us less.
+// Few cells of short tables: both by one CTA, a warp per cell.  The host takes 2 us less (11.3 against 13.5, which is longer than the GPU
+// takes either way); the GPU in a graph, in us, one launch against two: 32 cells of 20 pages 3.6 and 3.3, 24 of 40 4.0 and 3.6, 32 of 64
+// 5.2 and 3.5, of 128 7.5 and 4.2, of 250 5.6 and 5.3.
 constexpr int ONE_CELLS = 32, ONE_PAGES = 256;
 __global__ void __launch_bounds__(1024, 1) k_pages_fork_one(const ForkArgs a)
 {
@@ -583,11 +584,9 @@ __global__ void __launch_bounds__(1024, 1) k_pages_fork_one(const ForkArgs a)
     if (mine) hand_over<32, KE>(a, h, held, lane, first);
 }
 
-size_t append_list(const fw_pages &p, int m)
-{
-    const int64_t touched = ((int64_t)m + p.page_rows - 2) / p.page_rows + 1;
-    return (size_t)std::min<int64_t>(p.num_pages, touched * p.cells);
-}
+// Entries of a cell's table that m new rows touch, at most.
+int64_t touched(const fw_pages &p, int m) { return ((int64_t)m + p.page_rows - 2) / p.page_rows + 1; }
+size_t append_list(const fw_pages &p, int m) { return (size_t)std::min<int64_t>(p.num_pages, touched(p, m) * p.cells); }
 size_t compact_list(const fw_pages &p, int64_t total)
 {
     // (offsets out of order may name the same positions for several cells)
@@ -616,8 +615,11 @@ fw_status pages_append(const fw_pages &p, const fw_pages_new &r, int32_t *status
     a.granted = (int32_t *)(w + align256(append_list(p, r.m) * 4));
     const int units = (p.page_rows - 1 + r.m + UR - 1) / UR;
     const unsigned grid = BOOK + (unsigned)(((int64_t)p.cells * units + MW - 1) / MW);
-    // (4 cells x 509 rows, 33 pages each: a warp per cell 3 us, a thread 10)
-    const fw_status planned = launch_chained(r.m > 3 * p.page_rows ? k_pages_plan<AppendArgs, true> : k_pages_plan<AppendArgs, false>,
+    // A warp per cell, 32 cells at a time (about 2 us a turn), or a thread, an entry at a time (0.3 us each).  Whole calls in us, a warp
+    // against a thread, d = 64, pages of 16: 8 cells 6.6 and 6.9 for 64 rows, 7.4 and 11.0 for 300; 32 cells 7.4 and 7.3 for 40, 8.2
+    // and 12.6 for 300; 64 cells 9.1 and 7.4 for 64, 10.6 and 12.4 for 300; 256 cells 25 and 21 for 300; 2,048 cells 129 and 33 for 64.
+    const bool wide = touched(p, r.m) > 3 * (((int64_t)p.cells + 31) / 32);
+    const fw_status planned = launch_chained(wide ? k_pages_plan<AppendArgs, true> : k_pages_plan<AppendArgs, false>,
                                              dim3(1), PT, 0, 0, st, a);
     if (planned != FW_OK) return planned;
     return launch_chained(p.d == 128 ? k_pages_append<128> : k_pages_append<64>, dim3(grid), 32 * MW, 0, 0, st, a, units);
