@@ -387,3 +387,32 @@ def test_a_wait_that_gives_up_shows(fw, d, group, m, tile, warp, rows):
         assert torch.equal(out["lse"][~hit], want["lse"][~hit])
         for x in ("o", "lse", "status"):
             assert torch.equal(again[x], want[x])
+
+
+@pytest.mark.parametrize("d,beams", [(64, 4), (128, 8)])
+def test_cells_that_share_pages(fw, d, beams):
+    """Beams of two prompts that fork, decode on and fork again: every cell's attention is that over its own rows, and bit for bit
+    that over copies of them in pages of its own."""
+    gen = torch.Generator("cuda").manual_seed(d)
+    heads, P = 2, 16
+    cells = 2 * beams * heads
+    p = fw.pages_empty(cells, 40 * cells, d, max_pages=40, page_rows=P)
+    first = rand(gen, 2 * beams, 333, heads, d)
+    fw.pages_append(p, first, rand(gen, 2 * beams, 333, heads, d))
+    for i in range(3):
+        lead = [s // beams * beams + (s * (i + 1) + i) % beams // 2 for s in range(2 * beams)]  # (half of the beams go on, twice each)
+        fw.pages_fork(p, torch.tensor([s * heads + h for s in lead for h in range(heads)], dtype=torch.int32, device="cuda"))
+        fw.pages_append(p, rand(gen, 2 * beams, 5, heads, d), rand(gen, 2 * beams, 5, heads, d))
+    torch.cuda.synchronize()
+    counts = p.counts.tolist()
+    assert counts == [348] * cells and int((p.refs > 1).sum()) > 20 * heads
+    q = rand(gen, 2 * beams, 3, 4 * heads, d)
+    own = cache_of(fw, gen, counts, P, d)
+    r = torch.arange(348, device="cuda")
+    for h in range(cells):
+        to, at = own.table[h].long()[r // P], p.table[h].long()[r // P]
+        own.k[to, r % P], own.v[to, r % P] = p.k[at, r % P], p.v[at, r % P]
+    for longest in (0, 348):
+        out = check_all(fw, p, counts, q, heads, longest=longest)
+        other = fw.pages_attend(own, q, kv_heads=heads, longest=longest)
+        assert torch.equal(out["o"].view(torch.int16), other["o"].view(torch.int16)) and torch.equal(out["lse"], other["lse"])
