@@ -513,7 +513,9 @@ typedef struct {
     int32_t d;               /* 64 or 128                                            */
     int32_t page_rows;       /* 16, 32, 64 or 128                                    */
     int32_t num_pages;       /* pages of the pool; fewer than 2^31 rows in all       */
-    int32_t max_pages;       /* entries of a cell's table; cells * max_pages < 2^31  */
+    int32_t max_pages;       /* entries of a cell's table; cells * max_pages < 2^31,
+                                max_pages * page_rows < 2^31, and for the attention
+                                cells * max_pages * page_rows / 16 < 2^31            */
     void *k, *v;             /* device bf16 [num_pages][page_rows][d], 16-byte aligned */
     int32_t *table;          /* device [cells][max_pages]                            */
     int32_t *held, *counts;  /* device [cells]                                       */
@@ -572,7 +574,7 @@ size_t fw_pages_fork_workspace(const fw_pages *p);
 typedef struct {
     int32_t kv_heads;        /* cells = sequences x kv_heads                         */
     int32_t group;           /* query heads per KV head                              */
-    int32_t m;               /* tokens per sequence                                  */
+    int32_t m;               /* tokens per sequence; group * m at most 65535         */
     int32_t longest;         /* a host-side bound on counts, 0 where there is none: it
                                 chooses how the work is split, and no row is left out
                                 where it is wrong                                    */

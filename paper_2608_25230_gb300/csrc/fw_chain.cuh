@@ -5,8 +5,8 @@
 // all before it, in wait_for_the_one_before().  Every thread calls that before it reads or writes global memory, and no thread
 // leaves without: a kernel that ended without having waited would let the next one pass its own wait too soon.  One kernel reads
 // before its wait, k_pages_fork_end: tables that the kernel before it, k_pages_fork, does not change, and that all kernels before
-// that one are done with, since it lets the next start only behind its own wait.  A decode step's rotation, append and attention in a graph: 8 cells of 512 rows 13.2 us (14.3 launched one after another), of 4,096
-// 17.1 (18.2), 64 of 1,024 20.3 (21.3).
+// that one are done with, since it lets the next start only behind its own wait.  A decode step's rotation, append and attention
+// in a graph: 8 cells of 512 rows 13.2 us (14.3 launched one after another), of 4,096 17.1 (18.2), 64 of 1,024 20.3 (21.3).
 #pragma once
 
 #include "fw_internal.h"

@@ -170,7 +170,7 @@ __device__ __forceinline__ int scan_cta(int x, int &all, int (&s_scan)[32])
 }
 
 // One CTA: what every cell needs, the free pages for it, and for appends the books.  WIDE: a warp per cell instead of a
-// thread, for appends that touch several pages a cell.
+// thread, for appends that touch several pages of few cells each.
 template <typename Args, bool WIDE> __global__ void __launch_bounds__(PT, 1) k_pages_plan(const Args a)
 {
     constexpr bool APPEND = std::is_same<Args, AppendArgs>::value;

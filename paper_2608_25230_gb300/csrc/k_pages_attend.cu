@@ -2,7 +2,10 @@
 // of m sees the rows j < n - m + 1 + i:
 //   x_j = scale (q . k_j),  o = sum_j softmax_j(x) v_j,  lse = log sum_j e^x_j.
 //
-// Bound: the rows' bytes, each read once from memory.  Two ways over the cells:
+// Bound: the rows' bytes.  A cell reads each of its rows once; rows in pages that cells share are read by each of them, from the
+// cache where it still holds them (8 beams each over 2 prefixes of 16,384 rows, 8 heads, d = 128: 441 MB from memory where the
+// cells' rows are 1,074 and the distinct ones 134, 127 us against 190 with pages of their own; 4 beams over 4 of 8,192: 136 MB, 53
+// against 111).  Two ways over the cells:
 //   few short cells (k_pages_attend_few): a cluster of up to 12 CTAs per cell, its blocks dealt out to all
 //   their teams, whose states are joined in shared memory and sent to the CTA that joins a row's;
 //   many (k_pages_attend): the blocks of all cells in a row are divided evenly over the teams of
@@ -11,9 +14,9 @@
 //   workspace, and a second kernel, launched behind the first one's tail, joins them in their order.
 // A team is a warp for 8 query rows, or 2, 3, 4 or 6 warps, which read the same blocks against other query
 // rows.  It fetches its blocks by TMA into a ring of its own, through page numbers that its warps
-// have read 32 blocks ahead.  64 x 8 cells of about 16,384 rows, d = 128, 4 query rows: 601 us, 6.8 TB/s, the measured
-// copy rate; 24 x 4 cells of 5,000, 7 query rows 45 us (4.7 TB/s: 3 us to the first blocks, the teams finish up to 8 us
-// apart, 5 us to join); 8 cells of 4,096 7.4 us (latency: 2 us to the first block, 4 blocks a warp, 3 us to join).
+// have read 32 blocks ahead.  64 x 8 cells of about 16,384 rows, d = 128, 4 query rows: 593 to 601 us, 6.8 TB/s, the measured
+// copy rate; 24 x 4 cells of 5,000, 7 query rows 44.5 us (4.8 TB/s: 3 us to the first blocks, the teams finish up to 8 us
+// apart, 5 us to join); 8 cells of 4,096 7.5 us (latency: 2 us to the first block, 4 blocks a warp, 3 us to join).
 // (Ranges of a CTA each, with its warps' states joined at the end of each cell's share and the parts by the last CTA to come,
 // were faster for many long cells, 128 x 8 of 4,096 326 us against 338, and slower for others, 32 x 8 of 1,024 38 against 34, drafts
 // of 20 rows 56 against 47.)
@@ -22,7 +25,10 @@
 // warp-wide bf16 tensor instructions (a few query rows cannot fill a tcgen05 tile, and the stream
 // of rows leaves the slower instructions mostly idle: 13 % of their time with 8 query rows): S^T = K Q^T, then O^T += V^T P^T.
 // The weights enter as the sum of two bf16 numbers, the upper half of the fp32 weight's bits and what that leaves, so that 16
-// bits of each count; both are positive where the weight is, so that an infinite value stays one.  More query rows are bound
+// bits of each count (they are summed for the divisor in 32): the instructions take bf16 beside bf16 values, a third number would
+// add a third to the products, and what two leave out, at most 2^-16 of a weight, is below the 2^-8 of the output's own rounding by so
+// much that the distance from 64 bits is the same to five digits (1.7438e-3 in the 2-norm, 2.2e-3 with one number).  Both are
+// positive where the weight is, so that an infinite value stays one.  More query rows are bound
 // by the reading of the blocks from shared memory and by issue: an SM takes about 12 tiles of 8 rows x 16 keys a us (64 cells x 4,096 rows: 20
 // query rows 40 us, 32 45, 48 55, 64 73).
 #include <algorithm>
@@ -920,8 +926,9 @@ void clusters_at_once(int (&room)[SIZES])
 // over the cells, the joining, and the blocks of all over the GPU.  Clusters: a launch, and the longest cell's blocks over
 // its CTAs, which share the memory with all others at first and have their SMs' whole rate at the end.  (Of 57 shapes, 8 to 128
 // cells of 300 to 3,000 rows on average, 4 to 64 query rows, it takes the slower way for 2, by 1 to 3 us.  d = 128, 4 query rows,
-// clusters against ranges: 8 cells of 3,000 9.6 us against 12.8, 64 of 300 8.0 against 12.3, of 1,000 14.6 against 15.4, 128 of 3,000 62
-// against 39; 20 query rows, 64 of 3,000: 61 against 34.)
+// clusters against ranges: 8 cells of 3,000 9.6 us against 12.8, 64 of 300 6.6 against 11.3, of 1,000 14.6 against 15.4, 128 of 3,000 62
+// against 39; 20 query rows, 64 of 3,000: 61 against 34.  A bound 2 or 4 times the longest cell asks for ranges earlier and costs at most
+// what no bound costs: of 14 shapes, 2 times changed the way of 2, by 2 us, 4 times of 5, by 2 to 5: 8 cells of 4,000 7.6 to 12.0.)
 int cluster_of(const fw_pages &p, const fw_pages_query &q, int TW, int tiles, int sms)
 {
     if (q.longest == 0) return 0;

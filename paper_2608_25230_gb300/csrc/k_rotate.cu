@@ -3,11 +3,14 @@
 //   y = x / sqrt(mean_c x_c^2 + eps) * w;  (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
 // with t = pos * inv_freq[f] for the pair f of columns.
 //
-// Bound: memory, every row read and written once, and near it issue (58 % of the slots): 170 instructions a chunk of heads, 700 a
+// Bound: memory, every row read and written once, and near it issue (58 % of all slots, 66 % of the cycles in which an SM has
+// work): 170 instructions a chunk of heads, 700 a
 // token.  A lane holds 16 columns of a head, so chosen that a pair's two columns meet in it, and LPL lanes a head; a warp keeps
 // one token's cosines and sines, times the weights, in registers and goes over its heads, which it has asked for ahead into
 // shared memory.  16,381 tokens x 40 heads of 128: 54.5 us, 6.2 TB/s (registers alone, one chunk ahead: 67 us); 30,001 x
-// 40 of 64 59 us (a token's 700 instructions weigh twice); 40 tokens x 16 heads 3.1 us.
+// 40 of 64 58 us (a token's 700 instructions weigh twice); 40 tokens x 16 heads 3.3 us.  Three CTAs an SM leave 80 registers, and 24 to
+// 32 of them go to memory and back once or twice a token; with two CTAs nothing does, but less is under way: 55.4 us against 54.9 and
+// 61.6 against 58.2 for the two long ones, 2.9 against 3.3 for the short one.
 #include <algorithm>
 
 #include <cuda_bf16.h>
